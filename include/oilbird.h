@@ -405,6 +405,148 @@ int32_t oil_accept_walk(int32_t B, int32_t max_nodes, const int32_t *node_token,
                         const int32_t *node_parent, const int32_t *n_nodes, const int32_t *target,
                         int32_t *accept_len, int32_t *accept_nodes, int32_t *bonus, void *stream);
 
+/* ---- The verifier's key/value cache, held in 4 bits.  What verifies a merged
+ * tree in one forward (Sec. 4 (iv)) is attention of its nodes over everything
+ * committed so far and, under the tree's mask, over each other.  A cache holds
+ * one layer's committed keys and values of up to n_slots requests; the calls
+ * below fill it, attend over it, add up the attention weight its positions
+ * receive, and evict the lightest ones.
+ *
+ * A row x of head_dim values is held as z + s c: z the bf16 at or below
+ * min(x), s the bf16 at or above the binary32 quotient (max(x) - z) / 15, and
+ * c the nearest whole number (ties to even) to (x - z) / s as binary32 has it,
+ * 0 .. 15; with s = 0 every c is 0.  A row with a value that is not finite, or whose range
+ * or z passes what bf16 holds, reads back as NaN and makes the attention of every row that sees
+ * it NaN.
+ *
+ * Buffer layout, per slot and head: tiles of 32 positions, each
+ * 32 * W + 256 bytes, W = head_dim rounded up to 64 or 128: the keys' codes in
+ * MFMA operand order, the values' codes, transposed, likewise, then one (s, z)
+ * bf16 pair for each key and each value row.  At head_dim 128 a position
+ * takes 136 bytes a head, against 512 in bf16.  With key j = i % 32 of a tile,
+ *     key code d:    dword Q = (j / 16) * (W / 32) + d / 32 of lane
+ *                    j % 16 + 16 * ((d % 32) / 8), element e = d % 8;
+ *     value code d:  dword Q = d / 16 of lane d % 16 + 16 * ((j % 16) / 4),
+ *                    element e = 4 * (j / 16) + j % 4;
+ * dword Q of a lane lies at (Q / 4) * 1024 + lane * 16 + (Q % 4) * 4, and
+ * element e in its nibble e / 2 + 4 * (e % 2).
+ *
+ * The order of a cache's slots is its own: eviction moves rows.  Keys come
+ * with whatever position encoding they have; no call adds one.
+ *
+ * Common arguments: `slots` (B int32 or NULL) names the slot of each request,
+ * NULL meaning 0 .. B - 1; a request whose slot is outside [0, n_slots) is
+ * skipped (its outputs are those of a request without nodes).  A slot is named
+ * at most once per call.  Lengths live on the device, so that no call waits
+ * for the host and every call can be captured in a graph. */
+typedef struct oil_kv oil_kv;
+
+#define OIL_KV_MAX_DIM 128
+#define OIL_KV_MAX_HEADS 256
+#define OIL_KV_MAX_GROUP 64
+
+/* Bytes of the code buffer of a cache of n_slots * n_heads * capacity rows
+ * (key and value each); 0 for arguments oil_kv_create refuses. */
+size_t oil_kv_bytes(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity);
+
+/* Create a cache over caller-owned device buffers.
+ *   n_slots    requests, 1 .. 65535.   n_heads  key/value heads, 1 .. OIL_KV_MAX_HEADS.
+ *   head_dim   multiple of 8, 8 .. OIL_KV_MAX_DIM.   capacity  positions per
+ *              slot, 1 .. 2^30.
+ *   code_buf   oil_kv_bytes(...) bytes, 256-byte aligned.
+ *   pos_buf    n_slots x n_heads x capacity int32: the position of each row
+ *              (appended rows count on from 0), -1 past a slot's length.
+ *   weight_buf n_slots x n_heads x capacity float32: the attention weight
+ *              accumulated by each row, 0 past a slot's length.
+ *   state_buf  n_slots x 4 int32, 16-byte aligned: length, next position, and
+ *              two words of the library's own.
+ * Enqueues the clearing of pos, weight and state on `stream`.  Head dims past
+ * OIL_KV_MAX_DIM or more heads return OIL_E_UNSUPPORTED. */
+int32_t oil_kv_create(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity, void *code_buf,
+                      int32_t *pos_buf, float *weight_buf, int32_t *state_buf, void *stream, oil_kv **out);
+int32_t oil_kv_destroy(oil_kv *kv);
+
+/* Empty the slots of B requests: length and next position 0.  B 1 .. n_slots. */
+int32_t oil_kv_reset(oil_kv *kv, const int32_t *slots, int32_t B, void *stream);
+
+/* Append rows of B requests.
+ *   k, v       B x max_rows rows of n_heads x head_dim values, dtype OIL_F32 or
+ *              OIL_BF16, 16-byte aligned; consecutive rows ld elements apart
+ *              (ld >= n_heads * head_dim, a multiple of 8: a slice of a fused
+ *              projection's output serves), requests max_rows * ld apart.
+ *   nodes, count  which rows, and in which order.  Both NULL: all max_rows.
+ *              count alone (B int32): the first count[b].  Both (nodes
+ *              B x max_rows, as oil_accept_walk wrote them): row 0, the tree's
+ *              root, then nodes[b][0 .. count[b]), the committed path; an id
+ *              outside [0, max_rows) ends it; max_rows <= OIL_MAX_NODES.
+ *   weight     B x n_heads x max_rows float32 by row, or NULL for 0: what the rows
+ *              start with (a prompt's, from the attention that read it).
+ * Rows past the capacity are not stored (the length stops at the capacity;
+ * the next position counts them). */
+int32_t oil_kv_append(oil_kv *kv, const int32_t *slots, int32_t B, const void *k, const void *v, int32_t dtype,
+                      int64_t ld, int32_t max_rows, const int32_t *nodes, const int32_t *count,
+                      const float *weight, void *stream);
+
+/* Read rows first .. first + n - 1 of B requests back as the values they stand
+ * for: k_out, v_out B x n_heads x n x head_dim, OIL_F32 or OIL_BF16 (nearest-even), 16-byte
+ * aligned; zeros past a slot's length.  first >= 0, n >= 1, first + n <= capacity. */
+int32_t oil_kv_read(const oil_kv *kv, const int32_t *slots, int32_t B, int64_t first, int64_t n, void *k_out,
+                    void *v_out, int32_t dtype, void *stream);
+
+/* Workspace bytes of oil_kv_attend; 0 for arguments it refuses. */
+size_t oil_kv_attend_workspace_bytes(const oil_kv *kv, int32_t B, int32_t max_nodes, int32_t n_q_heads);
+
+/* Attention of B requests' nodes.  Row (i, a), node i and query head a, which
+ * reads key/value head a / (n_q_heads / n_heads), sees every cached position
+ * of its slot and those nodes of its request that its mask row names:
+ *     S = scale * q . k;  lse = log sum exp S;  out = sum exp(S - lse) v.
+ *   q          B x max_nodes rows of n_q_heads x head_dim bf16, 16-byte
+ *              aligned, rows q_ld elements apart (>= n_q_heads * head_dim, a
+ *              multiple of 8), requests max_nodes * q_ld apart.
+ *   k, v       the nodes' own rows, B x max_nodes of n_heads x head_dim bf16, rows
+ *              ld elements apart likewise, not yet in the cache; both NULL: no row sees a node.
+ *   n_nodes    B int32 (clamped to 0 .. max_nodes) or NULL: max_nodes each.
+ *   mask       B x max_nodes x ceil(max_nodes / 32) uint32 as oil_tree_mask
+ *              wrote it, or NULL: node i sees nodes 0 .. i (a chunk of a
+ *              prompt, or with max_nodes = 1 one token).  Bits past n_nodes
+ *              count as clear; needs k.
+ *   max_nodes  1 .. OIL_MAX_NODES.   n_q_heads  a multiple of n_heads, at
+ *              most OIL_KV_MAX_GROUP times it.   scale  finite.   B 1 .. OIL_MAX_B.
+ *   workspace  >= oil_kv_attend_workspace_bytes(...), 256-byte aligned.
+ *   out        B x max_nodes x n_q_heads x head_dim bf16, dense, 16-byte aligned.
+ *   lse        B x max_nodes x n_q_heads float32 (natural logarithm) or NULL.
+ * A row that sees nothing, and every row past n_nodes, gives zeros and -inf.
+ * What a row does not see does not reach it, whatever it holds. */
+int32_t oil_kv_attend(const oil_kv *kv, const int32_t *slots, int32_t B, const void *q, int64_t q_ld,
+                      int32_t n_q_heads, const void *k, const void *v, int64_t ld, const int32_t *n_nodes,
+                      const uint32_t *mask, int32_t max_nodes, float scale, void *workspace,
+                      size_t workspace_bytes, void *out, float *lse, void *stream);
+
+/* Add the attention weight that committed rows gave to the cached positions:
+ *     weight[slot][h][j] += sum over rows i and heads a of h of
+ *                           exp(scale * q_ia . k_j - lse_ia)
+ * for every cached j.  Called after oil_accept_walk and before the rows are
+ * appended, it counts what the committed tokens saw and nothing that rejected
+ * nodes did.  q, q_ld, lse and scale as oil_kv_attend took and wrote them;
+ * nodes and count name rows as in oil_kv_append.  A row whose lse is -inf adds nothing. */
+int32_t oil_kv_weigh(oil_kv *kv, const int32_t *slots, int32_t B, const void *q, int64_t q_ld,
+                     int32_t n_q_heads, const float *lse, int32_t max_nodes, const int32_t *nodes,
+                     const int32_t *count, float scale, void *stream);
+
+/* Workspace bytes of oil_kv_evict; 0 for arguments it refuses. */
+size_t oil_kv_evict_workspace_bytes(const oil_kv *kv, int32_t B, int64_t keep);
+
+/* Evict down to `keep` rows.  A slot of at most keep rows stays as it is.  In
+ * any other, each head keeps the rows of its last `recent` positions and,
+ * up to keep, those of largest weight (ties to the lower row index; NaN ranks
+ * lowest), and compacts in place: rows below keep that go leave holes, and the
+ * i-th hole takes the i-th row at or past keep that stays (code, position and
+ * weight), so that only those rows move.  The length becomes keep.
+ *   keep  1 .. capacity.   recent  0 .. keep.   B 1 .. OIL_MAX_B.
+ *   workspace  >= oil_kv_evict_workspace_bytes(kv, B, keep), 256-byte aligned. */
+int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, int64_t recent, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
 /* Benchmark instrumentation (host; not thread-safe).  While enabled, the
  * pool scans of oil_pool_query_topk calls on non-empty pools are counted
  * from 0, and scans 0, every, 2 * every, ... (up to max_launches of them,

@@ -10,7 +10,8 @@ binding's entry points raises.
 Entry points carry the names of the C calls without their ``oil_`` prefix:
 ``pool_create``, ``pool_append``, ``pool_size``, ``query_workspace_bytes``,
 ``pool_query_topk``, ``gather_continuations``, ``tree_merge``; ``Pool`` bundles
-a pool's buffers and handle.
+a pool's buffers and handle, ``RecyclePool`` those of the rejected-branch ring
+and ``KvCache`` those of the verifier's 4-bit key/value cache.
 """
 from __future__ import annotations
 
@@ -30,6 +31,7 @@ LEX_MAX_CTX, LEX_MAX_N, LEX_MAX_LEN, LEX_MAX_CAND = 32, 16, 64, 4096
 LEX_MAX_HIST = 1 << 20
 SCORE_ROOM_MAX = 2 << 30
 REC_DEPTH, REC_MAX_OUT = 6, 8
+KV_MAX_DIM, KV_MAX_HEADS, KV_MAX_GROUP = 128, 256, 64
 
 _lib = None
 
@@ -107,6 +109,18 @@ def lib():
             "oil_lexical_drafts": (i32, [P, P, P, i32, i32, P, P, P, i32, i32, i32, i32, i32, P, sz, P, P, P,
                                          P]),
             "oil_accept_walk": (i32, [i32, i32, P, P, P, P, P, P, P, P]),
+            "oil_kv_bytes": (sz, [i32, i32, i32, i64]),
+            "oil_kv_create": (i32, [i32, i32, i32, i64, P, P, P, P, P, ctypes.POINTER(P)]),
+            "oil_kv_destroy": (i32, [P]),
+            "oil_kv_reset": (i32, [P, P, i32, P]),
+            "oil_kv_append": (i32, [P, P, i32, P, P, i32, i64, i32, P, P, P, P]),
+            "oil_kv_read": (i32, [P, P, i32, i64, i64, P, P, i32, P]),
+            "oil_kv_attend_workspace_bytes": (sz, [P, i32, i32, i32]),
+            "oil_kv_attend": (i32, [P, P, i32, P, i64, i32, P, P, i64, P, P, i32, ctypes.c_float, P, sz, P, P,
+                                    P]),
+            "oil_kv_weigh": (i32, [P, P, i32, P, i64, i32, P, i32, P, P, ctypes.c_float, P]),
+            "oil_kv_evict_workspace_bytes": (sz, [P, i32, i64]),
+            "oil_kv_evict": (i32, [P, P, i32, i64, i64, P, sz, P]),
             "oil_read_stream": (i32, [P, sz, P, P]),
             "oil_scan_timer_start": (i32, [i32, i32]),
             "oil_scan_timer_stop": (i32, [ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_double)]),
@@ -151,6 +165,31 @@ def _i32(t, name):
     if t.dtype != torch.int32:
         raise ValueError(f"{name} must be int32")
     return t
+
+
+def _shaped(t, name, shape, dtype):
+    """A dense device tensor of exactly this shape and type, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _row_stride(t, name):
+    """Elements between consecutive rows of a (B, N, heads, dim) device tensor
+    whose rows are dense (a slice of a fused projection's output, say)."""
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have 4 dimensions (requests, rows, heads, dim)")
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    B, N, H, D = t.shape
+    if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D):
+        raise ValueError(f"{name}: the heads of a row must be dense")
+    ld = t.stride(1) if N > 1 else t.stride(0) if B > 1 else H * D
+    if B > 1 and t.stride(0) != N * ld:
+        raise ValueError(f"{name}: requests must be as far apart as their rows")
+    return ld
 
 
 # ---------------------------------------------------------------- C calls
@@ -500,6 +539,150 @@ class RecyclePool:
             ctypes.c_float(theta), n_out, L_out, _ptr(ws), ws.numel(), _ptr(sc), _ptr(tk), _ptr(ln),
             _stream(stream)))
         return sc, tk, ln
+
+
+class KvCache:
+    """One layer's committed keys and values of up to ``n_slots`` requests, held in
+    4 bits, and the device buffers they live in (torch tensors, caller-owned).
+
+    ``state`` (n_slots, 4) int32: length and next position first.  ``positions``
+    and ``weights`` (n_slots, n_heads, capacity): each row's position and the
+    attention weight it has accumulated (-1 and 0 past a slot's length).
+    ``slots`` (B,) int32 names the slots of a call's requests (None: 0 .. B - 1).
+    Calls on one cache are ordered by the caller, as on a pool."""
+
+    def __init__(self, n_slots: int, n_heads: int, head_dim: int, capacity: int, device="cuda", stream=None):
+        self.n_slots, self.n_heads, self.head_dim, self.capacity = n_slots, n_heads, head_dim, capacity
+        self.device = torch.device(device)
+        nbytes = lib().oil_kv_bytes(n_slots, n_heads, head_dim, capacity)
+        if nbytes == 0:
+            raise ValueError(f"unsupported cache: n_slots={n_slots} n_heads={n_heads} head_dim={head_dim} "
+                             f"capacity={capacity}")
+        self.codes = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        self.positions = torch.empty((n_slots, n_heads, capacity), dtype=torch.int32, device=self.device)
+        self.weights = torch.empty((n_slots, n_heads, capacity), dtype=torch.float32, device=self.device)
+        self.state = torch.empty((n_slots, 4), dtype=torch.int32, device=self.device)
+        h = ctypes.c_void_p()
+        _check("oil_kv_create", lib().oil_kv_create(
+            n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions), _ptr(self.weights),
+            _ptr(self.state), _stream(stream), ctypes.byref(h)))
+        self.handle = h
+        self._ws = {}
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h is not None and _lib is not None:
+            _lib.oil_kv_destroy(h)
+            self.handle = None
+
+    @property
+    def lengths(self):
+        return self.state[:, 0]
+
+    def _workspace(self, key, nbytes):
+        if nbytes == 0:
+            raise ValueError(f"unsupported cache call {key}")
+        if key not in self._ws:
+            self._ws[key] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        return self._ws[key]
+
+    def _heads(self, t, name):
+        if t.dim() != 4 or t.shape[3] != self.head_dim:
+            raise ValueError(f"{name} must be (requests, rows, heads, {self.head_dim}), got {tuple(t.shape)}")
+        return _row_stride(t, name)
+
+    def _own_rows(self, k, v, what):
+        """Stride of the rows k and v (B, N, n_heads, head_dim)."""
+        if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 4 or k.shape[2] != self.n_heads:
+            raise ValueError(f"{what}: k and v must be alike, (requests, rows, {self.n_heads}, {self.head_dim})")
+        ld = self._heads(k, "k")
+        if self._heads(v, "v") != ld:
+            raise ValueError(f"{what}: k and v must have the same strides")
+        return ld
+
+    def reset(self, slots=None, B=None, stream=None):
+        """Empty the named slots (all of them when neither slots nor B is given)."""
+        B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
+        _check("oil_kv_reset", lib().oil_kv_reset(self.handle, _shaped(slots, "slots", (B,), torch.int32), B,
+                                                  _stream(stream)))
+
+    def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None):
+        """Append rows of k, v (B, N, n_heads, head_dim), float32 or bfloat16: all
+        of them, the first ``count`` (B,), or with ``nodes`` (B, N) the root and the
+        accepted nodes as accept_walk returns them; ``weight`` (B, n_heads, N)."""
+        ld = self._own_rows(k, v, "append")
+        B, N = k.shape[:2]
+        _check("oil_kv_append", lib().oil_kv_append(
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, k.data_ptr(), v.data_ptr(), _dtype_code(k),
+            ld, N, _shaped(nodes, "nodes", (B, N), torch.int32), _shaped(count, "count", (B,), torch.int32),
+            _shaped(weight, "weight", (B, self.n_heads, N), torch.float32), _stream(stream)))
+
+    def read(self, first, n, B=None, slots=None, dtype=torch.bfloat16, stream=None, out=None):
+        """Rows first .. first + n - 1 as the values they stand for: (k, v), each
+        (B, n_heads, n, head_dim); zeros past a slot's length."""
+        B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
+        shape = (B, self.n_heads, n, self.head_dim)
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
+        k, v = out
+        _check("oil_kv_read", lib().oil_kv_read(
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, first, n, _shaped(k, "k", shape, k.dtype),
+            _shaped(v, "v", shape, k.dtype), _dtype_code(k), _stream(stream)))
+        return k, v
+
+    def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None):
+        """Attention of nodes q (B, N, n_q_heads, head_dim) bfloat16 over the cached
+        rows and, with k and v (B, N, n_heads, head_dim), over each other: where
+        ``mask`` (tree_mask's) says so, or causally.  Returns (out like q, dense,
+        lse (B, N, n_q_heads) float32)."""
+        q_ld = self._heads(q, "q")
+        B, N, Hq, D = q.shape
+        ld = 0
+        if (k is None) != (v is None):
+            raise ValueError("attend: k and v come together")
+        if k is not None:
+            ld = self._own_rows(k, v, "attend")
+            if tuple(k.shape[:2]) != (B, N):
+                raise ValueError("attend: k and v must have the rows of q")
+        for t, name in ((q, "q"), (k, "k")):
+            if t is not None and t.dtype != torch.bfloat16:
+                raise ValueError(f"attend: {name} must be bfloat16, got {t.dtype}")
+        scale = 1.0 / math.sqrt(D) if scale is None else scale
+        if out is None:
+            out = (torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=self.device),
+                   torch.empty((B, N, Hq), dtype=torch.float32, device=self.device))
+        o, lse = out
+        ws = self._workspace(("attend", B, N, Hq), lib().oil_kv_attend_workspace_bytes(self.handle, B, N, Hq))
+        _check("oil_kv_attend", lib().oil_kv_attend(
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
+            None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
+            _shaped(n_nodes, "n_nodes", (B,), torch.int32),
+            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, _ptr(ws), ws.numel(),
+            _shaped(o, "out", (B, N, Hq, D), torch.bfloat16), _shaped(lse, "lse", (B, N, Hq), torch.float32),
+            _stream(stream)))
+        return o, lse
+
+    def weigh(self, q, lse, nodes=None, count=None, scale=None, slots=None, stream=None):
+        """Add the attention weight of the committed rows (named as in append) of
+        q, lse, as attend took and returned them, to ``weights``."""
+        q_ld = self._heads(q, "q")
+        B, N, Hq, D = q.shape
+        if q.dtype != torch.bfloat16:
+            raise ValueError(f"weigh: q must be bfloat16, got {q.dtype}")
+        scale = 1.0 / math.sqrt(D) if scale is None else scale
+        _check("oil_kv_weigh", lib().oil_kv_weigh(
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
+            _shaped(lse, "lse", (B, N, Hq), torch.float32), N, _shaped(nodes, "nodes", (B, N), torch.int32),
+            _shaped(count, "count", (B,), torch.int32), scale, _stream(stream)))
+
+    def evict(self, keep, recent=0, B=None, slots=None, stream=None):
+        """Evict every head of the named slots down to ``keep`` rows: the last
+        ``recent`` positions and the heaviest others stay."""
+        B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
+        ws = self._workspace(("evict", B, keep), lib().oil_kv_evict_workspace_bytes(self.handle, B, keep))
+        _check("oil_kv_evict", lib().oil_kv_evict(
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, _ptr(ws), ws.numel(),
+            _stream(stream)))
 
 
 def merge_trees(anchor, lex_tokens, lex_len, lex_budget, sem_tokens, sem_len, sem_budget,

@@ -11,6 +11,7 @@
 #include "../../include/oilbird.h"
 #include "common.hpp"
 #include "internal.hpp"
+#include "kv.hpp"
 
 static_assert(OIL_MAX_K == OIL_TOPK_MAX, "top-k capacity");
 static_assert(OIL_MAX_NODES == OIL_NODES_MAX, "tree capacity");
@@ -26,6 +27,10 @@ struct oil_recycle {
     uint16_t* keys;
     int32_t *tokens, *rollouts;
     int64_t* head;
+};
+
+struct oil_kv {
+    oil::KvView c;
 };
 
 struct oil_pool {
@@ -655,6 +660,176 @@ int32_t oil_accept_walk(int32_t B, int32_t max_nodes, const int32_t* node_token,
         return OIL_E_UNSUPPORTED;
     return hip_status(oil::launch_accept_walk(B, max_nodes, node_token, node_parent, n_nodes, target,
                                               accept_len, accept_nodes, bonus, (hipStream_t)stream));
+}
+
+// ---- 4-bit key/value cache
+
+static int32_t kv_width(int32_t head_dim) { return head_dim <= 64 ? 64 : 128; }
+
+// Status of a cache's geometry.
+static int32_t kv_shape_status(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity)
+{
+    if (n_slots < 1 || n_heads < 1 || head_dim < 1 || capacity < 1 || n_slots > 65535 || capacity > (1 << 30) ||
+        head_dim % 8 != 0)
+        return OIL_E_INVALID;
+    if (n_heads > OIL_KV_MAX_HEADS || head_dim > OIL_KV_MAX_DIM)
+        return OIL_E_UNSUPPORTED;
+    return OIL_OK;
+}
+
+// Status of a row stride: n values a row, 16-byte alignment of every row.
+static bool kv_ld_fits(int64_t ld, int64_t n) { return ld >= n && ld % 8 == 0 && ld <= (1 << 24); }
+
+size_t oil_kv_bytes(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity)
+{
+    if (kv_shape_status(n_slots, n_heads, head_dim, capacity) != OIL_OK)
+        return 0;
+    const size_t tiles = (size_t)(capacity + oil::kKvTile - 1) / oil::kKvTile;
+    return (size_t)n_slots * (size_t)n_heads * tiles * ((size_t)kv_width(head_dim) * oil::kKvTile + 256);
+}
+
+int32_t oil_kv_create(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity, void* code_buf,
+                      int32_t* pos_buf, float* weight_buf, int32_t* state_buf, void* stream, oil_kv** out)
+{
+    if (!out)
+        return OIL_E_INVALID;
+    *out = nullptr;
+    const int32_t st = kv_shape_status(n_slots, n_heads, head_dim, capacity);
+    if (st != OIL_OK)
+        return st;
+    if (!code_buf || !pos_buf || !weight_buf || !state_buf || !aligned(code_buf, kAlign) || !aligned(pos_buf, 4) ||
+        !aligned(weight_buf, 4) || !aligned(state_buf, 16))
+        return OIL_E_INVALID;
+    oil_kv* kv = (oil_kv*)calloc(1, sizeof(oil_kv));
+    if (!kv)
+        return OIL_E_INVALID;
+    oil::KvView& c = kv->c;
+    c.codes = (uint8_t*)code_buf;
+    c.pos = pos_buf;
+    c.weight = weight_buf;
+    c.state = state_buf;
+    c.n_slots = n_slots;
+    c.H = n_heads;
+    c.D = head_dim;
+    c.W = kv_width(head_dim);
+    c.cap = capacity;
+    c.tiles = (capacity + oil::kKvTile - 1) / oil::kKvTile;
+    c.tile_bytes = (int64_t)c.W * oil::kKvTile + 256;
+    const int32_t done = hip_status(oil::launch_kv_clear(c, (hipStream_t)stream));
+    if (done != OIL_OK) {
+        free(kv);
+        return done;
+    }
+    *out = kv;
+    return OIL_OK;
+}
+
+int32_t oil_kv_destroy(oil_kv* kv)
+{
+    if (!kv)
+        return OIL_E_INVALID;
+    free(kv);
+    return OIL_OK;
+}
+
+int32_t oil_kv_reset(oil_kv* kv, const int32_t* slots, int32_t B, void* stream)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots)
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_kv_reset(kv->c, slots, B, (hipStream_t)stream));
+}
+
+int32_t oil_kv_append(oil_kv* kv, const int32_t* slots, int32_t B, const void* k, const void* v, int32_t dtype,
+                      int64_t ld, int32_t max_rows, const int32_t* nodes, const int32_t* count,
+                      const float* weight, void* stream)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || !k || !v || (dtype != OIL_F32 && dtype != OIL_BF16) || max_rows < 1 ||
+        (nodes && !count) || !kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D) || !aligned(k, 16) || !aligned(v, 16))
+        return OIL_E_INVALID;
+    if (nodes && max_rows > OIL_MAX_NODES)
+        return OIL_E_UNSUPPORTED;
+    return hip_status(oil::launch_kv_append(kv->c, slots, B, k, v, dtype, ld, max_rows, nodes, count, weight,
+                                            (hipStream_t)stream));
+}
+
+int32_t oil_kv_read(const oil_kv* kv, const int32_t* slots, int32_t B, int64_t first, int64_t n, void* k_out,
+                    void* v_out, int32_t dtype, void* stream)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || first < 0 || n < 1 || n > kv->c.cap || first > kv->c.cap - n || !k_out ||
+        !v_out || (dtype != OIL_F32 && dtype != OIL_BF16) || !aligned(k_out, 16) || !aligned(v_out, 16))
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_kv_read(kv->c, slots, B, first, n, k_out, v_out, dtype, (hipStream_t)stream));
+}
+
+// Checks shared by the calls that take queries.
+static int32_t kv_query_status(const oil_kv* kv, int32_t B, int32_t max_nodes, int32_t n_q_heads)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || max_nodes < 1 || n_q_heads < 1 || n_q_heads % kv->c.H != 0)
+        return OIL_E_INVALID;
+    if (B > OIL_MAX_B || max_nodes > OIL_MAX_NODES || n_q_heads / kv->c.H > OIL_KV_MAX_GROUP)
+        return OIL_E_UNSUPPORTED;
+    return OIL_OK;
+}
+
+size_t oil_kv_attend_workspace_bytes(const oil_kv* kv, int32_t B, int32_t max_nodes, int32_t n_q_heads)
+{
+    if (kv_query_status(kv, B, max_nodes, n_q_heads) != OIL_OK)
+        return 0;
+    return oil::kv_attend_workspace_bytes(kv->c, B, max_nodes, n_q_heads);
+}
+
+int32_t oil_kv_attend(const oil_kv* kv, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
+                      int32_t n_q_heads, const void* k, const void* v, int64_t ld, const int32_t* n_nodes,
+                      const uint32_t* mask, int32_t max_nodes, float scale, void* workspace,
+                      size_t workspace_bytes, void* out, float* lse, void* stream)
+{
+    const int32_t st = kv_query_status(kv, B, max_nodes, n_q_heads);
+    if (st != OIL_OK)
+        return st;
+    if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D) ||
+        !isfinite(scale) || !k != !v || (mask && !k))
+        return OIL_E_INVALID;
+    if (k && (!kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D) || !aligned(k, 16) || !aligned(v, 16)))
+        return OIL_E_INVALID;
+    if (!workspace || !aligned(workspace, kAlign) ||
+        workspace_bytes < oil::kv_attend_workspace_bytes(kv->c, B, max_nodes, n_q_heads))
+        return OIL_E_WORKSPACE;
+    return hip_status(oil::launch_kv_attend(kv->c, slots, B, q, q_ld, n_q_heads, k, v, ld, n_nodes, mask, max_nodes,
+                                            scale, workspace, out, lse, (hipStream_t)stream));
+}
+
+int32_t oil_kv_weigh(oil_kv* kv, const int32_t* slots, int32_t B, const void* q, int64_t q_ld, int32_t n_q_heads,
+                     const float* lse, int32_t max_nodes, const int32_t* nodes, const int32_t* count, float scale,
+                     void* stream)
+{
+    const int32_t st = kv_query_status(kv, B, max_nodes, n_q_heads);
+    if (st != OIL_OK)
+        return st;
+    if (!q || !lse || !aligned(q, 16) || !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D) || !isfinite(scale) ||
+        (nodes && !count))
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_kv_weigh(kv->c, slots, B, q, q_ld, n_q_heads, lse, max_nodes, nodes, count, scale,
+                                           (hipStream_t)stream));
+}
+
+size_t oil_kv_evict_workspace_bytes(const oil_kv* kv, int32_t B, int64_t keep)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || B > OIL_MAX_B || keep < 1 || keep > kv->c.cap)
+        return 0;
+    return oil::kv_evict_workspace_bytes(kv->c, B, keep);
+}
+
+int32_t oil_kv_evict(oil_kv* kv, const int32_t* slots, int32_t B, int64_t keep, int64_t recent, void* workspace,
+                     size_t workspace_bytes, void* stream)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || keep < 1 || keep > kv->c.cap || recent < 0 || recent > keep)
+        return OIL_E_INVALID;
+    if (B > OIL_MAX_B)
+        return OIL_E_UNSUPPORTED;
+    if (!workspace || !aligned(workspace, kAlign) ||
+        workspace_bytes < oil::kv_evict_workspace_bytes(kv->c, B, keep))
+        return OIL_E_WORKSPACE;
+    return hip_status(oil::launch_kv_evict(kv->c, slots, B, keep, recent, workspace, (hipStream_t)stream));
 }
 
 const char* oil_status_string(int32_t status)

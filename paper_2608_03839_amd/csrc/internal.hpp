@@ -139,4 +139,34 @@ hipError_t launch_accept_walk(int32_t B, int32_t max_nodes, const int32_t* node_
                               int32_t* accept_len, int32_t* accept_nodes, int32_t* bonus,
                               hipStream_t stream);
 
+// The 4-bit key/value cache (kvcache.hip, kvattend.hip).
+struct KvView {
+    uint8_t* codes;
+    int32_t* pos;
+    float* weight;
+    int32_t* state;  // 4 words a slot
+    int32_t n_slots, H, D, W;  // W: D padded to 64 or 128
+    int64_t cap, tiles;        // positions and 32-position tiles of a slot's head
+    int64_t tile_bytes;
+};
+
+hipError_t launch_kv_clear(const KvView& c, hipStream_t stream);
+hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hipStream_t stream);
+hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, const void* k, const void* v,
+                            int dtype, int64_t ld, int32_t max_rows, const int32_t* nodes, const int32_t* count,
+                            const float* weight, hipStream_t stream);
+hipError_t launch_kv_read(const KvView& c, const int32_t* slots, int32_t B, int64_t first, int64_t n, void* k_out,
+                          void* v_out, int dtype, hipStream_t stream);
+size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq);
+hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
+                            int32_t Hq, const void* k, const void* v, int64_t ld, const int32_t* n_nodes,
+                            const uint32_t* mask, int32_t max_nodes, float scale, void* workspace, void* out,
+                            float* lse, hipStream_t stream);
+hipError_t launch_kv_weigh(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
+                           int32_t Hq, const float* lse, int32_t max_nodes, const int32_t* nodes,
+                           const int32_t* count, float scale, hipStream_t stream);
+size_t kv_evict_workspace_bytes(const KvView& c, int32_t B, int64_t keep);
+hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int64_t keep, int64_t recent,
+                           void* workspace, hipStream_t stream);
+
 }  // namespace oil

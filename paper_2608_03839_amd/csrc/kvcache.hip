@@ -1,0 +1,592 @@
+// The verifier's 4-bit key/value cache: clearing, appending (quantising),
+// reading back and eviction.  Layout and contract: include/oilbird.h; the
+// attention that reads it: kvattend.hip.
+//
+// append: one workgroup per touched 32-position tile of a (request, head).  A
+// row is quantised by 8 lanes (extremes by shuffles), its codes staged in LDS
+// as bytes, and the tile's dwords, which hold 8 values of a key or 8 positions
+// of a value, packed from there; a value dword that also holds positions
+// appended earlier is read and merged.  The workgroup owns the tile, so there
+// is no race on a dword.
+//
+// evict: a row kept above the budget moves into a hole below it, so sources
+// and destinations are disjoint and every move is independent.  One workgroup
+// per (request, head) finds the budget-th largest weight by radix selection
+// and lists the moves with their positions and weights; a second kernel owns
+// one destination tile per workgroup.
+//
+// A slot's length changes when the last workgroup of the request has read it:
+// each takes a ticket when it is done.
+#include "kv.hpp"
+
+namespace oil {
+
+namespace {
+
+constexpr int64_t kMaxGridTiles = 16384;  // workgroups a (request, head); past that they take turns
+
+__global__ __launch_bounds__(256) void kv_clear_kernel(KvView c)
+{
+    const int64_t n = (int64_t)c.n_slots * c.H * c.cap;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        c.pos[i] = -1;
+        c.weight[i] = 0.f;
+    }
+    if (blockIdx.x == 0)
+        for (int64_t i = threadIdx.x; i < 4ll * c.n_slots; i += 256)
+            c.state[i] = 0;
+}
+
+// Whether this workgroup is the last of `total` of its request to be done; the
+// ticket is left at zero then.  Whatever the workgroup read of the state comes
+// before.
+__device__ __forceinline__ bool kv_last(const KvView& c, int slot, int total)
+{
+    __shared__ int last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int32_t* ticket = c.state + 4 * (int64_t)slot + kKvTicket;
+        __threadfence();
+        last = atomicAdd(ticket, 1) == total - 1;
+        if (last)
+            *ticket = 0;
+    }
+    __syncthreads();
+    return last;
+}
+
+__global__ __launch_bounds__(256) void kv_reset_kernel(KvView c, const int32_t* __restrict__ slots)
+{
+    const int b = blockIdx.z, h = blockIdx.y;
+    const int slot = kv_slot(c, slots, b);
+    if (slot < 0)
+        return;
+    const int32_t n = kv_len(c, slot);
+    const int64_t row = kv_row(c, slot, h);
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        c.pos[row + i] = -1;
+        c.weight[row + i] = 0.f;
+    }
+    if (kv_last(c, slot, gridDim.x * gridDim.y) && threadIdx.x == 0) {
+        c.state[4 * (int64_t)slot + kKvLen] = 0;
+        c.state[4 * (int64_t)slot + kKvNext] = 0;
+    }
+}
+
+// (s, z) of a row with extremes lo, hi; `fine`: every value is finite.
+__device__ __forceinline__ uint32_t kv_pair(float lo, float hi, bool fine)
+{
+    const uint32_t u = __float_as_uint(lo);
+    const uint32_t z = (u >> 31 ? u + 0xFFFFu : u) & 0xFFFF0000u;
+    const float q = (hi - __uint_as_float(z)) / 15.f;
+    const uint32_t s = (__float_as_uint(q) + 0xFFFFu) >> 16;  // q >= 0
+    if (!fine || (z & 0x7F800000u) == 0x7F800000u || s >= 0x7F80u)
+        return 0x7FC0u;
+    return s | z;
+}
+
+__device__ __forceinline__ uint32_t kv_quantise(float x, uint32_t pair)
+{
+    const float s = kv_s(pair);
+    if (!(s > 0.f))
+        return 0;
+    const float c = rintf((x - kv_z(pair)) / s);
+    return c < 0.f ? 0u : c > 15.f ? 15u : (uint32_t)c;
+}
+
+template <int W, typename T>
+__device__ __forceinline__ void kv_load_row(const T* __restrict__ row, int D, int part, float (&x)[W / 8])
+{
+#pragma unroll
+    for (int i = 0; i < W / 8; i += 8) {
+        const int d = part * (W / 8) + i;
+        if (d < D) {
+            if (sizeof(T) == 2) {
+                const u32x4 w = *(const u32x4*)(row + d);
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    x[i + 2 * j] = __uint_as_float(w[j] << 16);
+                    x[i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j += 4) {
+                    const floatx4 w = *(const floatx4*)(row + d + j);
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        x[i + j + e] = w[e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                x[i + j] = 0.f;
+        }
+    }
+}
+
+// Bytes 0 .. 7 of codes -> a dword of nibbles (element e in nibble e / 2 + 4 (e % 2)).
+__device__ __forceinline__ uint32_t kv_pack(const uint32_t (&c)[8])
+{
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        w |= c[e] << (4 * kv_nibble(e));
+    return w;
+}
+
+template <int W, typename T>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t* __restrict__ slots,
+                                                        const T* __restrict__ k, const T* __restrict__ v, int64_t ld,
+                                                        int32_t max_rows, const int32_t* __restrict__ nodes,
+                                                        const int32_t* __restrict__ count,
+                                                        const float* __restrict__ weight)
+{
+    constexpr int kRow = W + 8;
+    __shared__ __align__(8) uint8_t code[2][kKvTile][kRow];
+    __shared__ int bound;
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const int slot = kv_slot(c, slots, b);
+    if (slot < 0)
+        return;
+    const int32_t len = kv_len(c, slot), next = c.state[4 * (int64_t)slot + kKvNext];
+    const int cnt = kv_count(nodes, count, b, max_rows, &bound);
+    const int64_t end = len + (int64_t)cnt < c.cap ? len + (int64_t)cnt : c.cap;
+    for (int64_t first = (len / kKvTile + (int64_t)blockIdx.x) * kKvTile; first < end;
+         first += (int64_t)gridDim.x * kKvTile) {  // of the tile
+        uint8_t* tile = kv_tiles(c, slot, h) + first / kKvTile * c.tile_bytes;
+        const int key = tid >> 3, part = tid & 7;
+        const int64_t j = first + key;
+        const bool live = j >= len && j < end;
+        if (live) {  // the 8 lanes of a row alike
+            const int r = (int)(j - len), src = kv_source(nodes, b, max_rows, r);
+            const int64_t at = ((int64_t)b * max_rows + src) * ld + (int64_t)h * c.D;
+            for (int side = 0; side < 2; side++) {
+                float x[W / 8];
+                kv_load_row<W, T>((side ? v : k) + at, c.D, part, x);
+                float lo = INFINITY, hi = -INFINITY;
+                bool fine = true;
+#pragma unroll
+                for (int i = 0; i < W / 8; i++) {
+                    const bool in = part * (W / 8) + i < c.D;
+                    lo = in ? fminf(lo, x[i]) : lo;
+                    hi = in ? fmaxf(hi, x[i]) : hi;
+                    fine = fine && fabsf(x[i]) < INFINITY;
+                }
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) {
+                    lo = fminf(lo, __shfl_xor(lo, o, 8));
+                    hi = fmaxf(hi, __shfl_xor(hi, o, 8));
+                    fine = __shfl_xor((int)fine, o, 8) && fine;
+                }
+                const uint32_t pair = kv_pair(lo, hi, fine);
+#pragma unroll
+                for (int i = 0; i < W / 8; i++) {
+                    const int d = part * (W / 8) + i;
+                    code[side][key][d] = d < c.D ? (uint8_t)kv_quantise(x[i], pair) : (uint8_t)0;
+                }
+                if (part == 0)
+                    *(uint32_t*)(tile + (side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) + key * 4) = pair;
+            }
+            if (part == 0) {
+                const int64_t at_row = kv_row(c, slot, h) + j;
+                const int64_t pos = next + (int64_t)r;
+                c.pos[at_row] = pos < INT32_MAX ? (int32_t)pos : INT32_MAX;
+                c.weight[at_row] = weight ? weight[((int64_t)b * c.H + h) * max_rows + src] : 0.f;
+            }
+        }
+        __syncthreads();
+        uint32_t* kw = (uint32_t*)tile;
+        uint32_t* vw = (uint32_t*)(tile + KvTile<W>::kValues);
+        for (int w = tid; w < KvTile<W>::kWords; w += 256) {
+            int Q, lane;
+            kv_word(w, &Q, &lane);
+            const int g = lane >> 4;
+            uint32_t e[8];
+            {
+                const int kk = (lane & 15) + 16 * (Q / (W / 32)), d = 32 * (Q % (W / 32)) + 8 * g;
+                const int64_t jj = first + kk;
+                if (jj >= len && jj < end) {
+#pragma unroll
+                    for (int i = 0; i < 8; i++)
+                        e[i] = code[0][kk][d + i];
+                    kw[w] = kv_pack(e);
+                }
+            }
+            const int d = 16 * Q + (lane & 15);
+            uint32_t keep = 0;
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int kk = 16 * (i >> 2) + 4 * g + (i & 3);
+                const int64_t jj = first + kk;
+                const bool mine = jj >= len && jj < end;
+                e[i] = mine ? code[1][kk][d] : 0u;
+                any = any || mine;
+                if (jj < len)
+                    keep |= 15u << (4 * kv_nibble(i));
+            }
+            if (any)
+                vw[w] = kv_pack(e) | (keep ? vw[w] & keep : 0u);
+        }
+        __syncthreads();
+    }
+    if (kv_last(c, slot, gridDim.x * gridDim.y) && tid == 0) {
+        const int64_t after = next + (int64_t)cnt;
+        c.state[4 * (int64_t)slot + kKvLen] = (int32_t)end;
+        c.state[4 * (int64_t)slot + kKvNext] = after < INT32_MAX ? (int32_t)after : INT32_MAX;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ T kv_out(float x);
+template <>
+__device__ __forceinline__ float kv_out<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ uint16_t kv_out<uint16_t>(float x) { return float_to_bf16_rne(x); }
+
+// One workgroup per tile of a (request, head): codes to LDS, then one row's
+// eight values a thread.
+template <int W, typename T>
+__global__ __launch_bounds__(256) void kv_read_kernel(KvView c, const int32_t* __restrict__ slots, int64_t first,
+                                                      int64_t n, T* __restrict__ k_out, T* __restrict__ v_out)
+{
+    __shared__ uint32_t buf[KvTile<W>::kBytes / 4];
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const int slot = kv_slot(c, slots, b);
+    const int32_t len = slot < 0 ? 0 : kv_len(c, slot);
+    const int units = c.D / 8;
+    for (int64_t t0 = (first / kKvTile + (int64_t)blockIdx.x) * kKvTile; t0 < first + n;
+         t0 += (int64_t)gridDim.x * kKvTile) {
+    if (t0 < len) {
+        const uint32_t* tile = (const uint32_t*)(kv_tiles(c, slot, h) + t0 / kKvTile * c.tile_bytes);
+        for (int i = tid; i < KvTile<W>::kBytes / 4; i += 256)
+            buf[i] = tile[i];
+    }
+    __syncthreads();
+    for (int u = tid; u < 2 * kKvTile * units; u += 256) {
+        const int side = u / (kKvTile * units), key = u / units % kKvTile, d = u % units * 8;
+        const int64_t j = t0 + key;
+        if (j < first || j >= first + n)
+            continue;
+        T o[8];
+        if (j >= len) {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                o[i] = (T)0;
+        } else {
+            const uint32_t pair = buf[(side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4 + key];
+            const float s = kv_s(pair), z = kv_z(pair);
+            if (side == 0) {
+                const uint32_t w =
+                    buf[kv_word_at((key >> 4) * (W / 32) + (d >> 5), (key & 15) + 16 * ((d & 31) >> 3))];
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    o[i] = kv_out<T>(z + s * (float)kv_code(w, i));
+            } else {
+                const int e = 4 * (key >> 4) + (key & 3);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int dd = d + i;
+                    const uint32_t w = buf[KvTile<W>::kValues / 4 +
+                                           kv_word_at(dd >> 4, (dd & 15) + 16 * ((key & 15) >> 2))];
+                    o[i] = kv_out<T>(z + s * (float)kv_code(w, e));
+                }
+            }
+        }
+        T* to = (side ? v_out : k_out) + (((int64_t)b * c.H + h) * n + (j - first)) * c.D + d;
+#pragma unroll
+        for (int i = 0; i < 8 * (int)sizeof(T) / 16; i++)
+            ((u32x4*)to)[i] = ((const u32x4*)o)[i];
+    }
+    __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- eviction
+// A row that moves, with what else it carries.
+struct KvMove {
+    int32_t dst, src, pos;
+    float weight;
+};
+
+struct KvMoves {
+    int32_t n;      // rows before (0: nothing to do)
+    int32_t count;  // moves
+    int32_t pad[2];
+};
+
+__host__ __device__ __forceinline__ int64_t kv_moves_stride(int64_t cap, int64_t keep)
+{
+    const int64_t most = keep < cap - keep ? keep : cap - keep;
+    return (int64_t)sizeof(KvMoves) + most * (int64_t)sizeof(KvMove);
+}
+
+// Rank of a row: recent rows above every weight, NaN below.
+__device__ __forceinline__ uint32_t kv_rank(float w, bool young)
+{
+    if (young)
+        return 0xFFFFFFFFu;
+    return w != w ? 0u : score_code(w);
+}
+
+constexpr int kSelect = 1024;
+
+// Exclusive rank of `flag` among the block's threads, and the block's total.
+__device__ __forceinline__ int kv_scan(bool flag, int* waves, int* total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t m = __ballot(flag);
+    if (lane == 0)
+        waves[wave] = __popcll(m);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kSelect / 64; w++) {
+        before += w < wave ? waves[w] : 0;
+        all += waves[w];
+    }
+    __syncthreads();
+    *total = all;
+    return before + __popcll(m & ((1ull << lane) - 1));
+}
+
+__global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
+                                                            int64_t recent, uint8_t* __restrict__ work)
+{
+    __shared__ uint32_t hist[256];
+    __shared__ int waves[kSelect / 64];
+    __shared__ uint32_t digit, above;
+    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
+    uint8_t* mine = work + ((int64_t)b * c.H + h) * kv_moves_stride(c.cap, keep);
+    KvMoves* head = (KvMoves*)mine;
+    KvMove* moves = (KvMove*)(mine + sizeof(KvMoves));
+    const int slot = kv_slot(c, slots, b);
+    const int32_t n = slot < 0 ? 0 : kv_len(c, slot);
+    if (n <= keep) {
+        if (tid == 0) {
+            head->n = 0;
+            head->count = 0;
+        }
+        return;
+    }
+    const int64_t row = kv_row(c, slot, h);
+    const int64_t young = c.state[4 * (int64_t)slot + kKvNext] - recent;
+    auto rank = [&](int32_t i) { return kv_rank(c.weight[row + i], c.pos[row + i] >= young); };
+    // the keep-th largest rank, digit by digit
+    uint32_t prefix = 0, need = (uint32_t)keep;  // rows still to take at the prefix
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += kSelect)
+            hist[i] = 0;
+        __syncthreads();
+        for (int32_t i = tid; i < n; i += kSelect) {
+            const uint32_t r = rank(i);
+            if (shift == 24 || (r >> (shift + 8)) == (prefix >> (shift + 8)))
+                atomicAdd(&hist[(r >> shift) & 255], 1u);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            uint32_t sum = 0;
+            int at = 255;
+            while (at > 0 && sum + hist[at] < need)
+                sum += hist[at--];
+            digit = at;
+            above = sum;
+        }
+        __syncthreads();
+        prefix |= digit << shift;
+        need -= above;
+        __syncthreads();
+    }
+    // rows above the rank stay, and the first `need` at it
+    int tied = 0, holes = 0, late = 0;
+    for (int32_t i0 = 0; i0 < n; i0 += kSelect) {
+        const int32_t i = i0 + tid;
+        const uint32_t r = i < n ? rank(i) : 0;
+        const bool tie = i < n && r == prefix;
+        int total;
+        const int t = tied + kv_scan(tie, waves, &total);
+        tied += total;
+        const bool stays = i < n && (r > prefix || (tie && t < (int)need));
+        const int hole = holes + kv_scan(i < keep && !stays, waves, &total);
+        holes += total;
+        const int from = late + kv_scan(i >= keep && stays, waves, &total);
+        late += total;
+        if (i < keep && !stays)
+            moves[hole].dst = i;
+        if (i >= keep && stays) {
+            moves[from].src = i;
+            moves[from].pos = c.pos[row + i];
+            moves[from].weight = c.weight[row + i];
+        }
+    }
+    if (tid == 0) {
+        head->n = n;
+        head->count = holes;
+    }
+}
+
+template <int W>
+__global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
+                                                      const uint8_t* __restrict__ work)
+{
+    __shared__ int lo, hi;
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const int slot = kv_slot(c, slots, b);
+    if (slot < 0)
+        return;
+    const uint8_t* mine = work + ((int64_t)b * c.H + h) * kv_moves_stride(c.cap, keep);
+    const KvMoves* head = (const KvMoves*)mine;
+    const KvMove* moves = (const KvMove*)(mine + sizeof(KvMoves));
+    const int32_t n = head->n, count = head->count;
+    if (n == 0)
+        return;
+    const int64_t row = kv_row(c, slot, h);
+    // rows past the budget leave
+    for (int64_t i = keep + blockIdx.x * 256ll + tid; i < n; i += gridDim.x * 256ll) {
+        c.pos[row + i] = -1;
+        c.weight[row + i] = 0.f;
+    }
+    if (blockIdx.x == 0 && h == 0 && tid == 0)
+        c.state[4 * (int64_t)slot + kKvLen] = (int32_t)keep;
+    uint8_t* tiles = kv_tiles(c, slot, h);
+    for (int64_t t = blockIdx.x; t * kKvTile < keep; t += gridDim.x) {
+        // the moves into this tile: destinations ascend
+        if (tid < 2) {
+            const int64_t want = (t + tid) * kKvTile;
+            int a = 0, z = count;
+            while (a < z) {
+                const int m = (a + z) >> 1;
+                if (moves[m].dst < want)
+                    a = m + 1;
+                else
+                    z = m;
+            }
+            *(tid ? &hi : &lo) = a;
+        }
+        __syncthreads();
+        const int m0 = lo, m1 = hi;
+        __syncthreads();
+        if (m0 == m1)
+            continue;
+        uint8_t* tile = tiles + t * c.tile_bytes;
+        for (int w = tid; w < KvTile<W>::kWords; w += 256) {
+            int Q, lane;
+            kv_word(w, &Q, &lane);
+            const int g = lane >> 4;
+            uint32_t* to = (uint32_t*)(tile + KvTile<W>::kValues) + w;
+            // relaxed atomics: another workgroup may read nibbles of rows past
+            // the budget from this dword, which do not change
+            uint32_t word = __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            bool any = false;
+            for (int m = m0; m < m1; m++) {
+                const int dst = moves[m].dst & 31, src = moves[m].src & 31;
+                const uint8_t* from = tiles + (int64_t)(moves[m].src >> 5) * c.tile_bytes;
+                if (((dst & 15) >> 2) == g) {
+                    const uint32_t* sw = (const uint32_t*)(from + KvTile<W>::kValues) +
+                                         kv_word_at(Q, (lane & 15) + 16 * ((src & 15) >> 2));
+                    const int code = kv_code(__hip_atomic_load(sw, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                             4 * (src >> 4) + (src & 3));
+                    const int at = 4 * kv_nibble(4 * (dst >> 4) + (dst & 3));
+                    word = (word & ~(15u << at)) | ((uint32_t)code << at);
+                    any = true;
+                }
+                if ((dst & 15) == (lane & 15) && (dst >> 4) == Q / (W / 32))
+                    ((uint32_t*)tile)[w] =
+                        ((const uint32_t*)from)[kv_word_at((src >> 4) * (W / 32) + Q % (W / 32), (src & 15) + 16 * g)];
+            }
+            if (any)
+                __hip_atomic_store(to, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        for (int m = m0 + tid; m < m1; m += 256) {
+            const KvMove mv = moves[m];
+            const uint8_t* from = tiles + (int64_t)(mv.src >> 5) * c.tile_bytes;
+            ((uint32_t*)(tile + KvTile<W>::kKeyScales))[mv.dst & 31] =
+                ((const uint32_t*)(from + KvTile<W>::kKeyScales))[mv.src & 31];
+            ((uint32_t*)(tile + KvTile<W>::kValueScales))[mv.dst & 31] =
+                ((const uint32_t*)(from + KvTile<W>::kValueScales))[mv.src & 31];
+            c.pos[row + mv.dst] = mv.pos;
+            c.weight[row + mv.dst] = mv.weight;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_kv_clear(const KvView& c, hipStream_t stream)
+{
+    const int64_t n = (int64_t)c.n_slots * c.H * c.cap;
+    const int64_t blocks = (n + 2047) / 2048 < 2048 ? (n + 2047) / 2048 : 2048;
+    hipLaunchKernelGGL(kv_clear_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, c);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hipStream_t stream)
+{
+    const int64_t blocks = (c.cap + 4095) / 4096 < 64 ? (c.cap + 4095) / 4096 : 64;
+    hipLaunchKernelGGL(kv_reset_kernel, dim3((unsigned)blocks, c.H, B), dim3(256), 0, stream, c, slots);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, const void* k, const void* v,
+                            int dtype, int64_t ld, int32_t max_rows, const int32_t* nodes, const int32_t* count,
+                            const float* weight, hipStream_t stream)
+{
+    // tiles that max_rows rows can touch from any length on
+    int64_t tiles = ((int64_t)max_rows + kKvTile - 1 + kKvTile - 1) / kKvTile;
+    tiles = tiles < c.tiles ? tiles : c.tiles;
+    const dim3 grid((unsigned)(tiles < kMaxGridTiles ? tiles : kMaxGridTiles), c.H, B), block(256);
+#define OIL_KV_APPEND(W, T)                                                                                       \
+    hipLaunchKernelGGL((kv_append_kernel<W, T>), grid, block, 0, stream, c, slots, (const T*)k, (const T*)v, ld, \
+                       max_rows, nodes, count, weight)
+    if (c.W == 64 && dtype == 0)
+        OIL_KV_APPEND(64, float);
+    else if (c.W == 64)
+        OIL_KV_APPEND(64, uint16_t);
+    else if (dtype == 0)
+        OIL_KV_APPEND(128, float);
+    else
+        OIL_KV_APPEND(128, uint16_t);
+#undef OIL_KV_APPEND
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvView& c, const int32_t* slots, int32_t B, int64_t first, int64_t n, void* k_out,
+                          void* v_out, int dtype, hipStream_t stream)
+{
+    const int64_t tiles = (first + n - 1) / kKvTile - first / kKvTile + 1;
+    const dim3 grid((unsigned)(tiles < kMaxGridTiles ? tiles : kMaxGridTiles), c.H, B), block(256);
+#define OIL_KV_READ(W, T)                                                                                 \
+    hipLaunchKernelGGL((kv_read_kernel<W, T>), grid, block, 0, stream, c, slots, first, n, (T*)k_out, (T*)v_out)
+    if (c.W == 64 && dtype == 0)
+        OIL_KV_READ(64, float);
+    else if (c.W == 64)
+        OIL_KV_READ(64, uint16_t);
+    else if (dtype == 0)
+        OIL_KV_READ(128, float);
+    else
+        OIL_KV_READ(128, uint16_t);
+#undef OIL_KV_READ
+    return hipGetLastError();
+}
+
+size_t kv_evict_workspace_bytes(const KvView& c, int32_t B, int64_t keep)
+{
+    return (size_t)B * c.H * (size_t)kv_moves_stride(c.cap, keep);
+}
+
+hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int64_t keep, int64_t recent,
+                           void* workspace, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv_select_kernel, dim3(c.H, B), dim3(kSelect), 0, stream, c, slots, keep, recent,
+                       (uint8_t*)workspace);
+    const int64_t tiles = (keep + kKvTile - 1) / kKvTile;
+    const dim3 grid((unsigned)(tiles < 1024 ? tiles : 1024), c.H, B);
+    if (c.W == 64)
+        hipLaunchKernelGGL(kv_move_kernel<64>, grid, dim3(256), 0, stream, c, slots, keep, (const uint8_t*)workspace);
+    else
+        hipLaunchKernelGGL(kv_move_kernel<128>, grid, dim3(256), 0, stream, c, slots, keep,
+                           (const uint8_t*)workspace);
+    return hipGetLastError();
+}
+
+}  // namespace oil
