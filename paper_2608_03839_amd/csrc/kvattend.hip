@@ -1,12 +1,36 @@
 // Attention over the verifier's 4-bit cache and the nodes of a draft tree, and
 // the attention weight that committed rows give to cached positions.
+//
+// attend: a wave streams 32-position tiles of one head straight into registers
+// in MFMA operand order and multiplies them with 16 NT rows (node, query head)
+// at once: S^T = K Q^T puts a row's scores into one lane column, and the
+// probabilities of a lane are, as they are, the operand of O^T = V^T P^T.  No
+// tile passes through LDS and nothing in the loop waits for another wave.
+//
+// A code c of a 4-bit row enters the product as the binary16 subnormal c 2^-24
+// (its nibble is the mantissa; the MFMA takes subnormals as they are) or, for
+// every other pair, as 16 c 2^-24: eight codes cost four ANDs and a shift.
+// Queries are scaled to binary16 by a power of two per row, so every product is
+// exact and sums are binary32; z enters as z sum(q), and the values' z as
+// sum(p z), both in binary32.
+//
+// The softmax keeps, per row, a reference m and sums relative to it (base 2).
+// m moves only when a score passes it by 2^15, to 11 below the maximum: then
+// p <= 2^15 fits binary16, and a p below 2^-32 of the largest is the first that
+// rounds to nothing.  p times the value row's s, over a power of two E at or above every s
+// so far, is what the second product takes, rounded to binary16 (2^-12
+// relative).  z and s c may be far larger than the value they add up to, so that
+// rounding must not reach s c alone: with one row tile a second operand takes
+// what the first leaves (the product has time to spare there); with more, z is
+// weighted by the rounded p (z / s times the operand).  Tiles in which some s is
+// below a bound times E, where operands would lose bits, take two bf16 operands.
+//
+// The tree's nodes come as further tiles in bf16 (p rounded to 2^-9).
 #include "kv.hpp"
 
 namespace oil {
 
 namespace {
-
-constexpr int kChunk = 256;
 
 template <int W>
 __device__ __forceinline__ float kv_key_dot(const uint8_t* tile, int key, const float* q)
@@ -25,105 +49,665 @@ __device__ __forceinline__ float kv_key_dot(const uint8_t* tile, int key, const 
     return kv_s(pair) * dot + kv_z(pair) * sum;
 }
 
-template <int W>
-__device__ __forceinline__ float kv_value_at(const uint8_t* tile, int key, int d)
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLow = -1e38f;      // m of a row that has seen nothing
+constexpr float kHead = 11.f;       // the maximum's place above m
+constexpr float kRoom = 15.f;       // and the most a score may pass m by
+
+// How the rounding of a value operand is met (see the top), and the smallest
+// s / E it is met by.
+template <int NT>
+struct KvRounding {
+    static constexpr bool kTwo = NT == 1;
+    static constexpr float kLeast = kTwo ? 0x1p-16f : 0x1p-6f;
+};
+
+struct KvAttend {
+    KvView c;
+    const int32_t* slots;
+    const uint16_t* q;
+    const uint16_t *k, *v;
+    const int32_t* n_nodes;
+    const uint32_t* mask;
+    uint16_t* out;
+    float* lse;
+    float* part_o;   // splits > 1: unnormalised rows,
+    float* part_ml;  // and each one's (m, sum)
+    int64_t q_ld, ld;
+    int32_t B, Hq, G, max_nodes, splits, row_blocks;
+    float scale;
+};
+
+union Frag {
+    u32x4 w;
+    h16x8 h;
+    bf16x8 b;
+};
+
+// A dword's eight codes as binary16 subnormals: pairs 1 and 3 are 16 times too large.
+__device__ __forceinline__ h16x8 kv_codes(uint32_t w)
 {
-    const uint32_t w = ((const uint32_t*)(tile + KvTile<W>::kValues))[kv_word_at(d >> 4, (d & 15) + 16 * ((key & 15) >> 2))];
-    const uint32_t pair = *(const uint32_t*)(tile + KvTile<W>::kValueScales + key * 4);
-    return kv_z(pair) + kv_s(pair) * (float)kv_code(w, 4 * (key >> 4) + (key & 3));
+    Frag f;
+    const uint32_t x = w >> 8;
+    f.w[0] = w & 0x000F000Fu;
+    f.w[1] = w & 0x00F000F0u;
+    f.w[2] = x & 0x000F000Fu;
+    f.w[3] = x & 0x00F000F0u;
+    return f.h;
 }
 
-// One workgroup per row: chunks of 256 positions, a score a thread, then the
-// values by column with the running maximum and sum of the softmax.
-template <int W>
-__global__ __launch_bounds__(256) void kv_attend_kernel(KvView c, const int32_t* __restrict__ slots,
-                                                        const uint16_t* __restrict__ q, int64_t q_ld, int32_t Hq,
-                                                        const uint16_t* __restrict__ k,
-                                                        const uint16_t* __restrict__ v, int64_t ld,
-                                                        const int32_t* __restrict__ n_nodes,
-                                                        const uint32_t* __restrict__ mask, int32_t max_nodes,
-                                                        float scale, uint16_t* __restrict__ out,
-                                                        float* __restrict__ lse)
+__device__ __forceinline__ uint32_t pack_f16(float a, float b)
 {
-    __shared__ float qs[W], p[kChunk], red[8];
-    __shared__ float half[W];
-    const int a = blockIdx.x, i = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-    const int h = a / (Hq / c.H), D = c.D;
-    const int slot = kv_slot(c, slots, b);
-    int m = n_nodes ? n_nodes[b] : max_nodes;
-    m = m < 0 ? 0 : m > max_nodes ? max_nodes : m;
-    const bool live = slot >= 0 && i < m;
-    const int32_t len = live ? kv_len(c, slot) : 0;
-    const int extra = live && k ? m : 0;
-    const int64_t row = ((int64_t)b * max_nodes + i) * q_ld + (int64_t)a * D;
-    if (tid < W)
-        qs[tid] = live && tid < D ? bf16_bits_to_float(q[row + tid]) : 0.f;
-    __syncthreads();
-    float top = -INFINITY, total = 0.f, acc = 0.f;
-    const int d = tid % W, part = tid / W;  // column, and share of the chunk
-    const uint8_t* tiles = slot < 0 ? nullptr : kv_tiles(c, slot, h);
-    for (int64_t j0 = 0; j0 < (int64_t)len + extra; j0 += kChunk) {
-        const int64_t j = j0 + tid;
-        float s = -INFINITY;
-        if (j < len) {
-            s = scale * kv_key_dot<W>(tiles + j / kKvTile * c.tile_bytes, (int)(j % kKvTile), qs);
-        } else if (j < (int64_t)len + extra) {
-            const int u = (int)(j - len);
-            const uint32_t* bits = mask ? mask + ((int64_t)b * max_nodes + i) * ((max_nodes + 31) / 32) : nullptr;
-            if (bits ? (bits[u >> 5] >> (u & 31)) & 1 : u <= i) {
-                const uint16_t* kr = k + ((int64_t)b * max_nodes + u) * ld + (int64_t)h * D;
-                float dot = 0.f;
-                for (int e = 0; e < D; e++)
-                    dot += qs[e] * bf16_bits_to_float(kr[e]);
-                s = scale * dot;
+    const floatx2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, h16x2));
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const floatx2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+// A dword's eight codes in bf16, without the factors.
+__device__ __forceinline__ bf16x8 kv_codes_bf16(uint32_t w)
+{
+    Frag f;
+#pragma unroll
+    for (int p = 0; p < 4; p++)
+        f.w[p] = pack_bf16((float)kv_code(w, 2 * p), (float)kv_code(w, 2 * p + 1));
+    return f.b;
+}
+
+// Over the four lanes that share lane % 16.
+__device__ __forceinline__ float quad_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16, 64));
+    return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float quad_sum(float x)
+{
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
+// Raw bf16 operand of a row for columns 32 ks + 8 g ..; zeros past D or for no row.
+__device__ __forceinline__ u32x4 kv_raw(const uint16_t* row, int d, int D)
+{
+    u32x4 z = {0, 0, 0, 0};
+    return row && d < D ? *(const u32x4*)(row + d) : z;
+}
+
+// Scaled binary16 operands of a row, and the factors of its scores in base 2:
+// x = c1 (s dot) + c2 z.
+template <int W>
+__device__ __forceinline__ void kv_query(const uint16_t* row, int g, int D, float scale, Frag (&f)[W / 32], float* c1,
+                                         float* c2)
+{
+    u32x4 raw[W / 32];
+    uint32_t top = 0;
+    float sum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < W / 32; ks++) {
+        raw[ks] = kv_raw(row, 32 * ks + 8 * g, D);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t lo = raw[ks][j] & 0x7FFFu, hi = (raw[ks][j] >> 16) & 0x7FFFu;
+            top = max(top, max(lo, hi));
+            sum += __uint_as_float(raw[ks][j] << 16) + __uint_as_float(raw[ks][j] & 0xFFFF0000u);
+        }
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    const int e = max((int)(top >> 7) - 127, -112);
+    const float by = __uint_as_float((uint32_t)(127 + 14 - e) << 23);  // the largest value to [2^14, 2^15)
+#pragma unroll
+    for (int ks = 0; ks < W / 32; ks++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const float m = j & 1 ? by * 0.0625f : by;
+            f[ks].w[j] = pack_f16(__uint_as_float(raw[ks][j] << 16) * m,
+                                  __uint_as_float(raw[ks][j] & 0xFFFF0000u) * m);
+        }
+    *c1 = scale * kLog2e * __uint_as_float((uint32_t)min(127 + 24 - 14 + e, 254) << 23);
+    *c2 = scale * kLog2e * quad_sum(sum);
+}
+
+// One tile of the cache in registers.
+template <int W>
+struct KvTileRegs {
+    u32x4 k[W / 64], v[W / 64], ks[2], vs[2];
+
+    __device__ __forceinline__ void load(const uint8_t* tile, int lane)
+    {
+        const int g = lane >> 4;
+#pragma unroll
+        for (int p = 0; p < W / 64; p++)
+            k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
+#pragma unroll
+        for (int p = 0; p < W / 64; p++)
+            v[p] = *(const u32x4*)(tile + KvTile<W>::kValues + p * 1024 + lane * 16);
+#pragma unroll
+        for (int a = 0; a < 2; a++) {
+            ks[a] = *(const u32x4*)(tile + KvTile<W>::kKeyScales + 64 * a + 16 * g);
+            vs[a] = *(const u32x4*)(tile + KvTile<W>::kValueScales + 64 * a + 16 * g);
+        }
+    }
+    __device__ __forceinline__ uint32_t key_word(int Q) const { return k[Q >> 2][Q & 3]; }
+    __device__ __forceinline__ uint32_t value_word(int Q) const { return v[Q >> 2][Q & 3]; }
+};
+
+// The running state of a wave's 16 NT rows; a lane's column is row lane % 16 of
+// each 16.
+template <int W, int NT>
+struct KvRows {
+    floatx4 o[NT][W / 16];  // O^T / (E 2^24)
+    float m[NT], l[NT], w[NT];
+    float E;
+
+    __device__ __forceinline__ void init()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            m[t] = kLow;
+            l[t] = w[t] = 0.f;
+#pragma unroll
+            for (int mt = 0; mt < W / 16; mt++)
+                o[t][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        E = 0x1p-100f;
+    }
+    __device__ __forceinline__ void fade(int t, float by)
+    {
+        l[t] *= by;
+        w[t] *= by;
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++)
+            o[t][mt] *= by;
+    }
+    // m of row t up to `top` (any lane's; the row's lanes agree afterwards).
+    __device__ __forceinline__ void raise(int t, float top)
+    {
+        const float m_new = fmaxf(m[t], quad_max(top) - kHead);
+        fade(t, __builtin_amdgcn_exp2f(m[t] - m_new));
+        m[t] = m_new;
+    }
+    // E up to a power of two at or above `top` (any lane's).
+    __device__ __forceinline__ void widen(float top)
+    {
+        top = quad_max(top);  // lanes that share lane / 16 hold the same rows
+        const float up = __uint_as_float((__float_as_uint(top) + 0x7FFFFFu) & 0x7F800000u);
+        if (up > E) {
+            const float by = E / up;
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+#pragma unroll
+                for (int mt = 0; mt < W / 16; mt++)
+                    o[t][mt] *= by;
+            E = up;
+        }
+    }
+};
+
+// A tile of `valid` cached positions (32, or fewer at the end of a slot).
+template <int W, int NT, bool END>
+__device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int lane, const Frag (&q)[NT][W / 32],
+                                        const float (&c1)[NT], const float (&c2)[NT], KvRows<W, NT>& R)
+{
+    const int g = lane >> 4;
+    float ks[8], kz[8], vs[8], vz[8];
+    bool in[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const int key = 16 * (e >> 2) + 4 * g + (e & 3);
+        in[e] = !END || key < valid;
+        ks[e] = kv_s(T.ks[e >> 2][e & 3]);
+        kz[e] = kv_z(T.ks[e >> 2][e & 3]);
+        vs[e] = in[e] ? kv_s(T.vs[e >> 2][e & 3]) : 0.f;
+        vz[e] = in[e] ? kv_z(T.vs[e >> 2][e & 3]) : 0.f;
+    }
+    float hi = 0.f, lo = INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        hi = fmaxf(hi, vs[e]);
+        lo = fminf(lo, in[e] ? vs[e] : INFINITY);
+    }
+    if (__any(hi > R.E))
+        R.widen(hi);
+    const float by = 1.f / R.E;
+    constexpr bool kTwo = KvRounding<NT>::kTwo;
+    const bool rare = __any(lo < R.E * KvRounding<NT>::kLeast);
+    float vq[8];  // z over the operand's factor
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        vs[e] *= e & 2 ? by * 0.0625f : by;
+        vq[e] = kTwo || (END && !in[e]) ? 0.f : vz[e] * __builtin_amdgcn_rcpf(vs[e]);
+    }
+    floatx4 S[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; t++)
+        S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int a = 0; a < 2; a++)
+#pragma unroll
+        for (int s = 0; s < W / 32; s++) {
+            const h16x8 kf = kv_codes(T.key_word(a * (W / 32) + s));
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+                S[t][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[t][s].h, S[t][a], 0, 0, 0);
+        }
+    Frag p[NT], low[NT];  // low: what the first operands leave
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        float x[8];
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], fmaf(kz[e], c2[t], -R.m[t]));
+            if (END)
+                x[e] = in[e] ? x[e] : -INFINITY;
+            top = fmaxf(top, x[e]);
+        }
+        if (__any(top > kRoom)) {
+            top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], kz[e] * c2[t]);
+                if (END)
+                    x[e] = in[e] ? x[e] : -INFINITY;
+                top = fmaxf(top, x[e]);
+            }
+            R.raise(t, top);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], fmaf(kz[e], c2[t], -R.m[t]));
+            if (END)
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    x[e] = in[e] ? x[e] : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            x[e] = __builtin_amdgcn_exp2f(x[e]);
+            R.l[t] += x[e];
+            if (kTwo || rare)
+                R.w[t] = fmaf(x[e], vz[e], R.w[t]);
+            x[e] *= vs[e];
+        }
+        if (rare) {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                x[e] *= e & 2 ? 0x1p-20f : 0x1p-24f;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+                low[t].w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
+                                        x[2 * j + 1] - __uint_as_float(p[t].w[j] & 0xFFFF0000u));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                p[t].w[j] = pack_f16(x[2 * j], x[2 * j + 1]);
+            if (kTwo) {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    low[t].w[j] = pack_f16(x[2 * j] - (float)p[t].h[2 * j], x[2 * j + 1] - (float)p[t].h[2 * j + 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    R.w[t] = fmaf((float)p[t].h[e], vq[e], R.w[t]);
             }
         }
-        float t = s;
-        bool nan = s != s;
-        for (int o = 32; o >= 1; o >>= 1)
-            t = fmaxf(t, __shfl_xor(t, o, 64));
-        if ((tid & 63) == 0)
-            red[tid >> 6] = t;
-        __syncthreads();
-        const float m_new = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), top);
-        const float base = m_new == -INFINITY ? 0.f : m_new;
-        float e = s == -INFINITY ? 0.f : nan ? s : expf(s - base);
-        p[tid] = e;
-        for (int o = 32; o >= 1; o >>= 1)
-            e += __shfl_xor(e, o, 64);
-        if ((tid & 63) == 0)
-            red[4 + (tid >> 6)] = e;
-        __syncthreads();
-        const float fade = top == -INFINITY ? 0.f : expf(top - base);
-        total = total * fade + (red[4] + red[5] + red[6] + red[7]);
-        top = m_new;
-        acc *= fade;
-        for (int x = part; x < kChunk; x += 256 / W) {
-            const int64_t jj = j0 + x;
-            const float px = p[x];
-            if (d >= D || px == 0.f)
-                continue;
-            if (jj < len)
-                acc += px * kv_value_at<W>(tiles + jj / kKvTile * c.tile_bytes, (int)(jj % kKvTile), d);
-            else if (jj < (int64_t)len + extra)
-                acc += px * bf16_bits_to_float(v[((int64_t)b * max_nodes + (jj - len)) * ld + (int64_t)h * D + d]);
+    }
+    if (rare) {
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++) {
+            const bf16x8 vf = kv_codes_bf16(T.value_word(mt));
+#pragma unroll
+            for (int t = 0; t < NT; t++) {
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low[t].b, R.o[t][mt], 0, 0, 0);
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[t].b, R.o[t][mt], 0, 0, 0);
+            }
         }
+    } else {
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++) {
+            const h16x8 vf = kv_codes(T.value_word(mt));
+#pragma unroll
+            for (int t = 0; t < NT; t++) {
+                if (kTwo)
+                    R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, low[t].h, R.o[t][mt], 0, 0, 0);
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[t].h, R.o[t][mt], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// A tile of the tree: nodes n0 .. n0 + 31 of m.  `node` is the node of each of a
+// lane's rows, -1 for none; `row` its queries.
+template <int W, int NT>
+__device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0, int m, int lane,
+                                         const int (&node)[NT], const uint16_t* const (&row)[NT], KvRows<W, NT>& R)
+{
+    const int g = lane >> 4, r = lane & 15, D = A.c.D;
+    uint32_t sees[NT], any = 0;
+    const uint32_t live = m - n0 >= 32 ? 0xFFFFFFFFu : (1u << (m - n0)) - 1;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        sees[t] = 0;
+        if (node[t] >= 0) {
+            if (A.mask)
+                sees[t] = A.mask[((int64_t)b * A.max_nodes + node[t]) * ((A.max_nodes + 31) / 32) + n0 / 32] & live;
+            else if (node[t] >= n0)
+                sees[t] = (node[t] - n0 >= 31 ? 0xFFFFFFFFu : (2u << (node[t] - n0)) - 1) & live;
+        }
+        any |= sees[t];
+    }
+    if (!__any(any != 0))
+        return;
+    const int64_t base = ((int64_t)b * A.max_nodes + n0) * A.ld + (int64_t)h * D;
+    if (R.E < 1.f)
+        R.widen(1.f);
+    const float by = 0x1p-24f / R.E;
+    floatx4 S[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; t++)
+        S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < W / 32; s++) {
+        Frag kf[2];
+#pragma unroll
+        for (int a = 0; a < 2; a++)
+            kf[a].w = kv_raw(n0 + 16 * a + r < m ? A.k + base + (int64_t)(16 * a + r) * A.ld : nullptr,
+                             32 * s + 8 * g, D);
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            Frag qf;
+            qf.w = kv_raw(row[t], 32 * s + 8 * g, D);
+#pragma unroll
+            for (int a = 0; a < 2; a++)
+                S[t][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a].b, qf.b, S[t][a], 0, 0, 0);
+        }
+    }
+    Frag p[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        float x[8], top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const bool on = (sees[t] >> (16 * (e >> 2) + 4 * g + (e & 3))) & 1;
+            x[e] = on ? S[t][e >> 2][e & 3] * (A.scale * kLog2e) : -INFINITY;
+            top = fmaxf(top, x[e]);
+        }
+        if (__any(top - R.m[t] > kRoom))
+            R.raise(t, top);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            x[e] = __builtin_amdgcn_exp2f(x[e] - R.m[t]);
+            R.l[t] += x[e];
+            x[e] *= by;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+    }
+    bool odd = false;
+#pragma unroll
+    for (int mt = 0; mt < W / 16; mt++) {
+        const int d = 16 * mt + r;
+        Frag vf;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            uint32_t two = 0;
+#pragma unroll
+            for (int x = 0; x < 2; x++) {
+                const int e = 2 * j + x, key = 16 * (e >> 2) + 4 * g + (e & 3);
+                uint32_t u = n0 + key < m && d < D ? A.v[base + (int64_t)key * A.ld + d] : 0;
+                if ((u & 0x7F80u) == 0x7F80u) {  // not finite: added below, to the rows that see it
+                    odd = true;
+                    u = 0;
+                }
+                two |= u << (16 * x);
+            }
+            vf.w[j] = two;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; t++)
+            R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.b, p[t].b, R.o[t][mt], 0, 0, 0);
+    }
+    if (__any(odd)) {
+        for (int key = 0; key < 32 && n0 + key < m; key++)
+#pragma unroll
+            for (int mt = 0; mt < W / 16; mt++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int d = 16 * mt + 4 * g + i;
+                    const uint32_t u = d < D ? A.v[base + (int64_t)key * A.ld + d] : 0;
+                    if ((u & 0x7F80u) == 0x7F80u)
+#pragma unroll
+                        for (int t = 0; t < NT; t++)
+                            if ((sees[t] >> key) & 1)
+                                R.o[t][mt][i] += bf16_bits_to_float(u);
+                }
+    }
+}
+
+constexpr int kAttendWaves = 4;
+
+// Parts that a slot's units (tiles of the cache and of the tree) are split
+// into: at least two units a wave.
+__device__ __forceinline__ int kv_parts(int64_t units, int splits)
+{
+    const int64_t most = units / (2 * kAttendWaves);
+    return most < 1 ? 1 : most < splits ? (int)most : splits;
+}
+
+__device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
+{
+    if (slot < 0)
+        return 0;
+    const int m = A.n_nodes ? A.n_nodes[b] : A.max_nodes;
+    return m < 0 ? 0 : m > A.max_nodes ? A.max_nodes : m;
+}
+
+template <int W, int NT>
+__global__ __launch_bounds__(256) void kv_attend_kernel(KvAttend A)
+{
+    constexpr int kRows = 16 * NT;
+    __shared__ float sm[kAttendWaves][kRows], sl[kAttendWaves][kRows];
+    __shared__ floatx4 so[kAttendWaves / 2][NT][W / 16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    // the row blocks of one part of a head run on one XCD (its L2 serves the
+    // part's tiles to all of them)
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    const int rb = local % A.row_blocks, part = local / A.row_blocks * 8 + xcd;
+    if (part >= A.B * A.c.H * A.splits)
+        return;
+    const int sp = part % A.splits, h = part / A.splits % A.c.H, b = part / A.splits / A.c.H;
+    const int slot = kv_slot(A.c, A.slots, b);
+    const int m = kv_live_nodes(A, b, slot), D = A.c.D;
+    const int32_t len = slot < 0 ? 0 : kv_len(A.c, slot);
+    const bool dead = rb * kRows >= m * A.G;  // no live row
+    if (dead && A.splits > 1)
+        return;
+    int node[NT];
+    const uint16_t* row[NT];
+    Frag q[NT][W / 32];
+    float c1[NT], c2[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        const int r = rb * kRows + 16 * t + r16;
+        node[t] = r < m * A.G ? r / A.G : -1;
+        row[t] = node[t] < 0 ? nullptr
+                             : A.q + ((int64_t)b * A.max_nodes + node[t]) * A.q_ld +
+                                   (int64_t)(h * A.G + r % A.G) * D;
+        kv_query<W>(row[t], g, D, A.scale, q[t], &c1[t], &c2[t]);
+    }
+    const int64_t cached = ((int64_t)len + kKvTile - 1) / kKvTile;
+    const int64_t units = dead ? 0 : cached + (A.k ? (m + 31) / 32 : 0);
+    const int parts = kv_parts(units, A.splits);
+    if (sp >= parts)
+        return;
+    const int64_t u0 = units * sp / parts, u1 = units * (sp + 1) / parts;
+    KvRows<W, NT> R;
+    R.init();
+    const uint8_t* tiles = slot < 0 ? nullptr : kv_tiles(A.c, slot, h);
+    const int64_t full = len / kKvTile < u1 ? len / kKvTile : u1;  // tiles of 32 positions end here
+    int64_t u = u0 + wave;
+    if (u < full) {
+        KvTileRegs<W> now, next;
+        now.load(tiles + u * KvTile<W>::kBytes, lane);
+        for (; u + kAttendWaves < full; u += kAttendWaves) {
+            next.load(tiles + (u + kAttendWaves) * KvTile<W>::kBytes, lane);
+            kv_tile<W, NT, false>(now, 32, lane, q, c1, c2, R);
+            now = next;
+        }
+        kv_tile<W, NT, false>(now, 32, lane, q, c1, c2, R);
+        u += kAttendWaves;
+    }
+    if (u < u1 && u < cached) {
+        KvTileRegs<W> now;
+        now.load(tiles + u * KvTile<W>::kBytes, lane);
+        kv_tile<W, NT, true>(now, (int)(len - u * kKvTile), lane, q, c1, c2, R);
+        u += kAttendWaves;
+    }
+    for (; u < u1; u += kAttendWaves)
+        kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, node, row, R);
+    // the waves' shares, relative to the largest m
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        R.l[t] = quad_sum(R.l[t]);
+        R.w[t] = quad_sum(R.w[t]);
+        if (g == 0) {
+            sm[wave][16 * t + r16] = R.m[t];
+            sl[wave][16 * t + r16] = R.l[t];
+        }
+    }
+    __syncthreads();
+    float top[NT], total[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        top[t] = kLow;
+#pragma unroll
+        for (int x = 0; x < kAttendWaves; x++)
+            top[t] = fmaxf(top[t], sm[x][16 * t + r16]);
+        total[t] = 0.f;
+#pragma unroll
+        for (int x = 0; x < kAttendWaves; x++)
+            total[t] += sl[x][16 * t + r16] * __builtin_amdgcn_exp2f(sm[x][16 * t + r16] - top[t]);
+        const float f = __builtin_amdgcn_exp2f(R.m[t] - top[t]), of = R.E * 0x1p24f;
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : fmaf(R.o[t][mt][i], of, R.w[t]) * f;
+    }
+#pragma unroll
+    for (int half = kAttendWaves / 2; half >= 1; half >>= 1) {
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+#pragma unroll
+                for (int mt = 0; mt < W / 16; mt++)
+                    so[wave - half][t][mt][lane] = R.o[t][mt];
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+#pragma unroll
+                for (int mt = 0; mt < W / 16; mt++)
+                    R.o[t][mt] += so[wave][t][mt][lane];
         __syncthreads();
     }
-    // the column's shares
-    for (int s = 1; s < 256 / W; s++) {
-        if (part == s)
-            half[d] = acc;
-        __syncthreads();
-        if (part == 0)
-            acc += half[d];
-        __syncthreads();
+    if (wave != 0)
+        return;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+        const int r = rb * kRows + 16 * t + r16;
+        if (A.splits > 1) {
+            const int64_t at = (int64_t)part * (A.row_blocks * kRows) + r;
+            if (g == 0)
+                ((floatx2*)A.part_ml)[at] = floatx2{top[t], total[t]};
+#pragma unroll
+            for (int mt = 0; mt < W / 16; mt++)
+                *(floatx4*)(A.part_o + at * W + 16 * mt + 4 * g) = R.o[t][mt];
+        } else if (r < A.max_nodes * A.G) {
+            const int64_t at = ((int64_t)b * A.max_nodes + r / A.G) * A.Hq + h * A.G + r % A.G;
+            const bool none = node[t] < 0 || total[t] == 0.f;
+            const float by = none ? 0.f : 1.f / total[t];
+            if (g == 0 && A.lse)
+                A.lse[at] = none ? -INFINITY : kLn2 * (top[t] + __builtin_amdgcn_logf(total[t]));
+#pragma unroll
+            for (int mt = 0; mt < W / 16; mt++)
+                if (16 * mt + 4 * g < D) {
+                    uint2 o;
+                    o.x = none ? 0u : pack_bf16(R.o[t][mt][0] * by, R.o[t][mt][1] * by);
+                    o.y = none ? 0u : pack_bf16(R.o[t][mt][2] * by, R.o[t][mt][3] * by);
+                    *(uint2*)(A.out + at * D + 16 * mt + 4 * g) = o;
+                }
+        }
     }
-    const int64_t at = ((int64_t)b * max_nodes + i) * Hq + a;
-    if (part == 0 && d < D)
-        out[at * D + d] = total == 0.f ? (uint16_t)0 : float_to_bf16_rne(acc / total);
-    if (tid == 0 && lse)
-        lse[at] = total == 0.f ? -INFINITY : top + logf(total);
+}
+
+// One wave per row: the parts of a row joined.
+template <int W>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_part)
+{
+    const int lane = threadIdx.x & 63, b = blockIdx.z, h = blockIdx.y, D = A.c.D;
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= A.max_nodes * A.G)
+        return;
+    const int slot = kv_slot(A.c, A.slots, b);
+    const int m = kv_live_nodes(A, b, slot);
+    const int64_t at = ((int64_t)b * A.max_nodes + r / A.G) * A.Hq + h * A.G + r % A.G;
+    float total = 0.f, top = kLow;
+    floatx2 o = {0.f, 0.f};
+    const int d = W == 128 ? 2 * lane : lane;
+    if (r < m * A.G) {
+        const int32_t len = kv_len(A.c, slot);
+        const int64_t units = ((int64_t)len + kKvTile - 1) / kKvTile + (A.k ? (m + 31) / 32 : 0);
+        const int parts = kv_parts(units, A.splits);
+        const int64_t first = (int64_t)(b * A.c.H + h) * A.splits;
+        floatx2 ml = {kLow, 0.f};
+        if (lane < parts)
+            ml = ((const floatx2*)A.part_ml)[(first + lane) * rows_per_part + r];
+        top = ml[0];
+#pragma unroll
+        for (int x = 32; x >= 1; x >>= 1)
+            top = fmaxf(top, __shfl_xor(top, x, 64));
+        const float f = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
+        total = ml[1] * f;
+#pragma unroll
+        for (int x = 32; x >= 1; x >>= 1)
+            total += __shfl_xor(total, x, 64);
+        for (int s = 0; s < parts; s++) {
+            const float fs = __shfl(f, s, 64);
+            if (fs == 0.f)
+                continue;
+            const float* from = A.part_o + ((first + s) * rows_per_part + r) * W + d;
+            if (W == 128) {
+                const floatx2 x = *(const floatx2*)from;
+                o[0] = fmaf(fs, x[0], o[0]);
+                o[1] = fmaf(fs, x[1], o[1]);
+            } else {
+                o[0] = fmaf(fs, from[0], o[0]);
+            }
+        }
+    }
+    const bool none = total == 0.f;
+    const float by = none ? 0.f : 1.f / total;
+    if (d < D) {
+        if (W == 128)
+            *(uint32_t*)(A.out + at * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
+        else
+            A.out[at * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
+    }
+    if (lane == 0 && A.lse)
+        A.lse[at] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }
 
 // One thread per position: every committed row's probability at it.
@@ -164,23 +748,84 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
 
 }  // namespace
 
-size_t kv_attend_workspace_bytes(const KvView&, int32_t, int32_t, int32_t) { return 256; }
+// Rows a workgroup takes, and the parts a slot is split into.
+struct KvPlan {
+    int nt, row_blocks, splits;
+};
+
+static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
+{
+    KvPlan p;
+    const int rows = max_nodes * (Hq / c.H);
+    p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.row_blocks = (rows + 16 * p.nt - 1) / (16 * p.nt);
+    const int64_t groups = (int64_t)B * c.H * p.row_blocks;
+    const int64_t want = p.nt == 4 ? 1024 : 2048;
+    int64_t s = (want + groups - 1) / groups;
+    const int64_t most = (c.tiles + OIL_NODES_MAX / 32) / (2 * kAttendWaves);
+    s = s < most ? s : most;
+    p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    return p;
+}
+
+static size_t kv_part_rows(const KvView& c, int32_t B, const KvPlan& p)
+{
+    return p.splits == 1 ? 0 : (size_t)B * c.H * p.splits * p.row_blocks * 16 * p.nt;
+}
+
+size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
+{
+    const size_t n = kv_part_rows(c, B, kv_plan(c, B, max_nodes, Hq));
+    return n * (c.W + 2) * sizeof(float) + 256;
+}
+
+template <int W>
+static void kv_attend_launch(const KvAttend& A, const KvPlan& p, hipStream_t stream)
+{
+    const int64_t parts = (int64_t)A.B * A.c.H * p.splits;
+    const dim3 grid((unsigned)((parts + 7) / 8 * 8 * p.row_blocks)), block(64 * kAttendWaves);
+    if (p.nt == 1)
+        hipLaunchKernelGGL((kv_attend_kernel<W, 1>), grid, block, 0, stream, A);
+    else if (p.nt == 2)
+        hipLaunchKernelGGL((kv_attend_kernel<W, 2>), grid, block, 0, stream, A);
+    else
+        hipLaunchKernelGGL((kv_attend_kernel<W, 4>), grid, block, 0, stream, A);
+    if (p.splits > 1)
+        hipLaunchKernelGGL(kv_join_kernel<W>, dim3((A.max_nodes * A.G + 3) / 4, A.c.H, A.B), dim3(256), 0, stream, A,
+                           p.row_blocks * 16 * p.nt);
+}
 
 hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
                             int32_t Hq, const void* k, const void* v, int64_t ld, const int32_t* n_nodes,
-                            const uint32_t* mask, int32_t max_nodes, float scale, void*, void* out, float* lse,
-                            hipStream_t stream)
+                            const uint32_t* mask, int32_t max_nodes, float scale, void* workspace, void* out,
+                            float* lse, hipStream_t stream)
 {
-    const dim3 grid(Hq, max_nodes, B);
-#define OIL_KV_ATTEND(W)                                                                                          \
-    hipLaunchKernelGGL(kv_attend_kernel<W>, grid, dim3(256), 0, stream, c, slots, (const uint16_t*)q, q_ld, Hq, \
-                       (const uint16_t*)k, (const uint16_t*)v, ld, n_nodes, mask, max_nodes, scale,             \
-                       (uint16_t*)out, lse)
+    const KvPlan p = kv_plan(c, B, max_nodes, Hq);
+    KvAttend A;
+    A.c = c;
+    A.slots = slots;
+    A.q = (const uint16_t*)q;
+    A.k = (const uint16_t*)k;
+    A.v = (const uint16_t*)v;
+    A.n_nodes = n_nodes;
+    A.mask = mask;
+    A.out = (uint16_t*)out;
+    A.lse = lse;
+    A.part_o = (float*)workspace;
+    A.part_ml = (float*)workspace + kv_part_rows(c, B, p) * c.W;
+    A.q_ld = q_ld;
+    A.ld = ld;
+    A.B = B;
+    A.Hq = Hq;
+    A.G = Hq / c.H;
+    A.max_nodes = max_nodes;
+    A.splits = p.splits;
+    A.row_blocks = p.row_blocks;
+    A.scale = scale;
     if (c.W == 64)
-        OIL_KV_ATTEND(64);
+        kv_attend_launch<64>(A, p, stream);
     else
-        OIL_KV_ATTEND(128);
-#undef OIL_KV_ATTEND
+        kv_attend_launch<128>(A, p, stream);
     return hipGetLastError();
 }
 
