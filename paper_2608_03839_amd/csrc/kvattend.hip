@@ -123,16 +123,44 @@ __device__ __forceinline__ bf16x8 kv_codes_bf16(uint32_t w)
     return f.b;
 }
 
+// A value beside its counterpart 32 (16) lanes away.
+__device__ __forceinline__ void swap32(float x, float* a, float* b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *a = __uint_as_float(r[0]);
+    *b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap16(float x, float* a, float* b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *a = __uint_as_float(r[0]);
+    *b = __uint_as_float(r[1]);
+}
+
 // Over the four lanes that share lane % 16.
 __device__ __forceinline__ float quad_max(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16, 64));
-    return fmaxf(x, __shfl_xor(x, 32, 64));
+    float a, b;
+    swap16(x, &a, &b);
+    swap32(fmaxf(a, b), &a, &b);
+    return fmaxf(a, b);
 }
 __device__ __forceinline__ float quad_sum(float x)
 {
-    x += __shfl_xor(x, 16, 64);
-    return x + __shfl_xor(x, 32, 64);
+    float a, b;
+    swap16(x, &a, &b);
+    swap32(a + b, &a, &b);
+    return a + b;
+}
+
+// The largest of a wave.
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = quad_max(x);
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x201F)));
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x101F)));
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x081F)));
+    return fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x041F)));
 }
 
 // Raw bf16 operand of a row for columns 32 ks + 8 g ..; zeros past D or for no row.
@@ -161,8 +189,7 @@ __device__ __forceinline__ void kv_query(const uint16_t* row, int g, int D, floa
             sum += __uint_as_float(raw[ks][j] << 16) + __uint_as_float(raw[ks][j] & 0xFFFF0000u);
         }
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    top = (uint32_t)quad_max((float)top);
     const int e = max((int)(top >> 7) - 127, -112);
     const float by = __uint_as_float((uint32_t)(127 + 14 - e) << 23);  // the largest value to [2^14, 2^15)
 #pragma unroll
@@ -177,28 +204,31 @@ __device__ __forceinline__ void kv_query(const uint16_t* row, int g, int D, floa
     *c2 = scale * kLog2e * quad_sum(sum);
 }
 
-// One tile of the cache in registers.
+// One tile of the cache in registers: its codes, and one (s, z) pair a lane (the
+// keys' in lanes 0 .. 31, the values' in the others).
 template <int W>
 struct KvTileRegs {
-    u32x4 k[W / 64], v[W / 64], ks[2], vs[2];
+    u32x4 k[W / 64], v[W / 64];
+    uint32_t pair;
 
     __device__ __forceinline__ void load(const uint8_t* tile, int lane)
     {
-        const int g = lane >> 4;
 #pragma unroll
         for (int p = 0; p < W / 64; p++)
             k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
 #pragma unroll
         for (int p = 0; p < W / 64; p++)
             v[p] = *(const u32x4*)(tile + KvTile<W>::kValues + p * 1024 + lane * 16);
-#pragma unroll
-        for (int a = 0; a < 2; a++) {
-            ks[a] = *(const u32x4*)(tile + KvTile<W>::kKeyScales + 64 * a + 16 * g);
-            vs[a] = *(const u32x4*)(tile + KvTile<W>::kValueScales + 64 * a + 16 * g);
-        }
+        pair = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + lane * 4);
     }
     __device__ __forceinline__ uint32_t key_word(int Q) const { return k[Q >> 2][Q & 3]; }
     __device__ __forceinline__ uint32_t value_word(int Q) const { return v[Q >> 2][Q & 3]; }
+};
+
+// LDS of a wave for the scales of its tile: s of the 32 keys, the factors of the
+// 32 value operands; then z of the keys, and what z of the values enters by.
+struct KvScales {
+    float s[64], z[64];
 };
 
 // The running state of a wave's 16 NT rows; a lane's column is row lane % 16 of
@@ -239,10 +269,10 @@ struct KvRows {
     // E up to a power of two at or above `top` (any lane's).
     __device__ __forceinline__ void widen(float top)
     {
-        top = quad_max(top);  // lanes that share lane / 16 hold the same rows
+        top = wave_max(top);
         const float up = __uint_as_float((__float_as_uint(top) + 0x7FFFFFu) & 0x7F800000u);
         if (up > E) {
-            const float by = E / up;
+            const float by = E * (1.f / up);
 #pragma unroll
             for (int t = 0; t < NT; t++)
 #pragma unroll
@@ -253,54 +283,64 @@ struct KvRows {
     }
 };
 
-// A tile of `valid` cached positions (32, or fewer at the end of a slot).
+// A tile of `valid` cached positions (32, or fewer at the end of a slot).  Each
+// lane prepares one pair; the eight of its rows' scores come back through LDS.
 template <int W, int NT, bool END>
-__device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int lane, const Frag (&q)[NT][W / 32],
-                                        const float (&c1)[NT], const float (&c2)[NT], KvRows<W, NT>& R)
+__device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int lane, KvScales& L,
+                                        const u32x4 (*q)[W / 32][64], const float (&c1)[NT], const float (&c2)[NT],
+                                        KvRows<W, NT>& R)
 {
-    const int g = lane >> 4;
-    float ks[8], kz[8], vs[8], vz[8];
-    bool in[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const int key = 16 * (e >> 2) + 4 * g + (e & 3);
-        in[e] = !END || key < valid;
-        ks[e] = kv_s(T.ks[e >> 2][e & 3]);
-        kz[e] = kv_z(T.ks[e >> 2][e & 3]);
-        vs[e] = in[e] ? kv_s(T.vs[e >> 2][e & 3]) : 0.f;
-        vz[e] = in[e] ? kv_z(T.vs[e >> 2][e & 3]) : 0.f;
-    }
-    float hi = 0.f, lo = INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        hi = fmaxf(hi, vs[e]);
-        lo = fminf(lo, in[e] ? vs[e] : INFINITY);
-    }
-    if (__any(hi > R.E))
-        R.widen(hi);
-    const float by = 1.f / R.E;
     constexpr bool kTwo = KvRounding<NT>::kTwo;
-    const bool rare = __any(lo < R.E * KvRounding<NT>::kLeast);
-    float vq[8];  // z over the operand's factor
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        vs[e] *= e & 2 ? by * 0.0625f : by;
-        vq[e] = kTwo || (END && !in[e]) ? 0.f : vz[e] * __builtin_amdgcn_rcpf(vs[e]);
+    const int g = lane >> 4;
+    const bool on = !END || (lane & 31) < valid, value = lane >= 32;
+    float s = on ? kv_s(T.pair) : 0.f, z = on ? kv_z(T.pair) : 0.f;
+    if (__any(value && s > R.E))
+        R.widen(value ? s : 0.f);
+    const bool rare = __any(value && on && s < R.E * KvRounding<NT>::kLeast);
+    if (value) {
+        const float by = 1.f / R.E;
+        s *= lane & 2 ? by * 0.0625f : by;
+        if (!kTwo && !rare)
+            z = on ? z * __builtin_amdgcn_rcpf(s) : 0.f;
     }
+    L.s[lane] = s;
+    L.z[lane] = z;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");  // the queries are read from LDS tile by tile: their registers are wanted
     floatx4 S[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; t++)
         S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int a = 0; a < 2; a++)
+    for (int s = 0; s < W / 32; s++) {
+        const h16x8 k0 = kv_codes(T.key_word(s)), k1 = kv_codes(T.key_word(W / 32 + s));
 #pragma unroll
-        for (int s = 0; s < W / 32; s++) {
-            const h16x8 kf = kv_codes(T.key_word(a * (W / 32) + s));
-#pragma unroll
-            for (int t = 0; t < NT; t++)
-                S[t][a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[t][s].h, S[t][a], 0, 0, 0);
+        for (int t = 0; t < NT; t++) {
+            Frag qf;
+            qf.w = q[t][s][lane];
+            S[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf.h, S[t][0], 0, 0, 0);
+            S[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf.h, S[t][1], 0, 0, 0);
         }
-    Frag p[NT], low[NT];  // low: what the first operands leave
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    float ks[8], kz[8], vs[8], vz[8];
+    bool in[8];
+#pragma unroll
+    for (int a = 0; a < 2; a++) {
+        const floatx4 x0 = *(const floatx4*)&L.s[16 * a + 4 * g], x1 = *(const floatx4*)&L.z[16 * a + 4 * g];
+        const floatx4 x2 = *(const floatx4*)&L.s[32 + 16 * a + 4 * g], x3 = *(const floatx4*)&L.z[32 + 16 * a + 4 * g];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            ks[4 * a + i] = x0[i];
+            kz[4 * a + i] = x1[i];
+            vs[4 * a + i] = x2[i];
+            vz[4 * a + i] = x3[i];
+            in[4 * a + i] = !END || 16 * a + 4 * g + i < valid;
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+    Frag p[NT], low[kTwo ? NT : 1];  // low: what the first operands leave
 #pragma unroll
     for (int t = 0; t < NT; t++) {
         float x[8];
@@ -345,8 +385,14 @@ __device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int l
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-                low[t].w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
+                low[0].w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
                                         x[2 * j + 1] - __uint_as_float(p[t].w[j] & 0xFFFF0000u));
+            }
+#pragma unroll
+            for (int mt = 0; mt < W / 16; mt++) {
+                const bf16x8 vf = kv_codes_bf16(T.value_word(mt));
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low[0].b, R.o[t][mt], 0, 0, 0);
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[t].b, R.o[t][mt], 0, 0, 0);
             }
         } else {
 #pragma unroll
@@ -359,21 +405,11 @@ __device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int l
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
-                    R.w[t] = fmaf((float)p[t].h[e], vq[e], R.w[t]);
+                    R.w[t] = fmaf((float)p[t].h[e], vz[e], R.w[t]);
             }
         }
     }
-    if (rare) {
-#pragma unroll
-        for (int mt = 0; mt < W / 16; mt++) {
-            const bf16x8 vf = kv_codes_bf16(T.value_word(mt));
-#pragma unroll
-            for (int t = 0; t < NT; t++) {
-                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low[t].b, R.o[t][mt], 0, 0, 0);
-                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[t].b, R.o[t][mt], 0, 0, 0);
-            }
-        }
-    } else {
+    if (!rare) {
 #pragma unroll
         for (int mt = 0; mt < W / 16; mt++) {
             const h16x8 vf = kv_codes(T.value_word(mt));
@@ -387,13 +423,29 @@ __device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int l
     }
 }
 
-// A tile of the tree: nodes n0 .. n0 + 31 of m.  `node` is the node of each of a
-// lane's rows, -1 for none; `row` its queries.
+// The node of row r of a head, -1 for none, and the row's queries.
+__device__ __forceinline__ int kv_row_of(const KvAttend& A, int b, int h, int m, int r, const uint16_t** row)
+{
+    if (r >= m * A.G) {
+        *row = nullptr;
+        return -1;
+    }
+    const int node = r / A.G;
+    *row = A.q + ((int64_t)b * A.max_nodes + node) * A.q_ld + (int64_t)(h * A.G + r - node * A.G) * A.c.D;
+    return node;
+}
+
+// A tile of the tree: nodes n0 .. n0 + 31 of m, for rows r0 ...
 template <int W, int NT>
-__device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0, int m, int lane,
-                                         const int (&node)[NT], const uint16_t* const (&row)[NT], KvRows<W, NT>& R)
+__device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0, int m, int lane, int r0,
+                                         KvRows<W, NT>& R)
 {
     const int g = lane >> 4, r = lane & 15, D = A.c.D;
+    int node[NT];
+    const uint16_t* row[NT];
+#pragma unroll
+    for (int t = 0; t < NT; t++)
+        node[t] = kv_row_of(A, b, h, m, r0 + 16 * t + r, &row[t]);
     uint32_t sees[NT], any = 0;
     const uint32_t live = m - n0 >= 32 ? 0xFFFFFFFFu : (1u << (m - n0)) - 1;
 #pragma unroll
@@ -515,11 +567,13 @@ __device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
 }
 
 template <int W, int NT>
-__global__ __launch_bounds__(256) void kv_attend_kernel(KvAttend A)
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAttend A)
 {
     constexpr int kRows = 16 * NT;
     __shared__ float sm[kAttendWaves][kRows], sl[kAttendWaves][kRows];
     __shared__ floatx4 so[kAttendWaves / 2][NT][W / 16][64];
+    __shared__ u32x4 sq[NT][W / 32][64];
+    __shared__ __align__(16) KvScales scales[kAttendWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
     // the row blocks of one part of a head run on one XCD (its L2 serves the
     // part's tiles to all of them)
@@ -534,19 +588,19 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(KvAttend A)
     const bool dead = rb * kRows >= m * A.G;  // no live row
     if (dead && A.splits > 1)
         return;
-    int node[NT];
-    const uint16_t* row[NT];
-    Frag q[NT][W / 32];
     float c1[NT], c2[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
-        const int r = rb * kRows + 16 * t + r16;
-        node[t] = r < m * A.G ? r / A.G : -1;
-        row[t] = node[t] < 0 ? nullptr
-                             : A.q + ((int64_t)b * A.max_nodes + node[t]) * A.q_ld +
-                                   (int64_t)(h * A.G + r % A.G) * D;
-        kv_query<W>(row[t], g, D, A.scale, q[t], &c1[t], &c2[t]);
+        Frag q[W / 32];
+        const uint16_t* row;
+        kv_row_of(A, b, h, m, rb * kRows + 16 * t + r16, &row);
+        kv_query<W>(row, g, D, A.scale, q, &c1[t], &c2[t]);
+        if (wave == 0)
+#pragma unroll
+            for (int s = 0; s < W / 32; s++)
+                sq[t][s][lane] = q[s].w;
     }
+    __syncthreads();
     const int64_t cached = ((int64_t)len + kKvTile - 1) / kKvTile;
     const int64_t units = dead ? 0 : cached + (A.k ? (m + 31) / 32 : 0);
     const int parts = kv_parts(units, A.splits);
@@ -563,20 +617,20 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(KvAttend A)
         now.load(tiles + u * KvTile<W>::kBytes, lane);
         for (; u + kAttendWaves < full; u += kAttendWaves) {
             next.load(tiles + (u + kAttendWaves) * KvTile<W>::kBytes, lane);
-            kv_tile<W, NT, false>(now, 32, lane, q, c1, c2, R);
+            kv_tile<W, NT, false>(now, 32, lane, scales[wave], sq, c1, c2, R);
             now = next;
         }
-        kv_tile<W, NT, false>(now, 32, lane, q, c1, c2, R);
+        kv_tile<W, NT, false>(now, 32, lane, scales[wave], sq, c1, c2, R);
         u += kAttendWaves;
     }
     if (u < u1 && u < cached) {
         KvTileRegs<W> now;
         now.load(tiles + u * KvTile<W>::kBytes, lane);
-        kv_tile<W, NT, true>(now, (int)(len - u * kKvTile), lane, q, c1, c2, R);
+        kv_tile<W, NT, true>(now, (int)(len - u * kKvTile), lane, scales[wave], sq, c1, c2, R);
         u += kAttendWaves;
     }
     for (; u < u1; u += kAttendWaves)
-        kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, node, row, R);
+        kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, rb * kRows, R);
     // the waves' shares, relative to the largest m
 #pragma unroll
     for (int t = 0; t < NT; t++) {
@@ -637,7 +691,7 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(KvAttend A)
                 *(floatx4*)(A.part_o + at * W + 16 * mt + 4 * g) = R.o[t][mt];
         } else if (r < A.max_nodes * A.G) {
             const int64_t at = ((int64_t)b * A.max_nodes + r / A.G) * A.Hq + h * A.G + r % A.G;
-            const bool none = node[t] < 0 || total[t] == 0.f;
+            const bool none = r >= m * A.G || total[t] == 0.f;
             const float by = none ? 0.f : 1.f / total[t];
             if (g == 0 && A.lse)
                 A.lse[at] = none ? -INFINITY : kLn2 * (top[t] + __builtin_amdgcn_logf(total[t]));
@@ -757,10 +811,10 @@ static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
 {
     KvPlan p;
     const int rows = max_nodes * (Hq / c.H);
-    p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 3;
     p.row_blocks = (rows + 16 * p.nt - 1) / (16 * p.nt);
     const int64_t groups = (int64_t)B * c.H * p.row_blocks;
-    const int64_t want = p.nt == 4 ? 1024 : 2048;
+    const int64_t want = p.nt > 1 ? 1024 : 2048;
     int64_t s = (want + groups - 1) / groups;
     const int64_t most = (c.tiles + OIL_NODES_MAX / 32) / (2 * kAttendWaves);
     s = s < most ? s : most;
@@ -789,7 +843,7 @@ static void kv_attend_launch(const KvAttend& A, const KvPlan& p, hipStream_t str
     else if (p.nt == 2)
         hipLaunchKernelGGL((kv_attend_kernel<W, 2>), grid, block, 0, stream, A);
     else
-        hipLaunchKernelGGL((kv_attend_kernel<W, 4>), grid, block, 0, stream, A);
+        hipLaunchKernelGGL((kv_attend_kernel<W, 3>), grid, block, 0, stream, A);
     if (p.splits > 1)
         hipLaunchKernelGGL(kv_join_kernel<W>, dim3((A.max_nodes * A.G + 3) / 4, A.c.H, A.B), dim3(256), 0, stream, A,
                            p.row_blocks * 16 * p.nt);
