@@ -37,22 +37,53 @@ __global__ __launch_bounds__(256) void kv_clear_kernel(KvView c)
             c.state[i] = 0;
 }
 
+// Workgroups of a request up to which the last one writes the slot's state
+// (each takes a ticket, so it has read the state before): past that the tickets,
+// one address over all XCDs, cost more than a launch of their own.
+constexpr int kTickets = 64;
+
 // Whether this workgroup is the last of `total` of its request to be done; the
-// ticket is left at zero then.  Whatever the workgroup read of the state comes
-// before.
+// ticket is left at zero then.  Nothing is published by it but the order of the
+// state's reads and its write, so it needs no fence over the data.
 __device__ __forceinline__ bool kv_last(const KvView& c, int slot, int total)
 {
     __shared__ int last;
     __syncthreads();
     if (threadIdx.x == 0) {
         int32_t* ticket = c.state + 4 * (int64_t)slot + kKvTicket;
-        __threadfence();
-        last = atomicAdd(ticket, 1) == total - 1;
+        last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == total - 1;
         if (last)
-            *ticket = 0;
+            __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     return last;
+}
+
+__device__ __forceinline__ void kv_advance(const KvView& c, int slot, int32_t len, int cnt)
+{
+    int32_t* st = c.state + 4 * (int64_t)slot;
+    const int64_t end = len + (int64_t)cnt, next = st[kKvNext] + (int64_t)cnt;
+    st[kKvLen] = (int32_t)(end < c.cap ? end : c.cap);
+    st[kKvNext] = next < INT32_MAX ? (int32_t)next : INT32_MAX;
+}
+
+// The state after an append (rows of max_rows, nodes, count) or, with max_rows
+// 0, a reset; one workgroup per request.
+__global__ __launch_bounds__(64) void kv_state_kernel(KvView c, const int32_t* __restrict__ slots, int32_t max_rows,
+                                                      const int32_t* __restrict__ nodes,
+                                                      const int32_t* __restrict__ count)
+{
+    __shared__ int bound;
+    const int b = blockIdx.x, slot = kv_slot(c, slots, b);
+    if (slot < 0)
+        return;
+    const int cnt = max_rows ? kv_count(nodes, count, b, max_rows, &bound) : 0;
+    if (threadIdx.x != 0)
+        return;
+    if (max_rows)
+        kv_advance(c, slot, kv_len(c, slot), cnt);
+    else
+        c.state[4 * (int64_t)slot + kKvLen] = c.state[4 * (int64_t)slot + kKvNext] = 0;
 }
 
 __global__ __launch_bounds__(256) void kv_reset_kernel(KvView c, const int32_t* __restrict__ slots)
@@ -67,10 +98,8 @@ __global__ __launch_bounds__(256) void kv_reset_kernel(KvView c, const int32_t* 
         c.pos[row + i] = -1;
         c.weight[row + i] = 0.f;
     }
-    if (kv_last(c, slot, gridDim.x * gridDim.y) && threadIdx.x == 0) {
-        c.state[4 * (int64_t)slot + kKvLen] = 0;
-        c.state[4 * (int64_t)slot + kKvNext] = 0;
-    }
+    if (gridDim.x * gridDim.y <= kTickets && kv_last(c, slot, gridDim.x * gridDim.y) && threadIdx.x == 0)
+        c.state[4 * (int64_t)slot + kKvLen] = c.state[4 * (int64_t)slot + kKvNext] = 0;
 }
 
 // (s, z) of a row with extremes lo, hi; `fine`: every value is finite.
@@ -85,55 +114,69 @@ __device__ __forceinline__ uint32_t kv_pair(float lo, float hi, bool fine)
     return s | z;
 }
 
-__device__ __forceinline__ uint32_t kv_quantise(float x, uint32_t pair)
+// x / s to the nearest, as the binary32 division has it: two corrections of
+// x * inv by the exact remainder, with inv the correctly rounded 1 / s
+// (Markstein).  s is at least kLeastScale, so no remainder that matters underflows.
+constexpr float kLeastScale = 0x1p-90f;
+
+__device__ __forceinline__ float kv_quotient(float x, float s, float inv)
 {
-    const float s = kv_s(pair);
-    if (!(s > 0.f))
-        return 0;
-    const float c = rintf((x - kv_z(pair)) / s);
-    return c < 0.f ? 0u : c > 15.f ? 15u : (uint32_t)c;
+    float q = x * inv;
+    q = fmaf(fmaf(-s, q, x), inv, q);
+    return fmaf(fmaf(-s, q, x), inv, q);
+}
+
+// Codes of 8 values that lie on [z, z + 15 s], a nibble each of bits 0 .. 3 of a
+// byte (two words of four).  Adding 1.5 2^23 rounds to the nearest whole number, ties to even.
+__device__ __forceinline__ void kv_quantise(const float* x, float s, float z, float inv, uint32_t (&w)[2])
+{
+    float q[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        q[e] = kv_quotient(x[e] - z, s, inv);
+    if (!(s >= kLeastScale))
+        for (int e = 0; e < 8; e++)
+            q[e] = s > 0.f ? (x[e] - z) / s : 0.f;
+    uint32_t c[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        c[e] = __float_as_uint(q[e] + 12582912.f) & 15u;
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        w[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | c[4 * i + 3] << 24;
+}
+
+// The dword of nibbles (element e in nibble e / 2 + 4 (e % 2)) of eight codes in bytes.
+__device__ __forceinline__ uint32_t kv_pack(uint32_t lo, uint32_t hi)
+{
+    // elements 0, 2 and 1, 3 of each word to 16-bit halves, low nibbles side by side
+    const uint32_t even = (lo & 0x0F000Fu) | (hi & 0x0F000Fu) << 8;         // e0 . e2 ., e4 . e6 .
+    const uint32_t odd = (lo >> 8 & 0x0F000Fu) | (hi >> 8 & 0x0F000Fu) << 8;  // e1 . e3 ., e5 . e7 .
+    const uint32_t a = (even | even >> 12) & 0xFFFFu, b = (odd | odd >> 12) & 0xFFFFu;
+    return a | b << 16;
 }
 
 template <int W, typename T>
-__device__ __forceinline__ void kv_load_row(const T* __restrict__ row, int D, int part, float (&x)[W / 8])
-{
+struct KvRowRegs {
+    u32x4 w[W / 64][sizeof(T) / 2];  // 8 values each
+
+    __device__ __forceinline__ void load(const T* row, int part, int D)
+    {
 #pragma unroll
-    for (int i = 0; i < W / 8; i += 8) {
-        const int d = part * (W / 8) + i;
-        if (d < D) {
-            if (sizeof(T) == 2) {
-                const u32x4 w = *(const u32x4*)(row + d);
+        for (int i = 0; i < W / 64; i++) {
+            const int d = part * (W / 8) + 8 * i;
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    x[i + 2 * j] = __uint_as_float(w[j] << 16);
-                    x[i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; j += 4) {
-                    const floatx4 w = *(const floatx4*)(row + d + j);
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        x[i + j + e] = w[e];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; j++)
-                x[i + j] = 0.f;
+            for (int j = 0; j < (int)sizeof(T) / 2; j++)
+                w[i][j] = d < D ? ((const u32x4*)(row + d))[j] : u32x4{0, 0, 0, 0};
         }
     }
-}
-
-// Bytes 0 .. 7 of codes -> a dword of nibbles (element e in nibble e / 2 + 4 (e % 2)).
-__device__ __forceinline__ uint32_t kv_pack(const uint32_t (&c)[8])
-{
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 8; e++)
-        w |= c[e] << (4 * kv_nibble(e));
-    return w;
-}
+    __device__ __forceinline__ float at(int i, int e) const
+    {
+        if (sizeof(T) == 4)
+            return __uint_as_float(w[i][e >> 2][e & 3]);
+        return __uint_as_float(e & 1 ? w[i][0][e >> 1] & 0xFFFF0000u : w[i][0][e >> 1] << 16);
+    }
+};
 
 template <int W, typename T>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t* __restrict__ slots,
@@ -142,8 +185,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
                                                         const int32_t* __restrict__ count,
                                                         const float* __restrict__ weight)
 {
-    constexpr int kRow = W + 8;
-    __shared__ __align__(8) uint8_t code[2][kKvTile][kRow];
+    constexpr int kRow = W / 4 + 1;  // dwords of a row of value codes in LDS
+    __shared__ __align__(16) uint32_t image[2 * KvTile<W>::kWords];  // the tile's codes as they are stored
+    __shared__ uint32_t vcode[kKvTile][kRow];
     __shared__ int bound;
     const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
     const int slot = kv_slot(c, slots, b);
@@ -157,33 +201,54 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
         uint8_t* tile = kv_tiles(c, slot, h) + first / kKvTile * c.tile_bytes;
         const int key = tid >> 3, part = tid & 7;
         const int64_t j = first + key;
-        const bool live = j >= len && j < end;
-        if (live) {  // the 8 lanes of a row alike
+        if (j >= len && j < end) {  // the 8 lanes of a row alike
             const int r = (int)(j - len), src = kv_source(nodes, b, max_rows, r);
             const int64_t at = ((int64_t)b * max_rows + src) * ld + (int64_t)h * c.D;
+            KvRowRegs<W, T> rows[2];
+            rows[0].load(k + at, part, c.D);
+            rows[1].load(v + at, part, c.D);
+#pragma unroll
             for (int side = 0; side < 2; side++) {
                 float x[W / 8];
-                kv_load_row<W, T>((side ? v : k) + at, c.D, part, x);
                 float lo = INFINITY, hi = -INFINITY;
-                bool fine = true;
+                bool odd = false;
 #pragma unroll
-                for (int i = 0; i < W / 8; i++) {
-                    const bool in = part * (W / 8) + i < c.D;
-                    lo = in ? fminf(lo, x[i]) : lo;
-                    hi = in ? fmaxf(hi, x[i]) : hi;
-                    fine = fine && fabsf(x[i]) < INFINITY;
+                for (int i = 0; i < W / 64; i++) {
+                    const bool in = part * (W / 8) + 8 * i < c.D;
+                    float l = INFINITY, m = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        x[8 * i + e] = rows[side].at(i, e);
+                        l = fminf(l, x[8 * i + e]);
+                        m = fmaxf(m, x[8 * i + e]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        odd = odd || __builtin_isunordered(x[8 * i + e], x[8 * i + e + 1]);
+                    lo = in ? fminf(lo, l) : lo;
+                    hi = in ? fmaxf(hi, m) : hi;
                 }
 #pragma unroll
                 for (int o = 1; o < 8; o <<= 1) {
                     lo = fminf(lo, __shfl_xor(lo, o, 8));
                     hi = fmaxf(hi, __shfl_xor(hi, o, 8));
-                    fine = __shfl_xor((int)fine, o, 8) && fine;
                 }
-                const uint32_t pair = kv_pair(lo, hi, fine);
+                const uint64_t odds = __ballot(odd);
+                const uint32_t pair = kv_pair(lo, hi, ((odds >> (tid & 56)) & 255) == 0);
+                const float s = kv_s(pair), z = kv_z(pair), inv = 1.f / s;
 #pragma unroll
-                for (int i = 0; i < W / 8; i++) {
-                    const int d = part * (W / 8) + i;
-                    code[side][key][d] = d < c.D ? (uint8_t)kv_quantise(x[i], pair) : (uint8_t)0;
+                for (int i = 0; i < W / 64; i++) {
+                    const int d = part * (W / 8) + 8 * i;
+                    uint32_t codes[2] = {0, 0};
+                    if (d < c.D)
+                        kv_quantise(x + 8 * i, s, z, inv, codes);
+                    if (side == 0) {
+                        image[kv_word_at((key >> 4) * (W / 32) + (d >> 5), (key & 15) + 16 * ((d & 31) >> 3))] =
+                            kv_pack(codes[0], codes[1]);
+                    } else {
+                        vcode[key][d / 4] = codes[0];
+                        vcode[key][d / 4 + 1] = codes[1];
+                    }
                 }
                 if (part == 0)
                     *(uint32_t*)(tile + (side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) + key * 4) = pair;
@@ -196,46 +261,56 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
             }
         }
         __syncthreads();
-        uint32_t* kw = (uint32_t*)tile;
-        uint32_t* vw = (uint32_t*)(tile + KvTile<W>::kValues);
-        for (int w = tid; w < KvTile<W>::kWords; w += 256) {
-            int Q, lane;
-            kv_word(w, &Q, &lane);
-            const int g = lane >> 4;
-            uint32_t e[8];
-            {
-                const int kk = (lane & 15) + 16 * (Q / (W / 32)), d = 32 * (Q % (W / 32)) + 8 * g;
-                const int64_t jj = first + kk;
-                if (jj >= len && jj < end) {
+        // four columns' value dwords a thread: eight positions' bytes side by side
+        if (tid < W) {
+            const int g = tid / (W / 4), d4 = tid % (W / 4);
+            uint32_t w[8];
 #pragma unroll
-                    for (int i = 0; i < 8; i++)
-                        e[i] = code[0][kk][d + i];
-                    kw[w] = kv_pack(e);
+            for (int e = 0; e < 8; e++) {
+                const int kk = 16 * (e >> 2) + 4 * g + (e & 3);
+                const int64_t jj = first + kk;
+                w[kv_nibble(e)] = jj >= len && jj < end ? vcode[kk][d4] : 0u;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                uint32_t word = 0;
+#pragma unroll
+                for (int n = 0; n < 8; n++)
+                    word |= ((w[n] >> (8 * i)) & 15u) << (4 * n);
+                const int d = 4 * d4 + i;
+                image[KvTile<W>::kWords + kv_word_at(d >> 4, (d & 15) + 16 * g)] = word;
+            }
+        }
+        __syncthreads();
+        if (first >= len && first + kKvTile <= end) {
+            for (int i = tid; i < KvTile<W>::kWords / 2; i += 256)
+                ((u32x4*)tile)[i] = ((const u32x4*)image)[i];
+        } else {
+            uint32_t* to = (uint32_t*)tile;
+            for (int w = tid; w < KvTile<W>::kWords; w += 256) {
+                int Q, lane;
+                kv_word(w, &Q, &lane);
+                const int64_t jj = first + (lane & 15) + 16 * (Q / (W / 32));
+                if (jj >= len && jj < end)
+                    to[w] = image[w];
+                uint32_t keep = 0;
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const int64_t kk = first + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
+                    any = any || (kk >= len && kk < end);
+                    if (kk < len)
+                        keep |= 15u << (4 * kv_nibble(e));
                 }
+                if (any)
+                    to[KvTile<W>::kWords + w] =
+                        image[KvTile<W>::kWords + w] | (keep ? to[KvTile<W>::kWords + w] & keep : 0u);
             }
-            const int d = 16 * Q + (lane & 15);
-            uint32_t keep = 0;
-            bool any = false;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const int kk = 16 * (i >> 2) + 4 * g + (i & 3);
-                const int64_t jj = first + kk;
-                const bool mine = jj >= len && jj < end;
-                e[i] = mine ? code[1][kk][d] : 0u;
-                any = any || mine;
-                if (jj < len)
-                    keep |= 15u << (4 * kv_nibble(i));
-            }
-            if (any)
-                vw[w] = kv_pack(e) | (keep ? vw[w] & keep : 0u);
         }
         __syncthreads();
     }
-    if (kv_last(c, slot, gridDim.x * gridDim.y) && tid == 0) {
-        const int64_t after = next + (int64_t)cnt;
-        c.state[4 * (int64_t)slot + kKvLen] = (int32_t)end;
-        c.state[4 * (int64_t)slot + kKvNext] = after < INT32_MAX ? (int32_t)after : INT32_MAX;
-    }
+    if (gridDim.x * gridDim.y <= kTickets && kv_last(c, slot, gridDim.x * gridDim.y) && tid == 0)
+        kv_advance(c, slot, len, cnt);
 }
 
 template <typename T>
@@ -524,6 +599,8 @@ hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hip
 {
     const int64_t blocks = (c.cap + 4095) / 4096 < 64 ? (c.cap + 4095) / 4096 : 64;
     hipLaunchKernelGGL(kv_reset_kernel, dim3((unsigned)blocks, c.H, B), dim3(256), 0, stream, c, slots);
+    if (blocks * c.H > kTickets)
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, 0, nullptr, nullptr);
     return hipGetLastError();
 }
 
@@ -547,6 +624,8 @@ hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, co
     else
         OIL_KV_APPEND(128, uint16_t);
 #undef OIL_KV_APPEND
+    if ((int64_t)grid.x * c.H > kTickets)
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, max_rows, nodes, count);
     return hipGetLastError();
 }
 
