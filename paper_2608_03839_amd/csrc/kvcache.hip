@@ -391,10 +391,21 @@ struct KvMoves {
     int32_t pad[2];
 };
 
-__host__ __device__ __forceinline__ int64_t kv_moves_stride(int64_t cap, int64_t keep)
+// A head's part of the workspace: KvMoves, the tile that the budget ends in as
+// it was, the first move into each tile below the budget (and one past), the moves.
+struct KvMovesAt {
+    int64_t tile, first, moves, stride;
+};
+
+__host__ __device__ __forceinline__ KvMovesAt kv_moves_at(const KvView& c, int64_t keep)
 {
-    const int64_t most = keep < cap - keep ? keep : cap - keep;
-    return (int64_t)sizeof(KvMoves) + most * (int64_t)sizeof(KvMove);
+    KvMovesAt at;
+    const int64_t most = keep < c.cap - keep ? keep : c.cap - keep;
+    at.tile = sizeof(KvMoves);
+    at.first = at.tile + c.tile_bytes;
+    at.moves = at.first + (keep / kKvTile + 5) / 4 * 16;
+    at.stride = at.moves + most * (int64_t)sizeof(KvMove);
+    return at;
 }
 
 // Rank of a row: recent rows above every weight, NaN below.
@@ -405,36 +416,40 @@ __device__ __forceinline__ uint32_t kv_rank(float w, bool young)
     return w != w ? 0u : score_code(w);
 }
 
-constexpr int kSelect = 1024;
+constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
+constexpr int kDigit = 11, kBins = 1 << kDigit;
 
-// Exclusive rank of `flag` among the block's threads, and the block's total.
-__device__ __forceinline__ int kv_scan(bool flag, int* waves, int* total)
+// Sums of `mine` over the waves before this one, and over all (each wave's lanes alike).
+__device__ __forceinline__ int kv_before(int mine, int* waves, int* total)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t m = __ballot(flag);
-    if (lane == 0)
-        waves[wave] = __popcll(m);
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        waves[wave] = mine;
     __syncthreads();
     int before = 0, all = 0;
-    for (int w = 0; w < kSelect / 64; w++) {
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; w++) {
         before += w < wave ? waves[w] : 0;
         all += waves[w];
     }
-    __syncthreads();
     *total = all;
-    return before + __popcll(m & ((1ull << lane) - 1));
+    return before;
 }
 
+// One workgroup per (request, head).  The keep-th largest rank by three digits
+// of 11 bits; then, each wave over a stretch of its own in chunks of 64 rows,
+// ranks among ties, holes and late rows by ballots, with one exchange between the waves each.
 __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
                                                             int64_t recent, uint8_t* __restrict__ work)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ int waves[kSelect / 64];
+    __shared__ uint32_t hist[kBins];
+    __shared__ int waves[kSelectWaves];
     __shared__ uint32_t digit, above;
-    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-    uint8_t* mine = work + ((int64_t)b * c.H + h) * kv_moves_stride(c.cap, keep);
+    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const KvMovesAt at = kv_moves_at(c, keep);
+    uint8_t* mine = work + ((int64_t)b * c.H + h) * at.stride;
     KvMoves* head = (KvMoves*)mine;
-    KvMove* moves = (KvMove*)(mine + sizeof(KvMoves));
     const int slot = kv_slot(c, slots, b);
     const int32_t n = slot < 0 ? 0 : kv_len(c, slot);
     if (n <= keep) {
@@ -444,77 +459,129 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
         }
         return;
     }
+    KvMove* moves = (KvMove*)(mine + at.moves);
+    int32_t* first = (int32_t*)(mine + at.first);
     const int64_t row = kv_row(c, slot, h);
     const int64_t young = c.state[4 * (int64_t)slot + kKvNext] - recent;
     auto rank = [&](int32_t i) { return kv_rank(c.weight[row + i], c.pos[row + i] >= young); };
-    // the keep-th largest rank, digit by digit
     uint32_t prefix = 0, need = (uint32_t)keep;  // rows still to take at the prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelect)
+    for (int shift = 21; ; shift = shift > 10 ? shift - kDigit : 0) {
+        // digits of bits 31 .. 21, 20 .. 10, 9 .. 0
+        const int width = shift ? kDigit : 10;
+        for (int i = tid; i < kBins; i += kSelect)
             hist[i] = 0;
         __syncthreads();
+#pragma unroll 4
         for (int32_t i = tid; i < n; i += kSelect) {
             const uint32_t r = rank(i);
-            if (shift == 24 || (r >> (shift + 8)) == (prefix >> (shift + 8)))
-                atomicAdd(&hist[(r >> shift) & 255], 1u);
+            const bool counts = shift == 21 || (r >> (shift + width)) == (prefix >> (shift + width));
+            // recent rows share one rank: one lane adds them all
+            const uint64_t same = __ballot(counts && r == 0xFFFFFFFFu);
+            if (counts && (r != 0xFFFFFFFFu || lane == __ffsll((unsigned long long)same) - 1))
+                atomicAdd(&hist[(r >> shift) & ((1u << width) - 1)], r != 0xFFFFFFFFu ? 1u : (uint32_t)__popcll(same));
         }
         __syncthreads();
-        if (tid == 0) {
-            uint32_t sum = 0;
-            int at = 255;
-            while (at > 0 && sum + hist[at] < need)
-                sum += hist[at--];
-            digit = at;
-            above = sum;
+        // the digit: bins from the top until `need` rows are reached; a thread holds two
+        const int bin = kBins - 1 - 2 * tid;
+        const uint32_t x0 = hist[bin], x1 = hist[bin - 1];
+        uint32_t sum = x0 + x1;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t y = __shfl_up(sum, o, 64);
+            sum += lane >= o ? y : 0;
+        }
+        int all;
+        const uint32_t before = (uint32_t)kv_before((int)__shfl(sum, 63, 64), waves, &all) + sum - x0 - x1;
+        if (before < need && before + x0 >= need) {
+            digit = (uint32_t)bin;
+            above = before;
+        } else if (before + x0 < need && before + x0 + x1 >= need) {
+            digit = (uint32_t)bin - 1;
+            above = before + x0;
         }
         __syncthreads();
         prefix |= digit << shift;
         need -= above;
         __syncthreads();
+        if (shift == 0)
+            break;
     }
     // rows above the rank stay, and the first `need` at it
-    int tied = 0, holes = 0, late = 0;
-    for (int32_t i0 = 0; i0 < n; i0 += kSelect) {
-        const int32_t i = i0 + tid;
-        const uint32_t r = i < n ? rank(i) : 0;
-        const bool tie = i < n && r == prefix;
-        int total;
-        const int t = tied + kv_scan(tie, waves, &total);
-        tied += total;
-        const bool stays = i < n && (r > prefix || (tie && t < (int)need));
-        const int hole = holes + kv_scan(i < keep && !stays, waves, &total);
-        holes += total;
-        const int from = late + kv_scan(i >= keep && stays, waves, &total);
-        late += total;
-        if (i < keep && !stays)
-            moves[hole].dst = i;
-        if (i >= keep && stays) {
-            moves[from].src = i;
-            moves[from].pos = c.pos[row + i];
-            moves[from].weight = c.weight[row + i];
+    const int32_t span = ((n + kSelect - 1) / kSelect) * 64, i0 = wave * span, i1 = min(i0 + span, n);
+    int count = 0, total;
+    for (int32_t i = i0; i < i1; i += 64)
+        count += __popcll(__ballot(i + lane < i1 && rank(i + lane) == prefix));
+    const int tied = kv_before(count, waves, &total);
+    const uint64_t below = (1ull << lane) - 1;
+    // a chunk's masks of rows that stay, given the ties before it
+    auto stays = [&](int32_t i, int* ties, uint32_t* r) {
+        const bool in = i + lane < i1;
+        *r = in ? rank(i + lane) : 0;
+        const uint64_t eq = __ballot(in && *r == prefix);
+        const bool yes = in && (*r > prefix || (*r == prefix && *ties + __popcll(eq & below) < (int)need));
+        *ties += __popcll(eq);
+        return yes;
+    };
+    int ties = tied, holes = 0, late = 0;
+    uint32_t r;
+    for (int32_t i = i0; i < i1; i += 64) {
+        const bool yes = stays(i, &ties, &r);
+        holes += __popcll(__ballot(i + lane < i1 && i + lane < keep && !yes));
+        late += __popcll(__ballot(i + lane >= keep && yes));
+    }
+    int moving;
+    int hole = kv_before(holes, waves, &moving);
+    int from = kv_before(late, waves, &total);
+    ties = tied;
+    for (int32_t i = i0; i < i1; i += 64) {
+        const int32_t x = i + lane;
+        const bool yes = stays(i, &ties, &r);
+        const bool open = x < i1 && x < keep && !yes, moves_in = x >= keep && yes;
+        const uint64_t mo = __ballot(open), mf = __ballot(moves_in);
+        const int at_hole = hole + __popcll(mo & below);
+        if (open)
+            moves[at_hole].dst = x;
+        if (x < i1 && x < keep && (x & (kKvTile - 1)) == 0)
+            first[x / kKvTile] = at_hole;
+        if (moves_in) {
+            KvMove* m = moves + from + __popcll(mf & below);
+            m->src = x;
+            m->pos = c.pos[row + x];
+            m->weight = c.weight[row + x];
         }
+        hole += __popcll(mo);
+        from += __popcll(mf);
     }
     if (tid == 0) {
         head->n = n;
-        head->count = holes;
+        head->count = moving;
+        first[(keep + kKvTile - 1) / kKvTile] = moving;
+    }
+    if (keep % kKvTile) {
+        const u32x4* tile = (const u32x4*)(kv_tiles(c, slot, h) + keep / kKvTile * c.tile_bytes);
+        for (int i = tid; i < c.tile_bytes / 16; i += kSelect)
+            ((u32x4*)(mine + at.tile))[i] = tile[i];
     }
 }
 
+// A workgroup per destination tile.  Rows that move out of the tile that the
+// budget ends in are read from its copy: that tile may be written meanwhile.
 template <int W>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
                                                       const uint8_t* __restrict__ work)
 {
-    __shared__ int lo, hi;
+    __shared__ int32_t source[kKvTile];
     const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
     const int slot = kv_slot(c, slots, b);
     if (slot < 0)
         return;
-    const uint8_t* mine = work + ((int64_t)b * c.H + h) * kv_moves_stride(c.cap, keep);
-    const KvMoves* head = (const KvMoves*)mine;
-    const KvMove* moves = (const KvMove*)(mine + sizeof(KvMoves));
-    const int32_t n = head->n, count = head->count;
+    const KvMovesAt at = kv_moves_at(c, keep);
+    const uint8_t* mine = work + ((int64_t)b * c.H + h) * at.stride;
+    const int32_t n = ((const KvMoves*)mine)->n;
     if (n == 0)
         return;
+    const KvMove* moves = (const KvMove*)(mine + at.moves);
+    const int32_t* first = (const int32_t*)(mine + at.first);
     const int64_t row = kv_row(c, slot, h);
     // rows past the budget leave
     for (int64_t i = keep + blockIdx.x * 256ll + tid; i < n; i += gridDim.x * 256ll) {
@@ -524,63 +591,68 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
     if (blockIdx.x == 0 && h == 0 && tid == 0)
         c.state[4 * (int64_t)slot + kKvLen] = (int32_t)keep;
     uint8_t* tiles = kv_tiles(c, slot, h);
-    for (int64_t t = blockIdx.x; t * kKvTile < keep; t += gridDim.x) {
-        // the moves into this tile: destinations ascend
-        if (tid < 2) {
-            const int64_t want = (t + tid) * kKvTile;
-            int a = 0, z = count;
-            while (a < z) {
-                const int m = (a + z) >> 1;
-                if (moves[m].dst < want)
-                    a = m + 1;
-                else
-                    z = m;
-            }
-            *(tid ? &hi : &lo) = a;
-        }
-        __syncthreads();
-        const int m0 = lo, m1 = hi;
-        __syncthreads();
+    const int32_t edge = keep % kKvTile ? (int32_t)(keep / kKvTile) : -1;
+    auto from = [&](int32_t src) -> const uint8_t* {
+        return (src >> 5) == edge ? mine + at.tile : tiles + (int64_t)(src >> 5) * c.tile_bytes;
+    };
+    for (int32_t t = blockIdx.x; (int64_t)t * kKvTile < keep; t += gridDim.x) {
+        const int m0 = first[t], m1 = first[t + 1];
         if (m0 == m1)
             continue;
-        uint8_t* tile = tiles + t * c.tile_bytes;
-        for (int w = tid; w < KvTile<W>::kWords; w += 256) {
+        __syncthreads();
+        if (tid < kKvTile)
+            source[tid] = -1;
+        __syncthreads();
+        if (tid < m1 - m0) {
+            const KvMove m = moves[m0 + tid];
+            source[m.dst & 31] = m.src;
+            c.pos[row + m.dst] = m.pos;
+            c.weight[row + m.dst] = m.weight;
+        }
+        __syncthreads();
+        uint8_t* tile = tiles + (int64_t)t * c.tile_bytes;
+        if (tid < 4 * kKvTile) {  // keys: a quarter of a row a thread
+            const int key = tid >> 2, g = tid & 3;
+            const int32_t src = source[key];
+            if (src >= 0) {
+                const int to = kv_word_at((key >> 4) * (W / 32), (key & 15) + 16 * g);
+                const int at_src = kv_word_at(((src >> 4) & 1) * (W / 32), (src & 15) + 16 * g);
+                if (W == 128)
+                    *(u32x4*)((uint32_t*)tile + to) = *(const u32x4*)((const uint32_t*)from(src) + at_src);
+                else
+                    *(uint2*)((uint32_t*)tile + to) = *(const uint2*)((const uint32_t*)from(src) + at_src);
+            }
+        } else if (tid < 6 * kKvTile) {  // scales
+            const int x = tid - 4 * kKvTile, side = x >> 5;
+            const int32_t src = source[x & 31];
+            const int base = (side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4;
+            if (src >= 0)
+                ((uint32_t*)tile)[base + (x & 31)] = ((const uint32_t*)from(src))[base + (src & 31)];
+        }
+        for (int w = tid; w < KvTile<W>::kWords; w += 256) {  // values: a nibble of each dword a row
             int Q, lane;
             kv_word(w, &Q, &lane);
-            const int g = lane >> 4;
-            uint32_t* to = (uint32_t*)(tile + KvTile<W>::kValues) + w;
-            // relaxed atomics: another workgroup may read nibbles of rows past
-            // the budget from this dword, which do not change
-            uint32_t word = __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            bool any = false;
-            for (int m = m0; m < m1; m++) {
-                const int dst = moves[m].dst & 31, src = moves[m].src & 31;
-                const uint8_t* from = tiles + (int64_t)(moves[m].src >> 5) * c.tile_bytes;
-                if (((dst & 15) >> 2) == g) {
-                    const uint32_t* sw = (const uint32_t*)(from + KvTile<W>::kValues) +
-                                         kv_word_at(Q, (lane & 15) + 16 * ((src & 15) >> 2));
-                    const int code = kv_code(__hip_atomic_load(sw, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
-                                             4 * (src >> 4) + (src & 3));
-                    const int at = 4 * kv_nibble(4 * (dst >> 4) + (dst & 3));
-                    word = (word & ~(15u << at)) | ((uint32_t)code << at);
-                    any = true;
+            uint32_t got[8], clear = 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const int32_t src = source[16 * (e >> 2) + 4 * (lane >> 4) + (e & 3)];
+                got[e] = 0;
+                if (src >= 0) {
+                    clear |= 15u << (4 * kv_nibble(e));
+                    const uint32_t word =
+                        ((const uint32_t*)(from(src) + KvTile<W>::kValues))[kv_word_at(
+                            Q, (lane & 15) + 16 * ((src & 15) >> 2))];
+                    got[e] = (uint32_t)kv_code(word, 4 * ((src >> 4) & 1) + (src & 3)) << (4 * kv_nibble(e));
                 }
-                if ((dst & 15) == (lane & 15) && (dst >> 4) == Q / (W / 32))
-                    ((uint32_t*)tile)[w] =
-                        ((const uint32_t*)from)[kv_word_at((src >> 4) * (W / 32) + Q % (W / 32), (src & 15) + 16 * g)];
             }
-            if (any)
-                __hip_atomic_store(to, word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        for (int m = m0 + tid; m < m1; m += 256) {
-            const KvMove mv = moves[m];
-            const uint8_t* from = tiles + (int64_t)(mv.src >> 5) * c.tile_bytes;
-            ((uint32_t*)(tile + KvTile<W>::kKeyScales))[mv.dst & 31] =
-                ((const uint32_t*)(from + KvTile<W>::kKeyScales))[mv.src & 31];
-            ((uint32_t*)(tile + KvTile<W>::kValueScales))[mv.dst & 31] =
-                ((const uint32_t*)(from + KvTile<W>::kValueScales))[mv.src & 31];
-            c.pos[row + mv.dst] = mv.pos;
-            c.weight[row + mv.dst] = mv.weight;
+            if (clear) {
+                uint32_t* to = (uint32_t*)(tile + KvTile<W>::kValues) + w;
+                uint32_t word = *to & ~clear;
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    word |= got[e];
+                *to = word;
+            }
         }
     }
 }
@@ -650,7 +722,7 @@ hipError_t launch_kv_read(const KvView& c, const int32_t* slots, int32_t B, int6
 
 size_t kv_evict_workspace_bytes(const KvView& c, int32_t B, int64_t keep)
 {
-    return (size_t)B * c.H * (size_t)kv_moves_stride(c.cap, keep);
+    return (size_t)B * c.H * (size_t)kv_moves_at(c, keep).stride;
 }
 
 hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int64_t keep, int64_t recent,
