@@ -418,6 +418,7 @@ __device__ __forceinline__ uint32_t kv_rank(float w, bool young)
 
 constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
 constexpr int kDigit = 11, kBins = 1 << kDigit;
+constexpr int32_t kHeldRanks = 36864;  // ranks that fit LDS beside the bins
 
 // Sums of `mine` over the waves before this one, and over all (each wave's lanes alike).
 __device__ __forceinline__ int kv_before(int mine, int* waves, int* total)
@@ -443,6 +444,7 @@ __device__ __forceinline__ int kv_before(int mine, int* waves, int* total)
 __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
                                                             int64_t recent, uint8_t* __restrict__ work)
 {
+    __shared__ uint32_t held[kHeldRanks];
     __shared__ uint32_t hist[kBins];
     __shared__ int waves[kSelectWaves];
     __shared__ uint32_t digit, above;
@@ -463,7 +465,14 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
     int32_t* first = (int32_t*)(mine + at.first);
     const int64_t row = kv_row(c, slot, h);
     const int64_t young = c.state[4 * (int64_t)slot + kKvNext] - recent;
-    auto rank = [&](int32_t i) { return kv_rank(c.weight[row + i], c.pos[row + i] >= young); };
+    const bool holds = n <= kHeldRanks;
+    auto rank = [&](int32_t i) {
+        return holds ? held[i] : kv_rank(c.weight[row + i], c.pos[row + i] >= young);
+    };
+    if (holds)
+#pragma unroll 4
+        for (int32_t i = tid; i < n; i += kSelect)
+            held[i] = kv_rank(c.weight[row + i], c.pos[row + i] >= young);
     uint32_t prefix = 0, need = (uint32_t)keep;  // rows still to take at the prefix
     for (int shift = 21; ; shift = shift > 10 ? shift - kDigit : 0) {
         // digits of bits 31 .. 21, 20 .. 10, 9 .. 0
@@ -564,7 +573,9 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
     }
 }
 
-// A workgroup per destination tile.  Rows that move out of the tile that the
+// A workgroup per destination tile, of one wave where there are many (a tile's
+// dependent loads are the time, and tiles in flight cover it: 65,536 tiles 169 -> 128 us
+// against four waves), of four where there are few (1,024 tiles 12 -> 6.7 us).  Rows that move out of the tile that the
 // budget ends in are read from its copy: that tile may be written meanwhile.
 template <int W>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
@@ -584,7 +595,8 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
     const int32_t* first = (const int32_t*)(mine + at.first);
     const int64_t row = kv_row(c, slot, h);
     // rows past the budget leave
-    for (int64_t i = keep + blockIdx.x * 256ll + tid; i < n; i += gridDim.x * 256ll) {
+    for (int64_t i = keep + (int64_t)blockIdx.x * blockDim.x + tid; i < n;
+         i += (int64_t)gridDim.x * blockDim.x) {
         c.pos[row + i] = -1;
         c.weight[row + i] = 0.f;
     }
@@ -611,8 +623,8 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
         }
         __syncthreads();
         uint8_t* tile = tiles + (int64_t)t * c.tile_bytes;
-        if (tid < 4 * kKvTile) {  // keys: a quarter of a row a thread
-            const int key = tid >> 2, g = tid & 3;
+        for (int x = tid; x < 4 * kKvTile; x += blockDim.x) {  // keys: a quarter of a row a lane
+            const int key = x >> 2, g = x & 3;
             const int32_t src = source[key];
             if (src >= 0) {
                 const int to = kv_word_at((key >> 4) * (W / 32), (key & 15) + 16 * g);
@@ -622,14 +634,15 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
                 else
                     *(uint2*)((uint32_t*)tile + to) = *(const uint2*)((const uint32_t*)from(src) + at_src);
             }
-        } else if (tid < 6 * kKvTile) {  // scales
-            const int x = tid - 4 * kKvTile, side = x >> 5;
-            const int32_t src = source[x & 31];
-            const int base = (side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4;
-            if (src >= 0)
-                ((uint32_t*)tile)[base + (x & 31)] = ((const uint32_t*)from(src))[base + (src & 31)];
         }
-        for (int w = tid; w < KvTile<W>::kWords; w += 256) {  // values: a nibble of each dword a row
+        if (tid < 64) {  // scales
+            const int32_t src = source[tid & 31];
+            const int base = (tid >> 5 ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4;
+            if (src >= 0)
+                ((uint32_t*)tile)[base + (tid & 31)] = ((const uint32_t*)from(src))[base + (src & 31)];
+        }
+#pragma unroll 2
+        for (int w = tid; w < KvTile<W>::kWords; w += blockDim.x) {  // values: a nibble of each dword a row
             int Q, lane;
             kv_word(w, &Q, &lane);
             uint32_t got[8], clear = 0;
@@ -731,11 +744,11 @@ hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int
     hipLaunchKernelGGL(kv_select_kernel, dim3(c.H, B), dim3(kSelect), 0, stream, c, slots, keep, recent,
                        (uint8_t*)workspace);
     const int64_t tiles = (keep + kKvTile - 1) / kKvTile;
-    const dim3 grid((unsigned)(tiles < 1024 ? tiles : 1024), c.H, B);
+    const dim3 grid((unsigned)(tiles < 4096 ? tiles : 4096), c.H, B), block(tiles * c.H * B > 8192 ? 64 : 256);
     if (c.W == 64)
-        hipLaunchKernelGGL(kv_move_kernel<64>, grid, dim3(256), 0, stream, c, slots, keep, (const uint8_t*)workspace);
+        hipLaunchKernelGGL(kv_move_kernel<64>, grid, block, 0, stream, c, slots, keep, (const uint8_t*)workspace);
     else
-        hipLaunchKernelGGL(kv_move_kernel<128>, grid, dim3(256), 0, stream, c, slots, keep,
+        hipLaunchKernelGGL(kv_move_kernel<128>, grid, block, 0, stream, c, slots, keep,
                            (const uint8_t*)workspace);
     return hipGetLastError();
 }
