@@ -32,23 +32,6 @@ namespace oil {
 
 namespace {
 
-template <int W>
-__device__ __forceinline__ float kv_key_dot(const uint8_t* tile, int key, const float* q)
-{
-    float dot = 0.f, sum = 0.f;
-    for (int ks = 0; ks < W / 32; ks++)
-        for (int g = 0; g < 4; g++) {
-            const uint32_t w = ((const uint32_t*)tile)[kv_word_at((key >> 4) * (W / 32) + ks, (key & 15) + 16 * g)];
-            for (int e = 0; e < 8; e++) {
-                const float x = q[32 * ks + 8 * g + e];
-                dot += x * (float)kv_code(w, e);
-                sum += x;
-            }
-        }
-    const uint32_t pair = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + key * 4);
-    return kv_s(pair) * dot + kv_z(pair) * sum;
-}
-
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -764,39 +747,119 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_p
         A.lse[at] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }
 
-// One thread per position: every committed row's probability at it.
-template <int W>
+// A workgroup's waves stream tiles of keys; up to 64 rows at a time stand in LDS
+// as operands.  S = Q K^T puts a position into a lane column, so a position's sum
+// over rows is over a lane's registers and four lanes.  ONE: at most 16 rows,
+// whose operands stay in registers.
+template <int W, bool ONE>
 __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* __restrict__ slots,
                                                        const uint16_t* __restrict__ q, int64_t q_ld, int32_t Hq,
                                                        const float* __restrict__ lse, int32_t max_nodes,
                                                        const int32_t* __restrict__ nodes,
                                                        const int32_t* __restrict__ count, float scale)
 {
-    __shared__ float qs[W];
-    __shared__ int bound;
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, G = Hq / c.H;
+    constexpr int kTiles = ONE ? 1 : 4;
+    __shared__ u32x4 sq[kTiles][W / 32][64];
+    __shared__ floatx4 sc[kTiles][3][4];  // c1, c2 and lse (base 2) of a tile's rows
+    __shared__ int bound, some;
+    const int b = blockIdx.z, h = blockIdx.y, G = Hq / c.H;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
     const int slot = kv_slot(c, slots, b);
     if (slot < 0)
         return;
     const int32_t len = kv_len(c, slot);
-    const int rows = kv_count(nodes, count, b, max_nodes, &bound);
+    const int64_t u0 = (int64_t)blockIdx.x * 4 + wave, du = (int64_t)gridDim.x * 4;
+    const int64_t units = ((int64_t)len + kKvTile - 1) / kKvTile;
+    if ((int64_t)blockIdx.x * 4 >= units)
+        return;
+    const int rows = kv_count(nodes, count, b, max_nodes, &bound) * G;
     const uint8_t* tiles = kv_tiles(c, slot, h);
-    for (int64_t j0 = blockIdx.x * 256ll; j0 < len; j0 += gridDim.x * 256ll) {
-        const int64_t j = j0 + tid;
-        float sum = 0.f;
-        for (int r = 0; r < rows; r++)
-            for (int g = 0; g < G; g++) {
-                const int64_t at = (int64_t)b * max_nodes + kv_source(nodes, b, max_nodes, r);
-                __syncthreads();
-                if (tid < W)
-                    qs[tid] = tid < c.D ? bf16_bits_to_float(q[at * q_ld + (int64_t)(h * G + g) * c.D + tid]) : 0.f;
-                __syncthreads();
-                const float l = lse[at * Hq + h * G + g];
-                if (j < len && l != -INFINITY)
-                    sum += expf(scale * kv_key_dot<W>(tiles + j / kKvTile * c.tile_bytes, (int)(j % kKvTile), qs) - l);
+    float* weight = c.weight + kv_row(c, slot, h);
+    for (int r0 = 0; r0 < rows; r0 += 16 * kTiles) {
+        __syncthreads();
+        if (threadIdx.x == 0)
+            some = 0;
+        __syncthreads();
+        if (wave < kTiles) {
+            const int r = r0 + 16 * wave + r16;
+            const uint16_t* row = nullptr;
+            float l = -INFINITY;
+            if (r < rows) {
+                const int64_t at = (int64_t)b * max_nodes + kv_source(nodes, b, max_nodes, r / G);
+                l = lse[at * Hq + h * G + r % G];
+                if (l != -INFINITY)
+                    row = q + at * q_ld + (int64_t)(h * G + r % G) * c.D;
             }
-        if (j < len)
-            c.weight[kv_row(c, slot, h) + j] += sum;
+            Frag f[W / 32];
+            float c1, c2;
+            kv_query<W>(row, g, c.D, scale, f, &c1, &c2);
+#pragma unroll
+            for (int s = 0; s < W / 32; s++)
+                sq[wave][s][lane] = f[s].w;
+            if (g == 0) {
+                ((float*)sc[wave][0])[r16] = c1;
+                ((float*)sc[wave][1])[r16] = c2;
+                ((float*)sc[wave][2])[r16] = row ? l * kLog2e : INFINITY;  // no row: exp2 gives 0
+            }
+            if (row)
+                some = 1;
+        }
+        __syncthreads();
+        if (!some)
+            continue;
+        const int left = (rows - r0 + 15) / 16, tiles_now = left < kTiles ? left : kTiles;
+        u32x4 k[W / 64];
+        uint32_t pair[2];
+        float w = 0.f;
+        auto load = [&](int64_t u) {
+            const uint8_t* tile = tiles + u * KvTile<W>::kBytes;
+#pragma unroll
+            for (int p = 0; p < W / 64; p++)
+                k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
+#pragma unroll
+            for (int a = 0; a < 2; a++)
+                pair[a] = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + 64 * a + 4 * r16);
+            if (lane < 32 && u * kKvTile + lane < len)
+                w = weight[u * kKvTile + lane];
+        };
+        if (u0 < units)
+            load(u0);
+        for (int64_t u = u0; u < units; u += du) {
+            h16x8 kf[2][W / 32];
+#pragma unroll
+            for (int a = 0; a < 2; a++)
+#pragma unroll
+                for (int s = 0; s < W / 32; s++) {
+                    const int Q = a * (W / 32) + s;
+                    kf[a][s] = kv_codes(k[Q >> 2][Q & 3]);
+                }
+            const float ks[2] = {kv_s(pair[0]), kv_s(pair[1])}, kz[2] = {kv_z(pair[0]), kv_z(pair[1])};
+            const float before = w;
+            if (u + du < units)
+                load(u + du);
+            float sum[2] = {0.f, 0.f};
+            for (int t = 0; t < tiles_now; t++) {
+                floatx4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int s = 0; s < W / 32; s++) {
+                    Frag qf;
+                    qf.w = sq[t][s][lane];
+#pragma unroll
+                    for (int a = 0; a < 2; a++)
+                        S[a] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qf.h, kf[a][s], S[a], 0, 0, 0);
+                }
+                const floatx4 c1 = sc[t][0][g], c2 = sc[t][1][g], l = sc[t][2][g];
+#pragma unroll
+                for (int a = 0; a < 2; a++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        sum[a] += __builtin_amdgcn_exp2f(fmaf(ks[a] * S[a][i], c1[i], fmaf(kz[a], c2[i], -l[i])));
+            }
+            sum[0] = quad_sum(sum[0]);
+            sum[1] = quad_sum(sum[1]);
+            if (lane < 32 && u * kKvTile + lane < len)
+                weight[u * kKvTile + lane] = before + (lane < 16 ? sum[0] : sum[1]);
+        }
     }
 }
 
@@ -887,15 +950,23 @@ hipError_t launch_kv_weigh(const KvView& c, const int32_t* slots, int32_t B, con
                            int32_t Hq, const float* lse, int32_t max_nodes, const int32_t* nodes,
                            const int32_t* count, float scale, hipStream_t stream)
 {
-    const int64_t blocks = (c.cap + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 4096 ? blocks : 4096), c.H, B);
-#define OIL_KV_WEIGH(W)                                                                                            \
-    hipLaunchKernelGGL(kv_weigh_kernel<W>, grid, dim3(256), 0, stream, c, slots, (const uint16_t*)q, q_ld, Hq, lse, \
-                       max_nodes, nodes, count, scale)
-    if (c.W == 64)
-        OIL_KV_WEIGH(64);
+    // two tiles a wave at least, and enough workgroups for the chip's 1,024 SIMDs
+    const int64_t heads = (int64_t)B * c.H, most = (c.tiles + 7) / 8;
+    int64_t blocks = (2048 + heads - 1) / heads;
+    blocks = blocks < most ? blocks : most;
+    const dim3 grid((unsigned)blocks, c.H, B), block(256);
+    const bool one = max_nodes * (Hq / c.H) <= 16;
+#define OIL_KV_WEIGH(W, ONE)                                                                                      \
+    hipLaunchKernelGGL((kv_weigh_kernel<W, ONE>), grid, block, 0, stream, c, slots, (const uint16_t*)q, q_ld, Hq, \
+                       lse, max_nodes, nodes, count, scale)
+    if (c.W == 64 && one)
+        OIL_KV_WEIGH(64, true);
+    else if (c.W == 64)
+        OIL_KV_WEIGH(64, false);
+    else if (one)
+        OIL_KV_WEIGH(128, true);
     else
-        OIL_KV_WEIGH(128);
+        OIL_KV_WEIGH(128, false);
 #undef OIL_KV_WEIGH
     return hipGetLastError();
 }
