@@ -59,10 +59,13 @@ struct KvAttend {
     const uint32_t* mask;
     uint16_t* out;
     float* lse;
-    float* part_o;   // splits > 1: unnormalised rows,
+    int64_t* start;  // per request (and one past): units before it,
+    int64_t* items;  // items before it,
+    int64_t* shares; // (one word) shares the units are cut into;
+    float* part_o;   // per cut of an item: unnormalised rows,
     float* part_ml;  // and each one's (m, sum)
     int64_t q_ld, ld;
-    int32_t B, Hq, G, max_nodes, splits, row_blocks;
+    int32_t B, Hq, G, max_nodes;
     float scale;
 };
 
@@ -194,15 +197,18 @@ struct KvTileRegs {
     u32x4 k[W / 64], v[W / 64];
     uint32_t pair;
 
-    __device__ __forceinline__ void load(const uint8_t* tile, int lane)
+    __device__ __forceinline__ void load_keys(const uint8_t* tile, int lane)
     {
 #pragma unroll
         for (int p = 0; p < W / 64; p++)
             k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
+        pair = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + lane * 4);
+    }
+    __device__ __forceinline__ void load_values(const uint8_t* tile, int lane)
+    {
 #pragma unroll
         for (int p = 0; p < W / 64; p++)
             v[p] = *(const u32x4*)(tile + KvTile<W>::kValues + p * 1024 + lane * 16);
-        pair = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + lane * 4);
     }
     __device__ __forceinline__ uint32_t key_word(int Q) const { return k[Q >> 2][Q & 3]; }
     __device__ __forceinline__ uint32_t value_word(int Q) const { return v[Q >> 2][Q & 3]; }
@@ -268,8 +274,10 @@ struct KvRows {
 
 // A tile of `valid` cached positions (32, or fewer at the end of a slot).  Each
 // lane prepares one pair; the eight of its rows' scores come back through LDS.
+// The wave's next tile is loaded into the same registers, the keys when the first
+// product has taken them, the values after the second.
 template <int W, int NT, bool END>
-__device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int lane, KvScales& L,
+__device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, int valid, int lane, KvScales& L,
                                         const u32x4 (*q)[W / 32][64], const float (&c1)[NT], const float (&c2)[NT],
                                         KvRows<W, NT>& R)
 {
@@ -306,6 +314,8 @@ __device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int l
             S[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf.h, S[t][1], 0, 0, 0);
         }
     }
+    if (!END)
+        T.load_keys(next, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     float ks[8], kz[8], vs[8], vz[8];
     bool in[8];
@@ -404,6 +414,8 @@ __device__ __forceinline__ void kv_tile(const KvTileRegs<W>& T, int valid, int l
             }
         }
     }
+    if (!END)
+        T.load_values(next, lane);
 }
 
 // The node of row r of a head, -1 for none, and the row's queries.
@@ -532,14 +544,7 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
 }
 
 constexpr int kAttendWaves = 4;
-
-// Parts that a slot's units (tiles of the cache and of the tree) are split
-// into: at least two units a wave.
-__device__ __forceinline__ int kv_parts(int64_t units, int splits)
-{
-    const int64_t most = units / (2 * kAttendWaves);
-    return most < 1 ? 1 : most < splits ? (int)most : splits;
-}
+constexpr int kMaxB = 512;
 
 __device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
 {
@@ -549,202 +554,341 @@ __device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
     return m < 0 ? 0 : m > A.max_nodes ? A.max_nodes : m;
 }
 
+// Tiles that a live row of a request goes through: the cache's, then the tree's.
+__device__ __forceinline__ int64_t kv_units(const KvAttend& A, int32_t len, int m)
+{
+    return ((int64_t)len + kKvTile - 1) / kKvTile + (A.k ? (m + 31) / 32 : 0);
+}
+
+// The work of a call is one list of units: requests, in each its heads, in each
+// its blocks of 16 NT rows (an item), in each the tiles.  Equal shares of it go
+// to the workgroups, whatever the lengths; a share that begins or ends inside an
+// item leaves a part of it, numbered share + item (which no two parts have in
+// common), for the join.
+// Least units of a share: two tiles a wave.
+constexpr int64_t kLeastShare = 2 * kAttendWaves;
+
+// A value that all lanes hold alike, as a scalar.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
+__device__ __forceinline__ int64_t kv_cut(int64_t total, int64_t shares, int64_t w)
+{
+    return total / shares * w + (total % shares) * w / shares;
+}
+
 template <int W, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAttend A)
 {
     constexpr int kRows = 16 * NT;
+    __shared__ int64_t start[kMaxB + 1], items[kMaxB + 1];
+    __shared__ int64_t sums[2][kAttendWaves];
     __shared__ float sm[kAttendWaves][kRows], sl[kAttendWaves][kRows];
     __shared__ floatx4 so[kAttendWaves / 2][NT][W / 16][64];
     __shared__ u32x4 sq[NT][W / 32][64];
     __shared__ __align__(16) KvScales scales[kAttendWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
-    // the row blocks of one part of a head run on one XCD (its L2 serves the
-    // part's tiles to all of them)
-    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
-    const int rb = local % A.row_blocks, part = local / A.row_blocks * 8 + xcd;
-    if (part >= A.B * A.c.H * A.splits)
-        return;
-    const int sp = part % A.splits, h = part / A.splits % A.c.H, b = part / A.splits / A.c.H;
-    const int slot = kv_slot(A.c, A.slots, b);
-    const int m = kv_live_nodes(A, b, slot), D = A.c.D;
-    const int32_t len = slot < 0 ? 0 : kv_len(A.c, slot);
-    const bool dead = rb * kRows >= m * A.G;  // no live row
-    if (dead && A.splits > 1)
-        return;
-    float c1[NT], c2[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        Frag q[W / 32];
-        const uint16_t* row;
-        kv_row_of(A, b, h, m, rb * kRows + 16 * t + r16, &row);
-        kv_query<W>(row, g, D, A.scale, q, &c1[t], &c2[t]);
-        if (wave == 0)
-#pragma unroll
-            for (int s = 0; s < W / 32; s++)
-                sq[t][s][lane] = q[s].w;
-    }
-    __syncthreads();
-    const int64_t cached = ((int64_t)len + kKvTile - 1) / kKvTile;
-    const int64_t units = dead ? 0 : cached + (A.k ? (m + 31) / 32 : 0);
-    const int parts = kv_parts(units, A.splits);
-    if (sp >= parts)
-        return;
-    const int64_t u0 = units * sp / parts, u1 = units * (sp + 1) / parts;
-    KvRows<W, NT> R;
-    R.init();
-    const uint8_t* tiles = slot < 0 ? nullptr : kv_tiles(A.c, slot, h);
-    const int64_t full = len / kKvTile < u1 ? len / kKvTile : u1;  // tiles of 32 positions end here
-    int64_t u = u0 + wave;
-    if (u < full) {
-        KvTileRegs<W> now, next;
-        now.load(tiles + u * KvTile<W>::kBytes, lane);
-        for (; u + kAttendWaves < full; u += kAttendWaves) {
-            next.load(tiles + (u + kAttendWaves) * KvTile<W>::kBytes, lane);
-            kv_tile<W, NT, false>(now, 32, lane, scales[wave], sq, c1, c2, R);
-            now = next;
+    const int lane0 = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), D = A.c.D;
+    // units and items before each request
+    int64_t before[2] = {0, 0};
+    for (int b0 = 0; b0 < A.B; b0 += 256) {
+        const int b = b0 + (int)threadIdx.x;
+        int64_t x[2] = {0, 0};
+        if (b < A.B) {
+            const int slot = kv_slot(A.c, A.slots, b), m = kv_live_nodes(A, b, slot);
+            x[1] = (int64_t)A.c.H * ((m * A.G + kRows - 1) / kRows);
+            x[0] = m ? x[1] * kv_units(A, kv_len(A.c, slot), m) : 0;
         }
-        kv_tile<W, NT, false>(now, 32, lane, scales[wave], sq, c1, c2, R);
-        u += kAttendWaves;
-    }
-    if (u < u1 && u < cached) {
-        KvTileRegs<W> now;
-        now.load(tiles + u * KvTile<W>::kBytes, lane);
-        kv_tile<W, NT, true>(now, (int)(len - u * kKvTile), lane, scales[wave], sq, c1, c2, R);
-        u += kAttendWaves;
-    }
-    for (; u < u1; u += kAttendWaves)
-        kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, rb * kRows, R);
-    // the waves' shares, relative to the largest m
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        R.l[t] = quad_sum(R.l[t]);
-        R.w[t] = quad_sum(R.w[t]);
-        if (g == 0) {
-            sm[wave][16 * t + r16] = R.m[t];
-            sl[wave][16 * t + r16] = R.l[t];
+        for (int y = 0; y < 2; y++) {
+            int64_t run = x[y];
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int64_t z = __shfl_up(run, o, 64);
+                run += lane0 >= o ? z : 0;
+            }
+            if (lane0 == 63)
+                sums[y][wave] = run;
+            x[y] = run;
         }
-    }
-    __syncthreads();
-    float top[NT], total[NT];
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        top[t] = kLow;
-#pragma unroll
-        for (int x = 0; x < kAttendWaves; x++)
-            top[t] = fmaxf(top[t], sm[x][16 * t + r16]);
-        total[t] = 0.f;
-#pragma unroll
-        for (int x = 0; x < kAttendWaves; x++)
-            total[t] += sl[x][16 * t + r16] * __builtin_amdgcn_exp2f(sm[x][16 * t + r16] - top[t]);
-        const float f = __builtin_amdgcn_exp2f(R.m[t] - top[t]), of = R.E * 0x1p24f;
-#pragma unroll
-        for (int mt = 0; mt < W / 16; mt++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-                R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : fmaf(R.o[t][mt][i], of, R.w[t]) * f;
-    }
-#pragma unroll
-    for (int half = kAttendWaves / 2; half >= 1; half >>= 1) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int t = 0; t < NT; t++)
-#pragma unroll
-                for (int mt = 0; mt < W / 16; mt++)
-                    so[wave - half][t][mt][lane] = R.o[t][mt];
         __syncthreads();
-        if (wave < half)
 #pragma unroll
-            for (int t = 0; t < NT; t++)
-#pragma unroll
-                for (int mt = 0; mt < W / 16; mt++)
-                    R.o[t][mt] += so[wave][t][mt][lane];
+        for (int y = 0; y < 2; y++) {
+            int64_t all = 0, mine = before[y];
+            for (int w = 0; w < kAttendWaves; w++) {
+                mine += w < wave ? sums[y][w] : 0;
+                all += sums[y][w];
+            }
+            if (b < A.B)
+                (y ? items : start)[b + 1] = mine + x[y];
+            before[y] += all;
+        }
         __syncthreads();
     }
-    if (wave != 0)
+    if (threadIdx.x == 0)
+        start[0] = items[0] = 0;
+    __syncthreads();
+    const int64_t total = uniform(before[0]), most = (total + kLeastShare - 1) / kLeastShare;
+    const int64_t shares = most < 1 ? 1 : most < gridDim.x ? most : gridDim.x;
+    if (blockIdx.x == 0) {
+        for (int b = threadIdx.x; b <= A.B; b += 256) {
+            A.start[b] = start[b];
+            A.items[b] = items[b];
+        }
+        if (threadIdx.x == 0)
+            *A.shares = shares;
+    }
+    // neighbouring shares on one XCD: the row blocks of a head read the same tiles
+    const int64_t per_xcd = (shares + 7) / 8, share = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if ((int64_t)(blockIdx.x >> 3) >= per_xcd || share >= shares)
         return;
+    int64_t at = kv_cut(total, shares, share);
+    const int64_t end = kv_cut(total, shares, share + 1);
+    int b = 0;
+    for (int hi = A.B; hi - b > 1;) {  // the last request that begins at or before `at`
+        const int mid = (b + hi) >> 1;
+        if (uniform(start[mid]) <= at)
+            b = mid;
+        else
+            hi = mid;
+    }
+    while (at < end) {
+        // what follows from the lane is worked out anew for each item: kept over all
+        // of them it would take the registers that the tiles need
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));
+        const int r16 = lane & 15, g = lane >> 4;
+        while (uniform(start[b + 1]) <= at)
+            b++;
+        const int slot = uniform(kv_slot(A.c, A.slots, b)), m = uniform(kv_live_nodes(A, b, slot));
+        const int32_t len = uniform(kv_len(A.c, slot));
+        const int64_t begin = uniform(start[b]);
+        const int64_t cached = ((int64_t)len + kKvTile - 1) / kKvTile, units = kv_units(A, len, m);
+        const int64_t item = (at - begin) / units, row_blocks = (m * A.G + kRows - 1) / kRows;
+        const int h = (int)(item / row_blocks), rb = (int)(item % row_blocks);
+        const int64_t u0 = at - begin - item * units;
+        const int64_t u1 = end - at < units - u0 ? u0 + (end - at) : units;
+        const bool whole = u0 == 0 && u1 == units;
+        const int64_t part = share + uniform(items[b]) + item;
+        at += u1 - u0;
+        float c1[NT], c2[NT];
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const int r = rb * kRows + 16 * t + r16;
-        if (A.splits > 1) {
-            const int64_t at = (int64_t)part * (A.row_blocks * kRows) + r;
-            if (g == 0)
-                ((floatx2*)A.part_ml)[at] = floatx2{top[t], total[t]};
+        for (int t = 0; t < NT; t++) {
+            Frag q[W / 32];
+            const uint16_t* row;
+            kv_row_of(A, b, h, m, rb * kRows + 16 * t + r16, &row);
+            kv_query<W>(row, g, D, A.scale, q, &c1[t], &c2[t]);
+            if (wave == 0)
+#pragma unroll
+                for (int s = 0; s < W / 32; s++)
+                    sq[t][s][lane] = q[s].w;
+        }
+        __syncthreads();
+        KvRows<W, NT> R;
+        R.init();
+        const uint8_t* tiles = kv_tiles(A.c, slot, h);
+        const int64_t last = cached < u1 ? cached : u1, full = len / kKvTile < last ? len / kKvTile : last;
+        int64_t u = u0 + wave;
+        if (u < last) {
+            KvTileRegs<W> T;
+            T.load_keys(tiles + u * KvTile<W>::kBytes, lane);
+            T.load_values(tiles + u * KvTile<W>::kBytes, lane);
+            for (; u < full; u += kAttendWaves) {
+                const int64_t next = u + kAttendWaves < last ? u + kAttendWaves : u;
+                kv_tile<W, NT, false>(T, tiles + next * KvTile<W>::kBytes, 32, lane, scales[wave], sq, c1, c2, R);
+            }
+            if (u < last) {  // the slot's last tile, with fewer than 32 positions
+                kv_tile<W, NT, true>(T, nullptr, (int)(len - u * kKvTile), lane, scales[wave], sq, c1, c2, R);
+                u += kAttendWaves;
+            }
+        }
+        for (; u < u1; u += kAttendWaves)
+            kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, rb * kRows, R);
+        // the waves' shares, relative to the largest m
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            R.l[t] = quad_sum(R.l[t]);
+            R.w[t] = quad_sum(R.w[t]);
+            if (g == 0) {
+                sm[wave][16 * t + r16] = R.m[t];
+                sl[wave][16 * t + r16] = R.l[t];
+            }
+        }
+        __syncthreads();
+        float top[NT], sum[NT];
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            top[t] = kLow;
+#pragma unroll
+            for (int x = 0; x < kAttendWaves; x++)
+                top[t] = fmaxf(top[t], sm[x][16 * t + r16]);
+            sum[t] = 0.f;
+#pragma unroll
+            for (int x = 0; x < kAttendWaves; x++)
+                sum[t] += sl[x][16 * t + r16] * __builtin_amdgcn_exp2f(sm[x][16 * t + r16] - top[t]);
+            const float f = __builtin_amdgcn_exp2f(R.m[t] - top[t]), of = R.E * 0x1p24f;
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++)
-                *(floatx4*)(A.part_o + at * W + 16 * mt + 4 * g) = R.o[t][mt];
-        } else if (r < A.max_nodes * A.G) {
-            const int64_t at = ((int64_t)b * A.max_nodes + r / A.G) * A.Hq + h * A.G + r % A.G;
-            const bool none = r >= m * A.G || total[t] == 0.f;
-            const float by = none ? 0.f : 1.f / total[t];
-            if (g == 0 && A.lse)
-                A.lse[at] = none ? -INFINITY : kLn2 * (top[t] + __builtin_amdgcn_logf(total[t]));
 #pragma unroll
-            for (int mt = 0; mt < W / 16; mt++)
-                if (16 * mt + 4 * g < D) {
-                    uint2 o;
-                    o.x = none ? 0u : pack_bf16(R.o[t][mt][0] * by, R.o[t][mt][1] * by);
-                    o.y = none ? 0u : pack_bf16(R.o[t][mt][2] * by, R.o[t][mt][3] * by);
-                    *(uint2*)(A.out + at * D + 16 * mt + 4 * g) = o;
-                }
+                for (int i = 0; i < 4; i++)
+                    R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : fmaf(R.o[t][mt][i], of, R.w[t]) * f;
+        }
+#pragma unroll
+        for (int half = kAttendWaves / 2; half >= 1; half >>= 1) {
+            if (wave >= half && wave < 2 * half)
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int mt = 0; mt < W / 16; mt++)
+                        so[wave - half][t][mt][lane] = R.o[t][mt];
+            __syncthreads();
+            if (wave < half)
+#pragma unroll
+                for (int t = 0; t < NT; t++)
+#pragma unroll
+                    for (int mt = 0; mt < W / 16; mt++)
+                        R.o[t][mt] += so[wave][t][mt][lane];
+            __syncthreads();
+        }
+        if (wave != 0)
+            continue;
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            const int r = rb * kRows + 16 * t + r16;
+            if (r >= m * A.G)
+                continue;
+            if (!whole) {
+                const int64_t to = part * kRows + 16 * t + r16;
+                if (g == 0)
+                    ((floatx2*)A.part_ml)[to] = floatx2{top[t], sum[t]};
+#pragma unroll
+                for (int mt = 0; mt < W / 16; mt++)
+                    *(floatx4*)(A.part_o + to * W + 16 * mt + 4 * g) = R.o[t][mt];
+            } else {
+                const int node = r / A.G;
+                const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + h * A.G + (r - node * A.G);
+                const bool none = sum[t] == 0.f;
+                const float by = none ? 0.f : 1.f / sum[t];
+                if (g == 0 && A.lse)
+                    A.lse[to] = none ? -INFINITY : kLn2 * (top[t] + __builtin_amdgcn_logf(sum[t]));
+#pragma unroll
+                for (int mt = 0; mt < W / 16; mt++)
+                    if (16 * mt + 4 * g < D) {
+                        uint2 o;
+                        o.x = none ? 0u : pack_bf16(R.o[t][mt][0] * by, R.o[t][mt][1] * by);
+                        o.y = none ? 0u : pack_bf16(R.o[t][mt][2] * by, R.o[t][mt][3] * by);
+                        *(uint2*)(A.out + to * D + 16 * mt + 4 * g) = o;
+                    }
+            }
         }
     }
 }
 
-// One wave per row: the parts of a row joined.
-template <int W>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_part)
+// The parts of a row joined, by WR waves (4, or 1 where an item has few parts);
+// rows that no share covered whole, and rows that see nothing.
+constexpr int kMaxShares = 768;
+
+template <int W, int WR>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int kRows)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.z, h = blockIdx.y, D = A.c.D;
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    __shared__ float f[4 / WR][kMaxShares];
+    __shared__ float red[2][4];
+    __shared__ floatx2 so[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.z, h = blockIdx.y, D = A.c.D;
+    const int mine = WR == 4 ? 0 : wave, r = blockIdx.x * (4 / WR) + mine;
     if (r >= A.max_nodes * A.G)
         return;
-    const int slot = kv_slot(A.c, A.slots, b);
-    const int m = kv_live_nodes(A, b, slot);
-    const int64_t at = ((int64_t)b * A.max_nodes + r / A.G) * A.Hq + h * A.G + r % A.G;
+    const int slot = kv_slot(A.c, A.slots, b), m = kv_live_nodes(A, b, slot);
+    const int node = r / A.G, d = W == 128 ? 2 * lane : lane;
+    const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + h * A.G + (r - node * A.G);
     float total = 0.f, top = kLow;
     floatx2 o = {0.f, 0.f};
-    const int d = W == 128 ? 2 * lane : lane;
     if (r < m * A.G) {
-        const int32_t len = kv_len(A.c, slot);
-        const int64_t units = ((int64_t)len + kKvTile - 1) / kKvTile + (A.k ? (m + 31) / 32 : 0);
-        const int parts = kv_parts(units, A.splits);
-        const int64_t first = (int64_t)(b * A.c.H + h) * A.splits;
-        floatx2 ml = {kLow, 0.f};
-        if (lane < parts)
-            ml = ((const floatx2*)A.part_ml)[(first + lane) * rows_per_part + r];
-        top = ml[0];
+        const int64_t row_blocks = (m * A.G + kRows - 1) / kRows, in_b = h * row_blocks + r / kRows;
+        const int64_t item = A.items[b] + in_b, all = A.start[A.B], shares = *A.shares;
+        const int64_t units = (A.start[b + 1] - A.start[b]) / (A.items[b + 1] - A.items[b]);
+        const int64_t g0 = A.start[b] + in_b * units, g1 = g0 + units;
+        if (units > 0) {
+            // the shares that hold g0 and g1 - 1
+            int64_t w0 = (int64_t)((double)g0 * (double)shares / (double)all);
+            int64_t w1 = (int64_t)((double)(g1 - 1) * (double)shares / (double)all);
+            w0 = w0 < shares ? w0 : shares - 1;
+            w1 = w1 < shares ? w1 : shares - 1;
+            while (kv_cut(all, shares, w0) > g0)
+                w0--;
+            while (kv_cut(all, shares, w0 + 1) <= g0)
+                w0++;
+            while (kv_cut(all, shares, w1) > g1 - 1)
+                w1--;
+            while (kv_cut(all, shares, w1 + 1) <= g1 - 1)
+                w1++;
+            if (w0 == w1)
+                return;  // one share wrote the row
+            const int parts = (int)(w1 - w0) + 1;
+            const int64_t first = (w0 + item) * kRows + r % kRows;  // parts are kRows apart
+            const floatx2* ml = (const floatx2*)A.part_ml;
+            const int t0 = WR == 4 ? threadIdx.x : lane, dt = 64 * WR;
+            for (int p = t0; p < parts; p += dt)
+                top = fmaxf(top, ml[first + (int64_t)p * kRows][0]);
+            top = wave_max(top);
+            if (WR == 4) {
+                if (lane == 0)
+                    red[0][wave] = top;
+                __syncthreads();
+                top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+            }
+            for (int p = t0; p < parts; p += dt) {
+                const floatx2 x = ml[first + (int64_t)p * kRows];
+                const float by = x[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);
+                f[mine][p] = by;
+                total += x[1] * by;
+            }
 #pragma unroll
-        for (int x = 32; x >= 1; x >>= 1)
-            top = fmaxf(top, __shfl_xor(top, x, 64));
-        const float f = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);
-        total = ml[1] * f;
+            for (int x = 1; x < 64; x <<= 1)
+                total += __shfl_xor(total, x, 64);
+            if (WR == 4) {
+                if (lane == 0)
+                    red[1][wave] = total;
+                __syncthreads();
+                total = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+            }
+#pragma unroll 8
+            for (int p = WR == 4 ? wave : 0; p < parts; p += WR) {
+                const float by = f[mine][p];
+                const float* from = A.part_o + (first + (int64_t)p * kRows) * W + d;
+                if (W == 128) {
+                    const floatx2 x = *(const floatx2*)from;
+                    o[0] = by == 0.f ? o[0] : fmaf(by, x[0], o[0]);
+                    o[1] = by == 0.f ? o[1] : fmaf(by, x[1], o[1]);
+                } else {
+                    o[0] = by == 0.f ? o[0] : fmaf(by, from[0], o[0]);
+                }
+            }
+            if (WR == 4) {
+                so[wave][lane] = o;
+                __syncthreads();
+                if (wave != 0)
+                    return;
 #pragma unroll
-        for (int x = 32; x >= 1; x >>= 1)
-            total += __shfl_xor(total, x, 64);
-        for (int s = 0; s < parts; s++) {
-            const float fs = __shfl(f, s, 64);
-            if (fs == 0.f)
-                continue;
-            const float* from = A.part_o + ((first + s) * rows_per_part + r) * W + d;
-            if (W == 128) {
-                const floatx2 x = *(const floatx2*)from;
-                o[0] = fmaf(fs, x[0], o[0]);
-                o[1] = fmaf(fs, x[1], o[1]);
-            } else {
-                o[0] = fmaf(fs, from[0], o[0]);
+                for (int w = 1; w < 4; w++)
+                    o += so[w][lane];
             }
         }
     }
+    if (WR == 4 && wave != 0)
+        return;
     const bool none = total == 0.f;
     const float by = none ? 0.f : 1.f / total;
     if (d < D) {
         if (W == 128)
-            *(uint32_t*)(A.out + at * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
+            *(uint32_t*)(A.out + to * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
         else
-            A.out[at * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
+            A.out[to * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
     }
     if (lane == 0 && A.lse)
-        A.lse[at] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
+        A.lse[to] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }
 
 // A workgroup's waves stream tiles of keys; up to 64 rows at a time stand in LDS
@@ -865,9 +1009,12 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
 
 }  // namespace
 
-// Rows a workgroup takes, and the parts a slot is split into.
+// Rows a workgroup takes (16 nt), its items at most, and the workgroups that
+// share the work: as many as the chip holds at once (3 a CU with one row tile, 2
+// with more), fewer where the slots cannot hold so many units.
 struct KvPlan {
-    int nt, row_blocks, splits;
+    int nt, wgs;
+    int64_t items;
 };
 
 static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
@@ -875,41 +1022,38 @@ static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
     KvPlan p;
     const int rows = max_nodes * (Hq / c.H);
     p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 3;
-    p.row_blocks = (rows + 16 * p.nt - 1) / (16 * p.nt);
-    const int64_t groups = (int64_t)B * c.H * p.row_blocks;
-    const int64_t want = p.nt > 1 ? 1024 : 2048;
-    int64_t s = (want + groups - 1) / groups;
-    const int64_t most = (c.tiles + OIL_NODES_MAX / 32) / (2 * kAttendWaves);
-    s = s < most ? s : most;
-    p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    p.items = (int64_t)B * c.H * ((rows + 16 * p.nt - 1) / (16 * p.nt));
+    const int64_t units = p.items * (c.tiles + (max_nodes + 31) / 32);
+    const int64_t most = ((units + kLeastShare - 1) / kLeastShare + 7) / 8 * 8;
+    const int64_t chip = p.nt == 1 ? kMaxShares : 512;
+    p.wgs = (int)(most < chip ? most : chip);
     return p;
 }
 
-static size_t kv_part_rows(const KvView& c, int32_t B, const KvPlan& p)
-{
-    return p.splits == 1 ? 0 : (size_t)B * c.H * p.splits * p.row_blocks * 16 * p.nt;
-}
+static size_t kv_part_rows(const KvPlan& p) { return (size_t)(p.wgs + p.items) * 16 * p.nt; }
 
 size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
 {
-    const size_t n = kv_part_rows(c, B, kv_plan(c, B, max_nodes, Hq));
-    return n * (c.W + 2) * sizeof(float) + 256;
+    const size_t n = kv_part_rows(kv_plan(c, B, max_nodes, Hq));
+    return (2 * (size_t)(B + 1) + 2) * sizeof(int64_t) + 16 + n * (c.W + 2) * sizeof(float);
 }
 
 template <int W>
 static void kv_attend_launch(const KvAttend& A, const KvPlan& p, hipStream_t stream)
 {
-    const int64_t parts = (int64_t)A.B * A.c.H * p.splits;
-    const dim3 grid((unsigned)((parts + 7) / 8 * 8 * p.row_blocks)), block(64 * kAttendWaves);
+    const dim3 grid(p.wgs), block(64 * kAttendWaves);
     if (p.nt == 1)
         hipLaunchKernelGGL((kv_attend_kernel<W, 1>), grid, block, 0, stream, A);
     else if (p.nt == 2)
         hipLaunchKernelGGL((kv_attend_kernel<W, 2>), grid, block, 0, stream, A);
     else
         hipLaunchKernelGGL((kv_attend_kernel<W, 3>), grid, block, 0, stream, A);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(kv_join_kernel<W>, dim3((A.max_nodes * A.G + 3) / 4, A.c.H, A.B), dim3(256), 0, stream, A,
-                           p.row_blocks * 16 * p.nt);
+    const int rows = A.max_nodes * A.G;
+    if (p.wgs >= 8 * p.items)
+        hipLaunchKernelGGL((kv_join_kernel<W, 4>), dim3(rows, A.c.H, A.B), dim3(256), 0, stream, A, 16 * p.nt);
+    else
+        hipLaunchKernelGGL((kv_join_kernel<W, 1>), dim3((rows + 3) / 4, A.c.H, A.B), dim3(256), 0, stream, A,
+                           16 * p.nt);
 }
 
 hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
@@ -928,16 +1072,17 @@ hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, co
     A.mask = mask;
     A.out = (uint16_t*)out;
     A.lse = lse;
-    A.part_o = (float*)workspace;
-    A.part_ml = (float*)workspace + kv_part_rows(c, B, p) * c.W;
+    A.start = (int64_t*)workspace;
+    A.items = A.start + B + 1;
+    A.shares = A.items + B + 1;
+    A.part_o = (float*)(A.shares + 2);  // 16-byte aligned: an even number of words before
+    A.part_ml = A.part_o + kv_part_rows(p) * c.W;
     A.q_ld = q_ld;
     A.ld = ld;
     A.B = B;
     A.Hq = Hq;
     A.G = Hq / c.H;
     A.max_nodes = max_nodes;
-    A.splits = p.splits;
-    A.row_blocks = p.row_blocks;
     A.scale = scale;
     if (c.W == 64)
         kv_attend_launch<64>(A, p, stream);
