@@ -50,6 +50,15 @@ struct KvRounding {
     static constexpr float kLeast = kTwo ? 0x1p-16f : 0x1p-6f;
 };
 
+// The item that a share begins inside (parts 0: at one's start).
+struct KvCut {
+    int32_t b, h, row_block;
+    int32_t nth;     // share since the item's first
+    int32_t parts;   // of the item
+    int32_t first;   // its first part
+    int32_t pad[2];
+};
+
 struct KvAttend {
     KvView c;
     const int32_t* slots;
@@ -59,13 +68,12 @@ struct KvAttend {
     const uint32_t* mask;
     uint16_t* out;
     float* lse;
-    int64_t* start;  // per request (and one past): units before it,
-    int64_t* items;  // items before it,
-    int64_t* shares; // (one word) shares the units are cut into;
-    float* part_o;   // per cut of an item: unnormalised rows,
+    KvCut* cuts;     // where each share begins
+    float* part_o;   // per part of an item: unnormalised rows,
     float* part_ml;  // and each one's (m, sum)
     int64_t q_ld, ld;
     int32_t B, Hq, G, max_nodes;
+    int32_t shift;   // a unit is 2^shift tiles
     float scale;
 };
 
@@ -109,6 +117,9 @@ __device__ __forceinline__ bf16x8 kv_codes_bf16(uint32_t w)
     return f.b;
 }
 
+// What memory holds is read again after this: no load moves past it.
+__device__ __forceinline__ void read_anew() { asm volatile("" ::: "memory"); }
+
 // A value beside its counterpart 32 (16) lanes away.
 __device__ __forceinline__ void swap32(float x, float* a, float* b)
 {
@@ -149,25 +160,27 @@ __device__ __forceinline__ float wave_max(float x)
     return fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x041F)));
 }
 
-// Raw bf16 operand of a row for columns 32 ks + 8 g ..; zeros past D or for no row.
-__device__ __forceinline__ u32x4 kv_raw(const uint16_t* row, int d, int D)
+// Raw bf16 operand of a row for columns d .. d + 7; zeros past D or where it is
+// not wanted (the load is made all the same, inside the row, so that loads do not
+// wait for each other's conditions).
+__device__ __forceinline__ u32x4 kv_raw(const uint16_t* row, int d, int D, bool wanted = true)
 {
-    u32x4 z = {0, 0, 0, 0};
-    return row && d < D ? *(const u32x4*)(row + d) : z;
+    const u32x4 x = *(const u32x4*)(row + (d < D ? d : 0)), z = {0, 0, 0, 0};
+    return wanted && d < D ? x : z;
 }
 
 // Scaled binary16 operands of a row, and the factors of its scores in base 2:
 // x = c1 (s dot) + c2 z.
 template <int W>
-__device__ __forceinline__ void kv_query(const uint16_t* row, int g, int D, float scale, Frag (&f)[W / 32], float* c1,
-                                         float* c2)
+__device__ __forceinline__ void kv_query(const uint16_t* row, bool live, int g, int D, float scale,
+                                         Frag (&f)[W / 32], float* c1, float* c2)
 {
     u32x4 raw[W / 32];
     uint32_t top = 0;
     float sum = 0.f;
 #pragma unroll
     for (int ks = 0; ks < W / 32; ks++) {
-        raw[ks] = kv_raw(row, 32 * ks + 8 * g, D);
+        raw[ks] = kv_raw(row, 32 * ks + 8 * g, D, live);
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const uint32_t lo = raw[ks][j] & 0x7FFFu, hi = (raw[ks][j] >> 16) & 0x7FFFu;
@@ -278,14 +291,14 @@ struct KvRows {
 // product has taken them, the values after the second.
 template <int W, int NT, bool END>
 __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, int valid, int lane, KvScales& L,
-                                        const u32x4 (*q)[W / 32][64], const float (&c1)[NT], const float (&c2)[NT],
+                                        const u32x4 (*q)[W / 32][64], const float (*factors)[2][16],
                                         KvRows<W, NT>& R)
 {
     constexpr bool kTwo = KvRounding<NT>::kTwo;
     const int g = lane >> 4;
     const bool on = !END || (lane & 31) < valid, value = lane >= 32;
     float s = on ? kv_s(T.pair) : 0.f, z = on ? kv_z(T.pair) : 0.f;
-    if (__any(value && s > R.E))
+    if (__builtin_expect(__any(value && s > R.E), 0))
         R.widen(value ? s : 0.f);
     const bool rare = __any(value && on && s < R.E * KvRounding<NT>::kLeast);
     if (value) {
@@ -298,7 +311,7 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
     L.z[lane] = z;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    asm volatile("" ::: "memory");  // the queries are read from LDS tile by tile: their registers are wanted
+    read_anew();  // the queries are read from LDS tile by tile: their registers are wanted
     floatx4 S[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; t++)
@@ -336,20 +349,21 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
     Frag p[NT], low[kTwo ? NT : 1];  // low: what the first operands leave
 #pragma unroll
     for (int t = 0; t < NT; t++) {
+        const float c1 = factors[t][0][lane & 15], c2 = factors[t][1][lane & 15];
         float x[8];
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], fmaf(kz[e], c2[t], -R.m[t]));
+            x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1, fmaf(kz[e], c2, -R.m[t]));
             if (END)
                 x[e] = in[e] ? x[e] : -INFINITY;
             top = fmaxf(top, x[e]);
         }
-        if (__any(top > kRoom)) {
+        if (__builtin_expect(__any(top > kRoom), 0)) {
             top = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], kz[e] * c2[t]);
+                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1, kz[e] * c2);
                 if (END)
                     x[e] = in[e] ? x[e] : -INFINITY;
                 top = fmaxf(top, x[e]);
@@ -357,24 +371,20 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
             R.raise(t, top);
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1[t], fmaf(kz[e], c2[t], -R.m[t]));
+                x[e] = fmaf(ks[e] * S[t][e >> 2][e & 3], c1, fmaf(kz[e], c2, -R.m[t]));
             if (END)
 #pragma unroll
                 for (int e = 0; e < 8; e++)
                     x[e] = in[e] ? x[e] : -INFINITY;
         }
+        if (__builtin_expect(rare, 0)) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            x[e] = __builtin_amdgcn_exp2f(x[e]);
-            R.l[t] += x[e];
-            if (kTwo || rare)
+            for (int e = 0; e < 8; e++) {
+                x[e] = __builtin_amdgcn_exp2f(x[e]);
+                R.l[t] += x[e];
                 R.w[t] = fmaf(x[e], vz[e], R.w[t]);
-            x[e] *= vs[e];
-        }
-        if (rare) {
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-                x[e] *= e & 2 ? 0x1p-20f : 0x1p-24f;
+                x[e] *= vs[e] * (e & 2 ? 0x1p-20f : 0x1p-24f);
+            }
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
@@ -389,6 +399,14 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
             }
         } else {
 #pragma unroll
+            for (int e = 0; e < 8; e++) {
+                x[e] = __builtin_amdgcn_exp2f(x[e]);
+                R.l[t] += x[e];
+                if (kTwo)
+                    R.w[t] = fmaf(x[e], vz[e], R.w[t]);
+                x[e] *= vs[e];
+            }
+#pragma unroll
             for (int j = 0; j < 4; j++)
                 p[t].w[j] = pack_f16(x[2 * j], x[2 * j + 1]);
             if (kTwo) {
@@ -402,7 +420,7 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
             }
         }
     }
-    if (!rare) {
+    if (__builtin_expect(!rare, 1)) {
 #pragma unroll
         for (int mt = 0; mt < W / 16; mt++) {
             const h16x8 vf = kv_codes(T.value_word(mt));
@@ -418,16 +436,15 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
         T.load_values(next, lane);
 }
 
-// The node of row r of a head, -1 for none, and the row's queries.
+// The node of row r of a head, -1 for none, and the row's queries (for none:
+// those of row 0).
 __device__ __forceinline__ int kv_row_of(const KvAttend& A, int b, int h, int m, int r, const uint16_t** row)
 {
-    if (r >= m * A.G) {
-        *row = nullptr;
-        return -1;
-    }
+    const bool live = r < m * A.G;
+    r = live ? r : 0;
     const int node = r / A.G;
     *row = A.q + ((int64_t)b * A.max_nodes + node) * A.q_ld + (int64_t)(h * A.G + r - node * A.G) * A.c.D;
-    return node;
+    return live ? node : -1;
 }
 
 // A tile of the tree: nodes n0 .. n0 + 31 of m, for rows r0 ...
@@ -469,8 +486,7 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
         Frag kf[2];
 #pragma unroll
         for (int a = 0; a < 2; a++)
-            kf[a].w = kv_raw(n0 + 16 * a + r < m ? A.k + base + (int64_t)(16 * a + r) * A.ld : nullptr,
-                             32 * s + 8 * g, D);
+            kf[a].w = kv_raw(A.k + base + (int64_t)(n0 + 16 * a + r < m ? 16 * a + r : 0) * A.ld, 32 * s + 8 * g, D);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             Frag qf;
@@ -503,30 +519,42 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
             p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
     }
     bool odd = false;
+    constexpr int kGroup = NT == 1 ? 4 : 2;  // column tiles whose loads are in flight together
 #pragma unroll
-    for (int mt = 0; mt < W / 16; mt++) {
-        const int d = 16 * mt + r;
-        Frag vf;
+    for (int m0 = 0; m0 < W / 16; m0 += kGroup) {
+        read_anew();  // the next group's loads would take registers that the rows need
+        uint32_t raw[kGroup][8];
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            uint32_t two = 0;
+        for (int i = 0; i < kGroup; i++)
 #pragma unroll
-            for (int x = 0; x < 2; x++) {
-                const int e = 2 * j + x, key = 16 * (e >> 2) + 4 * g + (e & 3);
-                uint32_t u = n0 + key < m && d < D ? A.v[base + (int64_t)key * A.ld + d] : 0;
-                if ((u & 0x7F80u) == 0x7F80u) {  // not finite: added below, to the rows that see it
-                    odd = true;
-                    u = 0;
-                }
-                two |= u << (16 * x);
+            for (int e = 0; e < 8; e++) {
+                const int d = 16 * (m0 + i) + r, key = 16 * (e >> 2) + 4 * g + (e & 3);
+                raw[i][e] = A.v[base + (int64_t)(n0 + key < m ? key : 0) * A.ld + (d < D ? d : 0)];
             }
-            vf.w[j] = two;
-        }
 #pragma unroll
-        for (int t = 0; t < NT; t++)
-            R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.b, p[t].b, R.o[t][mt], 0, 0, 0);
+        for (int i = 0; i < kGroup; i++) {
+            const int d = 16 * (m0 + i) + r;
+            Frag vf;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                uint32_t two = 0;
+#pragma unroll
+                for (int x = 0; x < 2; x++) {
+                    const int e = 2 * j + x, key = 16 * (e >> 2) + 4 * g + (e & 3);
+                    const bool in = n0 + key < m && d < D;
+                    // not finite: added below, to the rows that see it
+                    const bool bad = (raw[i][e] & 0x7F80u) == 0x7F80u;
+                    odd = odd || (in && bad);
+                    two |= (in && !bad ? raw[i][e] : 0u) << (16 * x);
+                }
+                vf.w[j] = two;
+            }
+#pragma unroll
+            for (int t = 0; t < NT; t++)
+                R.o[t][m0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.b, p[t].b, R.o[t][m0 + i], 0, 0, 0);
+        }
     }
-    if (__any(odd)) {
+    if (__builtin_expect(__any(odd), 0)) {
         for (int key = 0; key < 32 && n0 + key < m; key++)
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++)
@@ -544,7 +572,6 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
 }
 
 constexpr int kAttendWaves = 4;
-constexpr int kMaxB = 512;
 
 __device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
 {
@@ -555,157 +582,297 @@ __device__ __forceinline__ int kv_live_nodes(const KvAttend& A, int b, int slot)
 }
 
 // Tiles that a live row of a request goes through: the cache's, then the tree's.
-__device__ __forceinline__ int64_t kv_units(const KvAttend& A, int32_t len, int m)
+__device__ __forceinline__ int kv_row_tiles(const KvAttend& A, int32_t len, int m)
 {
-    return ((int64_t)len + kKvTile - 1) / kKvTile + (A.k ? (m + 31) / 32 : 0);
+    return (len + kKvTile - 1) / kKvTile + (A.k ? (m + 31) / 32 : 0);
 }
 
 // The work of a call is one list of units: requests, in each its heads, in each
-// its blocks of 16 NT rows (an item), in each the tiles.  Equal shares of it go
+// its blocks of 16 NT rows (an item), in each the tiles (a unit is one, or so many
+// that there are fewer than 2^31).  Equal shares of it go
 // to the workgroups, whatever the lengths; a share that begins or ends inside an
 // item leaves a part of it, numbered share + item (which no two parts have in
 // common), for the join.
+
 // Least units of a share: two tiles a wave.
-constexpr int64_t kLeastShare = 2 * kAttendWaves;
+constexpr int kLeastShare = 2 * kAttendWaves;
+constexpr int kMaxShares = 768;
 
 // A value that all lanes hold alike, as a scalar.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x)
+
+// total units in `shares` equal ones: share w begins at each * w + left * w / shares.
+struct KvShares {
+    int total, shares, each, left;
+
+    __device__ __forceinline__ int cut(int w) const
+    {
+        return each * w + (int)((uint32_t)left * (uint32_t)w / (uint32_t)shares);
+    }
+    // The share that holds unit x.
+    __device__ __forceinline__ int of(int x) const
+    {
+        int w = (int)((float)x * (float)shares / (float)total);
+        w = w < shares ? w : shares - 1;
+        while (w > 0 && cut(w) > x)
+            w--;
+        while (w + 1 < shares && cut(w + 1) <= x)
+            w++;
+        return w;
+    }
+};
+
+// Sums over the lanes up to and with this one (rows of 16 by shifts, then the
+// last lane of each row to the rows after it).
+__device__ __forceinline__ int wave_scan(int x)
 {
-    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast:15
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row_bcast:31
+    return x;
 }
 
-__device__ __forceinline__ int64_t kv_cut(int64_t total, int64_t shares, int64_t w)
+// A request's part of the list.
+template <int NT>
+struct KvRequest {
+    int m, items, units;  // live nodes (0 without a tile), items, units of an item
+
+    __device__ __forceinline__ void load(const KvAttend& A, int b)
+    {
+        m = A.max_nodes;
+        items = units = 0;
+        if (b >= A.B)
+            return;
+        const int slot = kv_slot(A.c, A.slots, b);
+        m = kv_live_nodes(A, b, slot);
+        const int tiles = m ? kv_row_tiles(A, kv_len(A.c, slot), m) : 0;
+        units = (tiles + (1 << A.shift) - 1) >> A.shift;
+        m = tiles ? m : 0;
+        items = A.c.H * ((m * A.G + 16 * NT - 1) / (16 * NT));
+    }
+};
+
+// 64 requests in LDS, a copy a wave: read once an item, they would take registers
+// that the tiles need.
+struct KvRequestTable {
+    int m[64], units[64], items[64], upto[64], items_upto[64];
+
+    template <int NT>
+    __device__ __forceinline__ int put(const KvRequest<NT>& r, int lane)
+    {
+        const int sum = wave_scan(r.items * r.units);
+        m[lane] = r.m;
+        units[lane] = r.units;
+        items[lane] = r.items;
+        upto[lane] = sum;
+        items_upto[lane] = wave_scan(r.items);
+        return __builtin_amdgcn_readlane(sum, 63);
+    }
+};
+
+// Rows that see nothing (past a request's nodes, or without a tile) are cleared
+// by all workgroups together.
+template <int NT>
+__device__ __forceinline__ void kv_clear_dead(const KvAttend& A, int b0, int m)
 {
-    return total / shares * w + (total % shares) * w / shares;
+    const int D = A.c.D;
+    for (uint64_t some = __ballot(m < A.max_nodes); some; some &= some - 1) {
+        const int l = __ffsll((unsigned long long)some) - 1, live = __builtin_amdgcn_readlane(m, l);
+        const int64_t n = (int64_t)(A.max_nodes - live) * A.Hq;
+        const int64_t first = ((int64_t)(b0 + l) * A.max_nodes + live) * A.Hq;
+        for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n * (D / 8); i += gridDim.x * 256ll)
+            ((u32x4*)(A.out + first * D))[i] = u32x4{0, 0, 0, 0};
+        if (A.lse)
+            for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll)
+                A.lse[first + i] = -INFINITY;
+    }
+}
+
+// The part of an item in hand and where the share goes on: kept in LDS while the
+// tiles have the registers (scalar ones too: they spill into vector ones).
+struct KvPart {
+    int at, end, base, item_base, b0;  // the rest of the share; requests in the table
+    int b, h, row_block, m, len;
+    int part, whole, t0, t1;           // its number; tiles
+    const uint8_t* tiles;
+};
+
+// The kernel's arguments, read where they are wanted.
+__device__ __forceinline__ KvAttend kv_args()
+{
+    auto p = (const __attribute__((address_space(4))) KvAttend*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const KvAttend*)p;
+}
+
+// The next part of a share (at < end).
+template <int NT>
+__device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvRequestTable& table, const KvShares& S, int share,
+                                             int lane)
+{
+    int at = P.at, end = P.end, base = P.base, item_base = P.item_base, b0 = P.b0;
+    uint64_t past;
+    while (!(past = __ballot(table.upto[lane] > at - base))) {
+        base += uniform(table.upto[63]);
+        item_base += uniform(table.items_upto[63]);
+        b0 += 64;
+        KvRequest<NT> more;
+        more.load(A, b0 + lane);
+        table.put(more, lane);
+    }
+    const int l = __ffsll((unsigned long long)past) - 1, b = b0 + l;
+    const int m = uniform(table.m[l]), units = uniform(table.units[l]), items = uniform(table.items[l]);
+    const int begin = base + uniform(table.upto[l]) - items * units;
+    const int item0 = item_base + uniform(table.items_upto[l]) - items;
+    const int slot = uniform(kv_slot(A.c, A.slots, b));
+    const int32_t len = uniform(kv_len(A.c, slot));
+    const int row_tiles = kv_row_tiles(A, len, m);
+    const int row_blocks = (uint32_t)items / (uint32_t)A.c.H, item = (uint32_t)(at - begin) / (uint32_t)units;
+    const int h = (uint32_t)item / (uint32_t)row_blocks;
+    const int u0 = at - begin - item * units, u1 = end - at < units - u0 ? u0 + (end - at) : units;
+    if (u0 != 0 && threadIdx.x == 0) {  // the first of a share's parts at most
+        const int w0 = S.of(at - u0), w1 = S.of(at - u0 + units - 1);
+        KvCut cut;
+        cut.b = b;
+        cut.h = h;
+        cut.row_block = item - h * row_blocks;
+        cut.nth = share - w0;
+        cut.parts = w1 - w0 + 1;
+        cut.first = w0 + item0 + item;
+        A.cuts[share] = cut;
+    }
+    P.at = at + u1 - u0;
+    P.base = base;
+    P.item_base = item_base;
+    P.b0 = b0;
+    P.b = b;
+    P.h = h;
+    P.row_block = item - h * row_blocks;
+    P.m = m;
+    P.len = len;
+    P.part = share + item0 + item;
+    P.whole = u0 == 0 && u1 == units;
+    P.t0 = u0 << A.shift;
+    P.t1 = (u1 << A.shift) < row_tiles ? u1 << A.shift : row_tiles;
+    P.tiles = kv_tiles(A.c, slot, h);
 }
 
 template <int W, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAttend A)
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAttend)
 {
     constexpr int kRows = 16 * NT;
-    __shared__ int64_t start[kMaxB + 1], items[kMaxB + 1];
-    __shared__ int64_t sums[2][kAttendWaves];
     __shared__ float sm[kAttendWaves][kRows], sl[kAttendWaves][kRows];
     __shared__ floatx4 so[kAttendWaves / 2][NT][W / 16][64];
     __shared__ u32x4 sq[NT][W / 32][64];
+    __shared__ float factors[NT][2][16];
     __shared__ __align__(16) KvScales scales[kAttendWaves];
-    const int lane0 = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), D = A.c.D;
-    // units and items before each request
-    int64_t before[2] = {0, 0};
-    for (int b0 = 0; b0 < A.B; b0 += 256) {
-        const int b = b0 + (int)threadIdx.x;
-        int64_t x[2] = {0, 0};
-        if (b < A.B) {
-            const int slot = kv_slot(A.c, A.slots, b), m = kv_live_nodes(A, b, slot);
-            x[1] = (int64_t)A.c.H * ((m * A.G + kRows - 1) / kRows);
-            x[0] = m ? x[1] * kv_units(A, kv_len(A.c, slot), m) : 0;
+    __shared__ KvRequestTable tables[kAttendWaves];
+    __shared__ KvPart parts[kAttendWaves];
+    __shared__ KvShares shares;
+    const int wave = uniform((int)(threadIdx.x >> 6));
+    KvPart& P = parts[wave];
+    {
+        const KvAttend A = kv_args();
+        const int lane = threadIdx.x & 63;
+        KvShares S;
+        {
+            KvRequest<NT> first;
+            first.load(A, lane);
+            S.total = tables[wave].put(first, lane);
+            kv_clear_dead<NT>(A, 0, first.m);
         }
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-            int64_t run = x[y];
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int64_t z = __shfl_up(run, o, 64);
-                run += lane0 >= o ? z : 0;
-            }
-            if (lane0 == 63)
-                sums[y][wave] = run;
-            x[y] = run;
+        for (int b0 = 64; b0 < A.B; b0 += 64) {
+            KvRequest<NT> more;
+            more.load(A, b0 + lane);
+            kv_clear_dead<NT>(A, b0, more.m);
+            S.total += __builtin_amdgcn_readlane(wave_scan(more.items * more.units), 63);
         }
-        __syncthreads();
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-            int64_t all = 0, mine = before[y];
-            for (int w = 0; w < kAttendWaves; w++) {
-                mine += w < wave ? sums[y][w] : 0;
-                all += sums[y][w];
-            }
-            if (b < A.B)
-                (y ? items : start)[b + 1] = mine + x[y];
-            before[y] += all;
+        const int most = (int)(((uint32_t)S.total + kLeastShare - 1) / kLeastShare);
+        S.shares = most < 1 ? 1 : most < (int)gridDim.x ? most : (int)gridDim.x;
+        S.each = (int)((uint32_t)S.total / (uint32_t)S.shares);
+        S.left = S.total - S.each * S.shares;
+        // neighbouring shares on one XCD: the row blocks of a head read the same tiles
+        const int per_xcd = (S.shares + 7) / 8, share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+        if ((int)blockIdx.x >= S.shares && threadIdx.x == 0)
+            A.cuts[blockIdx.x].parts = 0;  // no such share
+        if ((int)(blockIdx.x >> 3) >= per_xcd || share >= S.shares)
+            return;
+        if (threadIdx.x == 0) {
+            A.cuts[share].parts = 0;
+            shares = S;
         }
-        __syncthreads();
+        P.at = S.cut(share);
+        P.end = S.cut(share + 1);
+        P.base = P.item_base = P.b0 = 0;
     }
-    if (threadIdx.x == 0)
-        start[0] = items[0] = 0;
     __syncthreads();
-    const int64_t total = uniform(before[0]), most = (total + kLeastShare - 1) / kLeastShare;
-    const int64_t shares = most < 1 ? 1 : most < gridDim.x ? most : gridDim.x;
-    if (blockIdx.x == 0) {
-        for (int b = threadIdx.x; b <= A.B; b += 256) {
-            A.start[b] = start[b];
-            A.items[b] = items[b];
-        }
-        if (threadIdx.x == 0)
-            *A.shares = shares;
-    }
-    // neighbouring shares on one XCD: the row blocks of a head read the same tiles
-    const int64_t per_xcd = (shares + 7) / 8, share = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((int64_t)(blockIdx.x >> 3) >= per_xcd || share >= shares)
-        return;
-    int64_t at = kv_cut(total, shares, share);
-    const int64_t end = kv_cut(total, shares, share + 1);
-    int b = 0;
-    for (int hi = A.B; hi - b > 1;) {  // the last request that begins at or before `at`
-        const int mid = (b + hi) >> 1;
-        if (uniform(start[mid]) <= at)
-            b = mid;
-        else
-            hi = mid;
-    }
-    while (at < end) {
-        // what follows from the lane is worked out anew for each item: kept over all
+    while (uniform(P.at) < uniform(P.end)) {
+        // what follows from the lane is worked out anew for each part: kept over all
         // of them it would take the registers that the tiles need
-        int lane = lane0;
+        int lane = threadIdx.x & 63;
         asm volatile("" : "+v"(lane));
         const int r16 = lane & 15, g = lane >> 4;
-        while (uniform(start[b + 1]) <= at)
-            b++;
-        const int slot = uniform(kv_slot(A.c, A.slots, b)), m = uniform(kv_live_nodes(A, b, slot));
-        const int32_t len = uniform(kv_len(A.c, slot));
-        const int64_t begin = uniform(start[b]);
-        const int64_t cached = ((int64_t)len + kKvTile - 1) / kKvTile, units = kv_units(A, len, m);
-        const int64_t item = (at - begin) / units, row_blocks = (m * A.G + kRows - 1) / kRows;
-        const int h = (int)(item / row_blocks), rb = (int)(item % row_blocks);
-        const int64_t u0 = at - begin - item * units;
-        const int64_t u1 = end - at < units - u0 ? u0 + (end - at) : units;
-        const bool whole = u0 == 0 && u1 == units;
-        const int64_t part = share + uniform(items[b]) + item;
-        at += u1 - u0;
-        float c1[NT], c2[NT];
+        {
+            const KvAttend A = kv_args();
+            const int per_xcd = (uniform(shares.shares) + 7) / 8;
+            kv_next_part<NT>(A, P, tables[wave], shares, (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), lane);
+            read_anew();
+            const int b = uniform(P.b), h = uniform(P.h), m = uniform(P.m), r0 = uniform(P.row_block) * kRows;
 #pragma unroll
-        for (int t = 0; t < NT; t++) {
-            Frag q[W / 32];
-            const uint16_t* row;
-            kv_row_of(A, b, h, m, rb * kRows + 16 * t + r16, &row);
-            kv_query<W>(row, g, D, A.scale, q, &c1[t], &c2[t]);
-            if (wave == 0)
+            for (int t = 0; t < NT; t++) {
+                Frag q[W / 32];
+                const uint16_t* row;
+                const int node = kv_row_of(A, b, h, m, r0 + 16 * t + r16, &row);
+                float c1, c2;
+                kv_query<W>(row, node >= 0, g, A.c.D, A.scale, q, &c1, &c2);
+                if (wave == 0) {
 #pragma unroll
-                for (int s = 0; s < W / 32; s++)
-                    sq[t][s][lane] = q[s].w;
+                    for (int s = 0; s < W / 32; s++)
+                        sq[t][s][lane] = q[s].w;
+                    factors[t][0][r16] = c1;  // the four lanes of a row alike
+                    factors[t][1][r16] = c2;
+                }
+            }
         }
         __syncthreads();
         KvRows<W, NT> R;
         R.init();
-        const uint8_t* tiles = kv_tiles(A.c, slot, h);
-        const int64_t last = cached < u1 ? cached : u1, full = len / kKvTile < last ? len / kKvTile : last;
-        int64_t u = u0 + wave;
-        if (u < last) {
-            KvTileRegs<W> T;
-            T.load_keys(tiles + u * KvTile<W>::kBytes, lane);
-            T.load_values(tiles + u * KvTile<W>::kBytes, lane);
-            for (; u < full; u += kAttendWaves) {
-                const int64_t next = u + kAttendWaves < last ? u + kAttendWaves : u;
-                kv_tile<W, NT, false>(T, tiles + next * KvTile<W>::kBytes, 32, lane, scales[wave], sq, c1, c2, R);
-            }
-            if (u < last) {  // the slot's last tile, with fewer than 32 positions
-                kv_tile<W, NT, true>(T, nullptr, (int)(len - u * kKvTile), lane, scales[wave], sq, c1, c2, R);
-                u += kAttendWaves;
+        int u;
+        {
+            const int len = uniform(P.len), cached = (len + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
+            const int last = cached < t1 ? cached : t1, full = len / kKvTile < last ? len / kKvTile : last;
+            const uint64_t base = (uint64_t)P.tiles;
+            const uint8_t* tiles = (const uint8_t*)((uint64_t)(uint32_t)uniform((int)(base >> 32)) << 32 |
+                                                    (uint32_t)uniform((int)base));
+            u = uniform(P.t0) + wave;
+            if (u < last) {
+                KvTileRegs<W> T;
+                T.load_keys(tiles + (int64_t)u * KvTile<W>::kBytes, lane);
+                T.load_values(tiles + (int64_t)u * KvTile<W>::kBytes, lane);
+                read_anew();
+                for (; u < full; u += kAttendWaves) {
+                    const int next = u + kAttendWaves < last ? u + kAttendWaves : u;
+                    kv_tile<W, NT, false>(T, tiles + (int64_t)next * KvTile<W>::kBytes, 32, lane, scales[wave], sq,
+                                          factors, R);
+                }
+                if (__builtin_expect(u < last, 0)) {  // the slot's last tile, with fewer than 32 positions
+                    kv_tile<W, NT, true>(T, nullptr, uniform(P.len) - u * kKvTile, lane, scales[wave], sq, factors,
+                                         R);
+                    u += kAttendWaves;
+                }
             }
         }
-        for (; u < u1; u += kAttendWaves)
-            kv_nodes<W, NT>(A, b, h, (int)(u - cached) * 32, m, lane, rb * kRows, R);
+        read_anew();
+        if (__builtin_expect(u < uniform(P.t1), 0)) {
+            const KvAttend A = kv_args();
+            const int cached = (uniform(P.len) + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
+            for (; u < t1; u += kAttendWaves)
+                kv_nodes<W, NT>(A, uniform(P.b), uniform(P.h), (u - cached) * 32, uniform(P.m), lane,
+                                uniform(P.row_block) * kRows, R);
+        }
         // the waves' shares, relative to the largest m
 #pragma unroll
         for (int t = 0; t < NT; t++) {
@@ -754,13 +921,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         }
         if (wave != 0)
             continue;
+        const KvAttend A = kv_args();
+        const int b = uniform(P.b), h = uniform(P.h), D = A.c.D, r0 = uniform(P.row_block) * kRows;
+        const int live = uniform(P.m) * A.G;
+        const bool whole = uniform(P.whole);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            const int r = rb * kRows + 16 * t + r16;
-            if (r >= m * A.G)
+            const int r = r0 + 16 * t + r16;
+            if (r >= live)
                 continue;
             if (!whole) {
-                const int64_t to = part * kRows + 16 * t + r16;
+                const int64_t to = (int64_t)uniform(P.part) * kRows + 16 * t + r16;
                 if (g == 0)
                     ((floatx2*)A.part_ml)[to] = floatx2{top[t], sum[t]};
 #pragma unroll
@@ -786,109 +957,105 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
     }
 }
 
-// The parts of a row joined, by WR waves (4, or 1 where an item has few parts);
-// rows that no share covered whole, and rows that see nothing.
-constexpr int kMaxShares = 768;
-
-template <int W, int WR>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int kRows)
+// The parts of the items that shares cut, joined: the workgroup of each share
+// that begins inside an item takes its part of that item's rows, with four waves
+// a row where the parts are many, else one.
+template <int W>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_item)
 {
-    __shared__ float f[4 / WR][kMaxShares];
+    constexpr int kFew = 8;
+    __shared__ float f[kMaxShares];
     __shared__ float red[2][4];
     __shared__ floatx2 so[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.z, h = blockIdx.y, D = A.c.D;
-    const int mine = WR == 4 ? 0 : wave, r = blockIdx.x * (4 / WR) + mine;
-    if (r >= A.max_nodes * A.G)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = A.c.D, d = W == 128 ? 2 * lane : lane;
+    const KvCut cut = A.cuts[blockIdx.x];
+    if (cut.parts < 2 || cut.nth < 1)
         return;
-    const int slot = kv_slot(A.c, A.slots, b), m = kv_live_nodes(A, b, slot);
-    const int node = r / A.G, d = W == 128 ? 2 * lane : lane;
-    const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + h * A.G + (r - node * A.G);
-    float total = 0.f, top = kLow;
-    floatx2 o = {0.f, 0.f};
-    if (r < m * A.G) {
-        const int64_t row_blocks = (m * A.G + kRows - 1) / kRows, in_b = h * row_blocks + r / kRows;
-        const int64_t item = A.items[b] + in_b, all = A.start[A.B], shares = *A.shares;
-        const int64_t units = (A.start[b + 1] - A.start[b]) / (A.items[b + 1] - A.items[b]);
-        const int64_t g0 = A.start[b] + in_b * units, g1 = g0 + units;
-        if (units > 0) {
-            // the shares that hold g0 and g1 - 1
-            int64_t w0 = (int64_t)((double)g0 * (double)shares / (double)all);
-            int64_t w1 = (int64_t)((double)(g1 - 1) * (double)shares / (double)all);
-            w0 = w0 < shares ? w0 : shares - 1;
-            w1 = w1 < shares ? w1 : shares - 1;
-            while (kv_cut(all, shares, w0) > g0)
-                w0--;
-            while (kv_cut(all, shares, w0 + 1) <= g0)
-                w0++;
-            while (kv_cut(all, shares, w1) > g1 - 1)
-                w1--;
-            while (kv_cut(all, shares, w1 + 1) <= g1 - 1)
-                w1++;
-            if (w0 == w1)
-                return;  // one share wrote the row
-            const int parts = (int)(w1 - w0) + 1;
-            const int64_t first = (w0 + item) * kRows + r % kRows;  // parts are kRows apart
-            const floatx2* ml = (const floatx2*)A.part_ml;
-            const int t0 = WR == 4 ? threadIdx.x : lane, dt = 64 * WR;
-            for (int p = t0; p < parts; p += dt)
-                top = fmaxf(top, ml[first + (int64_t)p * kRows][0]);
-            top = wave_max(top);
-            if (WR == 4) {
-                if (lane == 0)
-                    red[0][wave] = top;
-                __syncthreads();
-                top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    const int b = cut.b, m = kv_live_nodes(A, b, kv_slot(A.c, A.slots, b)), left = m * A.G - cut.row_block * rows_per_item;
+    const int rows = left < rows_per_item ? left : rows_per_item;
+    const bool few = cut.parts <= kFew;
+    const int step = few ? 4 * (cut.parts - 1) : cut.parts - 1;
+    for (int r = few ? 4 * (cut.nth - 1) + wave : cut.nth - 1; r < rows; r += step) {
+        const int64_t first = (int64_t)cut.first * rows_per_item + r;  // parts are rows_per_item apart
+        const floatx2* ml = (const floatx2*)A.part_ml;
+        const float* from = A.part_o + first * W + d;
+        float top = kLow, total = 0.f;
+        floatx2 o = {0.f, 0.f};
+        if (few) {
+            floatx2 x[kFew], y[kFew];
+#pragma unroll
+            for (int p = 0; p < kFew; p++) {
+                const int64_t at = (int64_t)(p < cut.parts ? p : 0) * rows_per_item;
+                x[p] = ml[first + at];
+                if (W == 128)
+                    y[p] = *(const floatx2*)(from + at * W);
+                else
+                    y[p][0] = from[at * W];
             }
-            for (int p = t0; p < parts; p += dt) {
-                const floatx2 x = ml[first + (int64_t)p * kRows];
+#pragma unroll
+            for (int p = 0; p < kFew; p++)
+                top = fmaxf(top, x[p][0]);
+#pragma unroll
+            for (int p = 0; p < kFew; p++) {
+                const float by = p >= cut.parts || x[p][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[p][0] - top);
+                total += p >= cut.parts ? 0.f : x[p][1] * by;
+                o[0] = by == 0.f ? o[0] : fmaf(by, y[p][0], o[0]);
+                o[1] = by == 0.f || W == 64 ? o[1] : fmaf(by, y[p][1], o[1]);
+            }
+        } else {
+            for (int p = threadIdx.x; p < cut.parts; p += 256)
+                top = fmaxf(top, ml[first + (int64_t)p * rows_per_item][0]);
+            top = wave_max(top);
+            __syncthreads();
+            if (lane == 0)
+                red[0][wave] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+            for (int p = threadIdx.x; p < cut.parts; p += 256) {
+                const floatx2 x = ml[first + (int64_t)p * rows_per_item];
                 const float by = x[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);
-                f[mine][p] = by;
+                f[p] = by;
                 total += x[1] * by;
             }
 #pragma unroll
             for (int x = 1; x < 64; x <<= 1)
                 total += __shfl_xor(total, x, 64);
-            if (WR == 4) {
-                if (lane == 0)
-                    red[1][wave] = total;
-                __syncthreads();
-                total = red[1][0] + red[1][1] + red[1][2] + red[1][3];
-            }
+            if (lane == 0)
+                red[1][wave] = total;
+            __syncthreads();
+            total = red[1][0] + red[1][1] + red[1][2] + red[1][3];
 #pragma unroll 8
-            for (int p = WR == 4 ? wave : 0; p < parts; p += WR) {
-                const float by = f[mine][p];
-                const float* from = A.part_o + (first + (int64_t)p * kRows) * W + d;
-                if (W == 128) {
-                    const floatx2 x = *(const floatx2*)from;
-                    o[0] = by == 0.f ? o[0] : fmaf(by, x[0], o[0]);
-                    o[1] = by == 0.f ? o[1] : fmaf(by, x[1], o[1]);
-                } else {
-                    o[0] = by == 0.f ? o[0] : fmaf(by, from[0], o[0]);
-                }
+            for (int p = wave; p < cut.parts; p += 4) {
+                const float by = f[p];
+                const float* at = from + (int64_t)p * rows_per_item * W;
+                floatx2 y = {at[0], 0.f};
+                if (W == 128)
+                    y = *(const floatx2*)at;
+                o[0] = by == 0.f ? o[0] : fmaf(by, y[0], o[0]);
+                o[1] = by == 0.f ? o[1] : fmaf(by, y[1], o[1]);
             }
-            if (WR == 4) {
-                so[wave][lane] = o;
-                __syncthreads();
-                if (wave != 0)
-                    return;
+            so[wave][lane] = o;
+            __syncthreads();
 #pragma unroll
-                for (int w = 1; w < 4; w++)
-                    o += so[w][lane];
-            }
+            for (int w = 1; w < 4; w++)
+                o += so[(wave + w) & 3][lane];
+            __syncthreads();
+            if (wave != 0)
+                continue;
         }
+        const int row = cut.row_block * rows_per_item + r, node = row / A.G;
+        const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + cut.h * A.G + (row - node * A.G);
+        const bool none = total == 0.f;
+        const float by = none ? 0.f : 1.f / total;
+        if (d < D) {
+            if (W == 128)
+                *(uint32_t*)(A.out + to * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
+            else
+                A.out[to * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
+        }
+        if (lane == 0 && A.lse)
+            A.lse[to] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
     }
-    if (WR == 4 && wave != 0)
-        return;
-    const bool none = total == 0.f;
-    const float by = none ? 0.f : 1.f / total;
-    if (d < D) {
-        if (W == 128)
-            *(uint32_t*)(A.out + to * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
-        else
-            A.out[to * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
-    }
-    if (lane == 0 && A.lse)
-        A.lse[to] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));
 }
 
 // A workgroup's waves stream tiles of keys; up to 64 rows at a time stand in LDS
@@ -926,17 +1093,13 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
         __syncthreads();
         if (wave < kTiles) {
             const int r = r0 + 16 * wave + r16;
-            const uint16_t* row = nullptr;
-            float l = -INFINITY;
-            if (r < rows) {
-                const int64_t at = (int64_t)b * max_nodes + kv_source(nodes, b, max_nodes, r / G);
-                l = lse[at * Hq + h * G + r % G];
-                if (l != -INFINITY)
-                    row = q + at * q_ld + (int64_t)(h * G + r % G) * c.D;
-            }
+            const int rr = r < rows ? r : 0, a = h * G + rr % G;
+            const int64_t at = (int64_t)b * max_nodes + kv_source(nodes, b, max_nodes, rr / G);
+            const float l = lse[at * Hq + a];
+            const bool row = r < rows && l != -INFINITY;
             Frag f[W / 32];
             float c1, c2;
-            kv_query<W>(row, g, c.D, scale, f, &c1, &c2);
+            kv_query<W>(q + at * q_ld + (int64_t)a * c.D, row, g, c.D, scale, f, &c1, &c2);
 #pragma unroll
             for (int s = 0; s < W / 32; s++)
                 sq[wave][s][lane] = f[s].w;
@@ -1013,7 +1176,7 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
 // share the work: as many as the chip holds at once (3 a CU with one row tile, 2
 // with more), fewer where the slots cannot hold so many units.
 struct KvPlan {
-    int nt, wgs;
+    int nt, wgs, shift;
     int64_t items;
 };
 
@@ -1023,7 +1186,9 @@ static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
     const int rows = max_nodes * (Hq / c.H);
     p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 3;
     p.items = (int64_t)B * c.H * ((rows + 16 * p.nt - 1) / (16 * p.nt));
-    const int64_t units = p.items * (c.tiles + (max_nodes + 31) / 32);
+    int64_t units = p.items * (c.tiles + (max_nodes + 31) / 32);
+    for (p.shift = 0; units >= 0x7FFFFFFF; p.shift++)
+        units = p.items * (((c.tiles + (max_nodes + 31) / 32) >> (p.shift + 1)) + 1);
     const int64_t most = ((units + kLeastShare - 1) / kLeastShare + 7) / 8 * 8;
     const int64_t chip = p.nt == 1 ? kMaxShares : 512;
     p.wgs = (int)(most < chip ? most : chip);
@@ -1035,7 +1200,7 @@ static size_t kv_part_rows(const KvPlan& p) { return (size_t)(p.wgs + p.items) *
 size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
 {
     const size_t n = kv_part_rows(kv_plan(c, B, max_nodes, Hq));
-    return (2 * (size_t)(B + 1) + 2) * sizeof(int64_t) + 16 + n * (c.W + 2) * sizeof(float);
+    return kMaxShares * sizeof(KvCut) + n * (c.W + 2) * sizeof(float);
 }
 
 template <int W>
@@ -1048,12 +1213,8 @@ static void kv_attend_launch(const KvAttend& A, const KvPlan& p, hipStream_t str
         hipLaunchKernelGGL((kv_attend_kernel<W, 2>), grid, block, 0, stream, A);
     else
         hipLaunchKernelGGL((kv_attend_kernel<W, 3>), grid, block, 0, stream, A);
-    const int rows = A.max_nodes * A.G;
-    if (p.wgs >= 8 * p.items)
-        hipLaunchKernelGGL((kv_join_kernel<W, 4>), dim3(rows, A.c.H, A.B), dim3(256), 0, stream, A, 16 * p.nt);
-    else
-        hipLaunchKernelGGL((kv_join_kernel<W, 1>), dim3((rows + 3) / 4, A.c.H, A.B), dim3(256), 0, stream, A,
-                           16 * p.nt);
+    if (p.wgs > 1)
+        hipLaunchKernelGGL(kv_join_kernel<W>, grid, dim3(256), 0, stream, A, 16 * p.nt);
 }
 
 hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
@@ -1072,10 +1233,8 @@ hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, co
     A.mask = mask;
     A.out = (uint16_t*)out;
     A.lse = lse;
-    A.start = (int64_t*)workspace;
-    A.items = A.start + B + 1;
-    A.shares = A.items + B + 1;
-    A.part_o = (float*)(A.shares + 2);  // 16-byte aligned: an even number of words before
+    A.cuts = (KvCut*)workspace;
+    A.part_o = (float*)(A.cuts + kMaxShares);
     A.part_ml = A.part_o + kv_part_rows(p) * c.W;
     A.q_ld = q_ld;
     A.ld = ld;
@@ -1083,6 +1242,7 @@ hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, co
     A.Hq = Hq;
     A.G = Hq / c.H;
     A.max_nodes = max_nodes;
+    A.shift = p.shift;
     A.scale = scale;
     if (c.W == 64)
         kv_attend_launch<64>(A, p, stream);
