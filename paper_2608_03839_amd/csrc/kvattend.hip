@@ -518,6 +518,13 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
         for (int j = 0; j < 4; j++)
             p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
     }
+    // the values, columns in lanes: two bytes a load, from eight rows at fixed distances
+    const uint16_t* from[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const int key = 16 * (e >> 2) + 4 * g + (e & 3);
+        from[e] = A.v + base + (int64_t)(n0 + key < m ? key : 0) * A.ld;
+    }
     bool odd = false;
     constexpr int kGroup = NT == 1 ? 4 : 2;  // column tiles whose loads are in flight together
 #pragma unroll
@@ -525,36 +532,42 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
         read_anew();  // the next group's loads would take registers that the rows need
         uint32_t raw[kGroup][8];
 #pragma unroll
+        for (int i = 0; i < kGroup; i++) {
+            // past D nothing is wanted; half a column tile repeats itself
+            const int at = D == W || 16 * (m0 + i) + 16 <= D ? 16 * (m0 + i) + r
+                                                             : 16 * (m0 + i) < D ? 16 * (m0 + i) + (r & 7) : 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                raw[i][e] = from[e][at];
+        }
+        Frag vf[kGroup];
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 top = {0, 0};
+#pragma unroll
         for (int i = 0; i < kGroup; i++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const int d = 16 * (m0 + i) + r, key = 16 * (e >> 2) + 4 * g + (e & 3);
-                raw[i][e] = A.v[base + (int64_t)(n0 + key < m ? key : 0) * A.ld + (d < D ? d : 0)];
-            }
-#pragma unroll
-        for (int i = 0; i < kGroup; i++) {
-            const int d = 16 * (m0 + i) + r;
-            Frag vf;
-#pragma unroll
             for (int j = 0; j < 4; j++) {
-                uint32_t two = 0;
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    const int e = 2 * j + x, key = 16 * (e >> 2) + 4 * g + (e & 3);
-                    const bool in = n0 + key < m && d < D;
-                    // not finite: added below, to the rows that see it
-                    const bool bad = (raw[i][e] & 0x7F80u) == 0x7F80u;
-                    odd = odd || (in && bad);
-                    two |= (in && !bad ? raw[i][e] : 0u) << (16 * x);
-                }
-                vf.w[j] = two;
+                vf[i].w[j] = raw[i][2 * j] | raw[i][2 * j + 1] << 16;
+                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[i].w[j] & 0x7FFF7FFFu));
             }
+        if (__builtin_expect(__any(top[0] >= 0x7F80 || top[1] >= 0x7F80), 0)) {
+            // not finite: nothing here, and added below to the rows that see it
+            odd = true;
+#pragma unroll
+            for (int i = 0; i < kGroup; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const uint32_t lo = vf[i].w[j] & 0xFFFFu, hi = vf[i].w[j] >> 16;
+                    vf[i].w[j] = ((lo & 0x7F80u) == 0x7F80u ? 0u : lo) | ((hi & 0x7F80u) == 0x7F80u ? 0u : hi << 16);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kGroup; i++)
 #pragma unroll
             for (int t = 0; t < NT; t++)
-                R.o[t][m0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.b, p[t].b, R.o[t][m0 + i], 0, 0, 0);
-        }
+                R.o[t][m0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i].b, p[t].b, R.o[t][m0 + i], 0, 0, 0);
     }
-    if (__builtin_expect(__any(odd), 0)) {
+    if (__builtin_expect(odd, 0)) {
         for (int key = 0; key < 32 && n0 + key < m; key++)
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++)
@@ -568,6 +581,65 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
                             if ((sees[t] >> key) & 1)
                                 R.o[t][mt][i] += bf16_bits_to_float(u);
                 }
+    }
+}
+
+// The same for one row tile and the few nodes of single tokens: lane by lane, in
+// binary32, a node at a time (at one node, a decode step's, 1 us where the
+// products above and their operands take 8).
+constexpr int kFewNodes = 4;
+
+template <int W>
+__device__ __forceinline__ void kv_few_nodes(const KvAttend& A, int b, int h, int m, int lane, KvRows<W, 1>& R)
+{
+    const int g = lane >> 4, D = A.c.D;
+    const uint16_t* row;
+    const int node = kv_row_of(A, b, h, m, lane & 15, &row);
+    u32x4 q[W / 32];
+#pragma unroll
+    for (int s = 0; s < W / 32; s++)
+        q[s] = kv_raw(row, 32 * s + 8 * g, D);
+    uint32_t sees = node < 0 ? 0 : (2u << node) - 1;
+    if (A.mask && node >= 0)
+        sees = A.mask[((int64_t)b * A.max_nodes + node) * ((A.max_nodes + 31) / 32)];
+    if (R.E < 1.f)
+        R.widen(1.f);
+    const float by = 0x1p-24f / R.E;
+    for (int u = 0; u < m; u++) {
+        const int64_t at = ((int64_t)b * A.max_nodes + u) * A.ld + (int64_t)h * D;
+        u32x4 k[W / 32];
+        uint2 v[W / 16];
+#pragma unroll
+        for (int s = 0; s < W / 32; s++)
+            k[s] = kv_raw(A.k + at, 32 * s + 8 * g, D);
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++)
+            v[mt] = *(const uint2*)(A.v + at + (16 * mt + 4 * g < D ? 16 * mt + 4 * g : 0));
+        float dot = 0.f;
+#pragma unroll
+        for (int s = 0; s < W / 32; s++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                dot = fmaf(__uint_as_float(q[s][j] << 16), __uint_as_float(k[s][j] << 16), dot);
+                dot = fmaf(__uint_as_float(q[s][j] & 0xFFFF0000u), __uint_as_float(k[s][j] & 0xFFFF0000u), dot);
+            }
+        dot = quad_sum(dot);
+        const bool on = (sees >> u) & 1;
+        const float x = on ? dot * (A.scale * kLog2e) : -INFINITY;
+        if (__any(x - R.m[0] > kRoom))
+            R.raise(0, x);
+        const float p = on ? __builtin_amdgcn_exp2f(x - R.m[0]) : 0.f;
+        R.l[0] += g == 0 ? p : 0.f;
+#pragma unroll
+        for (int mt = 0; mt < W / 16; mt++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t w = i < 2 ? v[mt].x : v[mt].y;
+                const uint32_t y = i & 1 ? w & 0xFFFF0000u : w << 16;
+                // not finite: itself, whatever p rounds to
+                const float f = (y & 0x7F800000u) == 0x7F800000u ? 1.f : p * by;
+                R.o[0][mt][i] = on ? fmaf(f, __uint_as_float(y), R.o[0][mt][i]) : R.o[0][mt][i];
+            }
     }
 }
 
@@ -638,17 +710,18 @@ __device__ __forceinline__ int wave_scan(int x)
 // A request's part of the list.
 template <int NT>
 struct KvRequest {
-    int m, items, units;  // live nodes (0 without a tile), items, units of an item
+    int slot, len, m, items, units;  // m: live nodes (0 without a tile); units of an item
 
     __device__ __forceinline__ void load(const KvAttend& A, int b)
     {
         m = A.max_nodes;
-        items = units = 0;
+        slot = len = items = units = 0;
         if (b >= A.B)
             return;
-        const int slot = kv_slot(A.c, A.slots, b);
+        slot = kv_slot(A.c, A.slots, b);
         m = kv_live_nodes(A, b, slot);
-        const int tiles = m ? kv_row_tiles(A, kv_len(A.c, slot), m) : 0;
+        len = m ? kv_len(A.c, slot) : 0;
+        const int tiles = m ? kv_row_tiles(A, len, m) : 0;
         units = (tiles + (1 << A.shift) - 1) >> A.shift;
         m = tiles ? m : 0;
         items = A.c.H * ((m * A.G + 16 * NT - 1) / (16 * NT));
@@ -658,12 +731,14 @@ struct KvRequest {
 // 64 requests in LDS, a copy a wave: read once an item, they would take registers
 // that the tiles need.
 struct KvRequestTable {
-    int m[64], units[64], items[64], upto[64], items_upto[64];
+    int slot[64], len[64], m[64], units[64], items[64], upto[64], items_upto[64];
 
     template <int NT>
     __device__ __forceinline__ int put(const KvRequest<NT>& r, int lane)
     {
         const int sum = wave_scan(r.items * r.units);
+        slot[lane] = r.slot;
+        len[lane] = r.len;
         m[lane] = r.m;
         units[lane] = r.units;
         items[lane] = r.items;
@@ -727,9 +802,7 @@ __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvReq
     const int m = uniform(table.m[l]), units = uniform(table.units[l]), items = uniform(table.items[l]);
     const int begin = base + uniform(table.upto[l]) - items * units;
     const int item0 = item_base + uniform(table.items_upto[l]) - items;
-    const int slot = uniform(kv_slot(A.c, A.slots, b));
-    const int32_t len = uniform(kv_len(A.c, slot));
-    const int row_tiles = kv_row_tiles(A, len, m);
+    const int slot = uniform(table.slot[l]), len = uniform(table.len[l]), row_tiles = kv_row_tiles(A, len, m);
     const int row_blocks = (uint32_t)items / (uint32_t)A.c.H, item = (uint32_t)(at - begin) / (uint32_t)units;
     const int h = (uint32_t)item / (uint32_t)row_blocks;
     const int u0 = at - begin - item * units, u1 = end - at < units - u0 ? u0 + (end - at) : units;
@@ -778,10 +851,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         const KvAttend A = kv_args();
         const int lane = threadIdx.x & 63;
         KvShares S;
+        int items;
         {
             KvRequest<NT> first;
             first.load(A, lane);
             S.total = tables[wave].put(first, lane);
+            items = __builtin_amdgcn_readlane(wave_scan(first.items), 63);
             kv_clear_dead<NT>(A, 0, first.m);
         }
         for (int b0 = 64; b0 < A.B; b0 += 64) {
@@ -789,9 +864,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
             more.load(A, b0 + lane);
             kv_clear_dead<NT>(A, b0, more.m);
             S.total += __builtin_amdgcn_readlane(wave_scan(more.items * more.units), 63);
+            items += __builtin_amdgcn_readlane(wave_scan(more.items), 63);
         }
         const int most = (int)(((uint32_t)S.total + kLeastShare - 1) / kLeastShare);
         S.shares = most < 1 ? 1 : most < (int)gridDim.x ? most : (int)gridDim.x;
+        // as many to each item, where there are more: items of one length then end
+        // with a share, and no workgroup has two parts
+        if (S.shares > items)
+            S.shares = items ? (int)((uint32_t)S.shares / (uint32_t)items * (uint32_t)items) : 1;
         S.each = (int)((uint32_t)S.total / (uint32_t)S.shares);
         S.left = S.total - S.each * S.shares;
         // neighbouring shares on one XCD: the row blocks of a head read the same tiles
@@ -869,6 +949,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         if (__builtin_expect(u < uniform(P.t1), 0)) {
             const KvAttend A = kv_args();
             const int cached = (uniform(P.len) + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
+            if constexpr (NT == 1) {
+                if (uniform(P.m) <= kFewNodes) {
+                    kv_few_nodes<W>(A, uniform(P.b), uniform(P.h), uniform(P.m), lane, R);
+                    u = t1;
+                }
+            }
             for (; u < t1; u += kAttendWaves)
                 kv_nodes<W, NT>(A, uniform(P.b), uniform(P.h), (u - cached) * 32, uniform(P.m), lane,
                                 uniform(P.row_block) * kRows, R);
@@ -963,7 +1049,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
 template <int W>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_item)
 {
-    constexpr int kFew = 8;
+    constexpr int kFew = 16;
     __shared__ float f[kMaxShares];
     __shared__ float red[2][4];
     __shared__ floatx2 so[4][64];
@@ -982,25 +1068,29 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
         float top = kLow, total = 0.f;
         floatx2 o = {0.f, 0.f};
         if (few) {
-            floatx2 x[kFew], y[kFew];
+            const floatx2 mine = ml[first + (int64_t)(lane < cut.parts ? lane : 0) * rows_per_item];
+            top = wave_max(mine[0]);
+            const float fade = lane >= cut.parts || mine[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(mine[0] - top);
+            total = lane >= cut.parts ? 0.f : mine[1] * fade;
 #pragma unroll
-            for (int p = 0; p < kFew; p++) {
-                const int64_t at = (int64_t)(p < cut.parts ? p : 0) * rows_per_item;
-                x[p] = ml[first + at];
-                if (W == 128)
-                    y[p] = *(const floatx2*)(from + at * W);
-                else
-                    y[p][0] = from[at * W];
-            }
+            for (int x = 1; x < 64; x <<= 1)
+                total += __shfl_xor(total, x, 64);
+            for (int p0 = 0; p0 < cut.parts; p0 += 4) {
+                floatx2 y[4];
 #pragma unroll
-            for (int p = 0; p < kFew; p++)
-                top = fmaxf(top, x[p][0]);
+                for (int p = 0; p < 4; p++) {
+                    const float* at = from + (int64_t)(p0 + p < cut.parts ? p0 + p : 0) * rows_per_item * W;
+                    if (W == 128)
+                        y[p] = *(const floatx2*)at;
+                    else
+                        y[p] = floatx2{at[0], 0.f};
+                }
 #pragma unroll
-            for (int p = 0; p < kFew; p++) {
-                const float by = p >= cut.parts || x[p][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[p][0] - top);
-                total += p >= cut.parts ? 0.f : x[p][1] * by;
-                o[0] = by == 0.f ? o[0] : fmaf(by, y[p][0], o[0]);
-                o[1] = by == 0.f || W == 64 ? o[1] : fmaf(by, y[p][1], o[1]);
+                for (int p = 0; p < 4; p++) {
+                    const float by = __shfl(fade, p0 + p, 64);  // 0 past the parts
+                    o[0] = by == 0.f ? o[0] : fmaf(by, y[p][0], o[0]);
+                    o[1] = by == 0.f ? o[1] : fmaf(by, y[p][1], o[1]);
+                }
             }
         } else {
             for (int p = threadIdx.x; p < cut.parts; p += 256)
