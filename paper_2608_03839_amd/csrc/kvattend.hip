@@ -20,10 +20,9 @@
 // rounds to nothing.  p times the value row's s, over a power of two E at or above every s
 // so far, is what the second product takes, rounded to binary16 (2^-12
 // relative).  z and s c may be far larger than the value they add up to, so that
-// rounding must not reach s c alone: with one row tile a second operand takes
-// what the first leaves (the product has time to spare there); with more, z is
-// weighted by the rounded p (z / s times the operand).  Tiles in which some s is
-// below a bound times E, where operands would lose bits, take two bf16 operands.
+// rounding must not reach s c alone: z is weighted by the rounded p too (z / s
+// times the operand).  Tiles in which some s is below 2^-6 E, where operands would
+// lose bits, take two bf16 operands, the second what the first leaves.
 //
 // The tree's nodes come as further tiles in bf16 (p rounded to 2^-9).
 #include "kv.hpp"
@@ -42,13 +41,7 @@ constexpr float kLow = -1e38f;      // m of a row that has seen nothing
 constexpr float kHead = 11.f;       // the maximum's place above m
 constexpr float kRoom = 15.f;       // and the most a score may pass m by
 
-// How the rounding of a value operand is met (see the top), and the smallest
-// s / E it is met by.
-template <int NT>
-struct KvRounding {
-    static constexpr bool kTwo = NT == 1;
-    static constexpr float kLeast = kTwo ? 0x1p-16f : 0x1p-6f;
-};
+constexpr float kLeast = 0x1p-6f;    // the smallest s / E that binary16 operands are taken at
 
 // The item that a share begins inside (parts 0: at one's start).
 struct KvCut {
@@ -294,17 +287,16 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
                                         const u32x4 (*q)[W / 32][64], const float (*factors)[2][16],
                                         KvRows<W, NT>& R)
 {
-    constexpr bool kTwo = KvRounding<NT>::kTwo;
     const int g = lane >> 4;
     const bool on = !END || (lane & 31) < valid, value = lane >= 32;
     float s = on ? kv_s(T.pair) : 0.f, z = on ? kv_z(T.pair) : 0.f;
     if (__builtin_expect(__any(value && s > R.E), 0))
         R.widen(value ? s : 0.f);
-    const bool rare = __any(value && on && s < R.E * KvRounding<NT>::kLeast);
+    const bool rare = __any(value && on && s < R.E * kLeast);
     if (value) {
         const float by = 1.f / R.E;
         s *= lane & 2 ? by * 0.0625f : by;
-        if (!kTwo && !rare)
+        if (!rare)
             z = on ? z * __builtin_amdgcn_rcpf(s) : 0.f;
     }
     L.s[lane] = s;
@@ -346,7 +338,7 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
         }
     }
     __builtin_amdgcn_wave_barrier();
-    Frag p[NT], low[kTwo ? NT : 1];  // low: what the first operands leave
+    Frag p[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
         const float c1 = factors[t][0][lane & 15], c2 = factors[t][1][lane & 15];
@@ -385,16 +377,18 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
                 R.w[t] = fmaf(x[e], vz[e], R.w[t]);
                 x[e] *= vs[e] * (e & 2 ? 0x1p-20f : 0x1p-24f);
             }
+            Frag low;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
-                low[0].w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
+                low.w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
                                         x[2 * j + 1] - __uint_as_float(p[t].w[j] & 0xFFFF0000u));
             }
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++) {
+                __builtin_amdgcn_sched_barrier(0);  // one after the other: registers, not time, are short
                 const bf16x8 vf = kv_codes_bf16(T.value_word(mt));
-                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low[0].b, R.o[t][mt], 0, 0, 0);
+                R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low.b, R.o[t][mt], 0, 0, 0);
                 R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[t].b, R.o[t][mt], 0, 0, 0);
             }
         } else {
@@ -402,22 +396,14 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
             for (int e = 0; e < 8; e++) {
                 x[e] = __builtin_amdgcn_exp2f(x[e]);
                 R.l[t] += x[e];
-                if (kTwo)
-                    R.w[t] = fmaf(x[e], vz[e], R.w[t]);
                 x[e] *= vs[e];
             }
 #pragma unroll
             for (int j = 0; j < 4; j++)
                 p[t].w[j] = pack_f16(x[2 * j], x[2 * j + 1]);
-            if (kTwo) {
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    low[t].w[j] = pack_f16(x[2 * j] - (float)p[t].h[2 * j], x[2 * j + 1] - (float)p[t].h[2 * j + 1]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    R.w[t] = fmaf((float)p[t].h[e], vz[e], R.w[t]);
-            }
+            for (int e = 0; e < 8; e++)
+                R.w[t] = fmaf((float)p[t].h[e], vz[e], R.w[t]);
         }
     }
     if (__builtin_expect(!rare, 1)) {
@@ -425,11 +411,8 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
         for (int mt = 0; mt < W / 16; mt++) {
             const h16x8 vf = kv_codes(T.value_word(mt));
 #pragma unroll
-            for (int t = 0; t < NT; t++) {
-                if (kTwo)
-                    R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, low[t].h, R.o[t][mt], 0, 0, 0);
+            for (int t = 0; t < NT; t++)
                 R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[t].h, R.o[t][mt], 0, 0, 0);
-            }
         }
     }
     if (!END)
