@@ -171,19 +171,21 @@ def _shaped(t, name, shape, dtype):
     """A dense device tensor of exactly this shape and type, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    if not t.is_cuda or not t.is_contiguous():
+        _ptr(t)   # raises
+    return t.data_ptr()
 
 
 def _row_stride(t, name):
     """Elements between consecutive rows of a (B, N, heads, dim) device tensor
     whose rows are dense (a slice of a fused projection's output, say)."""
-    if t.dim() != 4:
-        raise ValueError(f"{name} must have 4 dimensions (requests, rows, heads, dim)")
     if not t.is_cuda:
         raise ValueError("device tensor expected")
     B, N, H, D = t.shape
+    if t.is_contiguous():
+        return H * D
     if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D):
         raise ValueError(f"{name}: the heads of a row must be dense")
     ld = t.stride(1) if N > 1 else t.stride(0) if B > 1 else H * D
@@ -554,6 +556,7 @@ class KvCache:
     def __init__(self, n_slots: int, n_heads: int, head_dim: int, capacity: int, device="cuda", stream=None):
         self.n_slots, self.n_heads, self.head_dim, self.capacity = n_slots, n_heads, head_dim, capacity
         self.device = torch.device(device)
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         nbytes = lib().oil_kv_bytes(n_slots, n_heads, head_dim, capacity)
         if nbytes == 0:
             raise ValueError(f"unsupported cache: n_slots={n_slots} n_heads={n_heads} head_dim={head_dim} "
@@ -565,7 +568,7 @@ class KvCache:
         h = ctypes.c_void_p()
         _check("oil_kv_create", lib().oil_kv_create(
             n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions), _ptr(self.weights),
-            _ptr(self.state), _stream(stream), ctypes.byref(h)))
+            _ptr(self.state), self._on(stream), ctypes.byref(h)))
         self.handle = h
         self._ws = {}
 
@@ -579,12 +582,19 @@ class KvCache:
     def lengths(self):
         return self.state[:, 0]
 
-    def _workspace(self, key, nbytes):
-        if nbytes == 0:
-            raise ValueError(f"unsupported cache call {key}")
-        if key not in self._ws:
-            self._ws[key] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
-        return self._ws[key]
+    def _workspace(self, call, *sizes):
+        """The workspace of a call of these sizes, kept (captured graphs hold its address)."""
+        ws = self._ws.get((call, sizes))
+        if ws is None:
+            nbytes = getattr(lib(), f"oil_kv_{call}_workspace_bytes")(self.handle, *sizes)
+            if nbytes == 0:
+                raise ValueError(f"unsupported cache call: {call} {sizes}")
+            ws = self._ws[call, sizes] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
+        return ws
+
+    def _on(self, stream):
+        """The stream's handle: torch's current one of the cache's device by default."""
+        return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self._index)
 
     def _heads(self, t, name):
         if t.dim() != 4 or t.shape[3] != self.head_dim:
@@ -604,7 +614,7 @@ class KvCache:
         """Empty the named slots (all of them when neither slots nor B is given)."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
         _check("oil_kv_reset", lib().oil_kv_reset(self.handle, _shaped(slots, "slots", (B,), torch.int32), B,
-                                                  _stream(stream)))
+                                                  self._on(stream)))
 
     def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None):
         """Append rows of k, v (B, N, n_heads, head_dim), float32 or bfloat16: all
@@ -615,7 +625,7 @@ class KvCache:
         _check("oil_kv_append", lib().oil_kv_append(
             self.handle, _shaped(slots, "slots", (B,), torch.int32), B, k.data_ptr(), v.data_ptr(), _dtype_code(k),
             ld, N, _shaped(nodes, "nodes", (B, N), torch.int32), _shaped(count, "count", (B,), torch.int32),
-            _shaped(weight, "weight", (B, self.n_heads, N), torch.float32), _stream(stream)))
+            _shaped(weight, "weight", (B, self.n_heads, N), torch.float32), self._on(stream)))
 
     def read(self, first, n, B=None, slots=None, dtype=torch.bfloat16, stream=None, out=None):
         """Rows first .. first + n - 1 as the values they stand for: (k, v), each
@@ -627,7 +637,7 @@ class KvCache:
         k, v = out
         _check("oil_kv_read", lib().oil_kv_read(
             self.handle, _shaped(slots, "slots", (B,), torch.int32), B, first, n, _shaped(k, "k", shape, k.dtype),
-            _shaped(v, "v", shape, k.dtype), _dtype_code(k), _stream(stream)))
+            _shaped(v, "v", shape, k.dtype), _dtype_code(k), self._on(stream)))
         return k, v
 
     def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None):
@@ -652,14 +662,14 @@ class KvCache:
             out = (torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=self.device),
                    torch.empty((B, N, Hq), dtype=torch.float32, device=self.device))
         o, lse = out
-        ws = self._workspace(("attend", B, N, Hq), lib().oil_kv_attend_workspace_bytes(self.handle, B, N, Hq))
+        ws = self._workspace("attend", B, N, Hq)
         _check("oil_kv_attend", lib().oil_kv_attend(
             self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
             None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
             _shaped(n_nodes, "n_nodes", (B,), torch.int32),
-            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, _ptr(ws), ws.numel(),
+            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws.data_ptr(), ws.numel(),
             _shaped(o, "out", (B, N, Hq, D), torch.bfloat16), _shaped(lse, "lse", (B, N, Hq), torch.float32),
-            _stream(stream)))
+            self._on(stream)))
         return o, lse
 
     def weigh(self, q, lse, nodes=None, count=None, scale=None, slots=None, stream=None):
@@ -673,16 +683,16 @@ class KvCache:
         _check("oil_kv_weigh", lib().oil_kv_weigh(
             self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
             _shaped(lse, "lse", (B, N, Hq), torch.float32), N, _shaped(nodes, "nodes", (B, N), torch.int32),
-            _shaped(count, "count", (B,), torch.int32), scale, _stream(stream)))
+            _shaped(count, "count", (B,), torch.int32), scale, self._on(stream)))
 
     def evict(self, keep, recent=0, B=None, slots=None, stream=None):
         """Evict every head of the named slots down to ``keep`` rows: the last
         ``recent`` positions and the heaviest others stay."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
-        ws = self._workspace(("evict", B, keep), lib().oil_kv_evict_workspace_bytes(self.handle, B, keep))
+        ws = self._workspace("evict", B, keep)
         _check("oil_kv_evict", lib().oil_kv_evict(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, _ptr(ws), ws.numel(),
-            _stream(stream)))
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, ws.data_ptr(), ws.numel(),
+            self._on(stream)))
 
 
 def merge_trees(anchor, lex_tokens, lex_len, lex_budget, sem_tokens, sem_len, sem_budget,

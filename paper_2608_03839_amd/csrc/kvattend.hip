@@ -649,7 +649,7 @@ __device__ __forceinline__ int kv_row_tiles(const KvAttend& A, int32_t len, int 
 // item leaves a part of it, numbered share + item (which no two parts have in
 // common), for the join.
 
-// Least units of a share: two tiles a wave.
+// Least units of a share: two tiles a wave (or what an item has, if less).
 constexpr int kLeastShare = 2 * kAttendWaves;
 constexpr int kMaxShares = 768;
 
@@ -849,7 +849,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
             S.total += __builtin_amdgcn_readlane(wave_scan(more.items * more.units), 63);
             items += __builtin_amdgcn_readlane(wave_scan(more.items), 63);
         }
-        const int most = (int)(((uint32_t)S.total + kLeastShare - 1) / kLeastShare);
+        const int fine = (int)(((uint32_t)S.total + kLeastShare - 1) / kLeastShare), most = fine < items ? items : fine;
         S.shares = most < 1 ? 1 : most < (int)gridDim.x ? most : (int)gridDim.x;
         // as many to each item, where there are more: items of one length then end
         // with a share, and no workgroup has two parts
@@ -1262,7 +1262,7 @@ static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
     int64_t units = p.items * (c.tiles + (max_nodes + 31) / 32);
     for (p.shift = 0; units >= 0x7FFFFFFF; p.shift++)
         units = p.items * (((c.tiles + (max_nodes + 31) / 32) >> (p.shift + 1)) + 1);
-    const int64_t most = ((units + kLeastShare - 1) / kLeastShare + 7) / 8 * 8;
+    const int64_t fine = (units + kLeastShare - 1) / kLeastShare, most = ((fine < p.items ? p.items : fine) + 7) / 8 * 8;
     const int64_t chip = p.nt == 1 ? kMaxShares : 512;
     p.wgs = (int)(most < chip ? most : chip);
     return p;
