@@ -196,29 +196,55 @@ __device__ __forceinline__ void kv_query(const uint16_t* row, bool live, int g, 
     *c2 = scale * kLog2e * quad_sum(sum);
 }
 
-// One tile of the cache in registers: its codes, and one (s, z) pair a lane (the
-// keys' in lanes 0 .. 31, the values' in the others).
+// The halves of a tile of the cache in LDS, as they are stored.
 template <int W>
-struct KvTileRegs {
-    u32x4 k[W / 64], v[W / 64];
-    uint32_t pair;
-
-    __device__ __forceinline__ void load_keys(const uint8_t* tile, int lane)
-    {
-#pragma unroll
-        for (int p = 0; p < W / 64; p++)
-            k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
-        pair = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + lane * 4);
-    }
-    __device__ __forceinline__ void load_values(const uint8_t* tile, int lane)
-    {
-#pragma unroll
-        for (int p = 0; p < W / 64; p++)
-            v[p] = *(const u32x4*)(tile + KvTile<W>::kValues + p * 1024 + lane * 16);
-    }
-    __device__ __forceinline__ uint32_t key_word(int Q) const { return k[Q >> 2][Q & 3]; }
-    __device__ __forceinline__ uint32_t value_word(int Q) const { return v[Q >> 2][Q & 3]; }
+struct KvKeys {
+    u32x4 code[W / 64][64];
+    uint32_t pair[64];  // the keys' (s, z), the values'
 };
+template <int W>
+struct KvValues {
+    u32x4 code[W / 64][64];
+};
+
+// Loads of a wave straight to LDS (buffer loads: the compiler counts what is in
+// flight exactly, where it takes global ones to LDS for flat accesses).
+template <int W>
+struct KvLoads {
+    static constexpr int kAll = W / 32 + 1;  // of a tile
+
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(const uint8_t* tile)
+    {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)tile, (short)0, KvTile<W>::kBytes, 0x00020000);
+    }
+    static __device__ __forceinline__ void keys(KvKeys<W>& to, const uint8_t* tile, int lane)
+    {
+        const __amdgpu_buffer_rsrc_t r = at(tile);
+#pragma unroll
+        for (int p = 0; p < W / 64; p++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (void __attribute__((address_space(3)))*)&to.code[p][0], 16,
+                                                     lane * 16, p * 1024, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (void __attribute__((address_space(3)))*)&to.pair[0], 4, lane * 4,
+                                                 KvTile<W>::kKeyScales, 0, 0);
+    }
+    static __device__ __forceinline__ void values(KvValues<W>& to, const uint8_t* tile, int lane)
+    {
+        const __amdgpu_buffer_rsrc_t r = at(tile);
+#pragma unroll
+        for (int p = 0; p < W / 64; p++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (void __attribute__((address_space(3)))*)&to.code[p][0], 16,
+                                                     lane * 16, KvTile<W>::kValues + p * 1024, 0, 0);
+    }
+};
+
+// Waits until at most N of the wave's loads are in flight (expcnt and lgkmcnt as
+// they are).
+template <int N>
+__device__ __forceinline__ void loads_at_most()
+{
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // LDS of a wave for the scales of its tile: s of the 32 keys, the factors of the
 // 32 value operands; then z of the keys, and what z of the values enters by.
@@ -280,16 +306,21 @@ struct KvRows {
 
 // A tile of `valid` cached positions (32, or fewer at the end of a slot).  Each
 // lane prepares one pair; the eight of its rows' scores come back through LDS.
-// The wave's next tile is loaded into the same registers, the keys when the first
+// The tile after the wave's next goes to the same place, the keys when the first
 // product has taken them, the values after the second.
 template <int W, int NT, bool END>
-__device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, int valid, int lane, KvScales& L,
+__device__ __forceinline__ void kv_tile(KvKeys<W>& K, KvValues<W>& V, const uint8_t* later, int valid, int lane, KvScales& L,
                                         const u32x4 (*q)[W / 32][64], const float (*factors)[2][16],
                                         KvRows<W, NT>& R)
 {
     const int g = lane >> 4;
     const bool on = !END || (lane & 31) < valid, value = lane >= 32;
-    float s = on ? kv_s(T.pair) : 0.f, z = on ? kv_z(T.pair) : 0.f;
+    const uint32_t pair = K.pair[lane];
+    float s = on ? kv_s(pair) : 0.f, z = on ? kv_z(pair) : 0.f;
+    u32x4 code[W / 64];
+#pragma unroll
+    for (int p = 0; p < W / 64; p++)
+        code[p] = K.code[p][lane];
     if (__builtin_expect(__any(value && s > R.E), 0))
         R.widen(value ? s : 0.f);
     const bool rare = __any(value && on && s < R.E * kLeast);
@@ -310,7 +341,8 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
         S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < W / 32; s++) {
-        const h16x8 k0 = kv_codes(T.key_word(s)), k1 = kv_codes(T.key_word(W / 32 + s));
+        const int Q0 = s, Q1 = W / 32 + s;
+        const h16x8 k0 = kv_codes(code[Q0 >> 2][Q0 & 3]), k1 = kv_codes(code[Q1 >> 2][Q1 & 3]);
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             Frag qf;
@@ -319,8 +351,10 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
             S[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf.h, S[t][1], 0, 0, 0);
         }
     }
-    if (!END)
-        T.load_keys(next, lane);
+    if (!END) {
+        __builtin_amdgcn_sched_barrier(0);
+        KvLoads<W>::keys(K, later, lane);
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     float ks[8], kz[8], vs[8], vz[8];
     bool in[8];
@@ -338,6 +372,10 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
         }
     }
     __builtin_amdgcn_wave_barrier();
+    // (the values' codes follow while the scores are made)
+#pragma unroll
+    for (int p = 0; p < W / 64; p++)
+        code[p] = V.code[p][lane];
     Frag p[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
@@ -387,7 +425,7 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++) {
                 __builtin_amdgcn_sched_barrier(0);  // one after the other: registers, not time, are short
-                const bf16x8 vf = kv_codes_bf16(T.value_word(mt));
+                const bf16x8 vf = kv_codes_bf16(code[mt >> 2][mt & 3]);
                 R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, low.b, R.o[t][mt], 0, 0, 0);
                 R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[t].b, R.o[t][mt], 0, 0, 0);
             }
@@ -409,14 +447,16 @@ __device__ __forceinline__ void kv_tile(KvTileRegs<W>& T, const uint8_t* next, i
     if (__builtin_expect(!rare, 1)) {
 #pragma unroll
         for (int mt = 0; mt < W / 16; mt++) {
-            const h16x8 vf = kv_codes(T.value_word(mt));
+            const h16x8 vf = kv_codes(code[mt >> 2][mt & 3]);
 #pragma unroll
             for (int t = 0; t < NT; t++)
                 R.o[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, p[t].h, R.o[t][mt], 0, 0, 0);
         }
     }
-    if (!END)
-        T.load_values(next, lane);
+    if (!END) {
+        __builtin_amdgcn_sched_barrier(0);
+        KvLoads<W>::values(V, later, lane);
+    }
 }
 
 // The node of row r of a head, -1 for none, and the row's queries (for none:
@@ -821,7 +861,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
 {
     constexpr int kRows = 16 * NT;
     __shared__ float sm[kAttendWaves][kRows], sl[kAttendWaves][kRows];
-    __shared__ floatx4 so[kAttendWaves / 2][NT][W / 16][64];
+    // the waves' tiles, two each (objects of their own, so that what a read waits for
+    // is known), and after them the waves' sums
+    __shared__ KvKeys<W> keys0[kAttendWaves], keys1[kAttendWaves];
+    __shared__ KvValues<W> values0[kAttendWaves], values1[kAttendWaves];
+    constexpr int kSums = (W / 16) * 64;
+    static_assert(kSums * sizeof(floatx4) <= sizeof(values0), "sums of a row tile");
+    floatx4 *const so0 = (floatx4*)&values0[0], *const so1 = (floatx4*)&values1[0];
     __shared__ u32x4 sq[NT][W / 32][64];
     __shared__ float factors[NT][2][16];
     __shared__ __align__(16) KvScales scales[kAttendWaves];
@@ -912,18 +958,29 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                                                     (uint32_t)uniform((int)base));
             u = uniform(P.t0) + wave;
             if (u < last) {
-                KvTileRegs<W> T;
-                T.load_keys(tiles + (int64_t)u * KvTile<W>::kBytes, lane);
-                T.load_values(tiles + (int64_t)u * KvTile<W>::kBytes, lane);
-                read_anew();
-                for (; u < full; u += kAttendWaves) {
-                    const int next = u + kAttendWaves < last ? u + kAttendWaves : u;
-                    kv_tile<W, NT, false>(T, tiles + (int64_t)next * KvTile<W>::kBytes, 32, lane, scales[wave], sq,
-                                          factors, R);
+                auto tile = [&](int x) { return tiles + (int64_t)(x < last ? x : last - 1) * KvTile<W>::kBytes; };
+                KvLoads<W>::keys(keys0[wave], tile(u), lane);
+                KvLoads<W>::values(values0[wave], tile(u), lane);
+                KvLoads<W>::keys(keys1[wave], tile(u + kAttendWaves), lane);
+                KvLoads<W>::values(values1[wave], tile(u + kAttendWaves), lane);
+                bool second = false;
+                while (u < full) {
+                    loads_at_most<KvLoads<W>::kAll>();
+                    kv_tile<W, NT, false>(keys0[wave], values0[wave], tile(u + 2 * kAttendWaves), 32, lane,
+                                          scales[wave], sq, factors, R);
+                    u += kAttendWaves;
+                    second = u >= full;
+                    if (second)
+                        break;
+                    loads_at_most<KvLoads<W>::kAll>();
+                    kv_tile<W, NT, false>(keys1[wave], values1[wave], tile(u + 2 * kAttendWaves), 32, lane,
+                                          scales[wave], sq, factors, R);
+                    u += kAttendWaves;
                 }
+                loads_at_most<0>();
                 if (__builtin_expect(u < last, 0)) {  // the slot's last tile, with fewer than 32 positions
-                    kv_tile<W, NT, true>(T, nullptr, uniform(P.len) - u * kKvTile, lane, scales[wave], sq, factors,
-                                         R);
+                    kv_tile<W, NT, true>(second ? keys1[wave] : keys0[wave], second ? values1[wave] : values0[wave],
+                                         nullptr, uniform(P.len) - u * kKvTile, lane, scales[wave], sq, factors, R);
                     u += kAttendWaves;
                 }
             }
@@ -972,22 +1029,20 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                     R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : fmaf(R.o[t][mt][i], of, R.w[t]) * f;
         }
 #pragma unroll
-        for (int half = kAttendWaves / 2; half >= 1; half >>= 1) {
-            if (wave >= half && wave < 2 * half)
+        for (int t = 0; t < NT; t++)
 #pragma unroll
-                for (int t = 0; t < NT; t++)
-#pragma unroll
-                    for (int mt = 0; mt < W / 16; mt++)
-                        so[wave - half][t][mt][lane] = R.o[t][mt];
-            __syncthreads();
-            if (wave < half)
-#pragma unroll
-                for (int t = 0; t < NT; t++)
+            for (int half = kAttendWaves / 2; half >= 1; half >>= 1) {
+                if (wave >= half && wave < 2 * half)
 #pragma unroll
                     for (int mt = 0; mt < W / 16; mt++)
-                        R.o[t][mt] += so[wave][t][mt][lane];
-            __syncthreads();
-        }
+                        (wave == half ? so0 : so1)[mt * 64 + lane] = R.o[t][mt];
+                __syncthreads();
+                if (wave < half)
+#pragma unroll
+                    for (int mt = 0; mt < W / 16; mt++)
+                        R.o[t][mt] += (wave == 0 ? so0 : so1)[mt * 64 + lane];
+                __syncthreads();
+            }
         if (wave != 0)
             continue;
         const KvAttend A = kv_args();
