@@ -695,6 +695,11 @@ constexpr int kMaxShares = 768;
 
 // A value that all lanes hold alike, as a scalar.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p)
+{
+    const uint64_t x = (uint64_t)p;
+    return (const uint8_t*)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
 
 // total units in `shares` equal ones: share w begins at each * w + left * w / shares.
 struct KvShares {
@@ -929,6 +934,18 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
             const int per_xcd = (uniform(shares.shares) + 7) / 8;
             kv_next_part<NT>(A, P, tables[wave], shares, (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), lane);
             read_anew();
+            {  // the wave's first two tiles are on their way while the queries come
+                const int cached = (uniform(P.len) + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
+                const int last = cached < t1 ? cached : t1, u = uniform(P.t0) + wave;
+                const int v = u + kAttendWaves < last ? u + kAttendWaves : u;
+                if (u < last) {
+                    const uint8_t* tiles = uniform(P.tiles);
+                    KvLoads<W>::keys(keys0[wave], tiles + (int64_t)u * KvTile<W>::kBytes, lane);
+                    KvLoads<W>::values(values0[wave], tiles + (int64_t)u * KvTile<W>::kBytes, lane);
+                    KvLoads<W>::keys(keys1[wave], tiles + (int64_t)v * KvTile<W>::kBytes, lane);
+                    KvLoads<W>::values(values1[wave], tiles + (int64_t)v * KvTile<W>::kBytes, lane);
+                }
+            }
             const int b = uniform(P.b), h = uniform(P.h), m = uniform(P.m), r0 = uniform(P.row_block) * kRows;
 #pragma unroll
             for (int t = 0; t < NT; t++) {
@@ -953,16 +970,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         {
             const int len = uniform(P.len), cached = (len + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
             const int last = cached < t1 ? cached : t1, full = len / kKvTile < last ? len / kKvTile : last;
-            const uint64_t base = (uint64_t)P.tiles;
-            const uint8_t* tiles = (const uint8_t*)((uint64_t)(uint32_t)uniform((int)(base >> 32)) << 32 |
-                                                    (uint32_t)uniform((int)base));
+            const uint8_t* tiles = uniform(P.tiles);
             u = uniform(P.t0) + wave;
             if (u < last) {
                 auto tile = [&](int x) { return tiles + (int64_t)(x < last ? x : last - 1) * KvTile<W>::kBytes; };
-                KvLoads<W>::keys(keys0[wave], tile(u), lane);
-                KvLoads<W>::values(values0[wave], tile(u), lane);
-                KvLoads<W>::keys(keys1[wave], tile(u + kAttendWaves), lane);
-                KvLoads<W>::values(values1[wave], tile(u + kAttendWaves), lane);
                 bool second = false;
                 while (u < full) {
                     loads_at_most<KvLoads<W>::kAll>();
