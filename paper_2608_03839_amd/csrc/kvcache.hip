@@ -470,9 +470,20 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
         return holds ? held[i] : kv_rank(c.weight[row + i], c.pos[row + i] >= young);
     };
     if (holds)
-#pragma unroll 4
-        for (int32_t i = tid; i < n; i += kSelect)
-            held[i] = kv_rank(c.weight[row + i], c.pos[row + i] >= young);
+        for (int32_t i0 = 0; i0 < n; i0 += 8 * kSelect) {  // eight rows' loads of a thread at once
+            float w[8];
+            int32_t p[8];
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+                const int32_t i = i0 + x * kSelect + tid, at = i < n ? i : n - 1;
+                w[x] = c.weight[row + at];
+                p[x] = c.pos[row + at];
+            }
+#pragma unroll
+            for (int x = 0; x < 8; x++)
+                if (i0 + x * kSelect + tid < n)
+                    held[i0 + x * kSelect + tid] = kv_rank(w[x], p[x] >= young);
+        }
     uint32_t prefix = 0, need = (uint32_t)keep;  // rows still to take at the prefix
     for (int shift = 21; ; shift = shift > 10 ? shift - kDigit : 0) {
         // digits of bits 31 .. 21, 20 .. 10, 9 .. 0
@@ -552,14 +563,17 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
             moves[at_hole].dst = x;
         if (x < i1 && x < keep && (x & (kKvTile - 1)) == 0)
             first[x / kKvTile] = at_hole;
-        if (moves_in) {
-            KvMove* m = moves + from + __popcll(mf & below);
-            m->src = x;
-            m->pos = c.pos[row + x];
-            m->weight = c.weight[row + x];
-        }
+        if (moves_in)
+            moves[from + __popcll(mf & below)].src = x;
         hole += __popcll(mo);
         from += __popcll(mf);
+    }
+    // (the late rows are a few waves' stretches: all waves fetch what they carry)
+    __syncthreads();
+    for (int i = tid; i < moving; i += kSelect) {
+        const int32_t x = moves[i].src;
+        moves[i].pos = c.pos[row + x];
+        moves[i].weight = c.weight[row + x];
     }
     if (tid == 0) {
         head->n = n;
