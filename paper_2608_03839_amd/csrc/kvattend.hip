@@ -11,8 +11,10 @@
 // (its nibble is the mantissa; the MFMA takes subnormals as they are) or, for
 // every other pair, as 16 c 2^-24: eight codes cost four ANDs and a shift.
 // Queries are scaled to binary16 by a power of two per row, so every product is
-// exact and sums are binary32; z enters as z sum(q), and the values' z as
-// sum(p z), both in binary32.
+// exact and sums are binary32.  The keys' codes are taken from their middle: the
+// product starts at -7.5 sum(q) and y = z + 7.5 s enters as y sum(q), two small
+// terms where s c and z would be large ones that cancel.  The values' z enters as
+// sum(p z), in binary32.
 //
 // The softmax keeps, per row, a reference m and sums relative to it (base 2).
 // m moves only when a score passes it by 2^15, to 11 below the maximum: then
@@ -36,7 +38,8 @@ typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr double kLog2eDouble = 1.44269504088896340736;
+constexpr float kLog2e = (float)kLog2eDouble, kLn2 = 0.693147180559945309f;
 constexpr float kLow = -1e38f;      // m of a row that has seen nothing
 constexpr float kHead = 11.f;       // the maximum's place above m
 constexpr float kRoom = 15.f;       // and the most a score may pass m by
@@ -85,6 +88,25 @@ __device__ __forceinline__ h16x8 kv_codes(uint32_t w)
     f.w[1] = w & 0x00F000F0u;
     f.w[2] = x & 0x000F000Fu;
     f.w[3] = x & 0x00F000F0u;
+    return f.h;
+}
+
+// A dword's eight codes less 8, as they are: exact, and normal numbers, whose
+// products the MFMA sums to 1e-8 of their size (subnormals, whose leading bits it
+// cuts, to 2e-7; measured over 128 columns).
+__device__ __forceinline__ h16x8 kv_codes_less_8(uint32_t w)
+{
+    union {
+        h16x2 p[4];
+        h16x8 h;
+    } f;
+    const uint32_t x = w >> 8;
+    const h16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, less = {(_Float16)-72.f, (_Float16)-72.f};
+    const h16x2 off = {(_Float16)-1032.f, (_Float16)-1032.f};
+    f.p[0] = __builtin_bit_cast(h16x2, (w & 0x000F000Fu) | 0x64006400u) + off;  // 1024 + c
+    f.p[1] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (w & 0x00F000F0u) | 0x64006400u), sixteenth, less);
+    f.p[2] = __builtin_bit_cast(h16x2, (x & 0x000F000Fu) | 0x64006400u) + off;
+    f.p[3] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (x & 0x00F000F0u) | 0x64006400u), sixteenth, less);
     return f.h;
 }
 
@@ -162,15 +184,21 @@ __device__ __forceinline__ u32x4 kv_raw(const uint16_t* row, int d, int D, bool 
     return wanted && d < D ? x : z;
 }
 
-// Scaled binary16 operands of a row, and the factors of its scores in base 2:
-// x = c1 (s dot) + c2 z.
-template <int W>
-__device__ __forceinline__ void kv_query(const uint16_t* row, bool live, int g, int D, float scale,
-                                         Frag (&f)[W / 32], float* c1, float* c2)
+// Of a row's scores in base 2, x = c1 (s dot) + c2 y, with dot starting at `from`.
+struct KvFactors {
+    float c1, c2, from;
+};
+
+// Scaled binary16 operands of a row and its factors, for codes as subnormals or
+// (EXACT) codes less 8, which begin at 0 and take y = z + 8 s.  sum(q) is taken in binary64:
+// its error would be a row's alone, and grow by y.
+template <int W, bool EXACT>
+__device__ __forceinline__ KvFactors kv_query(const uint16_t* row, bool live, int g, int D, float scale,
+                                              Frag (&f)[W / 32])
 {
     u32x4 raw[W / 32];
     uint32_t top = 0;
-    float sum = 0.f;
+    double sum = 0.0;
 #pragma unroll
     for (int ks = 0; ks < W / 32; ks++) {
         raw[ks] = kv_raw(row, 32 * ks + 8 * g, D, live);
@@ -178,7 +206,7 @@ __device__ __forceinline__ void kv_query(const uint16_t* row, bool live, int g, 
         for (int j = 0; j < 4; j++) {
             const uint32_t lo = raw[ks][j] & 0x7FFFu, hi = (raw[ks][j] >> 16) & 0x7FFFu;
             top = max(top, max(lo, hi));
-            sum += __uint_as_float(raw[ks][j] << 16) + __uint_as_float(raw[ks][j] & 0xFFFF0000u);
+            sum += (double)__uint_as_float(raw[ks][j] << 16) + (double)__uint_as_float(raw[ks][j] & 0xFFFF0000u);
         }
     }
     top = (uint32_t)quad_max((float)top);
@@ -188,12 +216,18 @@ __device__ __forceinline__ void kv_query(const uint16_t* row, bool live, int g, 
     for (int ks = 0; ks < W / 32; ks++)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const float m = j & 1 ? by * 0.0625f : by;
+            const float m = (j & 1) && !EXACT ? by * 0.0625f : by;
             f[ks].w[j] = pack_f16(__uint_as_float(raw[ks][j] << 16) * m,
                                   __uint_as_float(raw[ks][j] & 0xFFFF0000u) * m);
         }
-    *c1 = scale * kLog2e * __uint_as_float((uint32_t)min(127 + 24 - 14 + e, 254) << 23);
-    *c2 = scale * kLog2e * quad_sum(sum);
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    const double in2 = (double)scale * kLog2eDouble;
+    KvFactors x;
+    x.c1 = (float)in2 * __uint_as_float((uint32_t)min(127 + (EXACT ? 0 : 24) - 14 + e, 254) << 23);
+    x.c2 = (float)(in2 * sum);
+    x.from = EXACT ? 0.f : (float)(-7.5 * 0x1p-24 * sum * (double)by);
+    return x;
 }
 
 // The halves of a tile of the cache in LDS, as they are stored.
@@ -310,7 +344,7 @@ struct KvRows {
 // product has taken them, the values after the second.
 template <int W, int NT, bool END>
 __device__ __forceinline__ void kv_tile(KvKeys<W>& K, KvValues<W>& V, const uint8_t* later, int valid, int lane, KvScales& L,
-                                        const u32x4 (*q)[W / 32][64], const float (*factors)[2][16],
+                                        const u32x4 (*q)[W / 32][64], const float (*factors)[3][16],
                                         KvRows<W, NT>& R)
 {
     const int g = lane >> 4;
@@ -331,14 +365,16 @@ __device__ __forceinline__ void kv_tile(KvKeys<W>& K, KvValues<W>& V, const uint
             z = on ? z * __builtin_amdgcn_rcpf(s) : 0.f;
     }
     L.s[lane] = s;
-    L.z[lane] = z;
+    L.z[lane] = value ? z : fmaf(7.5f, s, z);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     read_anew();  // the queries are read from LDS tile by tile: their registers are wanted
     floatx4 S[NT][2];
 #pragma unroll
-    for (int t = 0; t < NT; t++)
-        S[t][0] = S[t][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; t++) {
+        const float from = factors[t][2][lane & 15];
+        S[t][0] = S[t][1] = floatx4{from, from, from, from};
+    }
 #pragma unroll
     for (int s = 0; s < W / 32; s++) {
         const int Q0 = s, Q1 = W / 32 + s;
@@ -874,7 +910,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
     static_assert(kSums * sizeof(floatx4) <= sizeof(values0), "sums of a row tile");
     floatx4 *const so0 = (floatx4*)&values0[0], *const so1 = (floatx4*)&values1[0];
     __shared__ u32x4 sq[NT][W / 32][64];
-    __shared__ float factors[NT][2][16];
+    __shared__ float factors[NT][3][16];
     __shared__ __align__(16) KvScales scales[kAttendWaves];
     __shared__ KvRequestTable tables[kAttendWaves];
     __shared__ KvPart parts[kAttendWaves];
@@ -952,14 +988,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                 Frag q[W / 32];
                 const uint16_t* row;
                 const int node = kv_row_of(A, b, h, m, r0 + 16 * t + r16, &row);
-                float c1, c2;
-                kv_query<W>(row, node >= 0, g, A.c.D, A.scale, q, &c1, &c2);
+                const KvFactors f = kv_query<W, false>(row, node >= 0, g, A.c.D, A.scale, q);
                 if (wave == 0) {
 #pragma unroll
                     for (int s = 0; s < W / 32; s++)
                         sq[t][s][lane] = q[s].w;
-                    factors[t][0][r16] = c1;  // the four lanes of a row alike
-                    factors[t][1][r16] = c2;
+                    factors[t][0][r16] = f.c1;  // the four lanes of a row alike
+                    factors[t][1][r16] = f.c2;
+                    factors[t][2][r16] = f.from;
                 }
             }
         }
@@ -1237,15 +1273,14 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
             const float l = lse[at * Hq + a];
             const bool row = r < rows && l != -INFINITY;
             Frag f[W / 32];
-            float c1, c2;
-            kv_query<W>(q + at * q_ld + (int64_t)a * c.D, row, g, c.D, scale, f, &c1, &c2);
+            const KvFactors x = kv_query<W, true>(q + at * q_ld + (int64_t)a * c.D, row, g, c.D, scale, f);
 #pragma unroll
             for (int s = 0; s < W / 32; s++)
                 sq[wave][s][lane] = f[s].w;
             if (g == 0) {
-                ((float*)sc[wave][0])[r16] = c1;
-                ((float*)sc[wave][1])[r16] = c2;
-                ((float*)sc[wave][2])[r16] = row ? l * kLog2e : INFINITY;  // no row: exp2 gives 0
+                ((float*)sc[wave][0])[r16] = x.c1;
+                ((float*)sc[wave][1])[r16] = x.c2;
+                ((float*)sc[wave][2])[r16] = row ? (float)((double)l * kLog2eDouble) : INFINITY;  // no row: exp2 gives 0
             }
             if (row)
                 some = 1;
@@ -1277,9 +1312,10 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
 #pragma unroll
                 for (int s = 0; s < W / 32; s++) {
                     const int Q = a * (W / 32) + s;
-                    kf[a][s] = kv_codes(k[Q >> 2][Q & 3]);
+                    kf[a][s] = kv_codes_less_8(k[Q >> 2][Q & 3]);
                 }
-            const float ks[2] = {kv_s(pair[0]), kv_s(pair[1])}, kz[2] = {kv_z(pair[0]), kv_z(pair[1])};
+            const float ks[2] = {kv_s(pair[0]), kv_s(pair[1])};
+            const float kz[2] = {fmaf(8.f, ks[0], kv_z(pair[0])), fmaf(8.f, ks[1], kv_z(pair[1]))};
             const float before = w;
             if (u + du < units)
                 load(u + du);
