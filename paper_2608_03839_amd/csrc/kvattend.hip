@@ -1430,9 +1430,11 @@ hipError_t launch_kv_weigh(const KvView& c, const int32_t* slots, int32_t B, con
                            int32_t Hq, const float* lse, int32_t max_nodes, const int32_t* nodes,
                            const int32_t* count, float scale, hipStream_t stream)
 {
-    // two tiles a wave at least, and enough workgroups for the chip's 1,024 SIMDs
+    // two tiles a wave at least, and as many workgroups as the chip holds at once (4 a
+    // CU: 2,048 take 1.03 to 1.13 of the time, equal shares of all tiles whatever the
+    // lengths 0.95 to 1.12)
     const int64_t heads = (int64_t)B * c.H, most = (c.tiles + 7) / 8;
-    int64_t blocks = (2048 + heads - 1) / heads;
+    int64_t blocks = (1024 + heads - 1) / heads;
     blocks = blocks < most ? blocks : most;
     const dim3 grid((unsigned)blocks, c.H, B), block(256);
     const bool one = max_nodes * (Hq / c.H) <= 16;
