@@ -792,8 +792,8 @@ struct KvRequest {
     }
 };
 
-// 64 requests in LDS, a copy a wave: read once an item, they would take registers
-// that the tiles need.
+// 64 requests in LDS: read once an item, they would take registers that the tiles
+// need.
 struct KvRequestTable {
     int slot[64], len[64], m[64], units[64], items[64], upto[64], items_upto[64];
 
@@ -813,19 +813,19 @@ struct KvRequestTable {
 };
 
 // Rows that see nothing (past a request's nodes, or without a tile) are cleared
-// by all workgroups together.
+// by the first waves of all workgroups together.
 template <int NT>
-__device__ __forceinline__ void kv_clear_dead(const KvAttend& A, int b0, int m)
+__device__ __forceinline__ void kv_clear_dead(const KvAttend& A, int b0, int m, int lane)
 {
     const int D = A.c.D;
     for (uint64_t some = __ballot(m < A.max_nodes); some; some &= some - 1) {
         const int l = __ffsll((unsigned long long)some) - 1, live = __builtin_amdgcn_readlane(m, l);
         const int64_t n = (int64_t)(A.max_nodes - live) * A.Hq;
         const int64_t first = ((int64_t)(b0 + l) * A.max_nodes + live) * A.Hq;
-        for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n * (D / 8); i += gridDim.x * 256ll)
+        for (int64_t i = blockIdx.x * 64ll + lane; i < n * (D / 8); i += gridDim.x * 64ll)
             ((u32x4*)(A.out + first * D))[i] = u32x4{0, 0, 0, 0};
         if (A.lse)
-            for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll)
+            for (int64_t i = blockIdx.x * 64ll + lane; i < n; i += gridDim.x * 64ll)
                 A.lse[first + i] = -INFINITY;
     }
 }
@@ -833,6 +833,7 @@ __device__ __forceinline__ void kv_clear_dead(const KvAttend& A, int b0, int m)
 // The part of an item in hand and where the share goes on: kept in LDS while the
 // tiles have the registers (scalar ones too: they spill into vector ones).
 struct KvPart {
+    int more;                          // whether there is one
     int at, end, base, item_base, b0;  // the rest of the share; requests in the table
     int b, h, row_block, m, len;
     int part, whole, t0, t1;           // its number; tiles
@@ -847,17 +848,23 @@ __device__ __forceinline__ KvAttend kv_args()
     return *(const KvAttend*)p;
 }
 
-// The next part of a share (at < end).
+// The next part of a share, if there is one (a wave for its workgroup).
 template <int NT>
 __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvRequestTable& table, const KvShares& S, int share,
                                              int lane)
 {
-    int at = P.at, end = P.end, base = P.base, item_base = P.item_base, b0 = P.b0;
+    int at = uniform(P.at), end = uniform(P.end), base = uniform(P.base), item_base = uniform(P.item_base);
+    int b0 = uniform(P.b0);
+    P.more = 0;
+    if (at >= end)
+        return;
     uint64_t past;
     while (!(past = __ballot(table.upto[lane] > at - base))) {
         base += uniform(table.upto[63]);
         item_base += uniform(table.items_upto[63]);
         b0 += 64;
+        if (b0 >= A.B)
+            return;
         KvRequest<NT> more;
         more.load(A, b0 + lane);
         table.put(more, lane);
@@ -870,7 +877,7 @@ __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvReq
     const int row_blocks = (uint32_t)items / (uint32_t)A.c.H, item = (uint32_t)(at - begin) / (uint32_t)units;
     const int h = (uint32_t)item / (uint32_t)row_blocks;
     const int u0 = at - begin - item * units, u1 = end - at < units - u0 ? u0 + (end - at) : units;
-    if (u0 != 0 && threadIdx.x == 0) {  // the first of a share's parts at most
+    if (u0 != 0 && lane == 0) {  // the first of a share's parts at most
         const int w0 = S.of(at - u0), w1 = S.of(at - u0 + units - 1);
         KvCut cut;
         cut.b = b;
@@ -881,6 +888,7 @@ __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvReq
         cut.first = w0 + item0 + item;
         A.cuts[share] = cut;
     }
+    P.more = 1;
     P.at = at + u1 - u0;
     P.base = base;
     P.item_base = item_base;
@@ -912,27 +920,26 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
     __shared__ u32x4 sq[NT][W / 32][64];
     __shared__ float factors[NT][3][16];
     __shared__ __align__(16) KvScales scales[kAttendWaves];
-    __shared__ KvRequestTable tables[kAttendWaves];
-    __shared__ KvPart parts[kAttendWaves];
+    __shared__ KvRequestTable table;
+    __shared__ KvPart P;
     __shared__ KvShares shares;
     const int wave = uniform((int)(threadIdx.x >> 6));
-    KvPart& P = parts[wave];
-    {
+    if (wave == 0) {
         const KvAttend A = kv_args();
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x;
         KvShares S;
         int items;
         {
             KvRequest<NT> first;
             first.load(A, lane);
-            S.total = tables[wave].put(first, lane);
+            S.total = table.put(first, lane);
             items = __builtin_amdgcn_readlane(wave_scan(first.items), 63);
-            kv_clear_dead<NT>(A, 0, first.m);
+            kv_clear_dead<NT>(A, 0, first.m, lane);
         }
         for (int b0 = 64; b0 < A.B; b0 += 64) {
             KvRequest<NT> more;
             more.load(A, b0 + lane);
-            kv_clear_dead<NT>(A, b0, more.m);
+            kv_clear_dead<NT>(A, b0, more.m, lane);
             S.total += __builtin_amdgcn_readlane(wave_scan(more.items * more.units), 63);
             items += __builtin_amdgcn_readlane(wave_scan(more.items), 63);
         }
@@ -946,20 +953,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         S.left = S.total - S.each * S.shares;
         // neighbouring shares on one XCD: the row blocks of a head read the same tiles
         const int per_xcd = (S.shares + 7) / 8, share = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-        if ((int)blockIdx.x >= S.shares && threadIdx.x == 0)
+        const bool mine = (int)(blockIdx.x >> 3) < per_xcd && share < S.shares;
+        if ((int)blockIdx.x >= S.shares && lane == 0)
             A.cuts[blockIdx.x].parts = 0;  // no such share
-        if ((int)(blockIdx.x >> 3) >= per_xcd || share >= S.shares)
-            return;
-        if (threadIdx.x == 0) {
+        if (mine && lane == 0)
             A.cuts[share].parts = 0;
-            shares = S;
-        }
-        P.at = S.cut(share);
-        P.end = S.cut(share + 1);
+        shares = S;
+        P.at = mine ? S.cut(share) : 0;
+        P.end = mine ? S.cut(share + 1) : 0;
         P.base = P.item_base = P.b0 = 0;
     }
-    __syncthreads();
-    while (uniform(P.at) < uniform(P.end)) {
+    while (true) {
         // what follows from the lane is worked out anew for each part: kept over all
         // of them it would take the registers that the tiles need
         int lane = threadIdx.x & 63;
@@ -967,9 +971,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         const int r16 = lane & 15, g = lane >> 4;
         {
             const KvAttend A = kv_args();
-            const int per_xcd = (uniform(shares.shares) + 7) / 8;
-            kv_next_part<NT>(A, P, tables[wave], shares, (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), lane);
-            read_anew();
+            if (wave == 0) {
+                const int per_xcd = (uniform(shares.shares) + 7) / 8;
+                kv_next_part<NT>(A, P, table, shares, (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), lane);
+            }
+            __syncthreads();
+            if (!uniform(P.more))
+                break;
             {  // the wave's first two tiles are on their way while the queries come
                 const int cached = (uniform(P.len) + kKvTile - 1) / kKvTile, t1 = uniform(P.t1);
                 const int last = cached < t1 ? cached : t1, u = uniform(P.t0) + wave;
@@ -983,20 +991,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                 }
             }
             const int b = uniform(P.b), h = uniform(P.h), m = uniform(P.m), r0 = uniform(P.row_block) * kRows;
-#pragma unroll
-            for (int t = 0; t < NT; t++) {
+            if (wave < NT) {  // a row tile a wave
                 Frag q[W / 32];
                 const uint16_t* row;
-                const int node = kv_row_of(A, b, h, m, r0 + 16 * t + r16, &row);
+                const int node = kv_row_of(A, b, h, m, r0 + 16 * wave + r16, &row);
                 const KvFactors f = kv_query<W, false>(row, node >= 0, g, A.c.D, A.scale, q);
-                if (wave == 0) {
 #pragma unroll
-                    for (int s = 0; s < W / 32; s++)
-                        sq[t][s][lane] = q[s].w;
-                    factors[t][0][r16] = f.c1;  // the four lanes of a row alike
-                    factors[t][1][r16] = f.c2;
-                    factors[t][2][r16] = f.from;
-                }
+                for (int s = 0; s < W / 32; s++)
+                    sq[wave][s][lane] = q[s].w;
+                factors[wave][0][r16] = f.c1;  // the four lanes of a row alike
+                factors[wave][1][r16] = f.c2;
+                factors[wave][2][r16] = f.from;
             }
         }
         __syncthreads();
