@@ -103,10 +103,13 @@ __device__ __forceinline__ h16x8 kv_codes_less_8(uint32_t w)
     const uint32_t x = w >> 8;
     const h16x2 sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, less = {(_Float16)-72.f, (_Float16)-72.f};
     const h16x2 off = {(_Float16)-1032.f, (_Float16)-1032.f};
-    f.p[0] = __builtin_bit_cast(h16x2, (w & 0x000F000Fu) | 0x64006400u) + off;  // 1024 + c
-    f.p[1] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (w & 0x00F000F0u) | 0x64006400u), sixteenth, less);
-    f.p[2] = __builtin_bit_cast(h16x2, (x & 0x000F000Fu) | 0x64006400u) + off;
-    f.p[3] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (x & 0x00F000F0u) | 0x64006400u), sixteenth, less);
+    // 1024 + c and 1024 + 16 c; the masks in registers, so that and-or is one instruction
+    uint32_t low = 0x000F000Fu, high = 0x00F000F0u;
+    asm("" : "+v"(low), "+v"(high));
+    f.p[0] = __builtin_bit_cast(h16x2, (w & low) | 0x64006400u) + off;
+    f.p[1] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (w & high) | 0x64006400u), sixteenth, less);
+    f.p[2] = __builtin_bit_cast(h16x2, (x & low) | 0x64006400u) + off;
+    f.p[3] = __builtin_elementwise_fma(__builtin_bit_cast(h16x2, (x & high) | 0x64006400u), sixteenth, less);
     return f.h;
 }
 
@@ -1243,7 +1246,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
 // over rows is over a lane's registers and four lanes.  ONE: at most 16 rows,
 // whose operands stay in registers.
 template <int W, bool ONE>
-__global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* __restrict__ slots,
+__global__ __launch_bounds__(256, 4) void kv_weigh_kernel(KvView c, const int32_t* __restrict__ slots,
                                                        const uint16_t* __restrict__ q, int64_t q_ld, int32_t Hq,
                                                        const float* __restrict__ lse, int32_t max_nodes,
                                                        const int32_t* __restrict__ nodes,
@@ -1259,9 +1262,9 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
     if (slot < 0)
         return;
     const int32_t len = kv_len(c, slot);
-    const int64_t u0 = (int64_t)blockIdx.x * 4 + wave, du = (int64_t)gridDim.x * 4;
-    const int64_t units = ((int64_t)len + kKvTile - 1) / kKvTile;
-    if ((int64_t)blockIdx.x * 4 >= units)
+    const int units = (int)(((int64_t)len + kKvTile - 1) / kKvTile);
+    const int u0 = (int)blockIdx.x * 4 + uniform(wave), du = (int)gridDim.x * 4;
+    if ((int)blockIdx.x * 4 >= units)
         return;
     const int rows = kv_count(nodes, count, b, max_nodes, &bound) * G;
     const uint8_t* tiles = kv_tiles(c, slot, h);
@@ -1294,36 +1297,37 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
         if (!some)
             continue;
         const int left = (rows - r0 + 15) / 16, tiles_now = left < kTiles ? left : kTiles;
-        u32x4 k[W / 64];
-        uint32_t pair[2];
-        float w = 0.f;
-        auto load = [&](int64_t u) {
-            const uint8_t* tile = tiles + u * KvTile<W>::kBytes;
+        struct Tile {
+            u32x4 k[W / 64];
+            uint32_t pair[2];
+            float w;  // of position `mine`
+        };
+        const int mine = r16 + 16 * (g >> 1);  // whose sum this lane has in the end (odd g: a copy)
+        auto load = [&](Tile& x, int u) {
+            u = u < units ? u : units - 1;
+            const uint8_t* tile = tiles + (int64_t)u * KvTile<W>::kBytes;
 #pragma unroll
             for (int p = 0; p < W / 64; p++)
-                k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
+                x.k[p] = *(const u32x4*)(tile + p * 1024 + lane * 16);
 #pragma unroll
             for (int a = 0; a < 2; a++)
-                pair[a] = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + 64 * a + 4 * r16);
-            if (lane < 32 && u * kKvTile + lane < len)
-                w = weight[u * kKvTile + lane];
+                x.pair[a] = *(const uint32_t*)(tile + KvTile<W>::kKeyScales + 64 * a + 4 * r16);
+            const int left = len - u * kKvTile;
+            x.w = (weight + (int64_t)u * kKvTile)[mine < left ? mine : 0];
         };
-        if (u0 < units)
-            load(u0);
-        for (int64_t u = u0; u < units; u += du) {
+        auto add = [&](Tile& x, int u) {
             h16x8 kf[2][W / 32];
 #pragma unroll
             for (int a = 0; a < 2; a++)
 #pragma unroll
                 for (int s = 0; s < W / 32; s++) {
                     const int Q = a * (W / 32) + s;
-                    kf[a][s] = kv_codes_less_8(k[Q >> 2][Q & 3]);
+                    kf[a][s] = kv_codes_less_8(x.k[Q >> 2][Q & 3]);
                 }
-            const float ks[2] = {kv_s(pair[0]), kv_s(pair[1])};
-            const float kz[2] = {fmaf(8.f, ks[0], kv_z(pair[0])), fmaf(8.f, ks[1], kv_z(pair[1]))};
-            const float before = w;
-            if (u + du < units)
-                load(u + du);
+            const float ks[2] = {kv_s(x.pair[0]), kv_s(x.pair[1])};
+            const float kz[2] = {fmaf(8.f, ks[0], kv_z(x.pair[0])), fmaf(8.f, ks[1], kv_z(x.pair[1]))};
+            const float before = x.w;
+            load(x, u + 2 * du);
             float sum[2] = {0.f, 0.f};
             for (int t = 0; t < tiles_now; t++) {
                 floatx4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -1342,10 +1346,24 @@ __global__ __launch_bounds__(256) void kv_weigh_kernel(KvView c, const int32_t* 
                     for (int i = 0; i < 4; i++)
                         sum[a] += __builtin_amdgcn_exp2f(fmaf(ks[a] * S[a][i], c1[i], fmaf(kz[a], c2[i], -l[i])));
             }
-            sum[0] = quad_sum(sum[0]);
-            sum[1] = quad_sum(sum[1]);
-            if (lane < 32 && u * kKvTile + lane < len)
-                weight[u * kKvTile + lane] = before + (lane < 16 ? sum[0] : sum[1]);
+            // over the four lanes of a column, those of the second 16 columns to the upper half
+            const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[0]), __float_as_uint(sum[1]),
+                                                                 false, false);
+            float p, q;
+            swap16(__uint_as_float(halves[0]) + __uint_as_float(halves[1]), &p, &q);
+            if (!(g & 1) && mine < len - u * kKvTile)
+                (weight + (int64_t)u * kKvTile)[mine] = before + (p + q);
+        };
+        // two tiles of a wave in flight
+        Tile x, y;
+        load(x, u0);
+        __builtin_amdgcn_sched_barrier(0);
+        load(y, u0 + du);
+        __builtin_amdgcn_sched_barrier(0);
+        for (int u = u0; u < units; u += 2 * du) {
+            add(x, u);
+            if (u + du < units)
+                add(y, u + du);
         }
     }
 }
