@@ -502,7 +502,8 @@ size_t oil_kv_attend_workspace_bytes(const oil_kv *kv, int32_t B, int32_t max_no
  *     S = scale * q . k;  lse = log sum exp S;  out = sum exp(S - lse) v.
  *   q          B x max_nodes rows of n_q_heads x head_dim bf16, 16-byte
  *              aligned, rows q_ld elements apart (>= n_q_heads * head_dim, a
- *              multiple of 8), requests max_nodes * q_ld apart.
+ *              multiple of 8), requests max_nodes * q_ld apart.  Finite values are
+ *              below 2^117 in magnitude (scores are binary32).
  *   k, v       the nodes' own rows, B x max_nodes of n_heads x head_dim bf16, rows
  *              ld elements apart likewise, not yet in the cache; both NULL: no row sees a node.
  *   n_nodes    B int32 (clamped to 0 .. max_nodes) or NULL: max_nodes each.

@@ -1,17 +1,20 @@
 // Attention over the verifier's 4-bit cache and the nodes of a draft tree, and
 // the attention weight that committed rows give to cached positions.
 //
-// attend: a wave streams 32-position tiles of one head straight into registers
-// in MFMA operand order and multiplies them with 16 NT rows (node, query head)
-// at once: S^T = K Q^T puts a row's scores into one lane column, and the
-// probabilities of a lane are, as they are, the operand of O^T = V^T P^T.  No
-// tile passes through LDS and nothing in the loop waits for another wave.
+// attend: a wave streams 32-position tiles of one head, stored in MFMA operand
+// order, and multiplies them with 16 NT rows (node, query head) at once: S^T =
+// K Q^T puts a row's scores into one lane column, and the probabilities of a lane
+// are, as they are, the operand of O^T = V^T P^T.  Tiles are loaded straight to
+// LDS, two a wave in flight (a lane reads back what it loaded; in registers one
+// tile fits beside the sums), and nothing in the loop waits for another wave.
 //
 // A code c of a 4-bit row enters the product as the binary16 subnormal c 2^-24
-// (its nibble is the mantissa; the MFMA takes subnormals as they are) or, for
-// every other pair, as 16 c 2^-24: eight codes cost four ANDs and a shift.
-// Queries are scaled to binary16 by a power of two per row, so every product is
-// exact and sums are binary32.  The keys' codes are taken from their middle: the
+// (its nibble is the mantissa) or, for every other pair, as 16 c 2^-24: eight
+// codes cost four ANDs and a shift.  The MFMA cuts a subnormal product's low bits:
+// sums differ from exact ones by 2e-7 of their size (normal operands: 1e-8), which
+// is 1e-4 of what an output's bf16 rounds away.  Queries are scaled to binary16 by
+// a power of two per row, exactly for values within 2^-28 of the row's largest;
+// sums are binary32.  The keys' codes are taken from their middle: the
 // product starts at -7.5 sum(q) and y = z + 7.5 s enters as y sum(q), two small
 // terms where s c and z would be large ones that cancel.  The values' z enters as
 // sum(p z), in binary32.
@@ -27,6 +30,19 @@
 // lose bits, take two bf16 operands, the second what the first leaves.
 //
 // The tree's nodes come as further tiles in bf16 (p rounded to 2^-9).
+//
+// What bounds it, at 8 key/value heads of 128 columns.  Single tokens: the stream
+// of tiles (32 requests of up to 16,384 positions, 32 query heads: 364 MB in 73
+// us, 5.0 TB/s; one slot of 262,149, 40 query heads: 285 MB in 54 us; the tiles by
+// themselves stream at 7 TB/s, the rest is the share, the queries and the joining
+// of the waves).  Many rows: the softmax's instructions between the products
+// (about 330 VALU and 24 exponentials for 32 positions by 48 rows, two waves a
+// SIMD; 32 trees of up to 65 nodes over up to 8,192 positions, 32 query heads: 343
+// us, 444 TFLOP/s; 4 chunks of 256 nodes over 16,001, 64 query heads: 783 us, 691
+// TFLOP/s).  Few positions: the launch and five dependent steps of 1 to 2 us each
+// (2,047 positions, one token: 11 us).
+//
+// weigh: below.
 #include "kv.hpp"
 
 namespace oil {
@@ -43,7 +59,6 @@ constexpr float kLog2e = (float)kLog2eDouble, kLn2 = 0.693147180559945309f;
 constexpr float kLow = -1e38f;      // m of a row that has seen nothing
 constexpr float kHead = 11.f;       // the maximum's place above m
 constexpr float kRoom = 15.f;       // and the most a score may pass m by
-
 constexpr float kLeast = 0x1p-6f;    // the smallest s / E that binary16 operands are taken at
 
 // The item that a share begins inside (parts 0: at one's start).
@@ -92,8 +107,9 @@ __device__ __forceinline__ h16x8 kv_codes(uint32_t w)
 }
 
 // A dword's eight codes less 8, as they are: exact, and normal numbers, whose
-// products the MFMA sums to 1e-8 of their size (subnormals, whose leading bits it
-// cuts, to 2e-7; measured over 128 columns).
+// products the MFMA sums to 1e-8 of their size (subnormals, whose low bits it
+// cuts, to 2e-7; measured over 128 columns).  A weight is a sum of exponentials of
+// such scores, in binary32: there the difference shows.
 __device__ __forceinline__ h16x8 kv_codes_less_8(uint32_t w)
 {
     union {
@@ -227,7 +243,7 @@ __device__ __forceinline__ KvFactors kv_query(const uint16_t* row, bool live, in
     sum += __shfl_xor(sum, 32, 64);
     const double in2 = (double)scale * kLog2eDouble;
     KvFactors x;
-    x.c1 = (float)in2 * __uint_as_float((uint32_t)min(127 + (EXACT ? 0 : 24) - 14 + e, 254) << 23);
+    x.c1 = __builtin_ldexpf((float)in2, (EXACT ? 0 : 24) - 14 + e);
     x.c2 = (float)(in2 * sum);
     x.from = EXACT ? 0.f : (float)(-7.5 * 0x1p-24 * sum * (double)by);
     return x;
@@ -1136,9 +1152,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
     }
 }
 
-// The parts of the items that shares cut, joined: the workgroup of each share
-// that begins inside an item takes its part of that item's rows, with four waves
-// a row where the parts are many, else one.
+// The parts of the items that shares cut, joined: o = sum o_p 2^(m_p - m) over
+// sum l_p 2^(m_p - m), m the largest.  The workgroup of each share that begins
+// inside an item takes its part of that item's rows, with four waves a row where
+// the parts are many (past 16 a wave's loads would follow each other), else one.
+// Latencies bound it: a launch, a table entry, (m, l), rows: 4 to 6 us, 20 us where
+// 512 shares of 48 rows by 128 columns are joined (12 MB).
 template <int W>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_item)
 {
@@ -1241,10 +1260,15 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
     }
 }
 
-// A workgroup's waves stream tiles of keys; up to 64 rows at a time stand in LDS
-// as operands.  S = Q K^T puts a position into a lane column, so a position's sum
-// over rows is over a lane's registers and four lanes.  ONE: at most 16 rows,
-// whose operands stay in registers.
+// w[j] += sum over rows of exp(scale q.k_j - lse): the keys' half of each tile and
+// the weights are read once for up to 64 rows, which stand in LDS as operands.
+// S = Q K^T puts a position into a lane column, so a position's sum over rows is
+// over a lane's registers and four lanes; a wave owns its tiles' weights, so there
+// are no atomics and one result.  Bound by tiles in flight: with one in flight a
+// wave 32 requests of up to 16,384 positions took 47 us, with two 41 (205 MB, 5.0
+// TB/s; the longest requests' waves run on alone at the end); 8 requests of up to
+// 32,768 and up to 56 rows a head 33 us, much of it the exponentials' instructions.
+// ONE: at most 16 rows, whose loop over row tiles is gone.
 template <int W, bool ONE>
 __global__ __launch_bounds__(256, 4) void kv_weigh_kernel(KvView c, const int32_t* __restrict__ slots,
                                                        const uint16_t* __restrict__ q, int64_t q_ld, int32_t Hq,
@@ -1370,9 +1394,10 @@ __global__ __launch_bounds__(256, 4) void kv_weigh_kernel(KvView c, const int32_
 
 }  // namespace
 
-// Rows a workgroup takes (16 nt), its items at most, and the workgroups that
-// share the work: as many as the chip holds at once (3 a CU with one row tile, 2
-// with more), fewer where the slots cannot hold so many units.
+// Rows a workgroup takes (16 nt: three row tiles share a tile's unpacking; a fourth
+// would spill), its items at most, and the workgroups that share the work: as many
+// as the chip holds at once (3 a CU with one row tile, whose registers at 4 would
+// spill, 2 with more), fewer where the slots cannot hold so many units.
 struct KvPlan {
     int nt, wgs, shift;
     int64_t items;
