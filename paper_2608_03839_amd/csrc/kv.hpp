@@ -90,12 +90,14 @@ __device__ __forceinline__ int kv_code(uint32_t word, int e) { return (word >> (
 __device__ __forceinline__ float kv_s(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv_z(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
-__device__ __forceinline__ uint16_t float_to_bf16_rne(float x)
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+// Two values in bf16, to the nearest even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
-    const uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u)
-        return 0x7FC0;
-    return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1)) >> 16);
+    const floatx2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
 
 }  // namespace oil

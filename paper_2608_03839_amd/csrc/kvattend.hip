@@ -51,8 +51,6 @@ namespace {
 
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr double kLog2eDouble = 1.44269504088896340736;
 constexpr float kLog2e = (float)kLog2eDouble, kLn2 = 0.693147180559945309f;
@@ -133,12 +131,6 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b)
 {
     const floatx2 x = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, h16x2));
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    const floatx2 x = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
 
 // A dword's eight codes in bf16, without the factors.

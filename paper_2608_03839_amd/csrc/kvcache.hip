@@ -12,8 +12,8 @@
 // in and 38 MB out in 42 us, 4.1 TB/s (a copy reaches 4.9); small appends by their
 // latencies, 6 us.
 //
-// read: a tile's codes to LDS, y = z + s c, 16 bytes a lane; the same rows in 40 us
-// (36 MB in, 134 MB out, 4.2 TB/s).
+// read: a tile's codes to LDS, y = z + s c, 16 bytes a lane; the same rows in 27 us
+// (36 MB in, 134 MB out, 6.4 TB/s).
 //
 // evict: a row kept above the budget moves into a hole below it, so sources
 // and destinations are disjoint and every move is independent.  One workgroup
@@ -324,68 +324,76 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
         kv_advance(c, slot, len, cnt);
 }
 
-template <typename T>
-__device__ __forceinline__ T kv_out(float x);
-template <>
-__device__ __forceinline__ float kv_out<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ uint16_t kv_out<uint16_t>(float x) { return float_to_bf16_rne(x); }
+// z + s c for eight codes c, as they leave (16-byte stores).
+__device__ __forceinline__ void kv_put(float* to, const float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+        ((floatx4*)to)[i] = floatx4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+}
+__device__ __forceinline__ void kv_put(uint16_t* to, const float (&x)[8])
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    *(u32x4*)to = w;
+}
 
-// One workgroup per tile of a (request, head): codes to LDS, then one row's
-// eight values a thread.
+// One workgroup per tile of a (request, head): codes to LDS, then eight columns a
+// thread, of a key's one dword, or of two neighbouring positions' eight dwords (whose
+// nibbles lie 16 bits apart).
 template <int W, typename T>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, const int32_t* __restrict__ slots, int64_t first,
                                                       int64_t n, T* __restrict__ k_out, T* __restrict__ v_out)
 {
-    __shared__ uint32_t buf[KvTile<W>::kBytes / 4];
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    constexpr int kUnits = W / 8, kRows = 256 / kUnits;
+    __shared__ __align__(16) uint32_t buf[KvTile<W>::kBytes / 4];
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, d = tid % kUnits * 8, row = tid / kUnits;
     const int slot = kv_slot(c, slots, b);
     const int32_t len = slot < 0 ? 0 : kv_len(c, slot);
-    const int units = c.D / 8;
+    const int64_t out = ((int64_t)b * c.H + h) * n - first;
     for (int64_t t0 = (first / kKvTile + (int64_t)blockIdx.x) * kKvTile; t0 < first + n;
          t0 += (int64_t)gridDim.x * kKvTile) {
-    if (t0 < len) {
-        const uint32_t* tile = (const uint32_t*)(kv_tiles(c, slot, h) + t0 / kKvTile * c.tile_bytes);
-        for (int i = tid; i < KvTile<W>::kBytes / 4; i += 256)
-            buf[i] = tile[i];
-    }
-    __syncthreads();
-    for (int u = tid; u < 2 * kKvTile * units; u += 256) {
-        const int side = u / (kKvTile * units), key = u / units % kKvTile, d = u % units * 8;
-        const int64_t j = t0 + key;
-        if (j < first || j >= first + n)
-            continue;
-        T o[8];
-        if (j >= len) {
+        if (t0 < len) {
+            const u32x4* tile = (const u32x4*)(kv_tiles(c, slot, h) + t0 / kKvTile * c.tile_bytes);
+            for (int i = tid; i < KvTile<W>::kBytes / 16; i += 256)
+                ((u32x4*)buf)[i] = tile[i];
+        }
+        __syncthreads();
+        auto put = [&](T* to, int key, int scales, float (&x)[8]) {
+            const int64_t j = t0 + key;
+            if (j < first || j >= first + n || d >= c.D)
+                return;
+            const uint32_t pair = buf[scales / 4 + key];
+            const float s = kv_s(pair), z = kv_z(pair);
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                o[i] = (T)0;
-        } else {
-            const uint32_t pair = buf[(side ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4 + key];
-            const float s = kv_s(pair), z = kv_z(pair);
-            if (side == 0) {
-                const uint32_t w =
-                    buf[kv_word_at((key >> 4) * (W / 32) + (d >> 5), (key & 15) + 16 * ((d & 31) >> 3))];
+                x[i] = j < len ? fmaf(s, x[i], z) : 0.f;
+            kv_put(to + (out + j) * c.D + d, x);
+        };
+        for (int key = row; key < kKvTile; key += kRows) {
+            const uint32_t w = buf[kv_word_at((key >> 4) * (W / 32) + (d >> 5), (key & 15) + 16 * ((d & 31) >> 3))];
+            float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    o[i] = kv_out<T>(z + s * (float)kv_code(w, i));
-            } else {
-                const int e = 4 * (key >> 4) + (key & 3);
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const int dd = d + i;
-                    const uint32_t w = buf[KvTile<W>::kValues / 4 +
-                                           kv_word_at(dd >> 4, (dd & 15) + 16 * ((key & 15) >> 2))];
-                    o[i] = kv_out<T>(z + s * (float)kv_code(w, e));
-                }
-            }
+            for (int e = 0; e < 8; e++)
+                x[e] = (float)kv_code(w, e);
+            put(k_out, key, KvTile<W>::kKeyScales, x);
         }
-        T* to = (side ? v_out : k_out) + (((int64_t)b * c.H + h) * n + (j - first)) * c.D + d;
+        for (int two = row; two < kKvTile / 2; two += kRows) {
+            const int key = 2 * two, e = 4 * (key >> 4) + (key & 3);
+            float x[8], y[8];
 #pragma unroll
-        for (int i = 0; i < 8 * (int)sizeof(T) / 16; i++)
-            ((u32x4*)to)[i] = ((const u32x4*)o)[i];
-    }
-    __syncthreads();
+            for (int i = 0; i < 8; i++) {
+                const uint32_t w = buf[KvTile<W>::kValues / 4 +
+                                       kv_word_at(d >> 4, (d & 15) + i + 16 * ((key & 15) >> 2))] >> (4 * (e >> 1));
+                x[i] = (float)(w & 15u);
+                y[i] = (float)(w >> 16 & 15u);
+            }
+            put(v_out, key, KvTile<W>::kValueScales, x);
+            put(v_out, key + 1, KvTile<W>::kValueScales, y);
+        }
+        __syncthreads();
     }
 }
 
