@@ -113,33 +113,36 @@ __global__ __launch_bounds__(256) void kv_reset_kernel(KvView c, const int32_t* 
         c.state[4 * (int64_t)slot + kKvLen] = c.state[4 * (int64_t)slot + kKvNext] = 0;
 }
 
+// x / s to the nearest, as the binary32 division has it, for an s of 8 significant
+// bits and inv within a few units of 1 / s: x * inv is within a few units, its
+// remainder exact (a small multiple of the last places of s and q), and the sum
+// corrected by it is off by less than 2^-20 of a unit before it is rounded, while a
+// quotient by 8 bits lies at least 1 / 512 of a unit from where rounding turns.
+__device__ __forceinline__ float kv_quotient(float x, float s, float inv)
+{
+    const float q = x * inv;
+    return fmaf(fmaf(-s, q, x), inv, q);
+}
+
+// The least s that codes are made with this way: no remainder that matters
+// underflows.
+constexpr float kLeastScale = 0x1p-90f;
+
 // (s, z) of a row with extremes lo, hi; `fine`: every value is finite.
 __device__ __forceinline__ uint32_t kv_pair(float lo, float hi, bool fine)
 {
     const uint32_t u = __float_as_uint(lo);
     const uint32_t z = (u >> 31 ? u + 0xFFFFu : u) & 0xFFFF0000u;
-    const float q = (hi - __uint_as_float(z)) / 15.f;
+    const float q = kv_quotient(hi - __uint_as_float(z), 15.f, 1.f / 15.f);
     const uint32_t s = (__float_as_uint(q) + 0xFFFFu) >> 16;  // q >= 0
     if (!fine || (z & 0x7F800000u) == 0x7F800000u || s >= 0x7F80u)
         return 0x7FC0u;
     return s | z;
 }
 
-// x / s to the nearest, as the binary32 division has it: two corrections of
-// x * inv by the exact remainder, with inv the correctly rounded 1 / s
-// (Markstein).  s is at least kLeastScale, so no remainder that matters underflows.
-constexpr float kLeastScale = 0x1p-90f;
-
-__device__ __forceinline__ float kv_quotient(float x, float s, float inv)
-{
-    float q = x * inv;
-    q = fmaf(fmaf(-s, q, x), inv, q);
-    return fmaf(fmaf(-s, q, x), inv, q);
-}
-
-// Codes of 8 values that lie on [z, z + 15 s], a nibble each of bits 0 .. 3 of a
-// byte (two words of four).  Adding 1.5 2^23 rounds to the nearest whole number, ties to even.
-__device__ __forceinline__ void kv_quantise(const float* x, float s, float z, float inv, uint32_t (&w)[2])
+// Eight values that lie on [z, z + 15 s] as whole numbers 0 .. 15 in the low bits of
+// 0x4B400000: adding 1.5 2^23 rounds to the nearest, ties to even.
+__device__ __forceinline__ void kv_quantise(const float* x, float s, float z, float inv, uint32_t (&c)[8])
 {
     float q[8];
 #pragma unroll
@@ -148,23 +151,30 @@ __device__ __forceinline__ void kv_quantise(const float* x, float s, float z, fl
     if (!(s >= kLeastScale))
         for (int e = 0; e < 8; e++)
             q[e] = s > 0.f ? (x[e] - z) / s : 0.f;
-    uint32_t c[8];
 #pragma unroll
     for (int e = 0; e < 8; e++)
-        c[e] = __float_as_uint(q[e] + 12582912.f) & 15u;
-#pragma unroll
-    for (int i = 0; i < 2; i++)
-        w[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | c[4 * i + 3] << 24;
+        c[e] = __float_as_uint(q[e] + 12582912.f);
 }
 
-// The dword of nibbles (element e in nibble e / 2 + 4 (e % 2)) of eight codes in bytes.
-__device__ __forceinline__ uint32_t kv_pack(uint32_t lo, uint32_t hi)
+// Their dword of nibbles (element e in nibble e / 2 + 4 (e % 2)); the sum of the
+// 0x4B400000 at their places goes, modulo 2^32.
+__device__ __forceinline__ uint32_t kv_nibbles(const uint32_t (&c)[8])
 {
-    // elements 0, 2 and 1, 3 of each word to 16-bit halves, low nibbles side by side
-    const uint32_t even = (lo & 0x0F000Fu) | (hi & 0x0F000Fu) << 8;         // e0 . e2 ., e4 . e6 .
-    const uint32_t odd = (lo >> 8 & 0x0F000Fu) | (hi >> 8 & 0x0F000Fu) << 8;  // e1 . e3 ., e5 . e7 .
-    const uint32_t a = (even | even >> 12) & 0xFFFFu, b = (odd | odd >> 12) & 0xFFFFu;
-    return a | b << 16;
+    uint32_t w = c[7];
+    w = (w << 4) + c[5];
+    w = (w << 4) + c[3];
+    w = (w << 4) + c[1];
+    w = (w << 4) + c[6];
+    w = (w << 4) + c[4];
+    w = (w << 4) + c[2];
+    w = (w << 4) + c[0];
+    return w - (0x4B400000u * 0x11111111u);
+}
+
+// Four of them in bytes.
+__device__ __forceinline__ uint32_t kv_bytes(const uint32_t* c)
+{
+    return (((((c[3] << 8) + c[2]) << 8) + c[1]) << 8) + c[0] - 0x4B400000u * 0x01010101u;
 }
 
 template <int W, typename T>
@@ -246,19 +256,22 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
                 }
                 const uint64_t odds = __ballot(odd);
                 const uint32_t pair = kv_pair(lo, hi, ((odds >> (tid & 56)) & 255) == 0);
-                const float s = kv_s(pair), z = kv_z(pair), inv = 1.f / s;
+                const float s = kv_s(pair), z = kv_z(pair), inv = __builtin_amdgcn_rcpf(s);
 #pragma unroll
                 for (int i = 0; i < W / 64; i++) {
                     const int d = part * (W / 8) + 8 * i;
-                    uint32_t codes[2] = {0, 0};
+                    uint32_t codes[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        codes[e] = 0x4B400000u;
                     if (d < c.D)
                         kv_quantise(x + 8 * i, s, z, inv, codes);
                     if (side == 0) {
                         image[kv_word_at((key >> 4) * (W / 32) + (d >> 5), (key & 15) + 16 * ((d & 31) >> 3))] =
-                            kv_pack(codes[0], codes[1]);
+                            kv_nibbles(codes);
                     } else {
-                        vcode[key][d / 4] = codes[0];
-                        vcode[key][d / 4 + 1] = codes[1];
+                        vcode[key][d / 4] = kv_bytes(codes);
+                        vcode[key][d / 4 + 1] = kv_bytes(codes + 4);
                     }
                 }
                 if (part == 0)
@@ -272,28 +285,40 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
             }
         }
         __syncthreads();
-        // four columns' value dwords a thread: eight positions' bytes side by side
+        const bool full = first >= len && first + kKvTile <= end;
+        // four columns' value dwords a thread: eight positions' bytes, two to a byte,
+        // and the four by four bytes turned
         if (tid < W) {
             const int g = tid / (W / 4), d4 = tid % (W / 4);
             uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const int kk = 16 * (e >> 2) + 4 * g + (e & 3);
-                const int64_t jj = first + kk;
-                w[kv_nibble(e)] = jj >= len && jj < end ? vcode[kk][d4] : 0u;
-            }
+            for (int e = 0; e < 8; e++)
+                w[kv_nibble(e)] = vcode[16 * (e >> 2) + 4 * g + (e & 3)][d4];
+            if (!full)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const int64_t jj = first + 16 * (e >> 2) + 4 * g + (e & 3);
+                    w[kv_nibble(e)] = jj >= len && jj < end ? w[kv_nibble(e)] : 0u;
+                }
+            uint32_t two[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                two[i] = w[2 * i] | w[2 * i + 1] << 4;
+            // bytes 0 and 1 (2 and 3) of a pair, side by side
+            const uint32_t left = __builtin_amdgcn_perm(two[1], two[0], 0x05010400u);
+            const uint32_t right = __builtin_amdgcn_perm(two[3], two[2], 0x05010400u);
+            const uint32_t left2 = __builtin_amdgcn_perm(two[1], two[0], 0x07030602u);
+            const uint32_t right2 = __builtin_amdgcn_perm(two[3], two[2], 0x07030602u);
+            const uint32_t word[4] = {(left & 0xFFFFu) | right << 16, left >> 16 | (right & 0xFFFF0000u),
+                                      (left2 & 0xFFFFu) | right2 << 16, left2 >> 16 | (right2 & 0xFFFF0000u)};
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                uint32_t word = 0;
-#pragma unroll
-                for (int n = 0; n < 8; n++)
-                    word |= ((w[n] >> (8 * i)) & 15u) << (4 * n);
                 const int d = 4 * d4 + i;
-                image[KvTile<W>::kWords + kv_word_at(d >> 4, (d & 15) + 16 * g)] = word;
+                image[KvTile<W>::kWords + kv_word_at(d >> 4, (d & 15) + 16 * g)] = word[i];
             }
         }
         __syncthreads();
-        if (first >= len && first + kKvTile <= end) {
+        if (full) {
             for (int i = tid; i < KvTile<W>::kWords / 2; i += 256)
                 ((u32x4*)tile)[i] = ((const u32x4*)image)[i];
         } else {
