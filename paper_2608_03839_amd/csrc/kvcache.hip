@@ -8,8 +8,9 @@
 // are put together in LDS as they are stored and leave 16 bytes a lane; where the
 // tile also holds earlier positions, a value dword (8 positions of a column) is
 // read and merged.  The workgroup owns the tile, so there is no race on a dword.
-// Bound by memory: 4 prompts of 8,191 rows, 8 heads of 128 columns in bf16: 136 MB
-// in and 38 MB out in 42 us, 4.1 TB/s (a copy reaches 4.9); small appends by their
+// Bound by memory and by the VALU (18 instructions a value, whose issue is nearly
+// full) alike: 4 prompts of 8,191 rows, 8 heads of 128 columns in bf16: 136 MB in
+// and 38 MB out in 37 us, 4.7 TB/s (a copy reaches 4.9); small appends by their
 // latencies, 6 us.
 //
 // read: a tile's codes to LDS, y = z + s c, 16 bytes a lane; the same rows in 27 us
@@ -199,8 +200,10 @@ struct KvRowRegs {
     }
 };
 
+// (Six workgroups a CU: 4 x 8,191 rows in bf16 37 us, at five 39, at four 42; at
+// eight, or six with binary32 rows, registers spill.)
 template <int W, typename T>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t* __restrict__ slots,
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 6 : 5) void kv_append_kernel(KvView c, const int32_t* __restrict__ slots,
                                                         const T* __restrict__ k, const T* __restrict__ v, int64_t ld,
                                                         int32_t max_rows, const int32_t* __restrict__ nodes,
                                                         const int32_t* __restrict__ count,
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
             for (int side = 0; side < 2; side++) {
                 float x[W / 8];
                 float lo = INFINITY, hi = -INFINITY;
-                bool odd = false;
+                float none[2] = {0.f, 0.f};  // not 0 once a value is not finite
 #pragma unroll
                 for (int i = 0; i < W / 64; i++) {
                     const bool in = part * (W / 8) + 8 * i < c.D;
@@ -244,8 +247,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
                         m = fmaxf(m, x[8 * i + e]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2)
-                        odd = odd || __builtin_isunordered(x[8 * i + e], x[8 * i + e + 1]);
+                    for (int e = 0; e < 8; e++)
+                        none[e & 1] = fmaf(x[8 * i + e], 0.f, none[e & 1]);
                     lo = in ? fminf(lo, l) : lo;
                     hi = in ? fmaxf(hi, m) : hi;
                 }
@@ -254,7 +257,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, const int32_t*
                     lo = fminf(lo, __shfl_xor(lo, o, 8));
                     hi = fmaxf(hi, __shfl_xor(hi, o, 8));
                 }
-                const uint64_t odds = __ballot(odd);
+                const uint64_t odds = __ballot(!(none[0] + none[1] == 0.f));
                 const uint32_t pair = kv_pair(lo, hi, ((odds >> (tid & 56)) & 255) == 0);
                 const float s = kv_s(pair), z = kv_z(pair), inv = __builtin_amdgcn_rcpf(s);
 #pragma unroll
