@@ -684,50 +684,57 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
         }
         __syncthreads();
         uint8_t* tile = tiles + (int64_t)t * c.tile_bytes;
-        for (int x = tid; x < 4 * kKvTile; x += blockDim.x) {  // keys: a quarter of a row a lane
-            const int key = x >> 2, g = x & 3;
+        // a lane's loads are made wherever its row comes from, its own place for one that
+        // does not move, so that none waits for another's condition
+        typedef uint32_t quarter __attribute__((ext_vector_type(W / 32)));
+        quarter code[2];
+        uint32_t* to[2];
+        bool on[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {  // keys: a quarter of a row a lane
+            const int x = tid + i * (int)blockDim.x, key = (x >> 2) & 31, g = x & 3;
             const int32_t src = source[key];
-            if (src >= 0) {
-                const int to = kv_word_at((key >> 4) * (W / 32), (key & 15) + 16 * g);
-                const int at_src = kv_word_at(((src >> 4) & 1) * (W / 32), (src & 15) + 16 * g);
-                if (W == 128)
-                    *(u32x4*)((uint32_t*)tile + to) = *(const u32x4*)((const uint32_t*)from(src) + at_src);
-                else
-                    *(uint2*)((uint32_t*)tile + to) = *(const uint2*)((const uint32_t*)from(src) + at_src);
-            }
+            on[i] = src >= 0 && x < 4 * kKvTile;
+            to[i] = (uint32_t*)tile + kv_word_at((key >> 4) * (W / 32), (key & 15) + 16 * g);
+            const uint32_t* at_src = (const uint32_t*)from(src) + kv_word_at(((src >> 4) & 1) * (W / 32), (src & 15) + 16 * g);
+            code[i] = *(const quarter*)(on[i] ? at_src : to[i]);
         }
-        if (tid < 64) {  // scales
-            const int32_t src = source[tid & 31];
-            const int base = (tid >> 5 ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4;
-            if (src >= 0)
-                ((uint32_t*)tile)[base + (tid & 31)] = ((const uint32_t*)from(src))[base + (src & 31)];
-        }
+        const int32_t its = source[tid & 31];  // scales
+        const int pairs = ((tid >> 5) & 1 ? KvTile<W>::kValueScales : KvTile<W>::kKeyScales) / 4;
+        uint32_t* pair_to = (uint32_t*)tile + pairs + (tid & 31);
+        const uint32_t pair = *(its >= 0 ? (const uint32_t*)from(its) + pairs + (its & 31) : pair_to);
 #pragma unroll 2
         for (int w = tid; w < KvTile<W>::kWords; w += blockDim.x) {  // values: a nibble of each dword a row
             int Q, lane;
             kv_word(w, &Q, &lane);
-            uint32_t got[8], clear = 0;
+            uint32_t* word_to = (uint32_t*)(tile + KvTile<W>::kValues) + w;
+            uint32_t clear = 0, got[8];
+            int32_t src[8];
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const int32_t src = source[16 * (e >> 2) + 4 * (lane >> 4) + (e & 3)];
-                got[e] = 0;
-                if (src >= 0) {
-                    clear |= 15u << (4 * kv_nibble(e));
-                    const uint32_t word =
-                        ((const uint32_t*)(from(src) + KvTile<W>::kValues))[kv_word_at(
-                            Q, (lane & 15) + 16 * ((src & 15) >> 2))];
-                    got[e] = (uint32_t)kv_code(word, 4 * ((src >> 4) & 1) + (src & 3)) << (4 * kv_nibble(e));
-                }
+            for (int e = 0; e < 8; e++) {  // (one group of positions a wave)
+                src[e] = __builtin_amdgcn_readfirstlane(source[16 * (e >> 2) + 4 * (lane >> 4) + (e & 3)]);
+                clear |= src[e] >= 0 ? 15u << (4 * kv_nibble(e)) : 0u;
             }
-            if (clear) {
-                uint32_t* to = (uint32_t*)(tile + KvTile<W>::kValues) + w;
-                uint32_t word = *to & ~clear;
+            if (!clear)
+                continue;
 #pragma unroll
-                for (int e = 0; e < 8; e++)
-                    word |= got[e];
-                *to = word;
-            }
+            for (int e = 0; e < 8; e++)
+                got[e] = *(src[e] < 0 ? word_to
+                                      : (const uint32_t*)(from(src[e]) + KvTile<W>::kValues) +
+                                            kv_word_at(Q, (lane & 15) + 16 * ((src[e] & 15) >> 2)));
+            uint32_t word = *word_to & ~clear;
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (src[e] >= 0)
+                    word |= (uint32_t)kv_code(got[e], 4 * ((src[e] >> 4) & 1) + (src[e] & 3)) << (4 * kv_nibble(e));
+            *word_to = word;
         }
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            if (on[i])
+                *(quarter*)to[i] = code[i];
+        if (tid < 64 && its >= 0)
+            *pair_to = pair;
     }
 }
 
