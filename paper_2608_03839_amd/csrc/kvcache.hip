@@ -21,10 +21,10 @@
 // per (request, head) finds the budget-th largest weight by radix selection
 // and lists the moves with their positions and weights; a second kernel owns
 // one destination tile per workgroup.  16 requests of 8 heads, 20,481 rows to
-// 16,384: 43 us to select (128 workgroups for 256 CUs: a head's three passes over
-// LDS, one after the other, are the time) and 117 to 130 to move (a nibble of every
-// dword of the values changes with a row, so nearly every tile below the budget is
-// read and written: 305 MB in, 199 out, 3.9 TB/s).
+// 16,384: 44 us to select (128 workgroups for 256 CUs: a head's three passes over
+// LDS, one after the other, are the time) and 116 to move (a nibble of every dword of
+// the values changes with a row, so nearly every tile below the budget is read and
+// written: about 395 MB in, 150 out, 4.7 TB/s).
 //
 // A slot's length changes when the last workgroup of the request has read it:
 // each takes a ticket when it is done, or, where they are many, by a launch of its
@@ -635,9 +635,10 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(KvView c, const int3
 }
 
 // A workgroup per destination tile, of one wave where there are many (a tile's
-// dependent loads are the time, and tiles in flight cover it: 65,536 tiles 169 -> 128 us
-// against four waves), of four where there are few (1,024 tiles 12 -> 6.7 us).  Rows that move out of the tile that the
-// budget ends in are read from its copy: that tile may be written meanwhile.
+// dependent loads are the time, and tiles in flight cover it: 65,536 tiles 116 us,
+// with two waves 136, with four 188), of four where there are few (1,024 tiles 6.4 us,
+// with one 9.3).  Rows that move out of the tile that the budget ends in are read
+// from its copy: that tile may be written meanwhile.
 template <int W>
 __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* __restrict__ slots, int64_t keep,
                                                       const uint8_t* __restrict__ work)
@@ -685,7 +686,9 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, const int32_t* _
         __syncthreads();
         uint8_t* tile = tiles + (int64_t)t * c.tile_bytes;
         // a lane's loads are made wherever its row comes from, its own place for one that
-        // does not move, so that none waits for another's condition
+        // does not move, so that none waits for another's condition (the keys' own places
+        // are a quarter of what is read; without them 1 to 2% slower all the same, for
+        // lines that are then written in part)
         typedef uint32_t quarter __attribute__((ext_vector_type(W / 32)));
         quarter code[2];
         uint32_t* to[2];
