@@ -169,3 +169,24 @@ def test_append_of_many_tiles(oil):  # noqa: F811
     c.own.reset()
     c.ref.reset()
     c.same()
+
+
+@pytest.mark.parametrize("N,G", [(1, 4), (6, 2), (20, 1), (20, 3)])
+@pytest.mark.parametrize("e", [-90, 60, 100])
+def test_powers_of_two_pass_through(oil, N, G, e):  # noqa: F811
+    """Keys times 2^e under queries times 2^-e: the same bits throughout (at 2^-90 the
+    keys' codes come from divisions, the queries' factors from the end of their range)."""
+    rng = np.random.default_rng(98)
+    q, k, v = _rows(rng, 2, N, 2 * G, 128), _rows(rng, 2, N, 2, 128), _rows(rng, 2, N, 2, 128)
+    ck, cv = _rows(rng, 2, 333, 2, 128), _rows(rng, 2, 333, 2, 128)
+    got = []
+    for by in (np.float32(1.0), np.float32(2.0) ** np.float32(e)):
+        c = oil.KvCache(2, 2, 128, 400)
+        c.append(_cu(ck * by, torch.bfloat16), _cu(cv, torch.bfloat16), count=_cu(np.array([333, 41], np.int32)))
+        t = [_cu(q / by, torch.bfloat16), _cu(k * by, torch.bfloat16), _cu(v, torch.bfloat16)]
+        out, lse = c.attend(*t)
+        c.weigh(t[0], lse)
+        torch.cuda.synchronize()
+        got.append((out, lse, c.weights.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert got[0][2].any() and torch.isfinite(got[0][1]).all()
