@@ -1191,9 +1191,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 }
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
-                    const float by = __shfl(fade, p0 + p, 64);  // 0 past the parts
-                    o[0] = by == 0.f ? o[0] : fmaf(by, y[p][0], o[0]);
-                    o[1] = by == 0.f ? o[1] : fmaf(by, y[p][1], o[1]);
+                    const float by = __shfl(fade, p0 + p, 64);
+                    // (a part that weighs nothing is added too: its rows may be NaN)
+                    if (p0 + p < cut.parts) {
+                        o[0] = fmaf(by, y[p][0], o[0]);
+                        o[1] = fmaf(by, y[p][1], o[1]);
+                    }
                 }
             }
         } else {
@@ -1225,8 +1228,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 floatx2 y = {at[0], 0.f};
                 if (W == 128)
                     y = *(const floatx2*)at;
-                o[0] = by == 0.f ? o[0] : fmaf(by, y[0], o[0]);
-                o[1] = by == 0.f ? o[1] : fmaf(by, y[1], o[1]);
+                o[0] = fmaf(by, y[0], o[0]);
+                o[1] = fmaf(by, y[1], o[1]);
             }
             so[wave][lane] = o;
             __syncthreads();
