@@ -27,7 +27,10 @@
 // relative).  z and s c may be far larger than the value they add up to, so that
 // rounding must not reach s c alone: z is weighted by the rounded p too (z / s
 // times the operand).  Tiles in which some s is below 2^-6 E, where operands would
-// lose bits, take two bf16 operands, the second what the first leaves.
+// lose bits, take two bf16 operands, the second what the first leaves.  Sums are
+// kept over E 2^24, E also at or above every |z| 2^-64, and a wave's become
+// a mean before they are multiplied by E: nothing passes binary32 that the
+// values do not, and what lies within 2^90 of the largest value counts.
 //
 // The tree's nodes come as further tiles in bf16 (p rounded to 2^-9).
 //
@@ -58,6 +61,8 @@ constexpr float kLow = -1e38f;      // m of a row that has seen nothing
 constexpr float kHead = 11.f;       // the maximum's place above m
 constexpr float kRoom = 15.f;       // and the most a score may pass m by
 constexpr float kLeast = 0x1p-6f;    // the smallest s / E that binary16 operands are taken at
+constexpr float kOffset = 0x1p-64f;  // E / |z| at least
+constexpr float kUnit = 0x1p-24f;    // of sums, times 1 / E: a code's place in binary16
 
 // The item that a share begins inside (parts 0: at one's start).
 struct KvCut {
@@ -78,7 +83,7 @@ struct KvAttend {
     uint16_t* out;
     float* lse;
     KvCut* cuts;     // where each share begins
-    float* part_o;   // per part of an item: unnormalised rows,
+    float* part_o;   // per part of an item: its rows' means of the values,
     float* part_ml;  // and each one's (m, sum)
     int64_t q_ld, ld;
     int32_t B, Hq, G, max_nodes;
@@ -301,8 +306,8 @@ struct KvScales {
 // each 16.
 template <int W, int NT>
 struct KvRows {
-    floatx4 o[NT][W / 16];  // O^T / (E 2^24)
-    float m[NT], l[NT], w[NT];
+    floatx4 o[NT][W / 16];  // of O^T / (E 2^24) the codes' and the nodes' part
+    float m[NT], l[NT], w[NT];  // w: the part of z, over E 2^24 too
     float E;
 
     __device__ __forceinline__ void init()
@@ -340,10 +345,12 @@ struct KvRows {
         if (up > E) {
             const float by = E * (1.f / up);
 #pragma unroll
-            for (int t = 0; t < NT; t++)
+            for (int t = 0; t < NT; t++) {
+                w[t] *= by;
 #pragma unroll
                 for (int mt = 0; mt < W / 16; mt++)
                     o[t][mt] *= by;
+            }
             E = up;
         }
     }
@@ -366,12 +373,14 @@ __device__ __forceinline__ void kv_tile(KvKeys<W>& K, KvValues<W>& V, const uint
 #pragma unroll
     for (int p = 0; p < W / 64; p++)
         code[p] = K.code[p][lane];
-    if (__builtin_expect(__any(value && s > R.E), 0))
-        R.widen(value ? s : 0.f);
+    const float least = value ? fmaxf(s, fabsf(z) * kOffset) : 0.f;
+    if (__builtin_expect(__any(least > R.E), 0))
+        R.widen(least);
     const bool rare = __any(value && on && s < R.E * kLeast);
     if (value) {
         const float by = 1.f / R.E;
         s *= lane & 2 ? by * 0.0625f : by;
+        z *= by * kUnit;
         if (!rare)
             z = on ? z * __builtin_amdgcn_rcpf(s) : 0.f;
     }
@@ -546,7 +555,9 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
     const int64_t base = ((int64_t)b * A.max_nodes + n0) * A.ld + (int64_t)h * D;
     if (R.E < 1.f)
         R.widen(1.f);
-    const float by = 0x1p-24f / R.E;
+    // p / (E 2^24), or where that leaves bf16's range, part of it with the values
+    const bool far = R.E > 0x1p56f;
+    const float by = far ? 0x1p-80f : kUnit / R.E;
     floatx4 S[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; t++)
@@ -631,6 +642,15 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
                     vf[i].w[j] = ((lo & 0x7F80u) == 0x7F80u ? 0u : lo) | ((hi & 0x7F80u) == 0x7F80u ? 0u : hi << 16);
                 }
         }
+        if (__builtin_expect(far, 0)) {
+            const float rest = 0x1p56f / R.E;
+#pragma unroll
+            for (int i = 0; i < kGroup; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    vf[i].w[j] = pack_bf16(__uint_as_float(vf[i].w[j] << 16) * rest,
+                                           __uint_as_float(vf[i].w[j] & 0xFFFF0000u) * rest);
+        }
 #pragma unroll
         for (int i = 0; i < kGroup; i++)
 #pragma unroll
@@ -674,7 +694,7 @@ __device__ __forceinline__ void kv_few_nodes(const KvAttend& A, int b, int h, in
         sees = A.mask[((int64_t)b * A.max_nodes + node) * ((A.max_nodes + 31) / 32)];
     if (R.E < 1.f)
         R.widen(1.f);
-    const float by = 0x1p-24f / R.E;
+    const float by = 1.f / R.E;
     for (int u = 0; u < m; u++) {
         const int64_t at = ((int64_t)b * A.max_nodes + u) * A.ld + (int64_t)h * D;
         u32x4 k[W / 32];
@@ -707,8 +727,8 @@ __device__ __forceinline__ void kv_few_nodes(const KvAttend& A, int b, int h, in
                 const uint32_t w = i < 2 ? v[mt].x : v[mt].y;
                 const uint32_t y = i & 1 ? w & 0xFFFF0000u : w << 16;
                 // not finite: itself, whatever p rounds to
-                const float f = (y & 0x7F800000u) == 0x7F800000u ? 1.f : p * by;
-                R.o[0][mt][i] = on ? fmaf(f, __uint_as_float(y), R.o[0][mt][i]) : R.o[0][mt][i];
+                const float f = (y & 0x7F800000u) == 0x7F800000u ? 1.f : p * kUnit;
+                R.o[0][mt][i] = on ? fmaf(f, __uint_as_float(y) * by, R.o[0][mt][i]) : R.o[0][mt][i];
             }
     }
 }
@@ -1062,7 +1082,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                 kv_nodes<W, NT>(A, uniform(P.b), uniform(P.h), (u - cached) * 32, uniform(P.m), lane,
                                 uniform(P.row_block) * kRows, R);
         }
-        // the waves' shares, relative to the largest m
+        // the waves' shares of the mean, relative to the largest m
 #pragma unroll
         for (int t = 0; t < NT; t++) {
             R.l[t] = quad_sum(R.l[t]);
@@ -1084,12 +1104,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
 #pragma unroll
             for (int x = 0; x < kAttendWaves; x++)
                 sum[t] += sl[x][16 * t + r16] * __builtin_amdgcn_exp2f(sm[x][16 * t + r16] - top[t]);
-            const float f = __builtin_amdgcn_exp2f(R.m[t] - top[t]), of = R.E * 0x1p24f;
+            const float f = __builtin_amdgcn_exp2f(R.m[t] - top[t]) / (sum[t] * kUnit);
 #pragma unroll
             for (int mt = 0; mt < W / 16; mt++)
 #pragma unroll
                 for (int i = 0; i < 4; i++)
-                    R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : fmaf(R.o[t][mt][i], of, R.w[t]) * f;
+                    R.o[t][mt][i] = R.l[t] == 0.f ? 0.f : (R.o[t][mt][i] + R.w[t]) * f * R.E;
         }
 #pragma unroll
         for (int t = 0; t < NT; t++)
@@ -1128,15 +1148,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
                 const int node = r / A.G;
                 const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + h * A.G + (r - node * A.G);
                 const bool none = sum[t] == 0.f;
-                const float by = none ? 0.f : 1.f / sum[t];
                 if (g == 0 && A.lse)
                     A.lse[to] = none ? -INFINITY : kLn2 * (top[t] + __builtin_amdgcn_logf(sum[t]));
 #pragma unroll
                 for (int mt = 0; mt < W / 16; mt++)
                     if (16 * mt + 4 * g < D) {
                         uint2 o;
-                        o.x = none ? 0u : pack_bf16(R.o[t][mt][0] * by, R.o[t][mt][1] * by);
-                        o.y = none ? 0u : pack_bf16(R.o[t][mt][2] * by, R.o[t][mt][3] * by);
+                        o.x = pack_bf16(R.o[t][mt][0], R.o[t][mt][1]);
+                        o.y = pack_bf16(R.o[t][mt][2], R.o[t][mt][3]);
                         *(uint2*)(A.out + to * D + 16 * mt + 4 * g) = o;
                     }
             }
@@ -1144,7 +1163,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
     }
 }
 
-// The parts of the items that shares cut, joined: o = sum o_p 2^(m_p - m) over
+// The parts of the items that shares cut, joined: o = sum o_p l_p 2^(m_p - m) over
 // sum l_p 2^(m_p - m), m the largest.  The workgroup of each share that begins
 // inside an item takes its part of that item's rows, with four waves a row where
 // the parts are many (past 16 a wave's loads would follow each other), else one.
@@ -1174,11 +1193,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
         if (few) {
             const floatx2 mine = ml[first + (int64_t)(lane < cut.parts ? lane : 0) * rows_per_item];
             top = wave_max(mine[0]);
-            const float fade = lane >= cut.parts || mine[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(mine[0] - top);
-            total = lane >= cut.parts ? 0.f : mine[1] * fade;
+            float part = lane >= cut.parts || mine[1] == 0.f ? 0.f : mine[1] * __builtin_amdgcn_exp2f(mine[0] - top);
+            total = part;
 #pragma unroll
             for (int x = 1; x < 64; x <<= 1)
                 total += __shfl_xor(total, x, 64);
+            part = total == 0.f ? 0.f : part / total;
             for (int p0 = 0; p0 < cut.parts; p0 += 4) {
                 floatx2 y[4];
 #pragma unroll
@@ -1191,7 +1211,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 }
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
-                    const float by = __shfl(fade, p0 + p, 64);
+                    const float by = __shfl(part, p0 + p, 64);
                     // (a part that weighs nothing is added too: its rows may be NaN)
                     if (p0 + p < cut.parts) {
                         o[0] = fmaf(by, y[p][0], o[0]);
@@ -1210,9 +1230,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
             top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
             for (int p = threadIdx.x; p < cut.parts; p += 256) {
                 const floatx2 x = ml[first + (int64_t)p * rows_per_item];
-                const float by = x[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);
-                f[p] = by;
-                total += x[1] * by;
+                f[p] = x[1] == 0.f ? 0.f : x[1] * __builtin_amdgcn_exp2f(x[0] - top);
+                total += f[p];
             }
 #pragma unroll
             for (int x = 1; x < 64; x <<= 1)
@@ -1221,9 +1240,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 red[1][wave] = total;
             __syncthreads();
             total = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+            const float each = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll 8
             for (int p = wave; p < cut.parts; p += 4) {
-                const float by = f[p];
+                const float by = f[p] * each;
                 const float* at = from + (int64_t)p * rows_per_item * W;
                 floatx2 y = {at[0], 0.f};
                 if (W == 128)
@@ -1243,12 +1263,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
         const int row = cut.row_block * rows_per_item + r, node = row / A.G;
         const int64_t to = ((int64_t)b * A.max_nodes + node) * A.Hq + cut.h * A.G + (row - node * A.G);
         const bool none = total == 0.f;
-        const float by = none ? 0.f : 1.f / total;
         if (d < D) {
             if (W == 128)
-                *(uint32_t*)(A.out + to * D + d) = none ? 0u : pack_bf16(o[0] * by, o[1] * by);
+                *(uint32_t*)(A.out + to * D + d) = pack_bf16(o[0], o[1]);
             else
-                A.out[to * D + d] = none ? (uint16_t)0 : (uint16_t)pack_bf16(o[0] * by, 0.f);
+                A.out[to * D + d] = (uint16_t)pack_bf16(o[0], 0.f);
         }
         if (lane == 0 && A.lse)
             A.lse[to] = none ? -INFINITY : kLn2 * (top + __builtin_amdgcn_logf(total));

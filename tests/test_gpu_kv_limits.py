@@ -5,6 +5,7 @@ test_gpu_kv.py, where the bound on the scores is derived."""
 import numpy as np
 import pytest
 
+from tests import _kv_ref as ref
 from tests.test_gpu_kv import Both, _rows, oil  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +30,76 @@ def test_not_finite_value_row_reaches_whatever_outweighs_it(oil, n, N, G):  # no
         q[..., 0] = 16.0
         out, lse = c.attend(q, scale=1.0)
         assert np.isfinite(out[0]).all() and np.isnan(out[1]).all() and np.isfinite(lse).all()
+
+
+# ------------------------------------------------------------------ ranges of values
+LARGEST = float(np.float32(3.3895314e38))    # of bf16
+
+
+def _sized(rng, shape, size):
+    return ref.bf16((size * rng.uniform(-1, 1, shape)).astype(np.float32))
+
+
+@pytest.mark.parametrize("size", [1e30, 1e32, 1e36, 1.6e38])
+@pytest.mark.parametrize("N,G", [(1, 4), (3, 2), (20, 1), (45, 1)])
+def test_large_values(oil, size, N, G):  # noqa: F811
+    """Outputs are means of values: they stay within binary32 wherever the values do."""
+    rng = np.random.default_rng(N)
+    n = 2048
+    c = Both(oil, 3, 1, 64, n)
+    c.append(_rows(rng, 3, n, 1, 64), _sized(rng, (3, n, 1, 64), size), count=[n, 77, 0])
+    q = ref.bf16(_rows(rng, 3, N, G, 64) * np.float32(0.1))
+    k, v = _rows(rng, 3, N, 1, 64), _sized(rng, (3, N, 1, 64), size)
+    assert np.isfinite(c.attend(q * 0, k, v)[0]).all()       # every position weighs the same
+    assert np.isfinite(c.attend(q, k, v)[0]).all()
+    c.attend(q)
+    c.attend(q, k, v / np.float32(2.0 ** 100))               # the nodes' far below the cached
+    small = Both(oil, 3, 1, 64, n)
+    small.append(_rows(rng, 3, n, 1, 64), _rows(rng, 3, n, 1, 64), count=[n, 77, 0])
+    small.attend(q, k, v)                                     # and far above
+
+
+@pytest.mark.parametrize("N,G", [(1, 1), (20, 1), (45, 1)])
+def test_large_offsets_of_values(oil, N, G):  # noqa: F811
+    """Rows of one value and rows far from zero, up to the largest bf16, beside small ones."""
+    rng = np.random.default_rng(7 * N)
+    n = 700
+    v = _rows(rng, 2, n, 1, 128)
+    v[0, 100:200] = LARGEST
+    v[0, 200:300] = -LARGEST
+    v[0, 300:420] = ref.bf16((1e38 * rng.uniform(2, 3.3, (120, 1, 128))).astype(np.float32))
+    v[1] = ref.bf16((1e37 * rng.uniform(1, 1.01, (n, 1, 128))).astype(np.float32))
+    v[1, 600:] = 3.0
+    c = Both(oil, 2, 1, 128, n)
+    c.append(_rows(rng, 2, n, 1, 128), v)
+    q = ref.bf16(_rows(rng, 2, N, G, 128) * np.float32(0.05))
+    own = np.full((2, N, 1, 128), LARGEST, np.float32)
+    for k, w in ((None, None), (_rows(rng, 2, N, 1, 128), own), (_rows(rng, 2, N, 1, 128), _rows(rng, 2, N, 1, 128))):
+        c.attend(q, k, w)
+        c.attend(q * 0, k, w)
+
+
+def test_many_large_values(oil):  # noqa: F811
+    rng = np.random.default_rng(11)
+    n = 262144
+    c = Both(oil, 1, 1, 8, n)
+    c.append(_rows(rng, 1, n, 1, 8), _sized(rng, (1, n, 1, 8), 1e37))
+    c.attend(np.zeros((1, 1, 2, 8), np.float32))
+    c.attend(np.zeros((1, 9, 2, 8), np.float32))
+
+
+@pytest.mark.parametrize("N", [1, 20])
+def test_large_values_of_no_weight(oil, N):  # noqa: F811
+    """Value rows 2^90 above the others whose probability is nothing leave the others' output as it is."""
+    rng = np.random.default_rng(12)
+    n = 900
+    k = np.zeros((1, n, 1, 64), np.float32)
+    k[0, 300:340, 0, 0] = -32.0
+    v = ref.bf16(_rows(rng, 1, n, 1, 64) * np.float32(2.0 ** -30))
+    v[0, 300:340] *= np.float32(2.0 ** 90)
+    c = Both(oil, 1, 1, 64, n)
+    c.append(k, v)
+    q = np.zeros((1, N, 2, 64), np.float32)
+    q[..., 0] = 16.0
+    c.attend(q, scale=1.0)
+    c.attend(q, np.zeros((1, N, 1, 64), np.float32), ref.bf16(_rows(rng, 1, N, 1, 64) * np.float32(2.0 ** -30)), scale=1.0)
