@@ -191,6 +191,16 @@ __device__ __forceinline__ float wave_max(float x)
     return fmaxf(x, __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x041F)));
 }
 
+// The sum over a wave.
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = quad_sum(x);
+    x += __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x201F));
+    x += __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x101F));
+    x += __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x081F));
+    return x + __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x041F));
+}
+
 // Raw bf16 operand of a row for columns d .. d + 7; zeros past D or where it is
 // not wanted (the load is made all the same, inside the row, so that loads do not
 // wait for each other's conditions).
@@ -631,25 +641,18 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
                 vf[i].w[j] = raw[i][2 * j] | raw[i][2 * j + 1] << 16;
                 top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[i].w[j] & 0x7FFF7FFFu));
             }
-        if (__builtin_expect(__any(top[0] >= 0x7F80 || top[1] >= 0x7F80), 0)) {
+        if (__builtin_expect(__any(top[0] >= 0x7F80 || top[1] >= 0x7F80) || far, 0)) {
             // not finite: nothing here, and added below to the rows that see it
             odd = true;
+            const float rest = far ? 0x1p56f / R.E : 1.f;
 #pragma unroll
             for (int i = 0; i < kGroup; i++)
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
-                    const uint32_t lo = vf[i].w[j] & 0xFFFFu, hi = vf[i].w[j] >> 16;
-                    vf[i].w[j] = ((lo & 0x7F80u) == 0x7F80u ? 0u : lo) | ((hi & 0x7F80u) == 0x7F80u ? 0u : hi << 16);
+                    const uint32_t lo = vf[i].w[j] << 16, hi = vf[i].w[j] & 0xFFFF0000u;
+                    vf[i].w[j] = pack_bf16((lo & 0x7F800000u) == 0x7F800000u ? 0.f : __uint_as_float(lo) * rest,
+                                           (hi & 0x7F800000u) == 0x7F800000u ? 0.f : __uint_as_float(hi) * rest);
                 }
-        }
-        if (__builtin_expect(far, 0)) {
-            const float rest = 0x1p56f / R.E;
-#pragma unroll
-            for (int i = 0; i < kGroup; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++)
-                    vf[i].w[j] = pack_bf16(__uint_as_float(vf[i].w[j] << 16) * rest,
-                                           __uint_as_float(vf[i].w[j] & 0xFFFF0000u) * rest);
         }
 #pragma unroll
         for (int i = 0; i < kGroup; i++)
@@ -1194,10 +1197,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
             const floatx2 mine = ml[first + (int64_t)(lane < cut.parts ? lane : 0) * rows_per_item];
             top = wave_max(mine[0]);
             float part = lane >= cut.parts || mine[1] == 0.f ? 0.f : mine[1] * __builtin_amdgcn_exp2f(mine[0] - top);
-            total = part;
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1)
-                total += __shfl_xor(total, x, 64);
+            total = wave_sum(part);
             part = total == 0.f ? 0.f : part / total;
             for (int p0 = 0; p0 < cut.parts; p0 += 4) {
                 floatx2 y[4];
@@ -1211,12 +1211,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 }
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
-                    const float by = __shfl(part, p0 + p, 64);
+                    const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(part), p0 + p));
                     // (a part that weighs nothing is added too: its rows may be NaN)
-                    if (p0 + p < cut.parts) {
-                        o[0] = fmaf(by, y[p][0], o[0]);
-                        o[1] = fmaf(by, y[p][1], o[1]);
-                    }
+                    const bool real = p0 + p < cut.parts;
+                    o[0] = real ? fmaf(by, y[p][0], o[0]) : o[0];
+                    o[1] = real ? fmaf(by, y[p][1], o[1]) : o[1];
                 }
             }
         } else {
@@ -1233,9 +1232,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 f[p] = x[1] == 0.f ? 0.f : x[1] * __builtin_amdgcn_exp2f(x[0] - top);
                 total += f[p];
             }
-#pragma unroll
-            for (int x = 1; x < 64; x <<= 1)
-                total += __shfl_xor(total, x, 64);
+            total = wave_sum(total);
             if (lane == 0)
                 red[1][wave] = total;
             __syncthreads();
