@@ -69,7 +69,7 @@ struct KvCut {
     int32_t b, h, row_block;
     int32_t nth;     // share since the item's first
     int32_t parts;   // of the item
-    int32_t first;   // its first part
+    int32_t first;   // the item's first share
     int32_t pad[2];
 };
 
@@ -756,8 +756,12 @@ __device__ __forceinline__ int kv_row_tiles(const KvAttend& A, int32_t len, int 
 // its blocks of 16 NT rows (an item), in each the tiles (a unit is one, or so many
 // that there are fewer than 2^31).  Equal shares of it go
 // to the workgroups, whatever the lengths; a share that begins or ends inside an
-// item leaves a part of it, numbered share + item (which no two parts have in
-// common), for the join.
+// item leaves a part of it for the join: one that begins inside one as part 2 share,
+// one that starts an item and ends inside it as 2 share + 1.  So the workspace grows
+// with the workgroups alone.
+
+// Where part p of the item whose first share is `first` stands.
+__device__ __forceinline__ int kv_part_at(int first, int p) { return 2 * (first + p) + (p == 0); }
 
 // Least units of a share: two tiles a wave (or what an item has, if less).
 constexpr int kLeastShare = 2 * kAttendWaves;
@@ -829,7 +833,7 @@ struct KvRequest {
 // 64 requests in LDS: read once an item, they would take registers that the tiles
 // need.
 struct KvRequestTable {
-    int slot[64], len[64], m[64], units[64], items[64], upto[64], items_upto[64];
+    int slot[64], len[64], m[64], units[64], items[64], upto[64];
 
     template <int NT>
     __device__ __forceinline__ int put(const KvRequest<NT>& r, int lane)
@@ -841,7 +845,6 @@ struct KvRequestTable {
         units[lane] = r.units;
         items[lane] = r.items;
         upto[lane] = sum;
-        items_upto[lane] = wave_scan(r.items);
         return __builtin_amdgcn_readlane(sum, 63);
     }
 };
@@ -868,7 +871,7 @@ __device__ __forceinline__ void kv_clear_dead(const KvAttend& A, int b0, int m, 
 // tiles have the registers (scalar ones too: they spill into vector ones).
 struct KvPart {
     int more;                          // whether there is one
-    int at, end, base, item_base, b0;  // the rest of the share; requests in the table
+    int at, end, base, b0;             // the rest of the share; requests in the table
     int b, h, row_block, m, len;
     int part, whole, t0, t1;           // its number; tiles
     const uint8_t* tiles;
@@ -887,15 +890,13 @@ template <int NT>
 __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvRequestTable& table, const KvShares& S, int share,
                                              int lane)
 {
-    int at = uniform(P.at), end = uniform(P.end), base = uniform(P.base), item_base = uniform(P.item_base);
-    int b0 = uniform(P.b0);
+    int at = uniform(P.at), end = uniform(P.end), base = uniform(P.base), b0 = uniform(P.b0);
     P.more = 0;
     if (at >= end)
         return;
     uint64_t past;
     while (!(past = __ballot(table.upto[lane] > at - base))) {
         base += uniform(table.upto[63]);
-        item_base += uniform(table.items_upto[63]);
         b0 += 64;
         if (b0 >= A.B)
             return;
@@ -906,7 +907,6 @@ __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvReq
     const int l = __ffsll((unsigned long long)past) - 1, b = b0 + l;
     const int m = uniform(table.m[l]), units = uniform(table.units[l]), items = uniform(table.items[l]);
     const int begin = base + uniform(table.upto[l]) - items * units;
-    const int item0 = item_base + uniform(table.items_upto[l]) - items;
     const int slot = uniform(table.slot[l]), len = uniform(table.len[l]), row_tiles = kv_row_tiles(A, len, m);
     const int row_blocks = (uint32_t)items / (uint32_t)A.c.H, item = (uint32_t)(at - begin) / (uint32_t)units;
     const int h = (uint32_t)item / (uint32_t)row_blocks;
@@ -919,20 +919,19 @@ __device__ __forceinline__ void kv_next_part(const KvAttend& A, KvPart& P, KvReq
         cut.row_block = item - h * row_blocks;
         cut.nth = share - w0;
         cut.parts = w1 - w0 + 1;
-        cut.first = w0 + item0 + item;
+        cut.first = w0;
         A.cuts[share] = cut;
     }
     P.more = 1;
     P.at = at + u1 - u0;
     P.base = base;
-    P.item_base = item_base;
     P.b0 = b0;
     P.b = b;
     P.h = h;
     P.row_block = item - h * row_blocks;
     P.m = m;
     P.len = len;
-    P.part = share + item0 + item;
+    P.part = 2 * share + (u0 == 0);
     P.whole = u0 == 0 && u1 == units;
     P.t0 = u0 << A.shift;
     P.t1 = (u1 << A.shift) < row_tiles ? u1 << A.shift : row_tiles;
@@ -995,7 +994,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
         shares = S;
         P.at = mine ? S.cut(share) : 0;
         P.end = mine ? S.cut(share + 1) : 0;
-        P.base = P.item_base = P.b0 = 0;
+        P.base = P.b0 = 0;
     }
     while (true) {
         // what follows from the lane is worked out anew for each part: kept over all
@@ -1188,13 +1187,13 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
     const bool few = cut.parts <= kFew;
     const int step = few ? 4 * (cut.parts - 1) : cut.parts - 1;
     for (int r = few ? 4 * (cut.nth - 1) + wave : cut.nth - 1; r < rows; r += step) {
-        const int64_t first = (int64_t)cut.first * rows_per_item + r;  // parts are rows_per_item apart
+        auto at = [&](int p) { return (int64_t)kv_part_at(cut.first, p) * rows_per_item + r; };  // part p's row
         const floatx2* ml = (const floatx2*)A.part_ml;
-        const float* from = A.part_o + first * W + d;
+        const float* from = A.part_o + d;
         float top = kLow, total = 0.f;
         floatx2 o = {0.f, 0.f};
         if (few) {
-            const floatx2 mine = ml[first + (int64_t)(lane < cut.parts ? lane : 0) * rows_per_item];
+            const floatx2 mine = ml[at(lane < cut.parts ? lane : 0)];
             top = wave_max(mine[0]);
             float part = lane >= cut.parts || mine[1] == 0.f ? 0.f : mine[1] * __builtin_amdgcn_exp2f(mine[0] - top);
             total = wave_sum(part);
@@ -1203,11 +1202,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
                 floatx2 y[4];
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
-                    const float* at = from + (int64_t)(p0 + p < cut.parts ? p0 + p : 0) * rows_per_item * W;
+                    const float* row = from + at(p0 + p < cut.parts ? p0 + p : 0) * W;
                     if (W == 128)
-                        y[p] = *(const floatx2*)at;
+                        y[p] = *(const floatx2*)row;
                     else
-                        y[p] = floatx2{at[0], 0.f};
+                        y[p] = floatx2{row[0], 0.f};
                 }
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
@@ -1220,7 +1219,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
             }
         } else {
             for (int p = threadIdx.x; p < cut.parts; p += 256)
-                top = fmaxf(top, ml[first + (int64_t)p * rows_per_item][0]);
+                top = fmaxf(top, ml[at(p)][0]);
             top = wave_max(top);
             __syncthreads();
             if (lane == 0)
@@ -1228,7 +1227,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
             __syncthreads();
             top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
             for (int p = threadIdx.x; p < cut.parts; p += 256) {
-                const floatx2 x = ml[first + (int64_t)p * rows_per_item];
+                const floatx2 x = ml[at(p)];
                 f[p] = x[1] == 0.f ? 0.f : x[1] * __builtin_amdgcn_exp2f(x[0] - top);
                 total += f[p];
             }
@@ -1241,10 +1240,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
 #pragma unroll 8
             for (int p = wave; p < cut.parts; p += 4) {
                 const float by = f[p] * each;
-                const float* at = from + (int64_t)p * rows_per_item * W;
-                floatx2 y = {at[0], 0.f};
+                const float* part = from + at(p) * W;
+                floatx2 y = {part[0], 0.f};
                 if (W == 128)
-                    y = *(const floatx2*)at;
+                    y = *(const floatx2*)part;
                 o[0] = fmaf(by, y[0], o[0]);
                 o[1] = fmaf(by, y[1], o[1]);
             }
@@ -1429,7 +1428,7 @@ static KvPlan kv_plan(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
     return p;
 }
 
-static size_t kv_part_rows(const KvPlan& p) { return (size_t)(p.wgs + p.items) * 16 * p.nt; }
+static size_t kv_part_rows(const KvPlan& p) { return (size_t)(2 * p.wgs) * 16 * p.nt; }
 
 size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq)
 {

@@ -4,9 +4,10 @@ offsets and batches, and inputs whose results are exact.  u = 2^-24 as in
 test_gpu_kv.py, where the bound on the scores is derived."""
 import numpy as np
 import pytest
+import torch
 
 from tests import _kv_ref as ref
-from tests.test_gpu_kv import Both, _rows, oil  # noqa: F401
+from tests.test_gpu_kv import Both, _cu, _rows, oil  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +104,36 @@ def test_large_values_of_no_weight(oil, N):  # noqa: F811
     q[..., 0] = 16.0
     c.attend(q, scale=1.0)
     c.attend(q, np.zeros((1, N, 1, 64), np.float32), ref.bf16(_rows(rng, 1, N, 1, 64) * np.float32(2.0 ** -30)), scale=1.0)
+
+
+# ------------------------------------------------------------------ workspace, units of several tiles
+def test_attend_workspace_is_bounded(oil):  # noqa: F811
+    """A call's workspace holds two parts of 48 rows for each of its workgroups (512), or of
+    16 for 768, whatever the requests and nodes."""
+    for D, H in ((64, 2), (128, 2), (128, 8)):
+        c = oil.KvCache(512, H, D, 40)
+        W = 64 if D <= 64 else 128
+        bound = 768 * 32 + 2 * 512 * 48 * (W + 2) * 4
+        for B in (1, 7, 64, 512):
+            for N in (1, 4, 17, 65, 256):
+                for G in (1, 4, 8, 64):
+                    need = oil.lib().oil_kv_attend_workspace_bytes(c.handle, B, N, H * G)
+                    assert 0 < need <= bound, (D, H, B, N, G, need)
+
+
+def test_units_of_several_tiles(oil):  # noqa: F811
+    """A capacity at which a call's list is counted in units of two tiles (342 row blocks
+    over 2^23 tiles), slots short and long."""
+    rng = np.random.default_rng(14)
+    c = oil.KvCache(1, 1, 64, 1 << 28)
+    r = Both(oil, 1, 1, 64, 5000)
+    for n in (5, 40, 1235, 1900):
+        k, v = _rows(rng, 1, n, 1, 64), _rows(rng, 1, n, 1, 64)
+        c.append(_cu(k, torch.bfloat16), _cu(v, torch.bfloat16))
+        r.append(k, v)
+        q, k, v = _rows(rng, 1, 256, 64, 64), _rows(rng, 1, 256, 1, 64), _rows(rng, 1, 256, 1, 64)
+        t = [_cu(x, torch.bfloat16) for x in (q, k, v)]
+        got = [c.attend(*t), r.own.attend(*t)]
+        torch.cuda.synchronize()
+        assert torch.allclose(*(g[1] for g in got), rtol=0, atol=1e-5)
+        assert torch.allclose(*(g[0].float() for g in got), rtol=2 ** -7, atol=2 ** -7)
