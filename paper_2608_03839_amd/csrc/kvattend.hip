@@ -32,7 +32,9 @@
 // a mean before they are multiplied by E: nothing passes binary32 that the
 // values do not, and what lies within 2^90 of the largest value counts.
 //
-// The tree's nodes come as further tiles in bf16 (p rounded to 2^-9).
+// The tree's nodes come as further tiles in bf16, p as two operands, the second
+// what the first leaves (2^-16 of p: one alone, 2^-8, would show in outputs of
+// bf16 where the nodes hold the weight).
 //
 // What bounds it, at 8 key/value heads of 128 columns.  Single tokens: the stream
 // of tiles (32 requests of up to 16,384 positions, 32 query heads: 364 MB in 73
@@ -587,7 +589,7 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
                 S[t][a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a].b, qf.b, S[t][a], 0, 0, 0);
         }
     }
-    Frag p[NT];
+    Frag p[NT], low[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
         float x[8], top = -INFINITY;
@@ -606,8 +608,11 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
             x[e] *= by;
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+        for (int j = 0; j < 4; j++) {
             p[t].w[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+            low[t].w[j] = pack_bf16(x[2 * j] - __uint_as_float(p[t].w[j] << 16),
+                                    x[2 * j + 1] - __uint_as_float(p[t].w[j] & 0xFFFF0000u));
+        }
     }
     // the values, columns in lanes: two bytes a load, from eight rows at fixed distances
     const uint16_t* from[8];
@@ -657,8 +662,10 @@ __device__ __forceinline__ void kv_nodes(const KvAttend& A, int b, int h, int n0
 #pragma unroll
         for (int i = 0; i < kGroup; i++)
 #pragma unroll
-            for (int t = 0; t < NT; t++)
+            for (int t = 0; t < NT; t++) {
+                R.o[t][m0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i].b, low[t].b, R.o[t][m0 + i], 0, 0, 0);
                 R.o[t][m0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i].b, p[t].b, R.o[t][m0 + i], 0, 0, 0);
+            }
     }
     if (__builtin_expect(odd, 0)) {
         for (int key = 0; key < 32 && n0 + key < m; key++)

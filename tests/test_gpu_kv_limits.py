@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import _kv_ref as ref
-from tests.test_gpu_kv import Both, _cu, _rows, oil  # noqa: F401
+from tests.test_gpu_kv import U, Both, _cu, _rows, _tree_mask, oil  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -137,3 +137,47 @@ def test_units_of_several_tiles(oil):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.allclose(*(g[1] for g in got), rtol=0, atol=1e-5)
         assert torch.allclose(*(g[0].float() for g in got), rtol=2 ** -7, atol=2 ** -7)
+
+
+# ------------------------------------------------------------------ probabilities
+def _half_spacing(x):
+    """Half the distance between bf16 values at |x|."""
+    return np.exp2(np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -126))) - 8)
+
+
+def _close(c, q, k, v, n_nodes, mask, roundoff):
+    """The output within half a spacing of bf16, `roundoff` of sum p |v|, and the scores' error."""
+    scale = c.D ** -0.5
+    t = [None if x is None else _cu(x, torch.bfloat16) for x in (q, k, v)]
+    out, _ = c.own.attend(*t, Both._i32(n_nodes), None if mask is None else _cu(mask.view(np.int32)), scale)
+    torch.cuda.synchronize()
+    out = out.float().cpu().numpy().astype(np.float64)
+    want, _, size, spread = c.ref.attend(q, k, v, n_nodes, mask, scale)
+    ds = 4 * (c.D + 8) * U * (size + c._zero_size(q, scale, None))
+    off = (roundoff + 2.0 ** -17 + 2 * ds[..., None]) * spread
+    bound = off + _half_spacing(np.abs(want) + off)
+    assert (np.abs(out - want) <= bound).all(), ((np.abs(out - want) - bound) / spread.clip(1e-30)).max()
+
+
+@pytest.mark.parametrize("N,G,D", [(2, 4, 64), (5, 4, 128), (17, 1, 128), (17, 2, 64), (61, 4, 128), (256, 1, 128)])
+def test_probabilities_of_nodes(oil, N, G, D):  # noqa: F811
+    """Nodes over an empty cache hold all the mass: their probabilities are two bf16 (2^-16)."""
+    rng = np.random.default_rng(N + G)
+    c = Both(oil, 3, 2, D, 40)
+    n_nodes = np.array([N, max(1, N - 1), N], np.int32)
+    q = ref.bf16(rng.standard_normal((3, N, 2 * G, D)).astype(np.float32))
+    k, v = (ref.bf16(rng.standard_normal((3, N, 2, D)).astype(np.float32)) for _ in range(2))
+    _close(c, q, k, v, n_nodes, _tree_mask(rng, 3, N, n_nodes), 2.0 ** -16)
+    _close(c, q, k, v, n_nodes, None, 2.0 ** -16)
+
+
+@pytest.mark.parametrize("N,G,D", [(1, 4, 128), (20, 1, 64), (45, 1, 128)])
+@pytest.mark.parametrize("n", [2, 3, 9, 70])
+def test_probabilities_of_cached_rows(oil, N, G, D, n):  # noqa: F811
+    """Few cached rows, so that roundings do not average: probabilities in binary16 (2^-11)."""
+    rng = np.random.default_rng(100 * N + n)
+    c = Both(oil, 2, 2, D, 80)
+    k, v = (ref.bf16(rng.standard_normal((2, n, 2, D)).astype(np.float32)) for _ in range(2))
+    c.append(k, v)
+    q = ref.bf16(rng.standard_normal((2, N, 2 * G, D)).astype(np.float32))
+    _close(c, q, None, None, None, None, 2.0 ** -11)
