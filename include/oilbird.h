@@ -472,8 +472,9 @@ int32_t oil_kv_reset(oil_kv *kv, const int32_t *slots, int32_t B, void *stream);
 /* Append rows of B requests.
  *   k, v       B x max_rows rows of n_heads x head_dim values, dtype OIL_F32 or
  *              OIL_BF16, 16-byte aligned; consecutive rows ld elements apart
- *              (ld >= n_heads * head_dim, a multiple of 8: a slice of a fused
- *              projection's output serves), requests max_rows * ld apart.
+ *              (ld >= n_heads * head_dim, a multiple of 8, B * max_rows * ld <=
+ *              2^60: a slice of a fused projection's output serves), requests
+ *              max_rows * ld apart.
  *   nodes, count  which rows, and in which order.  Both NULL: all max_rows.
  *              count alone (B int32): the first count[b].  Both (nodes
  *              B x max_rows, as oil_accept_walk wrote them): row 0, the tree's
@@ -502,8 +503,9 @@ size_t oil_kv_attend_workspace_bytes(const oil_kv *kv, int32_t B, int32_t max_no
  *     S = scale * q . k;  lse = log sum exp S;  out = sum exp(S - lse) v.
  *   q          B x max_nodes rows of n_q_heads x head_dim bf16, 16-byte
  *              aligned, rows q_ld elements apart (>= n_q_heads * head_dim, a
- *              multiple of 8), requests max_nodes * q_ld apart.  Finite values are
- *              below 2^117 in magnitude (scores are binary32).
+ *              multiple of 8, bounded as append's ld), requests max_nodes * q_ld
+ *              apart.  Finite values are below 2^117 in magnitude (scores are
+ *              binary32).
  *   k, v       the nodes' own rows, B x max_nodes of n_heads x head_dim bf16, rows
  *              ld elements apart likewise, not yet in the cache; both NULL: no row sees a node.
  *   n_nodes    B int32 (clamped to 0 .. max_nodes) or NULL: max_nodes each.

@@ -677,8 +677,12 @@ static int32_t kv_shape_status(int32_t n_slots, int32_t n_heads, int32_t head_di
     return OIL_OK;
 }
 
-// Status of a row stride: n values a row, 16-byte alignment of every row.
-static bool kv_ld_fits(int64_t ld, int64_t n) { return ld >= n && ld % 8 == 0 && ld <= (1 << 24); }
+// Whether a row stride serves B requests of max_rows rows of n values: 16-byte alignment
+// of every row, and byte offsets that 64 bits hold.
+static bool kv_ld_fits(int64_t ld, int64_t n, int32_t B, int32_t max_rows)
+{
+    return ld >= n && ld % 8 == 0 && ld <= ((int64_t)1 << 60) / ((int64_t)B * max_rows);
+}
 
 size_t oil_kv_bytes(int32_t n_slots, int32_t n_heads, int32_t head_dim, int64_t capacity)
 {
@@ -744,7 +748,8 @@ int32_t oil_kv_append(oil_kv* kv, const int32_t* slots, int32_t B, const void* k
                       const float* weight, void* stream)
 {
     if (!kv || B < 1 || B > kv->c.n_slots || !k || !v || (dtype != OIL_F32 && dtype != OIL_BF16) || max_rows < 1 ||
-        (nodes && !count) || !kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D) || !aligned(k, 16) || !aligned(v, 16))
+        (nodes && !count) || !kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D, B, max_rows) || !aligned(k, 16) ||
+        !aligned(v, 16))
         return OIL_E_INVALID;
     if (nodes && max_rows > OIL_MAX_NODES)
         return OIL_E_UNSUPPORTED;
@@ -786,10 +791,11 @@ int32_t oil_kv_attend(const oil_kv* kv, const int32_t* slots, int32_t B, const v
     const int32_t st = kv_query_status(kv, B, max_nodes, n_q_heads);
     if (st != OIL_OK)
         return st;
-    if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D) ||
+    if (!q || !out || !aligned(q, 16) || !aligned(out, 16) ||
+        !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D, B, max_nodes) ||
         !isfinite(scale) || !k != !v || (mask && !k))
         return OIL_E_INVALID;
-    if (k && (!kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D) || !aligned(k, 16) || !aligned(v, 16)))
+    if (k && (!kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D, B, max_nodes) || !aligned(k, 16) || !aligned(v, 16)))
         return OIL_E_INVALID;
     if (!workspace || !aligned(workspace, kAlign) ||
         workspace_bytes < oil::kv_attend_workspace_bytes(kv->c, B, max_nodes, n_q_heads))
@@ -805,8 +811,8 @@ int32_t oil_kv_weigh(oil_kv* kv, const int32_t* slots, int32_t B, const void* q,
     const int32_t st = kv_query_status(kv, B, max_nodes, n_q_heads);
     if (st != OIL_OK)
         return st;
-    if (!q || !lse || !aligned(q, 16) || !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D) || !isfinite(scale) ||
-        (nodes && !count))
+    if (!q || !lse || !aligned(q, 16) || !kv_ld_fits(q_ld, (int64_t)n_q_heads * kv->c.D, B, max_nodes) ||
+        !isfinite(scale) || (nodes && !count))
         return OIL_E_INVALID;
     return hip_status(oil::launch_kv_weigh(kv->c, slots, B, q, q_ld, n_q_heads, lse, max_nodes, nodes, count, scale,
                                            (hipStream_t)stream));

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from tests import _kv_ref as ref
-from tests.test_gpu_kv import U, Both, _cu, _rows, _tree_mask, oil  # noqa: F401
+from tests.test_gpu_kv import U, Both, _check_weights, _cu, _rows, _tree_mask, oil  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -181,3 +181,37 @@ def test_probabilities_of_cached_rows(oil, N, G, D, n):  # noqa: F811
     c.append(k, v)
     q = ref.bf16(rng.standard_normal((2, N, 2 * G, D)).astype(np.float32))
     _close(c, q, None, None, None, None, 2.0 ** -11)
+
+
+# ------------------------------------------------------------------ strides
+def test_last_rows_of_long_projections(oil):  # noqa: F811
+    """The last token's heads out of a fused projection of 2,800 rows a request: requests
+    lie more than 2^24 elements apart."""
+    rng = np.random.default_rng(15)
+    fused = torch.zeros((2, 2800, 48, 128), dtype=torch.bfloat16, device="cuda")
+    assert fused.stride(0) > 1 << 24
+    x = _rows(rng, 2, 1, 48, 128)
+    fused[:, -1:] = _cu(x, torch.bfloat16)
+    last = fused[:, -1:]
+    q, k, v = last[:, :, :32], last[:, :, 32:40], last[:, :, 40:]
+    c = Both(oil, 2, 8, 128, 64)
+    c.fill(rng, [11, 40])
+    _, lse = c.attend(x[:, :, :32], x[:, :, 32:40], x[:, :, 40:], tensors=[q, k, v])
+    lse = lse.astype(np.float32)
+    c.own.weigh(q, _cu(lse))
+    c.ref.weigh(x[:, :, :32], lse, scale=128 ** -0.5)
+    _check_weights(c, None, x[:, :, :32], lse, 128 ** -0.5)
+    c.own.append(k, v)
+    c.ref.append(x[:, :, 32:40], x[:, :, 40:])
+    c.same(weights=False)
+
+
+def test_strides_past_64_bits_are_refused(oil):  # noqa: F811
+    c = oil.KvCache(4, 2, 64, 40)
+    x = torch.zeros((1 << 16,), dtype=torch.bfloat16, device="cuda")
+    p, L = x.data_ptr(), oil.lib()
+    for ld in (1 << 60, (1 << 57) + 8, 1 << 62):
+        assert L.oil_kv_append(c.handle, None, 4, p, p, 1, ld, 2, None, None, None, None) == -1
+        assert L.oil_kv_attend(c.handle, None, 4, p, ld, 2, None, None, 0, None, None, 2, 1.0, p, 1 << 16, p, p, None) == -1
+        assert L.oil_kv_attend(c.handle, None, 4, p, 128, 2, p, p, ld, None, None, 2, 1.0, p, 1 << 16, p, p, None) == -1
+        assert L.oil_kv_weigh(c.handle, None, 4, p, ld, 2, p, 2, None, None, 1.0, None) == -1
