@@ -543,6 +543,26 @@ class RecyclePool:
         return sc, tk, ln
 
 
+class _Workspaces:
+    """A stream's workspaces: beginnings of one buffer, whose size at least doubles when
+    it grows.  Outgrown buffers are kept, as captured graphs may hold their addresses;
+    all together stay below four times the largest need."""
+
+    SIZES = 4096  # calls' sizes remembered
+
+    def __init__(self):
+        self.buffers, self.by_sizes = [], {}
+
+    def get(self, key, nbytes, device):
+        if not self.buffers or self.buffers[-1].numel() < nbytes:
+            least = 2 * self.buffers[-1].numel() if self.buffers else 0
+            self.buffers.append(torch.empty((max(nbytes, least),), dtype=torch.uint8, device=device))
+        if len(self.by_sizes) >= self.SIZES:
+            self.by_sizes.clear()
+        ws = self.by_sizes[key] = self.buffers[-1][:nbytes]
+        return ws
+
+
 class KvCache:
     """One layer's committed keys and values of up to ``n_slots`` requests, held in
     4 bits, and the device buffers they live in (torch tensors, caller-owned).
@@ -551,7 +571,13 @@ class KvCache:
     and ``weights`` (n_slots, n_heads, capacity): each row's position and the
     attention weight it has accumulated (-1 and 0 past a slot's length).
     ``slots`` (B,) int32 names the slots of a call's requests (None: 0 .. B - 1).
-    Calls on one cache are ordered by the caller, as on a pool."""
+    Calls on one cache are ordered by the caller, as on a pool, but for ``attend``
+    and ``read``, which change nothing: several may run on streams of their own.
+
+    A stream's calls share one kept workspace, and so do the graphs captured on it:
+    their replays are ordered like the calls.  ``workspace``, a dense device tensor
+    of at least ``attend_workspace_bytes`` (``evict_workspace_bytes``) bytes, is
+    taken in its place, so that the caches of many layers can share one."""
 
     def __init__(self, n_slots: int, n_heads: int, head_dim: int, capacity: int, device="cuda", stream=None):
         self.n_slots, self.n_heads, self.head_dim, self.capacity = n_slots, n_heads, head_dim, capacity
@@ -570,7 +596,7 @@ class KvCache:
             n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions), _ptr(self.weights),
             _ptr(self.state), self._on(stream), ctypes.byref(h)))
         self.handle = h
-        self._ws = {}
+        self._kept = {}
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -582,15 +608,38 @@ class KvCache:
     def lengths(self):
         return self.state[:, 0]
 
-    def _workspace(self, call, *sizes):
-        """The workspace of a call of these sizes, kept (captured graphs hold its address)."""
-        ws = self._ws.get((call, sizes))
+    def attend_workspace_bytes(self, B, N, n_q_heads):
+        return lib().oil_kv_attend_workspace_bytes(self.handle, B, N, n_q_heads)
+
+    def evict_workspace_bytes(self, B, keep):
+        return lib().oil_kv_evict_workspace_bytes(self.handle, B, keep)
+
+    @property
+    def _ws(self):
+        """Workspaces of the calls on torch's current stream, by call and sizes."""
+        return self._kept_on(self._on(None)).by_sizes
+
+    def _kept_on(self, on):
+        kept = self._kept.get(on)
+        if kept is None:
+            kept = self._kept[on] = _Workspaces()
+        return kept
+
+    def _workspace(self, on, given, call, *sizes):
+        """Address and bytes of the workspace of a call of these sizes on the stream ``on``:
+        the given one, or the beginning of the stream's kept buffer."""
+        if given is not None:
+            if not given.is_cuda or not given.is_contiguous():
+                raise ValueError("workspace must be a dense device tensor")
+            return given.data_ptr(), given.numel() * given.element_size()
+        kept = self._kept_on(on)
+        ws = kept.by_sizes.get((call, sizes))
         if ws is None:
-            nbytes = getattr(lib(), f"oil_kv_{call}_workspace_bytes")(self.handle, *sizes)
+            nbytes = getattr(self, f"{call}_workspace_bytes")(*sizes)
             if nbytes == 0:
                 raise ValueError(f"unsupported cache call: {call} {sizes}")
-            ws = self._ws[call, sizes] = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
-        return ws
+            ws = kept.get((call, sizes), nbytes, self.device)
+        return ws.data_ptr(), ws.numel()
 
     def _on(self, stream):
         """The stream's handle: torch's current one of the cache's device by default."""
@@ -640,7 +689,8 @@ class KvCache:
             _shaped(v, "v", shape, k.dtype), _dtype_code(k), self._on(stream)))
         return k, v
 
-    def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None):
+    def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None,
+               workspace=None):
         """Attention of nodes q (B, N, n_q_heads, head_dim) bfloat16 over the cached
         rows and, with k and v (B, N, n_heads, head_dim), over each other: where
         ``mask`` (tree_mask's) says so, or causally.  Returns (out like q, dense,
@@ -662,14 +712,14 @@ class KvCache:
             out = (torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=self.device),
                    torch.empty((B, N, Hq), dtype=torch.float32, device=self.device))
         o, lse = out
-        ws = self._workspace("attend", B, N, Hq)
+        on = self._on(stream)
+        ws, ws_bytes = self._workspace(on, workspace, "attend", B, N, Hq)
         _check("oil_kv_attend", lib().oil_kv_attend(
             self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
             None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
             _shaped(n_nodes, "n_nodes", (B,), torch.int32),
-            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws.data_ptr(), ws.numel(),
-            _shaped(o, "out", (B, N, Hq, D), torch.bfloat16), _shaped(lse, "lse", (B, N, Hq), torch.float32),
-            self._on(stream)))
+            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws, ws_bytes,
+            _shaped(o, "out", (B, N, Hq, D), torch.bfloat16), _shaped(lse, "lse", (B, N, Hq), torch.float32), on))
         return o, lse
 
     def weigh(self, q, lse, nodes=None, count=None, scale=None, slots=None, stream=None):
@@ -685,14 +735,14 @@ class KvCache:
             _shaped(lse, "lse", (B, N, Hq), torch.float32), N, _shaped(nodes, "nodes", (B, N), torch.int32),
             _shaped(count, "count", (B,), torch.int32), scale, self._on(stream)))
 
-    def evict(self, keep, recent=0, B=None, slots=None, stream=None):
+    def evict(self, keep, recent=0, B=None, slots=None, stream=None, workspace=None):
         """Evict every head of the named slots down to ``keep`` rows: the last
         ``recent`` positions and the heaviest others stay."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
-        ws = self._workspace("evict", B, keep)
+        on = self._on(stream)
+        ws, ws_bytes = self._workspace(on, workspace, "evict", B, keep)
         _check("oil_kv_evict", lib().oil_kv_evict(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, ws.data_ptr(), ws.numel(),
-            self._on(stream)))
+            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, ws, ws_bytes, on))
 
 
 def merge_trees(anchor, lex_tokens, lex_len, lex_budget, sem_tokens, sem_len, sem_budget,
