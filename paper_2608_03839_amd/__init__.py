@@ -167,22 +167,27 @@ def _i32(t, name):
     return t
 
 
-def _shaped(t, name, shape, dtype):
-    """A dense device tensor of exactly this shape and type, or None."""
+def _on_device(t, name, index):
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
+
+
+def _shaped(t, name, shape, dtype, index):
+    """Address of a dense tensor of exactly this shape and type on device ``index``, or None."""
     if t is None:
         return None
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if not t.is_cuda or not t.is_contiguous():
-        _ptr(t)   # raises
+    _on_device(t, name, index)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _row_stride(t, name):
-    """Elements between consecutive rows of a (B, N, heads, dim) device tensor
+def _row_stride(t, name, index):
+    """Elements between consecutive rows of a (B, N, heads, dim) tensor on device ``index``
     whose rows are dense (a slice of a fused projection's output, say)."""
-    if not t.is_cuda:
-        raise ValueError("device tensor expected")
+    _on_device(t, name, index)
     B, N, H, D = t.shape
     if t.is_contiguous():
         return H * D
@@ -571,6 +576,7 @@ class KvCache:
     and ``weights`` (n_slots, n_heads, capacity): each row's position and the
     attention weight it has accumulated (-1 and 0 past a slot's length).
     ``slots`` (B,) int32 names the slots of a call's requests (None: 0 .. B - 1).
+    Every tensor and stream of a call is on the cache's device, whichever is current.
     Calls on one cache are ordered by the caller, as on a pool, but for ``attend``
     and ``read``, which change nothing: several may run on streams of their own.
 
@@ -581,8 +587,9 @@ class KvCache:
 
     def __init__(self, n_slots: int, n_heads: int, head_dim: int, capacity: int, device="cuda", stream=None):
         self.n_slots, self.n_heads, self.head_dim, self.capacity = n_slots, n_heads, head_dim, capacity
-        self.device = torch.device(device)
-        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        device = torch.device(device)
+        self._index = device.index if device.index is not None else torch.cuda.current_device()
+        self.device = torch.device(device.type, self._index)
         nbytes = lib().oil_kv_bytes(n_slots, n_heads, head_dim, capacity)
         if nbytes == 0:
             raise ValueError(f"unsupported cache: n_slots={n_slots} n_heads={n_heads} head_dim={head_dim} "
@@ -592,9 +599,8 @@ class KvCache:
         self.weights = torch.empty((n_slots, n_heads, capacity), dtype=torch.float32, device=self.device)
         self.state = torch.empty((n_slots, 4), dtype=torch.int32, device=self.device)
         h = ctypes.c_void_p()
-        _check("oil_kv_create", lib().oil_kv_create(
-            n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions), _ptr(self.weights),
-            _ptr(self.state), self._on(stream), ctypes.byref(h)))
+        self._call("oil_kv_create", n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions),
+                   _ptr(self.weights), _ptr(self.state), self._on(stream), ctypes.byref(h))
         self.handle = h
         self._kept = {}
 
@@ -625,12 +631,23 @@ class KvCache:
             kept = self._kept[on] = _Workspaces()
         return kept
 
+    def _call(self, name, *args):
+        """The C call with the cache's device current, which launches go to."""
+        call = getattr(lib(), name)
+        if torch._C._cuda_getDevice() == self._index:
+            status = call(*args)
+        else:
+            with torch.cuda.device(self._index):
+                status = call(*args)
+        _check(name, status)
+
     def _workspace(self, on, given, call, *sizes):
         """Address and bytes of the workspace of a call of these sizes on the stream ``on``:
         the given one, or the beginning of the stream's kept buffer."""
         if given is not None:
-            if not given.is_cuda or not given.is_contiguous():
-                raise ValueError("workspace must be a dense device tensor")
+            _on_device(given, "workspace", self._index)
+            if not given.is_contiguous():
+                raise ValueError("workspace must be dense")
             return given.data_ptr(), given.numel() * given.element_size()
         kept = self._kept_on(on)
         ws = kept.by_sizes.get((call, sizes))
@@ -643,12 +660,19 @@ class KvCache:
 
     def _on(self, stream):
         """The stream's handle: torch's current one of the cache's device by default."""
-        return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self._index)
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        if stream.device.index != self._index:
+            raise ValueError(f"the stream must be on cuda:{self._index}, got {stream.device}")
+        return stream.cuda_stream
+
+    def _dense(self, t, name, shape, dtype):
+        return _shaped(t, name, shape, dtype, self._index)
 
     def _heads(self, t, name):
         if t.dim() != 4 or t.shape[3] != self.head_dim:
             raise ValueError(f"{name} must be (requests, rows, heads, {self.head_dim}), got {tuple(t.shape)}")
-        return _row_stride(t, name)
+        return _row_stride(t, name, self._index)
 
     def _own_rows(self, k, v, what):
         """Stride of the rows k and v (B, N, n_heads, head_dim)."""
@@ -662,8 +686,7 @@ class KvCache:
     def reset(self, slots=None, B=None, stream=None):
         """Empty the named slots (all of them when neither slots nor B is given)."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
-        _check("oil_kv_reset", lib().oil_kv_reset(self.handle, _shaped(slots, "slots", (B,), torch.int32), B,
-                                                  self._on(stream)))
+        self._call("oil_kv_reset", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, self._on(stream))
 
     def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None):
         """Append rows of k, v (B, N, n_heads, head_dim), float32 or bfloat16: all
@@ -671,10 +694,11 @@ class KvCache:
         accepted nodes as accept_walk returns them; ``weight`` (B, n_heads, N)."""
         ld = self._own_rows(k, v, "append")
         B, N = k.shape[:2]
-        _check("oil_kv_append", lib().oil_kv_append(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, k.data_ptr(), v.data_ptr(), _dtype_code(k),
-            ld, N, _shaped(nodes, "nodes", (B, N), torch.int32), _shaped(count, "count", (B,), torch.int32),
-            _shaped(weight, "weight", (B, self.n_heads, N), torch.float32), self._on(stream)))
+        self._call(
+            "oil_kv_append", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, k.data_ptr(), v.data_ptr(),
+            _dtype_code(k), ld, N, self._dense(nodes, "nodes", (B, N), torch.int32),
+            self._dense(count, "count", (B,), torch.int32),
+            self._dense(weight, "weight", (B, self.n_heads, N), torch.float32), self._on(stream))
 
     def read(self, first, n, B=None, slots=None, dtype=torch.bfloat16, stream=None, out=None):
         """Rows first .. first + n - 1 as the values they stand for: (k, v), each
@@ -684,9 +708,9 @@ class KvCache:
         if out is None:
             out = tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
         k, v = out
-        _check("oil_kv_read", lib().oil_kv_read(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, first, n, _shaped(k, "k", shape, k.dtype),
-            _shaped(v, "v", shape, k.dtype), _dtype_code(k), self._on(stream)))
+        self._call(
+            "oil_kv_read", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, first, n,
+            self._dense(k, "k", shape, k.dtype), self._dense(v, "v", shape, k.dtype), _dtype_code(k), self._on(stream))
         return k, v
 
     def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None,
@@ -714,12 +738,12 @@ class KvCache:
         o, lse = out
         on = self._on(stream)
         ws, ws_bytes = self._workspace(on, workspace, "attend", B, N, Hq)
-        _check("oil_kv_attend", lib().oil_kv_attend(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
+        self._call(
+            "oil_kv_attend", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
             None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
-            _shaped(n_nodes, "n_nodes", (B,), torch.int32),
-            _shaped(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws, ws_bytes,
-            _shaped(o, "out", (B, N, Hq, D), torch.bfloat16), _shaped(lse, "lse", (B, N, Hq), torch.float32), on))
+            self._dense(n_nodes, "n_nodes", (B,), torch.int32),
+            self._dense(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws, ws_bytes,
+            self._dense(o, "out", (B, N, Hq, D), torch.bfloat16), self._dense(lse, "lse", (B, N, Hq), torch.float32), on)
         return o, lse
 
     def weigh(self, q, lse, nodes=None, count=None, scale=None, slots=None, stream=None):
@@ -730,10 +754,10 @@ class KvCache:
         if q.dtype != torch.bfloat16:
             raise ValueError(f"weigh: q must be bfloat16, got {q.dtype}")
         scale = 1.0 / math.sqrt(D) if scale is None else scale
-        _check("oil_kv_weigh", lib().oil_kv_weigh(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
-            _shaped(lse, "lse", (B, N, Hq), torch.float32), N, _shaped(nodes, "nodes", (B, N), torch.int32),
-            _shaped(count, "count", (B,), torch.int32), scale, self._on(stream)))
+        self._call(
+            "oil_kv_weigh", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
+            self._dense(lse, "lse", (B, N, Hq), torch.float32), N, self._dense(nodes, "nodes", (B, N), torch.int32),
+            self._dense(count, "count", (B,), torch.int32), scale, self._on(stream))
 
     def evict(self, keep, recent=0, B=None, slots=None, stream=None, workspace=None):
         """Evict every head of the named slots down to ``keep`` rows: the last
@@ -741,8 +765,8 @@ class KvCache:
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
         on = self._on(stream)
         ws, ws_bytes = self._workspace(on, workspace, "evict", B, keep)
-        _check("oil_kv_evict", lib().oil_kv_evict(
-            self.handle, _shaped(slots, "slots", (B,), torch.int32), B, keep, recent, ws, ws_bytes, on))
+        self._call("oil_kv_evict", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, keep, recent, ws,
+                   ws_bytes, on)
 
 
 def merge_trees(anchor, lex_tokens, lex_len, lex_budget, sem_tokens, sem_len, sem_budget,
