@@ -167,9 +167,17 @@ def _i32(t, name):
     return t
 
 
-def _on_device(t, name, index):
-    if t.get_device() != index:
-        raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
+def _empty(shape, dtype, device, stream=None):
+    """Memory for work on ``stream``: what torch's allocator gives on another stream may
+    still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _elsewhere(t, name, index):
+    raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
 
 
 def _shaped(t, name, shape, dtype, index):
@@ -178,7 +186,8 @@ def _shaped(t, name, shape, dtype, index):
         return None
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    _on_device(t, name, index)
+    if t.get_device() != index:
+        _elsewhere(t, name, index)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
@@ -187,7 +196,8 @@ def _shaped(t, name, shape, dtype, index):
 def _row_stride(t, name, index):
     """Elements between consecutive rows of a (B, N, heads, dim) tensor on device ``index``
     whose rows are dense (a slice of a fused projection's output, say)."""
-    _on_device(t, name, index)
+    if t.get_device() != index:
+        _elsewhere(t, name, index)
     B, N, H, D = t.shape
     if t.is_contiguous():
         return H * D
@@ -558,10 +568,10 @@ class _Workspaces:
     def __init__(self):
         self.buffers, self.by_sizes = [], {}
 
-    def get(self, key, nbytes, device):
+    def get(self, key, nbytes, device, stream=None):
         if not self.buffers or self.buffers[-1].numel() < nbytes:
             least = 2 * self.buffers[-1].numel() if self.buffers else 0
-            self.buffers.append(torch.empty((max(nbytes, least),), dtype=torch.uint8, device=device))
+            self.buffers.append(_empty((max(nbytes, least),), torch.uint8, device, stream))
         if len(self.by_sizes) >= self.SIZES:
             self.by_sizes.clear()
         ws = self.by_sizes[key] = self.buffers[-1][:nbytes]
@@ -576,7 +586,8 @@ class KvCache:
     and ``weights`` (n_slots, n_heads, capacity): each row's position and the
     attention weight it has accumulated (-1 and 0 past a slot's length).
     ``slots`` (B,) int32 names the slots of a call's requests (None: 0 .. B - 1).
-    Every tensor and stream of a call is on the cache's device, whichever is current.
+    Every tensor and stream of a call is on the cache's device, whichever is current;
+    what a call makes itself is the memory of the stream that it is given.
     Calls on one cache are ordered by the caller, as on a pool, but for ``attend``
     and ``read``, which change nothing: several may run on streams of their own.
 
@@ -594,13 +605,14 @@ class KvCache:
         if nbytes == 0:
             raise ValueError(f"unsupported cache: n_slots={n_slots} n_heads={n_heads} head_dim={head_dim} "
                              f"capacity={capacity}")
-        self.codes = torch.empty((nbytes,), dtype=torch.uint8, device=self.device)
-        self.positions = torch.empty((n_slots, n_heads, capacity), dtype=torch.int32, device=self.device)
-        self.weights = torch.empty((n_slots, n_heads, capacity), dtype=torch.float32, device=self.device)
-        self.state = torch.empty((n_slots, 4), dtype=torch.int32, device=self.device)
+        on = self._on(stream)
+        self.codes = _empty((nbytes,), torch.uint8, self.device, stream)
+        self.positions = _empty((n_slots, n_heads, capacity), torch.int32, self.device, stream)
+        self.weights = _empty((n_slots, n_heads, capacity), torch.float32, self.device, stream)
+        self.state = _empty((n_slots, 4), torch.int32, self.device, stream)
         h = ctypes.c_void_p()
         self._call("oil_kv_create", n_slots, n_heads, head_dim, capacity, _ptr(self.codes), _ptr(self.positions),
-                   _ptr(self.weights), _ptr(self.state), self._on(stream), ctypes.byref(h))
+                   _ptr(self.weights), _ptr(self.state), on, ctypes.byref(h))
         self.handle = h
         self._kept = {}
 
@@ -641,21 +653,23 @@ class KvCache:
                 status = call(*args)
         _check(name, status)
 
-    def _workspace(self, on, given, call, *sizes):
+    def _workspace(self, stream, on, given, call, *sizes):
         """Address and bytes of the workspace of a call of these sizes on the stream ``on``:
         the given one, or the beginning of the stream's kept buffer."""
         if given is not None:
-            _on_device(given, "workspace", self._index)
+            if given.get_device() != self._index:
+                _elsewhere(given, "workspace", self._index)
             if not given.is_contiguous():
                 raise ValueError("workspace must be dense")
             return given.data_ptr(), given.numel() * given.element_size()
-        kept = self._kept_on(on)
-        ws = kept.by_sizes.get((call, sizes))
+        kept = self._kept.get(on)
+        ws = kept.by_sizes.get((call, sizes)) if kept is not None else None
         if ws is None:
+            kept = self._kept_on(on)
             nbytes = getattr(self, f"{call}_workspace_bytes")(*sizes)
             if nbytes == 0:
                 raise ValueError(f"unsupported cache call: {call} {sizes}")
-            ws = kept.get((call, sizes), nbytes, self.device)
+            ws = kept.get((call, sizes), nbytes, self.device, stream)
         return ws.data_ptr(), ws.numel()
 
     def _on(self, stream):
@@ -665,9 +679,6 @@ class KvCache:
         if stream.device.index != self._index:
             raise ValueError(f"the stream must be on cuda:{self._index}, got {stream.device}")
         return stream.cuda_stream
-
-    def _dense(self, t, name, shape, dtype):
-        return _shaped(t, name, shape, dtype, self._index)
 
     def _heads(self, t, name):
         if t.dim() != 4 or t.shape[3] != self.head_dim:
@@ -686,7 +697,8 @@ class KvCache:
     def reset(self, slots=None, B=None, stream=None):
         """Empty the named slots (all of them when neither slots nor B is given)."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
-        self._call("oil_kv_reset", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, self._on(stream))
+        self._call("oil_kv_reset", self.handle, _shaped(slots, "slots", (B,), torch.int32, self._index), B,
+                   self._on(stream))
 
     def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None):
         """Append rows of k, v (B, N, n_heads, head_dim), float32 or bfloat16: all
@@ -694,23 +706,23 @@ class KvCache:
         accepted nodes as accept_walk returns them; ``weight`` (B, n_heads, N)."""
         ld = self._own_rows(k, v, "append")
         B, N = k.shape[:2]
-        self._call(
-            "oil_kv_append", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, k.data_ptr(), v.data_ptr(),
-            _dtype_code(k), ld, N, self._dense(nodes, "nodes", (B, N), torch.int32),
-            self._dense(count, "count", (B,), torch.int32),
-            self._dense(weight, "weight", (B, self.n_heads, N), torch.float32), self._on(stream))
+        on, i, i32 = self._on(stream), self._index, torch.int32
+        self._call("oil_kv_append", self.handle, _shaped(slots, "slots", (B,), i32, i), B, k.data_ptr(), v.data_ptr(),
+                   _dtype_code(k), ld, N, _shaped(nodes, "nodes", (B, N), i32, i),
+                   _shaped(count, "count", (B,), i32, i),
+                   _shaped(weight, "weight", (B, self.n_heads, N), torch.float32, i), on)
 
     def read(self, first, n, B=None, slots=None, dtype=torch.bfloat16, stream=None, out=None):
         """Rows first .. first + n - 1 as the values they stand for: (k, v), each
         (B, n_heads, n, head_dim); zeros past a slot's length."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
         shape = (B, self.n_heads, n, self.head_dim)
+        on, i = self._on(stream), self._index
         if out is None:
-            out = tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
+            out = tuple(_empty(shape, dtype, self.device, stream) for _ in range(2))
         k, v = out
-        self._call(
-            "oil_kv_read", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, first, n,
-            self._dense(k, "k", shape, k.dtype), self._dense(v, "v", shape, k.dtype), _dtype_code(k), self._on(stream))
+        self._call("oil_kv_read", self.handle, _shaped(slots, "slots", (B,), torch.int32, i), B, first, n,
+                   _shaped(k, "k", shape, k.dtype, i), _shaped(v, "v", shape, k.dtype, i), _dtype_code(k), on)
         return k, v
 
     def attend(self, q, k=None, v=None, n_nodes=None, mask=None, scale=None, slots=None, stream=None, out=None,
@@ -732,18 +744,17 @@ class KvCache:
             if t is not None and t.dtype != torch.bfloat16:
                 raise ValueError(f"attend: {name} must be bfloat16, got {t.dtype}")
         scale = 1.0 / math.sqrt(D) if scale is None else scale
+        on, i, i32 = self._on(stream), self._index, torch.int32
         if out is None:
-            out = (torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=self.device),
-                   torch.empty((B, N, Hq), dtype=torch.float32, device=self.device))
+            out = (_empty((B, N, Hq, D), torch.bfloat16, self.device, stream),
+                   _empty((B, N, Hq), torch.float32, self.device, stream))
         o, lse = out
-        on = self._on(stream)
-        ws, ws_bytes = self._workspace(on, workspace, "attend", B, N, Hq)
-        self._call(
-            "oil_kv_attend", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
-            None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
-            self._dense(n_nodes, "n_nodes", (B,), torch.int32),
-            self._dense(mask, "mask", (B, N, (N + 31) // 32), torch.int32), N, scale, ws, ws_bytes,
-            self._dense(o, "out", (B, N, Hq, D), torch.bfloat16), self._dense(lse, "lse", (B, N, Hq), torch.float32), on)
+        ws, ws_bytes = self._workspace(stream, on, workspace, "attend", B, N, Hq)
+        self._call("oil_kv_attend", self.handle, _shaped(slots, "slots", (B,), i32, i), B, q.data_ptr(), q_ld, Hq,
+                   None if k is None else k.data_ptr(), None if v is None else v.data_ptr(), ld,
+                   _shaped(n_nodes, "n_nodes", (B,), i32, i), _shaped(mask, "mask", (B, N, (N + 31) // 32), i32, i), N,
+                   scale, ws, ws_bytes, _shaped(o, "out", (B, N, Hq, D), torch.bfloat16, i),
+                   _shaped(lse, "lse", (B, N, Hq), torch.float32, i), on)
         return o, lse
 
     def weigh(self, q, lse, nodes=None, count=None, scale=None, slots=None, stream=None):
@@ -754,18 +765,18 @@ class KvCache:
         if q.dtype != torch.bfloat16:
             raise ValueError(f"weigh: q must be bfloat16, got {q.dtype}")
         scale = 1.0 / math.sqrt(D) if scale is None else scale
-        self._call(
-            "oil_kv_weigh", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, q.data_ptr(), q_ld, Hq,
-            self._dense(lse, "lse", (B, N, Hq), torch.float32), N, self._dense(nodes, "nodes", (B, N), torch.int32),
-            self._dense(count, "count", (B,), torch.int32), scale, self._on(stream))
+        on, i, i32 = self._on(stream), self._index, torch.int32
+        self._call("oil_kv_weigh", self.handle, _shaped(slots, "slots", (B,), i32, i), B, q.data_ptr(), q_ld, Hq,
+                   _shaped(lse, "lse", (B, N, Hq), torch.float32, i), N, _shaped(nodes, "nodes", (B, N), i32, i),
+                   _shaped(count, "count", (B,), i32, i), scale, on)
 
     def evict(self, keep, recent=0, B=None, slots=None, stream=None, workspace=None):
         """Evict every head of the named slots down to ``keep`` rows: the last
         ``recent`` positions and the heaviest others stay."""
         B = slots.shape[0] if slots is not None else self.n_slots if B is None else B
-        on = self._on(stream)
-        ws, ws_bytes = self._workspace(on, workspace, "evict", B, keep)
-        self._call("oil_kv_evict", self.handle, self._dense(slots, "slots", (B,), torch.int32), B, keep, recent, ws,
+        on, i = self._on(stream), self._index
+        ws, ws_bytes = self._workspace(stream, on, workspace, "evict", B, keep)
+        self._call("oil_kv_evict", self.handle, _shaped(slots, "slots", (B,), torch.int32, i), B, keep, recent, ws,
                    ws_bytes, on)
 
 

@@ -103,3 +103,29 @@ def test_graph_keeps_its_workspace(oil):  # noqa: F811
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
     assert all(torch.isnan(x).all() for x in others)
+
+
+def _stream_of(x):
+    """The stream whose memory of torch's allocator x lies in."""
+    at = x.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+def test_memory_of_the_stream_given(oil):  # noqa: F811
+    """With a stream given, what a call makes is allocated for that stream: what is free on the
+    current one may still be in use there."""
+    side = torch.cuda.Stream()
+    c = _filled(oil)
+    q, k, v = _nodes(8, 17)
+    torch.cuda.synchronize()
+    made = [*c.attend(q, k, v, stream=side), *c.read(3, 70, stream=side)]
+    c.evict(90, stream=side)
+    with torch.cuda.stream(side):
+        made += list(c._ws.values())
+    assert len(made) == 6
+    d = oil.KvCache(3, 2, 64, 40, stream=side)
+    made += [d.codes, d.positions, d.weights, d.state]
+    side.synchronize()
+    assert [_stream_of(x) for x in made] == [side.cuda_stream] * len(made)
+    assert _stream_of(c.attend(q, k, v)[0]) == 0
+    torch.cuda.synchronize()
