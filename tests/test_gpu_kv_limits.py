@@ -215,3 +215,67 @@ def test_strides_past_64_bits_are_refused(oil):  # noqa: F811
         assert L.oil_kv_attend(c.handle, None, 4, p, ld, 2, None, None, 0, None, None, 2, 1.0, p, 1 << 16, p, p, None) == -1
         assert L.oil_kv_attend(c.handle, None, 4, p, 128, 2, p, p, ld, None, None, 2, 1.0, p, 1 << 16, p, p, None) == -1
         assert L.oil_kv_weigh(c.handle, None, 4, p, ld, 2, p, 2, None, None, 1.0, None) == -1
+
+
+# ------------------------------------------------------------------ exact inputs
+@pytest.mark.parametrize("N,G", [(1, 4), (9, 2), (20, 1), (45, 1)])
+@pytest.mark.parametrize("n", [33, 700])
+def test_one_position_takes_all(oil, N, G, n):  # noqa: F811
+    """Large scores that are exact: keys of whole numbers 0 .. 15 that 4 bits hold as they
+    are, queries of one large power of two.  Each row's winner leads by at least 64, so that
+    the output is the winner's held value row and lse its score."""
+    rng = np.random.default_rng(n + N)
+    D = 64
+    k = np.zeros((2, n, 1, D), np.float32)
+    k[:, :, 0, 1] = 15.0                               # s = 1, z = 0 in every row
+    for d in range(2, 34):
+        k[:, d - 2, 0, d] = 9 + (d % 5)                # row d - 2 alone has column d
+    v = _rows(rng, 2, n, 1, D)
+    c = Both(oil, 2, 1, D, n)
+    c.append(k, v)
+    q = np.zeros((2, N, G, D), np.float32)
+    winner = rng.integers(0, 32, (2, N, G))
+    for b, i, a in np.ndindex(*winner.shape):
+        q[b, i, a, 2 + winner[b, i, a]] = 64.0
+    out, lse = c.own.attend(_cu(q, torch.bfloat16), scale=1.0)
+    torch.cuda.synchronize()
+    out, lse = out.float().cpu().numpy(), lse.cpu().numpy()
+    for b, i, a in np.ndindex(*winner.shape):
+        w = winner[b, i, a]
+        score = 64.0 * (9 + ((w + 2) % 5))         # rounded factors and sums: 16 u of it, 64 u of the sum
+        assert abs(lse[b, i, a] - score) <= (16 * (1 + score) + 64) * U
+        want = c.ref.v[b][0, w]
+        off = 2.0 ** -10 * np.abs(want).max()      # the probability's rounding to binary16, twice over
+        assert (np.abs(out[b, i, a] - want) <= off + _half_spacing(np.abs(want) + off)).all()
+
+
+# ------------------------------------------------------------------ eviction
+def test_evict_of_many_requests(oil):  # noqa: F811
+    """Which rows of more than 64 requests stay, at weights given with the rows."""
+    rng = np.random.default_rng(16)
+    B, n = 130, 70
+    c = Both(oil, B, 2, 64, n)
+    w = np.stack([rng.permutation(2 * n).reshape(2, n) for _ in range(B)]).astype(np.float32)
+    c.append(_rows(rng, B, n, 2, 64), _rows(rng, B, n, 2, 64), count=rng.integers(0, n + 1, B), weight=w)
+    c.own.evict(40, 8)
+    c.ref.evict(40, 8)
+    c.same()
+    slots = rng.permutation(B)[:100]
+    c.own.evict(17, 3, slots=Both._i32(slots))
+    c.ref.evict(17, 3, slots=slots)
+    c.same()
+
+
+@pytest.mark.parametrize("D", [8, 128])
+@pytest.mark.parametrize("keep,n", [(4130, 4300), (4128, 4300), (4101, 4600)])
+def test_evict_by_one_wave_a_tile(oil, D, keep, n):  # noqa: F811
+    """More than 8,192 destination tiles, budgets that end inside a tile and at its edge."""
+    rng = np.random.default_rng(keep + D)
+    B, H = 8, 8
+    c = Both(oil, B, H, D, n)
+    w = rng.random((B, H, n)).astype(np.float32)
+    rows = [_rows(rng, B, n, H, D) for _ in range(2)]
+    c.append(*rows, weight=w)
+    c.own.evict(keep, 100)
+    c.ref.evict(keep, 100)
+    c.same()
