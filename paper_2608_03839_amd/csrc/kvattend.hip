@@ -1453,8 +1453,7 @@ static void kv_attend_launch(const KvAttend& A, const KvPlan& p, hipStream_t str
         hipLaunchKernelGGL((kv_attend_kernel<W, 2>), grid, block, 0, stream, A);
     else
         hipLaunchKernelGGL((kv_attend_kernel<W, 3>), grid, block, 0, stream, A);
-    if (p.wgs > 1)
-        hipLaunchKernelGGL(kv_join_kernel<W>, grid, dim3(256), 0, stream, A, 16 * p.nt);
+    hipLaunchKernelGGL(kv_join_kernel<W>, grid, dim3(256), 0, stream, A, 16 * p.nt);
 }
 
 hipError_t launch_kv_attend(const KvView& c, const int32_t* slots, int32_t B, const void* q, int64_t q_ld,
