@@ -21,31 +21,32 @@
 //
 // The softmax keeps, per row, a reference m and sums relative to it (base 2).
 // m moves only when a score passes it by 2^15, to 11 below the maximum: then
-// p <= 2^15 fits binary16, and a p below 2^-32 of the largest is the first that
-// rounds to nothing.  p times the value row's s, over a power of two E at or above every s
-// so far, is what the second product takes, rounded to binary16 (2^-12
-// relative).  z and s c may be far larger than the value they add up to, so that
-// rounding must not reach s c alone: z is weighted by the rounded p too (z / s
-// times the operand).  Tiles in which some s is below 2^-6 E, where operands would
-// lose bits, take two bf16 operands, the second what the first leaves.  Sums are
-// kept over E 2^24, E also at or above every |z| 2^-64, and a wave's become
-// a mean before they are multiplied by E: nothing passes binary32 that the
-// values do not, and what lies within 2^90 of the largest value counts.
+// p <= 2^15 fits binary16, and a p below 2^-31 of the largest (2^-26 where s is far
+// below E) is the first that rounds to nothing.  p times the value row's s, over a
+// power of two E at or above every s so far, is what the second product takes,
+// rounded to binary16 (2^-11 of it).  z and s c may be far larger than the value
+// they add up to, so that rounding must not reach s c alone: z is weighted by the
+// rounded p too (z / s times the operand).  Tiles in which some s is below 2^-6 E,
+// where operands would lose bits, take two bf16 operands, the second what the first
+// leaves.  Sums are kept over E 2^24, E also at or above every |z| 2^-64, and a
+// wave's become a mean before they are multiplied by E: nothing passes binary32
+// that the values do not, and what lies within 2^90 of the largest value counts.
 //
 // The tree's nodes come as further tiles in bf16, p as two operands, the second
 // what the first leaves (2^-16 of p: one alone, 2^-8, would show in outputs of
 // bf16 where the nodes hold the weight).
 //
 // What bounds it, at 8 key/value heads of 128 columns.  Single tokens: the stream
-// of tiles (32 requests of up to 16,384 positions, 32 query heads: 364 MB in 73
-// us, 5.0 TB/s; one slot of 262,149, 40 query heads: 285 MB in 54 us; the tiles by
+// of tiles (32 requests of up to 16,384 positions, 32 query heads: 364 MB in 75
+// us, 4.9 TB/s; one slot of 262,149, 40 query heads: 286 MB in 58 us; the tiles by
 // themselves stream at 7 TB/s, the rest is the share, the queries and the joining
 // of the waves).  Many rows: the softmax's instructions between the products
 // (about 330 VALU and 24 exponentials for 32 positions by 48 rows, two waves a
-// SIMD; 32 trees of up to 65 nodes over up to 8,192 positions, 32 query heads: 343
-// us, 444 TFLOP/s; 4 chunks of 256 nodes over 16,001, 64 query heads: 783 us, 691
-// TFLOP/s).  Few positions: the launch and five dependent steps of 1 to 2 us each
-// (2,047 positions, one token: 11 us).
+// SIMD; calls with their join: 32 trees of up to 65 nodes over up to 8,192
+// positions, 32 query heads, 343 us, 443 TFLOP/s; 4 chunks of 256 nodes over
+// 16,001, 64 query heads, 790 us, 685 TFLOP/s).  Few positions: the launch and five
+// dependent steps of 1 to 2 us each (2,047 positions, one token: 11 us; 61 nodes
+// over empty slots, 32 requests: 46 us, most of it the nodes' own tiles).
 //
 // weigh: below.
 #include "kv.hpp"
@@ -1176,8 +1177,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv_attend_kernel(KvAtten
 // sum l_p 2^(m_p - m), m the largest.  The workgroup of each share that begins
 // inside an item takes its part of that item's rows, with four waves a row where
 // the parts are many (past 16 a wave's loads would follow each other), else one.
-// Latencies bound it: a launch, a table entry, (m, l), rows: 4 to 6 us, 20 us where
-// 512 shares of 48 rows by 128 columns are joined (12 MB).
+// Latencies bound it: a launch, a table entry, (m, l), rows: 4 to 6 us, 19 us where
+// 512 shares of 48 rows by 128 columns are joined (23 MB).  Factors of parts go from
+// lane to lane by reads of a lane and sums by swaps and swizzles: as LDS shuffles they
+// stood before the rows' loads could be used (23 us).
 template <int W>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_item)
 {
@@ -1282,9 +1285,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend A, int rows_per_i
 // S = Q K^T puts a position into a lane column, so a position's sum over rows is
 // over a lane's registers and four lanes; a wave owns its tiles' weights, so there
 // are no atomics and one result.  Bound by tiles in flight: with one in flight a
-// wave 32 requests of up to 16,384 positions took 47 us, with two 41 (205 MB, 5.0
-// TB/s; the longest requests' waves run on alone at the end); 8 requests of up to
-// 32,768 and up to 56 rows a head 33 us, much of it the exponentials' instructions.
+// wave 32 requests of up to 16,384 positions took 51.5 us, with two 47.7 (205 MB,
+// 4.3 TB/s; the longest requests' waves run on alone at the end); 8 requests of up
+// to 32,768 and up to 56 rows a head 33 us, much of it the exponentials' instructions.
 // ONE: at most 16 rows, whose loop over row tiles is gone.
 template <int W, bool ONE>
 __global__ __launch_bounds__(256, 4) void kv_weigh_kernel(KvView c, const int32_t* __restrict__ slots,

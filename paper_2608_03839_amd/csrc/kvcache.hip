@@ -8,10 +8,11 @@
 // are put together in LDS as they are stored and leave 16 bytes a lane; where the
 // tile also holds earlier positions, a value dword (8 positions of a column) is
 // read and merged.  The workgroup owns the tile, so there is no race on a dword.
-// Bound by memory and by the VALU (18 instructions a value, whose issue is nearly
-// full) alike: 4 prompts of 8,191 rows, 8 heads of 128 columns in bf16: 136 MB in
-// and 38 MB out in 37 us, 4.7 TB/s (a copy reaches 4.9); small appends by their
-// latencies, 6 us.
+// Bound by memory and by the VALU (18 instructions a value, 0.8 of its issue) alike:
+// 4 prompts of 8,191 rows, 8 heads of 128 columns in bf16: 136 MB in and 38 MB out in
+// 45 us, 3.9 TB/s, from memory, 37 from the last-level cache; in binary32 64 us (306
+// MB, 4.8 TB/s); 16 requests of 4,097 rows 69 us (5.0 TB/s; a copy reaches 4.9).  Small
+// appends by their latencies, 6 us; the committed paths of 32 trees 8 us.
 //
 // read: a tile's codes to LDS, y = z + s c, 16 bytes a lane; the same rows in 27 us
 // (36 MB in, 134 MB out, 6.4 TB/s).
@@ -22,9 +23,12 @@
 // and lists the moves with their positions and weights; a second kernel owns
 // one destination tile per workgroup.  16 requests of 8 heads, 20,481 rows to
 // 16,384: 44 us to select (128 workgroups for 256 CUs: a head's three passes over
-// LDS, one after the other, are the time) and 116 to move (a nibble of every dword of
+// LDS, one after the other, are the time) and 129 to move (a nibble of every dword of
 // the values changes with a row, so nearly every tile below the budget is read and
-// written: about 395 MB in, 150 out, 4.7 TB/s).
+// written: 430 MB in, 169 out, 4.6 TB/s; turn after turn fewer rows move, 106 us).
+// A head's ranks fit LDS up to 36,864 rows.  Past that each pass reads weights and
+// positions again (from the caches), through one workgroup a head still: of one
+// request, 8 heads, 36,864 rows take 62 us, 40,960 118, 147,456 411, 393,216 1,200.
 //
 // A slot's length changes when the last workgroup of the request has read it:
 // each takes a ticket when it is done, or, where they are many, by a launch of its
