@@ -524,12 +524,15 @@ size_t oil_kv_attend_workspace_bytes(const oil_kv *kv, int32_t B, int32_t max_no
  * Sums, the softmax's statistics and lse are binary32.  Rounded to fewer bits are:
  *   q          over the cache, to binary16 under a power of two a row: exact for
  *              values within 2^-28 of the row's largest;
- *   scores     over the cache, sums of q times 4-bit codes off by 2e-7 of sum |q k|;
+ *   scores     over the cache, off by 2e-7 of sum |q|(|z| + s c) where many columns
+ *              share it, by 5e-6 where one or two hold it;
  *   weights    exp(S - lse) of a cached position to binary16 (2^-11 of it, or 2^-26
  *              of the row's largest weight if that is more) or, among positions
  *              whose values have scales far apart (2^6), to two bf16 (2^-16); of a
  *              node to two bf16; the sum that divides them is of unrounded ones;
- *   out        to the nearest bf16, which is 2^-8.
+ *   out        to the nearest bf16, which is 2^-8; before that, sums of weights
+ *              times s c are off by 2^-18 of themselves, at most 2^-14, which shows
+ *              in columns where s c and z cancel.
  * Values may be any that rows hold: a mean of values is finite where they are, and
  * values of at least 2^-90 of a head's largest count, however little that weighs. */
 int32_t oil_kv_attend(const oil_kv *kv, const int32_t *slots, int32_t B, const void *q, int64_t q_ld,

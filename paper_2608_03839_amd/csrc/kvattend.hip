@@ -10,9 +10,11 @@
 //
 // A code c of a 4-bit row enters the product as the binary16 subnormal c 2^-24
 // (its nibble is the mantissa) or, for every other pair, as 16 c 2^-24: eight
-// codes cost four ANDs and a shift.  The MFMA cuts a subnormal product's low bits:
-// sums differ from exact ones by 2e-7 of their size (normal operands: 1e-8), which
-// is 1e-4 of what an output's bf16 rounds away.  Queries are scaled to binary16 by
+// codes cost four ANDs and a shift.  The MFMA cuts a subnormal product's low bits,
+// by the place that its exponent would have: scores differ from exact ones by 2e-7 of
+// sum |q|(|z| + s c) where 128 columns share it (normal operands: 1e-8), by up to
+// 5e-6 where one or two hold it, and sums p s c by 2^-18 of themselves, at most 2^-14
+// (measured over equal value rows): outputs are bf16, 2^-8.  Queries are scaled to binary16 by
 // a power of two per row, exactly for values within 2^-28 of the row's largest;
 // sums are binary32.  The keys' codes are taken from their middle: the
 // product starts at -7.5 sum(q) and y = z + 7.5 s enters as y sum(q), two small

@@ -183,6 +183,25 @@ def test_probabilities_of_cached_rows(oil, N, G, D, n):  # noqa: F811
     _close(c, q, None, None, None, None, 2.0 ** -11)
 
 
+@pytest.mark.parametrize("n", [1, 5, 32, 300])
+@pytest.mark.parametrize("G", [4, 20, 40])
+def test_values_that_cancel_their_zero_points(oil, n, G):  # noqa: F811
+    """Equal value rows under any weights: the output is the row, to the weights' 2^-11, half a
+    spacing of bf16 and 2^-14 of s c, which may be far larger than the value."""
+    rng = np.random.default_rng(n + G)
+    B, D = 60, 128
+    c = oil.KvCache(B, 1, D, n)
+    v = np.broadcast_to(_rows(rng, B, 1, 1, D), (B, n, 1, D)).copy()
+    c.append(_cu(_rows(rng, B, n, 1, D), torch.bfloat16), _cu(v, torch.bfloat16))
+    out, _ = c.attend(_cu(_rows(rng, B, 1, G, D), torch.bfloat16))
+    torch.cuda.synchronize()
+    out = out.float().cpu().numpy().astype(np.float64)[:, 0]
+    codes, s, z = (x.astype(np.float64) for x in ref.quantise(v[:, :1, 0]))
+    want = z + s * codes
+    off = (2.0 ** -11 + 2.0 ** -16) * np.abs(want) + 2.0 ** -14 * s * codes
+    assert (np.abs(out - want) <= off + _half_spacing(np.abs(want) + off)).all()
+
+
 # ------------------------------------------------------------------ strides
 def test_last_rows_of_long_projections(oil):  # noqa: F811
     """The last token's heads out of a fused projection of 2,800 rows a request: requests
