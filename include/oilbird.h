@@ -488,6 +488,16 @@ int32_t oil_kv_append(oil_kv *kv, const int32_t *slots, int32_t B, const void *k
                       int64_t ld, int32_t max_rows, const int32_t *nodes, const int32_t *count,
                       const float *weight, void *stream);
 
+/* Append packed sequences: request b's rows are starts[b] .. starts[b + 1] - 1 of the
+ * `total` rows of k and v, whose other arguments are oil_kv_append's.
+ *   starts     B + 1 int32 (device), ascending within 0 .. total; values past those
+ *              bounds count as the bound, a sequence that ends before it begins as empty.
+ *   total      1 .. OIL_PROMPT_MAX_ROWS.
+ *   weight     n_heads x total float32 by row, as oil_prompt_weigh wrote it, or NULL for 0. */
+int32_t oil_kv_append_packed(oil_kv *kv, const int32_t *slots, int32_t B, const int32_t *starts, int64_t total,
+                             const void *k, const void *v, int32_t dtype, int64_t ld, const float *weight,
+                             void *stream);
+
 /* Read rows first .. first + n - 1 of B requests back as the values they stand
  * for: k_out, v_out B x n_heads x n x head_dim, OIL_F32 or OIL_BF16 (nearest-even), 16-byte
  * aligned; zeros past a slot's length.  first >= 0, n >= 1, first + n <= capacity. */
@@ -564,6 +574,82 @@ size_t oil_kv_evict_workspace_bytes(const oil_kv *kv, int32_t B, int64_t keep);
  *   workspace  >= oil_kv_evict_workspace_bytes(kv, B, keep), 256-byte aligned. */
 int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, int64_t recent, void *workspace,
                      size_t workspace_bytes, void *stream);
+
+/* ---- Whole prompts, before they enter a cache: packed sequences, one after the
+ * other in the rows of one buffer, attend to themselves exactly as they are, not as 4
+ * bits hold them, and what they saw becomes the weights that their rows start with
+ * (oil_kv_append_packed).
+ *
+ * Common arguments:
+ *   starts     B + 1 int32 (device) as in oil_kv_append_packed.  B 1 .. OIL_MAX_B.
+ *   total      rows of every buffer, 1 .. OIL_PROMPT_MAX_ROWS; times n_q_heads at most 2^30.
+ *   q          total rows of n_q_heads x head_dim bf16, 16-byte aligned, rows q_ld
+ *              elements apart (>= n_q_heads * head_dim, a multiple of 8, at most
+ *              OIL_PROMPT_MAX_LD).
+ *   k, v       total rows of n_heads x head_dim bf16, rows ld elements apart likewise.
+ *   n_heads    1 .. OIL_KV_MAX_HEADS.   n_q_heads  a multiple of it, at most
+ *              OIL_KV_MAX_GROUP times.   head_dim  a multiple of 8, 8 .. OIL_KV_MAX_DIM.
+ *   scale      finite.
+ * Rows outside every sequence are neither read nor written. */
+#define OIL_PROMPT_MAX_ROWS (1 << 28)
+#define OIL_PROMPT_MAX_LD (1 << 24)
+
+/* Causal attention of packed sequences.  Query head a reads key/value head
+ * a / (n_q_heads / n_heads); row i sees the rows of its sequence up to its own:
+ *     S = scale * q . k;  lse = log sum exp S;  out = sum exp(S - lse) v.
+ *   out        total x n_q_heads x head_dim bf16, dense, 16-byte aligned.
+ *   lse        total x n_q_heads float32 (natural logarithm) or NULL.
+ * What a row does not see does not reach it, whatever it holds.  A row whose scores are
+ * all -inf gives zeros and -inf; a score that is NaN or passes binary32 makes its row NaN.
+ * Sums, the softmax's statistics and lse are binary32.  Rounded to fewer bits are the
+ * weights exp(S - m), m a number for each row, to bf16 for their product with v (half a
+ * step is 2^-8 of each; the sum that divides is of unrounded ones), and out. */
+int32_t oil_prompt_attend(const int32_t *starts, int32_t B, int64_t total, const void *q, int64_t q_ld,
+                          int32_t n_q_heads, const void *k, const void *v, int64_t ld, int32_t n_heads,
+                          int32_t head_dim, float scale, void *out, float *lse, void *stream);
+
+/* The attention weight that positions received from the last `last` rows of their
+ * sequence (all of them where last is at least its length):
+ *     weight[h][j] = sum over those rows i >= j and heads a of h of
+ *                    exp(scale * q_ia . k_j - lse_ia).
+ *   lse        as oil_prompt_attend wrote it; a row at -inf adds nothing.
+ *   last       >= 1.
+ *   weight     n_heads x total float32.
+ * Sums are binary32, each added up by one workgroup in one order. */
+int32_t oil_prompt_weigh(const int32_t *starts, int32_t B, int64_t total, const void *q, int64_t q_ld,
+                         int32_t n_q_heads, const float *lse, const void *k, int64_t ld, int32_t n_heads,
+                         int32_t head_dim, int64_t last, float scale, float *weight, void *stream);
+
+/* ---- What a verifier's rows of logits say: the predictions that oil_accept_walk takes
+ * (top_tokens with top = 1), the log probabilities of drafted tokens, alternatives. */
+
+/* Largest B * max_rows of oil_token_logprobs. */
+#define OIL_LOGITS_MAX_ROWS (1 << 23)
+
+/* Workspace bytes of oil_token_logprobs; 0 for arguments it refuses. */
+size_t oil_token_logprobs_workspace_bytes(int32_t B, int64_t max_rows, int32_t vocab, int32_t dtype, int32_t top);
+
+/* Log probabilities.  Of every row x of logits, with log p = x - log sum exp x:
+ *   logits     B x max_rows rows of vocab values, dtype OIL_F32 or OIL_BF16, ld >= vocab
+ *              elements apart (B * max_rows * ld <= 2^60), requests max_rows * ld apart;
+ *              aligned to their type.  -inf marks tokens that may not follow.
+ *   n_rows     B int32 or NULL: the rows of each request from n_rows[b] on are not read and
+ *              give what a row of -inf gives.
+ *   tokens     B x max_rows x n_tokens int32 (n_tokens >= 0; NULL with 0).
+ *   top        0 .. OIL_MAX_K.
+ *   workspace  >= oil_token_logprobs_workspace_bytes(...), 256-byte aligned.
+ *   logprob    B x max_rows x n_tokens float32: log p of the given tokens, -inf for an id
+ *              outside [0, vocab).
+ *   entropy    B x max_rows float32 or NULL: -sum p log p.
+ *   top_tokens, top_logprobs  B x max_rows x top: the largest logits' tokens, ties to the
+ *              lower token, and their log p; -1 and -inf past the tokens above -inf.
+ * A row of -inf alone gives -inf, entropy 0 and no alternatives.  A row that holds NaN or
+ * +inf gives NaN (its alternatives are ranked all the same, NaN never among them).
+ * Sums are binary32 of terms relative to the row's largest logit. */
+int32_t oil_token_logprobs(int32_t B, int64_t max_rows, const int32_t *n_rows, const void *logits, int32_t dtype,
+                           int32_t vocab, int64_t ld, const int32_t *tokens, int32_t n_tokens, int32_t top,
+                           void *workspace, size_t workspace_bytes, float *logprob, float *entropy,
+                           int32_t *top_tokens, float *top_logprobs, void *stream);
 
 /* Benchmark instrumentation (host; not thread-safe).  While enabled, the
  * pool scans of oil_pool_query_topk calls on non-empty pools are counted

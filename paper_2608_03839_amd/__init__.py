@@ -11,7 +11,9 @@ Entry points carry the names of the C calls without their ``oil_`` prefix:
 ``pool_create``, ``pool_append``, ``pool_size``, ``query_workspace_bytes``,
 ``pool_query_topk``, ``gather_continuations``, ``tree_merge``; ``Pool`` bundles
 a pool's buffers and handle, ``RecyclePool`` those of the rejected-branch ring
-and ``KvCache`` those of the verifier's 4-bit key/value cache.
+and ``KvCache`` those of the verifier's 4-bit key/value cache.  ``prompt_attend`` and
+``prompt_weigh`` take whole prompts before they enter a cache, ``token_logprobs``
+what the verifier answers.
 """
 from __future__ import annotations
 
@@ -32,6 +34,7 @@ LEX_MAX_HIST = 1 << 20
 SCORE_ROOM_MAX = 2 << 30
 REC_DEPTH, REC_MAX_OUT = 6, 8
 KV_MAX_DIM, KV_MAX_HEADS, KV_MAX_GROUP = 128, 256, 64
+PROMPT_MAX_ROWS, PROMPT_MAX_LD, LOGITS_MAX_ROWS = 1 << 28, 1 << 24, 1 << 23
 
 _lib = None
 
@@ -114,6 +117,11 @@ def lib():
             "oil_kv_destroy": (i32, [P]),
             "oil_kv_reset": (i32, [P, P, i32, P]),
             "oil_kv_append": (i32, [P, P, i32, P, P, i32, i64, i32, P, P, P, P]),
+            "oil_kv_append_packed": (i32, [P, P, i32, P, i64, P, P, i32, i64, P, P]),
+            "oil_prompt_attend": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, ctypes.c_float, P, P, P]),
+            "oil_prompt_weigh": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, i64, ctypes.c_float, P, P]),
+            "oil_token_logprobs_workspace_bytes": (sz, [i32, i64, i32, i32, i32]),
+            "oil_token_logprobs": (i32, [i32, i64, P, P, i32, i32, i64, P, i32, i32, P, sz, P, P, P, P, P]),
             "oil_kv_read": (i32, [P, P, i32, i64, i64, P, P, i32, P]),
             "oil_kv_attend_workspace_bytes": (sz, [P, i32, i32, i32]),
             "oil_kv_attend": (i32, [P, P, i32, P, i64, i32, P, P, i64, P, P, i32, ctypes.c_float, P, sz, P, P,
@@ -207,6 +215,46 @@ def _row_stride(t, name, index):
     if B > 1 and t.stride(0) != N * ld:
         raise ValueError(f"{name}: requests must be as far apart as their rows")
     return ld
+
+
+def _packed_stride(t, name, index):
+    """Elements between consecutive rows of a (rows, heads, dim) tensor on device ``index``
+    whose rows are dense."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be (rows, heads, dim), got {tuple(t.shape)}")
+    if t.get_device() != index:
+        _elsewhere(t, name, index)
+    T, H, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: the heads of a row must be dense")
+    return t.stride(0) if T > 1 else H * D
+
+
+def _stream_on(stream, index):
+    """The stream's handle: torch's current one of device ``index`` by default."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    if stream.device.index != index:
+        raise ValueError(f"the stream must be on cuda:{index}, got {stream.device}")
+    return stream.cuda_stream
+
+
+def _call_on(index, name, *args):
+    """The C call with device ``index`` current, which launches go to."""
+    call = getattr(lib(), name)
+    if torch._C._cuda_getDevice() == index:
+        status = call(*args)
+    else:
+        with torch.cuda.device(index):
+            status = call(*args)
+    _check(name, status)
+
+
+def _device_of(t, name):
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name} must be on a device, got {t.device}")
+    return index
 
 
 # ---------------------------------------------------------------- C calls
@@ -355,6 +403,99 @@ def accept_walk(node_token, node_parent, n_nodes, target, out=None, stream=None)
         _ptr(_i32(n_nodes, "n_nodes")), _ptr(_i32(target, "target")), _ptr(al), _ptr(an), _ptr(bo),
         _stream(stream)))
     return al, an, bo
+
+
+def _prompt(q, k, v, starts):
+    """(device, T, Hq, D, q's stride, H, k's stride, B) of packed rows of queries, keys and values."""
+    index = _device_of(q, "q")
+    q_ld, ld = _packed_stride(q, "q", index), _packed_stride(k, "k", index)
+    T, Hq, D = q.shape
+    if k.shape[0] != T or k.shape[2] != D:
+        raise ValueError(f"k must be ({T}, heads, {D}), got {tuple(k.shape)}")
+    if v is not None and (v.shape != k.shape or _packed_stride(v, "v", index) != ld):
+        raise ValueError("k and v must have the same shape and strides")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if t is not None and t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
+    return index, T, Hq, D, q_ld, k.shape[1], ld, starts.numel() - 1
+
+
+def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None):
+    """Causal attention of packed prompts.  ``q`` (T, Hq, D), ``k`` and ``v`` (T, H, D)
+    bfloat16, whose rows may be slices of a fused projection's; ``starts`` (B + 1,) int32:
+    sequence b has rows starts[b] .. starts[b + 1] - 1, and query head a reads head
+    a / (Hq / H).  Returns (out (T, Hq, D) bfloat16, lse (T, Hq) float32); rows of no
+    sequence are left as they were."""
+    index, T, Hq, D, q_ld, H, ld, B = _prompt(q, k, v, starts)
+    on = _stream_on(stream, index)
+    if out is None:
+        out = (_empty((T, Hq, D), torch.bfloat16, q.device, stream), _empty((T, Hq), torch.float32, q.device, stream))
+    o, lse = out
+    _call_on(index, "oil_prompt_attend", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
+             q_ld, Hq, k.data_ptr(), v.data_ptr(), ld, H, D, 1.0 / math.sqrt(D) if scale is None else scale,
+             _shaped(o, "out", (T, Hq, D), torch.bfloat16, index),
+             _shaped(lse, "lse", (T, Hq), torch.float32, index), on)
+    return o, lse
+
+
+def prompt_weigh(q, k, lse, starts, last=None, scale=None, stream=None, out=None):
+    """The attention weight that each position of packed prompts received from the last
+    ``last`` rows (None: all) of its sequence: (H, T) float32, what append's ``weight``
+    takes.  ``lse`` as prompt_attend returned it, the others as it took them."""
+    index, T, Hq, D, q_ld, H, ld, B = _prompt(q, k, None, starts)
+    on = _stream_on(stream, index)
+    if out is None:
+        out = _empty((H, T), torch.float32, q.device, stream)
+    _call_on(index, "oil_prompt_weigh", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
+             q_ld, Hq, _shaped(lse, "lse", (T, Hq), torch.float32, index), k.data_ptr(), ld, H, D,
+             T if last is None else last, 1.0 / math.sqrt(D) if scale is None else scale,
+             _shaped(out, "out", (H, T), torch.float32, index), on)
+    return out
+
+
+def token_logprobs(logits, tokens=None, top=0, n_rows=None, stream=None, out=None, workspace=None):
+    """Log probabilities from rows of logits (B, N, V), float32 or bfloat16: (logprob
+    (B, N, M) of the given ``tokens`` (B, N, M) int32, or None without; entropy (B, N);
+    the ``top`` most likely tokens (B, N, top) int32, ties to the lower one; their log
+    probabilities).  ``n_rows`` (B,) int32: the rows that count; the others give -inf,
+    0, -1 and -inf.  A token outside the vocabulary has -inf."""
+    index = _device_of(logits, "logits")
+    if logits.dim() != 3:
+        raise ValueError(f"logits must be (requests, rows, vocabulary), got {tuple(logits.shape)}")
+    B, N, V = logits.shape
+    if V > 1 and logits.stride(2) != 1:
+        raise ValueError("logits: a row must be dense")
+    ld = logits.stride(1) if N > 1 else logits.stride(0) if B > 1 else V
+    if B > 1 and logits.stride(0) != N * ld:
+        raise ValueError("logits: requests must be as far apart as their rows")
+    on, f32, i32 = _stream_on(stream, index), torch.float32, torch.int32
+    M = 0
+    if tokens is not None:
+        if tokens.dim() != 3:
+            raise ValueError(f"tokens must be (requests, rows, tokens), got {tuple(tokens.shape)}")
+        M = tokens.shape[2]
+    if out is None:
+        dev = logits.device
+        out = (None if tokens is None else _empty((B, N, M), f32, dev, stream), _empty((B, N), f32, dev, stream),
+               _empty((B, N, top), i32, dev, stream), _empty((B, N, top), f32, dev, stream))
+    logprob, entropy, top_tokens, top_logprobs = out
+    code = _dtype_code(logits)
+    nbytes = lib().oil_token_logprobs_workspace_bytes(B, N, V, code, top)
+    if nbytes == 0:
+        raise ValueError(f"unsupported logits: {tuple(logits.shape)} top={top}")
+    if workspace is None:
+        workspace = _empty((nbytes,), torch.uint8, logits.device, stream)
+    elif workspace.get_device() != index:
+        _elsewhere(workspace, "workspace", index)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be dense")
+    _call_on(index, "oil_token_logprobs", B, N, _shaped(n_rows, "n_rows", (B,), i32, index), logits.data_ptr(), code, V,
+             ld, _shaped(tokens, "tokens", (B, N, M), i32, index), M, top, workspace.data_ptr(),
+             workspace.numel() * workspace.element_size(), _shaped(logprob, "logprob", (B, N, M), f32, index),
+             _shaped(entropy, "entropy", (B, N), f32, index),
+             _shaped(top_tokens, "top_tokens", (B, N, top), i32, index),
+             _shaped(top_logprobs, "top_logprobs", (B, N, top), f32, index), on)
+    return out
 
 
 def read_stream(buf, sink, stream=None):
@@ -645,13 +786,7 @@ class KvCache:
 
     def _call(self, name, *args):
         """The C call with the cache's device current, which launches go to."""
-        call = getattr(lib(), name)
-        if torch._C._cuda_getDevice() == self._index:
-            status = call(*args)
-        else:
-            with torch.cuda.device(self._index):
-                status = call(*args)
-        _check(name, status)
+        _call_on(self._index, name, *args)
 
     def _workspace(self, stream, on, given, call, *sizes):
         """Address and bytes of the workspace of a call of these sizes on the stream ``on``:
@@ -674,11 +809,7 @@ class KvCache:
 
     def _on(self, stream):
         """The stream's handle: torch's current one of the cache's device by default."""
-        if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self._index)
-        if stream.device.index != self._index:
-            raise ValueError(f"the stream must be on cuda:{self._index}, got {stream.device}")
-        return stream.cuda_stream
+        return _stream_on(stream, self._index)
 
     def _heads(self, t, name):
         if t.dim() != 4 or t.shape[3] != self.head_dim:
@@ -700,10 +831,16 @@ class KvCache:
         self._call("oil_kv_reset", self.handle, _shaped(slots, "slots", (B,), torch.int32, self._index), B,
                    self._on(stream))
 
-    def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None):
+    def append(self, k, v, nodes=None, count=None, weight=None, slots=None, stream=None, starts=None):
         """Append rows of k, v (B, N, n_heads, head_dim), float32 or bfloat16: all
         of them, the first ``count`` (B,), or with ``nodes`` (B, N) the root and the
-        accepted nodes as accept_walk returns them; ``weight`` (B, n_heads, N)."""
+        accepted nodes as accept_walk returns them; ``weight`` (B, n_heads, N).
+
+        With ``starts`` (B + 1,) int32, packed sequences: k, v (T, n_heads, head_dim),
+        request b's rows starts[b] .. starts[b + 1] - 1 of them; ``weight`` (n_heads, T)
+        as prompt_weigh returns it."""
+        if starts is not None:
+            return self._append_packed(k, v, nodes, count, weight, slots, stream, starts)
         ld = self._own_rows(k, v, "append")
         B, N = k.shape[:2]
         on, i, i32 = self._on(stream), self._index, torch.int32
@@ -711,6 +848,21 @@ class KvCache:
                    _dtype_code(k), ld, N, _shaped(nodes, "nodes", (B, N), i32, i),
                    _shaped(count, "count", (B,), i32, i),
                    _shaped(weight, "weight", (B, self.n_heads, N), torch.float32, i), on)
+
+    def _append_packed(self, k, v, nodes, count, weight, slots, stream, starts):
+        if nodes is not None or count is not None:
+            raise ValueError("append: packed sequences take neither nodes nor count")
+        i, i32 = self._index, torch.int32
+        if k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (self.n_heads, self.head_dim):
+            raise ValueError(f"append: packed k and v must be alike, (rows, {self.n_heads}, {self.head_dim})")
+        ld = _packed_stride(k, "k", i)
+        if _packed_stride(v, "v", i) != ld:
+            raise ValueError("append: k and v must have the same strides")
+        T, B = k.shape[0], starts.numel() - 1
+        on = self._on(stream)
+        self._call("oil_kv_append_packed", self.handle, _shaped(slots, "slots", (B,), i32, i), B,
+                   _shaped(starts, "starts", (B + 1,), i32, i), T, k.data_ptr(), v.data_ptr(), _dtype_code(k), ld,
+                   _shaped(weight, "weight", (self.n_heads, T), torch.float32, i), on)
 
     def read(self, first, n, B=None, slots=None, dtype=torch.bfloat16, stream=None, out=None):
         """Rows first .. first + n - 1 as the values they stand for: (k, v), each

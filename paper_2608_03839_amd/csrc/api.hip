@@ -757,6 +757,21 @@ int32_t oil_kv_append(oil_kv* kv, const int32_t* slots, int32_t B, const void* k
                                             (hipStream_t)stream));
 }
 
+int32_t oil_kv_append_packed(oil_kv* kv, const int32_t* slots, int32_t B, const int32_t* starts, int64_t total,
+                             const void* k, const void* v, int32_t dtype, int64_t ld, const float* weight,
+                             void* stream)
+{
+    if (!kv || B < 1 || B > kv->c.n_slots || !starts || total < 1 || !k || !v ||
+        (dtype != OIL_F32 && dtype != OIL_BF16) || !aligned(k, 16) || !aligned(v, 16))
+        return OIL_E_INVALID;
+    if (total > OIL_PROMPT_MAX_ROWS)
+        return OIL_E_UNSUPPORTED;
+    if (!kv_ld_fits(ld, (int64_t)kv->c.H * kv->c.D, 1, (int32_t)total))
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_kv_append_packed(kv->c, slots, B, starts, (int32_t)total, k, v, dtype, ld, weight,
+                                                   (hipStream_t)stream));
+}
+
 int32_t oil_kv_read(const oil_kv* kv, const int32_t* slots, int32_t B, int64_t first, int64_t n, void* k_out,
                     void* v_out, int32_t dtype, void* stream)
 {
@@ -836,6 +851,91 @@ int32_t oil_kv_evict(oil_kv* kv, const int32_t* slots, int32_t B, int64_t keep, 
         workspace_bytes < oil::kv_evict_workspace_bytes(kv->c, B, keep))
         return OIL_E_WORKSPACE;
     return hip_status(oil::launch_kv_evict(kv->c, slots, B, keep, recent, workspace, (hipStream_t)stream));
+}
+
+// ---- packed prompts
+
+// Checks shared by the calls on packed rows of queries and keys.
+static int32_t prompt_status(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
+                             int32_t n_q_heads, const void* k, int64_t ld, int32_t n_heads, int32_t head_dim,
+                             float scale)
+{
+    if (!starts || B < 1 || total < 1 || !q || !k || n_heads < 1 || n_q_heads < 1 || n_q_heads % n_heads != 0 ||
+        head_dim < 1 || head_dim % 8 != 0 || !isfinite(scale) || !aligned(q, 16) || !aligned(k, 16))
+        return OIL_E_INVALID;
+    if (B > OIL_MAX_B || total > OIL_PROMPT_MAX_ROWS || n_heads > OIL_KV_MAX_HEADS || head_dim > OIL_KV_MAX_DIM ||
+        n_q_heads / n_heads > OIL_KV_MAX_GROUP || total > ((int64_t)1 << 30) / n_q_heads)
+        return OIL_E_UNSUPPORTED;
+    if (!kv_ld_fits(q_ld, (int64_t)n_q_heads * head_dim, 1, (int32_t)total) ||
+        !kv_ld_fits(ld, (int64_t)n_heads * head_dim, 1, (int32_t)total))
+        return OIL_E_INVALID;
+    return q_ld > OIL_PROMPT_MAX_LD || ld > OIL_PROMPT_MAX_LD ? OIL_E_UNSUPPORTED : OIL_OK;
+}
+
+int32_t oil_prompt_attend(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
+                          int32_t n_q_heads, const void* k, const void* v, int64_t ld, int32_t n_heads,
+                          int32_t head_dim, float scale, void* out, float* lse, void* stream)
+{
+    const int32_t st = prompt_status(starts, B, total, q, q_ld, n_q_heads, k, ld, n_heads, head_dim, scale);
+    if (st != OIL_OK)
+        return st;
+    if (!v || !out || !aligned(v, 16) || !aligned(out, 16))
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_prompt_attend(starts, B, (int32_t)total, q, q_ld, n_q_heads, k, v, ld, n_heads,
+                                                head_dim, scale, out, lse, (hipStream_t)stream));
+}
+
+int32_t oil_prompt_weigh(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
+                         int32_t n_q_heads, const float* lse, const void* k, int64_t ld, int32_t n_heads,
+                         int32_t head_dim, int64_t last, float scale, float* weight, void* stream)
+{
+    const int32_t st = prompt_status(starts, B, total, q, q_ld, n_q_heads, k, ld, n_heads, head_dim, scale);
+    if (st != OIL_OK)
+        return st;
+    if (!lse || !weight || last < 1)
+        return OIL_E_INVALID;
+    return hip_status(oil::launch_prompt_weigh(starts, B, (int32_t)total, q, q_ld, n_q_heads, lse, k, ld, n_heads,
+                                               head_dim, (int32_t)(last < total ? last : total), scale, weight,
+                                               (hipStream_t)stream));
+}
+
+// ---- log probabilities
+
+// Checks of a call's sizes.
+static int32_t logprobs_status(int32_t B, int64_t max_rows, int32_t vocab, int32_t dtype, int32_t top)
+{
+    if (B < 1 || max_rows < 1 || vocab < 1 || (dtype != OIL_F32 && dtype != OIL_BF16) || top < 0)
+        return OIL_E_INVALID;
+    if (top > OIL_MAX_K || max_rows > OIL_LOGITS_MAX_ROWS / B)
+        return OIL_E_UNSUPPORTED;
+    return OIL_OK;
+}
+
+size_t oil_token_logprobs_workspace_bytes(int32_t B, int64_t max_rows, int32_t vocab, int32_t dtype, int32_t top)
+{
+    if (logprobs_status(B, max_rows, vocab, dtype, top) != OIL_OK)
+        return 0;
+    return oil::logprobs_workspace_bytes(B * max_rows, vocab, dtype, top);
+}
+
+int32_t oil_token_logprobs(int32_t B, int64_t max_rows, const int32_t* n_rows, const void* logits, int32_t dtype,
+                           int32_t vocab, int64_t ld, const int32_t* tokens, int32_t n_tokens, int32_t top,
+                           void* workspace, size_t workspace_bytes, float* logprob, float* entropy,
+                           int32_t* top_tokens, float* top_logprobs, void* stream)
+{
+    const int32_t st = logprobs_status(B, max_rows, vocab, dtype, top);
+    if (st != OIL_OK)
+        return st;
+    if (!logits || !aligned(logits, dtype == OIL_F32 ? 4 : 2) || ld < vocab ||
+        ld > ((int64_t)1 << 60) / (B * max_rows) || n_tokens < 0 || (n_tokens > 0 && (!tokens || !logprob)) ||
+        (top > 0 && (!top_tokens || !top_logprobs)))
+        return OIL_E_INVALID;
+    if (!workspace || !aligned(workspace, kAlign) ||
+        workspace_bytes < oil::logprobs_workspace_bytes(B * max_rows, vocab, dtype, top))
+        return OIL_E_WORKSPACE;
+    return hip_status(oil::launch_logprobs(B * max_rows, (int32_t)max_rows, n_rows, logits, dtype, vocab, ld, tokens,
+                                           n_tokens, top, workspace, logprob, entropy, top_tokens, top_logprobs,
+                                           (hipStream_t)stream));
 }
 
 const char* oil_status_string(int32_t status)

@@ -81,6 +81,20 @@ __device__ __forceinline__ float code_score(uint32_t c)
     return __uint_as_float(b);
 }
 
+// Packed sequences: sequence s has rows seq_first .. seq_end of total, whatever starts
+// holds (it ascends where the caller keeps to the contract).
+__device__ __forceinline__ int seq_first(const int32_t* starts, int32_t total, int s)
+{
+    const int a = starts[s];
+    return a < 0 ? 0 : a > total ? total : a;
+}
+
+__device__ __forceinline__ int seq_end(const int32_t* starts, int32_t total, int s)
+{
+    const int a = seq_first(starts, total, s), z = starts[s + 1];
+    return z < a ? a : z > total ? total : z;
+}
+
 constexpr uint32_t kNoScoreBits = 0xFFFFFFFFu;
 
 // Total order key of a (score, position) pair: score descending, then

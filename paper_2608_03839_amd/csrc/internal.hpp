@@ -155,6 +155,9 @@ hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hip
 hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, const void* k, const void* v,
                             int dtype, int64_t ld, int32_t max_rows, const int32_t* nodes, const int32_t* count,
                             const float* weight, hipStream_t stream);
+hipError_t launch_kv_append_packed(const KvView& c, const int32_t* slots, int32_t B, const int32_t* starts,
+                                   int32_t total, const void* k, const void* v, int dtype, int64_t ld,
+                                   const float* weight, hipStream_t stream);
 hipError_t launch_kv_read(const KvView& c, const int32_t* slots, int32_t B, int64_t first, int64_t n, void* k_out,
                           void* v_out, int dtype, hipStream_t stream);
 size_t kv_attend_workspace_bytes(const KvView& c, int32_t B, int32_t max_nodes, int32_t Hq);
@@ -168,5 +171,20 @@ hipError_t launch_kv_weigh(const KvView& c, const int32_t* slots, int32_t B, con
 size_t kv_evict_workspace_bytes(const KvView& c, int32_t B, int64_t keep);
 hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int64_t keep, int64_t recent,
                            void* workspace, hipStream_t stream);
+
+// Packed prompts (prompt.hip).
+hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
+                                const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale, void* out,
+                                float* lse, hipStream_t stream);
+hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
+                               const float* lse, const void* k, int64_t ld, int32_t H, int32_t D, int32_t last,
+                               float scale, float* weight, hipStream_t stream);
+
+// Log probabilities (logits.hip).
+size_t logprobs_workspace_bytes(int64_t rows, int32_t V, int dtype, int32_t k);
+hipError_t launch_logprobs(int64_t rows, int32_t max_rows, const int32_t* n_rows, const void* logits, int dtype,
+                           int32_t V, int64_t ld, const int32_t* tokens, int32_t M, int32_t k, void* workspace,
+                           float* logprob, float* entropy, int32_t* top_tokens, float* top_logprobs,
+                           hipStream_t stream);
 
 }  // namespace oil

@@ -83,17 +83,20 @@ __device__ __forceinline__ void kv_advance(const KvView& c, int slot, int32_t le
     st[kKvNext] = next < INT32_MAX ? (int32_t)next : INT32_MAX;
 }
 
-// The state after an append (rows of max_rows, nodes, count) or, with max_rows
-// 0, a reset; one workgroup per request.
+// The state after an append (rows of max_rows, nodes, count; or of packed sequences,
+// with starts) or, with max_rows 0, a reset; one workgroup per request.
 __global__ __launch_bounds__(64) void kv_state_kernel(KvView c, const int32_t* __restrict__ slots, int32_t max_rows,
                                                       const int32_t* __restrict__ nodes,
-                                                      const int32_t* __restrict__ count)
+                                                      const int32_t* __restrict__ count,
+                                                      const int32_t* __restrict__ starts)
 {
     __shared__ int bound;
     const int b = blockIdx.x, slot = kv_slot(c, slots, b);
     if (slot < 0)
         return;
-    const int cnt = max_rows ? kv_count(nodes, count, b, max_rows, &bound) : 0;
+    const int cnt = starts     ? seq_end(starts, max_rows, b) - seq_first(starts, max_rows, b)
+                    : max_rows ? kv_count(nodes, count, b, max_rows, &bound)
+                               : 0;
     if (threadIdx.x != 0)
         return;
     if (max_rows)
@@ -204,34 +207,61 @@ struct KvRowRegs {
     }
 };
 
+// Packed sequences: the place of a request's first workgroup.  It has at least as many
+// as its n rows touch tiles, n / 32 + 2 whatever the slot's length, and the places
+// ascend without a sum over the requests.
+__device__ __forceinline__ int64_t kv_packed_place(const int32_t* starts, int32_t total, int b)
+{
+    return seq_first(starts, total, b) / kKvTile + 2ll * b;
+}
+
+// kPacked: `starts` tells the rows of each of the B requests (oil_kv_append_packed), of
+// max_rows in all; a workgroup finds its request by bisection and has one tile.
 // (Six workgroups a CU: 4 x 8,191 rows in bf16 37 us, at five 39, at four 42; at
 // eight, or six with binary32 rows, registers spill.)
-template <int W, typename T>
+template <int W, typename T, bool kPacked>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 6 : 5) void kv_append_kernel(KvView c, const int32_t* __restrict__ slots,
                                                         const T* __restrict__ k, const T* __restrict__ v, int64_t ld,
                                                         int32_t max_rows, const int32_t* __restrict__ nodes,
                                                         const int32_t* __restrict__ count,
-                                                        const float* __restrict__ weight)
+                                                        const float* __restrict__ weight,
+                                                        const int32_t* __restrict__ starts, int32_t B)
 {
     constexpr int kRow = W / 4 + 1;  // dwords of a row of value codes in LDS
     __shared__ __align__(16) uint32_t image[2 * KvTile<W>::kWords];  // the tile's codes as they are stored
     __shared__ uint32_t vcode[kKvTile][kRow];
     __shared__ int bound;
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+    const int h = blockIdx.y, tid = threadIdx.x;
+    int b = blockIdx.z;
+    int64_t turn = blockIdx.x;
+    if (kPacked) {
+        int past = B;
+        while (past - b > 1) {
+            const int mid = b + (past - b) / 2;
+            if (kv_packed_place(starts, max_rows, mid) <= turn)
+                b = mid;
+            else
+                past = mid;
+        }
+        turn -= kv_packed_place(starts, max_rows, b);
+        if (turn < 0)
+            return;
+    }
     const int slot = kv_slot(c, slots, b);
     if (slot < 0)
         return;
     const int32_t len = kv_len(c, slot), next = c.state[4 * (int64_t)slot + kKvNext];
-    const int cnt = kv_count(nodes, count, b, max_rows, &bound);
+    const int row0 = kPacked ? seq_first(starts, max_rows, b) : 0;
+    const int cnt = kPacked ? seq_end(starts, max_rows, b) - row0 : kv_count(nodes, count, b, max_rows, &bound);
     const int64_t end = len + (int64_t)cnt < c.cap ? len + (int64_t)cnt : c.cap;
-    for (int64_t first = (len / kKvTile + (int64_t)blockIdx.x) * kKvTile; first < end;
+    for (int64_t first = (len / kKvTile + turn) * kKvTile; first < end;
          first += (int64_t)gridDim.x * kKvTile) {  // of the tile
         uint8_t* tile = kv_tiles(c, slot, h) + first / kKvTile * c.tile_bytes;
         const int key = tid >> 3, part = tid & 7;
         const int64_t j = first + key;
         if (j >= len && j < end) {  // the 8 lanes of a row alike
-            const int r = (int)(j - len), src = kv_source(nodes, b, max_rows, r);
-            const int64_t at = ((int64_t)b * max_rows + src) * ld + (int64_t)h * c.D;
+            const int r = (int)(j - len), src = kPacked ? row0 + r : kv_source(nodes, b, max_rows, r);
+            const int64_t at = ((kPacked ? 0 : (int64_t)b * max_rows) + src) * ld + (int64_t)h * c.D;
             KvRowRegs<W, T> rows[2];
             rows[0].load(k + at, part, c.D);
             rows[1].load(v + at, part, c.D);
@@ -288,7 +318,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 6 : 5) void kv_append_kernel(
                 const int64_t at_row = kv_row(c, slot, h) + j;
                 const int64_t pos = next + (int64_t)r;
                 c.pos[at_row] = pos < INT32_MAX ? (int32_t)pos : INT32_MAX;
-                c.weight[at_row] = weight ? weight[((int64_t)b * c.H + h) * max_rows + src] : 0.f;
+                c.weight[at_row] = weight ? weight[((kPacked ? 0 : (int64_t)b * c.H) + h) * max_rows + src] : 0.f;
             }
         }
         __syncthreads();
@@ -351,8 +381,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 6 : 5) void kv_append_kernel(
             }
         }
         __syncthreads();
+        if (kPacked)
+            return;
     }
-    if (gridDim.x * gridDim.y <= kTickets && kv_last(c, slot, gridDim.x * gridDim.y) && tid == 0)
+    if (!kPacked && gridDim.x * gridDim.y <= kTickets && kv_last(c, slot, gridDim.x * gridDim.y) && tid == 0)
         kv_advance(c, slot, len, cnt);
 }
 
@@ -760,7 +792,7 @@ hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hip
     const int64_t blocks = (c.cap + 4095) / 4096 < 64 ? (c.cap + 4095) / 4096 : 64;
     hipLaunchKernelGGL(kv_reset_kernel, dim3((unsigned)blocks, c.H, B), dim3(256), 0, stream, c, slots);
     if (blocks * c.H > kTickets)
-        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, 0, nullptr, nullptr);
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, 0, nullptr, nullptr, nullptr);
     return hipGetLastError();
 }
 
@@ -773,8 +805,8 @@ hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, co
     tiles = tiles < c.tiles ? tiles : c.tiles;
     const dim3 grid((unsigned)(tiles < kMaxGridTiles ? tiles : kMaxGridTiles), c.H, B), block(256);
 #define OIL_KV_APPEND(W, T)                                                                                       \
-    hipLaunchKernelGGL((kv_append_kernel<W, T>), grid, block, 0, stream, c, slots, (const T*)k, (const T*)v, ld, \
-                       max_rows, nodes, count, weight)
+    hipLaunchKernelGGL((kv_append_kernel<W, T, false>), grid, block, 0, stream, c, slots, (const T*)k, (const T*)v, \
+                       ld, max_rows, nodes, count, weight, nullptr, 0)
     if (c.W == 64 && dtype == 0)
         OIL_KV_APPEND(64, float);
     else if (c.W == 64)
@@ -785,7 +817,28 @@ hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, co
         OIL_KV_APPEND(128, uint16_t);
 #undef OIL_KV_APPEND
     if ((int64_t)grid.x * c.H > kTickets)
-        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, max_rows, nodes, count);
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, max_rows, nodes, count, nullptr);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_append_packed(const KvView& c, const int32_t* slots, int32_t B, const int32_t* starts,
+                                   int32_t total, const void* k, const void* v, int dtype, int64_t ld,
+                                   const float* weight, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(total / kKvTile + 2ll * B), c.H), block(256);
+#define OIL_KV_APPEND(W, T)                                                                                      \
+    hipLaunchKernelGGL((kv_append_kernel<W, T, true>), grid, block, 0, stream, c, slots, (const T*)k, (const T*)v, \
+                       ld, total, nullptr, nullptr, weight, starts, B)
+    if (c.W == 64 && dtype == 0)
+        OIL_KV_APPEND(64, float);
+    else if (c.W == 64)
+        OIL_KV_APPEND(64, uint16_t);
+    else if (dtype == 0)
+        OIL_KV_APPEND(128, float);
+    else
+        OIL_KV_APPEND(128, uint16_t);
+#undef OIL_KV_APPEND
+    hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, total, nullptr, nullptr, starts);
     return hipGetLastError();
 }
 
