@@ -590,9 +590,14 @@ int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, 
  *   n_heads    1 .. OIL_KV_MAX_HEADS.   n_q_heads  a multiple of it, at most
  *              OIL_KV_MAX_GROUP times.   head_dim  a multiple of 8, 8 .. OIL_KV_MAX_DIM.
  *   scale      finite.
+ *   workspace  >= oil_prompt_workspace_bytes(...), 256-byte aligned; calls on one stream may
+ *              share it.
  * Rows outside every sequence are neither read nor written. */
 #define OIL_PROMPT_MAX_ROWS (1 << 28)
 #define OIL_PROMPT_MAX_LD (1 << 24)
+
+/* Workspace bytes of the two calls; 0 for arguments they refuse. */
+size_t oil_prompt_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads);
 
 /* Causal attention of packed sequences.  Query head a reads key/value head
  * a / (n_q_heads / n_heads); row i sees the rows of its sequence up to its own:
@@ -606,7 +611,8 @@ int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, 
  * step is 2^-8 of each; the sum that divides is of unrounded ones), and out. */
 int32_t oil_prompt_attend(const int32_t *starts, int32_t B, int64_t total, const void *q, int64_t q_ld,
                           int32_t n_q_heads, const void *k, const void *v, int64_t ld, int32_t n_heads,
-                          int32_t head_dim, float scale, void *out, float *lse, void *stream);
+                          int32_t head_dim, float scale, void *workspace, size_t workspace_bytes, void *out,
+                          float *lse, void *stream);
 
 /* The attention weight that positions received from the last `last` rows of their
  * sequence (all of them where last is at least its length):
@@ -618,7 +624,8 @@ int32_t oil_prompt_attend(const int32_t *starts, int32_t B, int64_t total, const
  * Sums are binary32, each added up by one workgroup in one order. */
 int32_t oil_prompt_weigh(const int32_t *starts, int32_t B, int64_t total, const void *q, int64_t q_ld,
                          int32_t n_q_heads, const float *lse, const void *k, int64_t ld, int32_t n_heads,
-                         int32_t head_dim, int64_t last, float scale, float *weight, void *stream);
+                         int32_t head_dim, int64_t last, float scale, void *workspace, size_t workspace_bytes,
+                         float *weight, void *stream);
 
 /* ---- What a verifier's rows of logits say: the predictions that oil_accept_walk takes
  * (top_tokens with top = 1), the log probabilities of drafted tokens, alternatives. */

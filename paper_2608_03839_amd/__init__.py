@@ -118,8 +118,10 @@ def lib():
             "oil_kv_reset": (i32, [P, P, i32, P]),
             "oil_kv_append": (i32, [P, P, i32, P, P, i32, i64, i32, P, P, P, P]),
             "oil_kv_append_packed": (i32, [P, P, i32, P, i64, P, P, i32, i64, P, P]),
-            "oil_prompt_attend": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, ctypes.c_float, P, P, P]),
-            "oil_prompt_weigh": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, i64, ctypes.c_float, P, P]),
+            "oil_prompt_workspace_bytes": (sz, [i32, i64, i32, i32]),
+            "oil_prompt_attend": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, ctypes.c_float, P, sz, P, P, P]),
+            "oil_prompt_weigh": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, i64, ctypes.c_float, P, sz, P,
+                                       P]),
             "oil_token_logprobs_workspace_bytes": (sz, [i32, i64, i32, i32, i32]),
             "oil_token_logprobs": (i32, [i32, i64, P, P, i32, i32, i64, P, i32, i32, P, sz, P, P, P, P, P]),
             "oil_kv_read": (i32, [P, P, i32, i64, i64, P, P, i32, P]),
@@ -420,7 +422,18 @@ def _prompt(q, k, v, starts):
     return index, T, Hq, D, q_ld, k.shape[1], ld, starts.numel() - 1
 
 
-def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None):
+def _given_or_new(workspace, nbytes, index, device, stream):
+    """A call's workspace: the one given, or torch's memory on the call's stream."""
+    if workspace is None:
+        return _empty((nbytes,), torch.uint8, device, stream)
+    if workspace.get_device() != index:
+        _elsewhere(workspace, "workspace", index)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be dense")
+    return workspace
+
+
+def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None, workspace=None):
     """Causal attention of packed prompts.  ``q`` (T, Hq, D), ``k`` and ``v`` (T, H, D)
     bfloat16, whose rows may be slices of a fused projection's; ``starts`` (B + 1,) int32:
     sequence b has rows starts[b] .. starts[b + 1] - 1, and query head a reads head
@@ -431,14 +444,16 @@ def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None):
     if out is None:
         out = (_empty((T, Hq, D), torch.bfloat16, q.device, stream), _empty((T, Hq), torch.float32, q.device, stream))
     o, lse = out
+    ws = _given_or_new(workspace, lib().oil_prompt_workspace_bytes(B, T, Hq, H), index, q.device, stream)
     _call_on(index, "oil_prompt_attend", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
              q_ld, Hq, k.data_ptr(), v.data_ptr(), ld, H, D, 1.0 / math.sqrt(D) if scale is None else scale,
+             ws.data_ptr(), ws.numel() * ws.element_size(),
              _shaped(o, "out", (T, Hq, D), torch.bfloat16, index),
              _shaped(lse, "lse", (T, Hq), torch.float32, index), on)
     return o, lse
 
 
-def prompt_weigh(q, k, lse, starts, last=None, scale=None, stream=None, out=None):
+def prompt_weigh(q, k, lse, starts, last=None, scale=None, stream=None, out=None, workspace=None):
     """The attention weight that each position of packed prompts received from the last
     ``last`` rows (None: all) of its sequence: (H, T) float32, what append's ``weight``
     takes.  ``lse`` as prompt_attend returned it, the others as it took them."""
@@ -446,10 +461,11 @@ def prompt_weigh(q, k, lse, starts, last=None, scale=None, stream=None, out=None
     on = _stream_on(stream, index)
     if out is None:
         out = _empty((H, T), torch.float32, q.device, stream)
+    ws = _given_or_new(workspace, lib().oil_prompt_workspace_bytes(B, T, Hq, H), index, q.device, stream)
     _call_on(index, "oil_prompt_weigh", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
              q_ld, Hq, _shaped(lse, "lse", (T, Hq), torch.float32, index), k.data_ptr(), ld, H, D,
-             T if last is None else last, 1.0 / math.sqrt(D) if scale is None else scale,
-             _shaped(out, "out", (H, T), torch.float32, index), on)
+             T if last is None else last, 1.0 / math.sqrt(D) if scale is None else scale, ws.data_ptr(),
+             ws.numel() * ws.element_size(), _shaped(out, "out", (H, T), torch.float32, index), on)
     return out
 
 
@@ -483,12 +499,7 @@ def token_logprobs(logits, tokens=None, top=0, n_rows=None, stream=None, out=Non
     nbytes = lib().oil_token_logprobs_workspace_bytes(B, N, V, code, top)
     if nbytes == 0:
         raise ValueError(f"unsupported logits: {tuple(logits.shape)} top={top}")
-    if workspace is None:
-        workspace = _empty((nbytes,), torch.uint8, logits.device, stream)
-    elif workspace.get_device() != index:
-        _elsewhere(workspace, "workspace", index)
-    elif not workspace.is_contiguous():
-        raise ValueError("workspace must be dense")
+    workspace = _given_or_new(workspace, nbytes, index, logits.device, stream)
     _call_on(index, "oil_token_logprobs", B, N, _shaped(n_rows, "n_rows", (B,), i32, index), logits.data_ptr(), code, V,
              ld, _shaped(tokens, "tokens", (B, N, M), i32, index), M, top, workspace.data_ptr(),
              workspace.numel() * workspace.element_size(), _shaped(logprob, "logprob", (B, N, M), f32, index),

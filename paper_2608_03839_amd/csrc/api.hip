@@ -872,31 +872,53 @@ static int32_t prompt_status(const int32_t* starts, int32_t B, int64_t total, co
     return q_ld > OIL_PROMPT_MAX_LD || ld > OIL_PROMPT_MAX_LD ? OIL_E_UNSUPPORTED : OIL_OK;
 }
 
+size_t oil_prompt_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads)
+{
+    if (B < 1 || B > OIL_MAX_B || total < 1 || total > OIL_PROMPT_MAX_ROWS || n_heads < 1 ||
+        n_heads > OIL_KV_MAX_HEADS || n_q_heads < 1 || n_q_heads % n_heads != 0 ||
+        n_q_heads / n_heads > OIL_KV_MAX_GROUP || total > ((int64_t)1 << 30) / n_q_heads)
+        return 0;
+    return oil::prompt_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads);
+}
+
+static bool prompt_workspace_fits(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads, const void* workspace,
+                                  size_t bytes)
+{
+    return workspace && aligned(workspace, kAlign) &&
+           bytes >= oil::prompt_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads);
+}
+
 int32_t oil_prompt_attend(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
                           int32_t n_q_heads, const void* k, const void* v, int64_t ld, int32_t n_heads,
-                          int32_t head_dim, float scale, void* out, float* lse, void* stream)
+                          int32_t head_dim, float scale, void* workspace, size_t workspace_bytes, void* out,
+                          float* lse, void* stream)
 {
     const int32_t st = prompt_status(starts, B, total, q, q_ld, n_q_heads, k, ld, n_heads, head_dim, scale);
     if (st != OIL_OK)
         return st;
     if (!v || !out || !aligned(v, 16) || !aligned(out, 16))
         return OIL_E_INVALID;
+    if (!prompt_workspace_fits(B, total, n_q_heads, n_heads, workspace, workspace_bytes))
+        return OIL_E_WORKSPACE;
     return hip_status(oil::launch_prompt_attend(starts, B, (int32_t)total, q, q_ld, n_q_heads, k, v, ld, n_heads,
-                                                head_dim, scale, out, lse, (hipStream_t)stream));
+                                                head_dim, scale, workspace, out, lse, (hipStream_t)stream));
 }
 
 int32_t oil_prompt_weigh(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
                          int32_t n_q_heads, const float* lse, const void* k, int64_t ld, int32_t n_heads,
-                         int32_t head_dim, int64_t last, float scale, float* weight, void* stream)
+                         int32_t head_dim, int64_t last, float scale, void* workspace, size_t workspace_bytes,
+                         float* weight, void* stream)
 {
     const int32_t st = prompt_status(starts, B, total, q, q_ld, n_q_heads, k, ld, n_heads, head_dim, scale);
     if (st != OIL_OK)
         return st;
     if (!lse || !weight || last < 1)
         return OIL_E_INVALID;
+    if (!prompt_workspace_fits(B, total, n_q_heads, n_heads, workspace, workspace_bytes))
+        return OIL_E_WORKSPACE;
     return hip_status(oil::launch_prompt_weigh(starts, B, (int32_t)total, q, q_ld, n_q_heads, lse, k, ld, n_heads,
-                                               head_dim, (int32_t)(last < total ? last : total), scale, weight,
-                                               (hipStream_t)stream));
+                                               head_dim, (int32_t)(last < total ? last : total), scale, workspace,
+                                               weight, (hipStream_t)stream));
 }
 
 // ---- log probabilities

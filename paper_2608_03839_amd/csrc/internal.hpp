@@ -173,12 +173,13 @@ hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int
                            void* workspace, hipStream_t stream);
 
 // Packed prompts (prompt.hip).
+size_t prompt_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H);
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
-                                const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale, void* out,
-                                float* lse, hipStream_t stream);
+                                const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale,
+                                void* workspace, void* out, float* lse, hipStream_t stream);
 hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
                                const float* lse, const void* k, int64_t ld, int32_t H, int32_t D, int32_t last,
-                               float scale, float* weight, hipStream_t stream);
+                               float scale, void* workspace, float* weight, hipStream_t stream);
 
 // Log probabilities (logits.hip).
 size_t logprobs_workspace_bytes(int64_t rows, int32_t V, int dtype, int32_t k);

@@ -18,6 +18,8 @@
 #include "common.hpp"
 #include "internal.hpp"
 
+#include <type_traits>
+
 namespace oil {
 
 namespace {
@@ -41,6 +43,13 @@ union Operand {
     shortx4 h[2];
 };
 
+// The larger of each two 16-bit whole numbers.
+__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     const floatx2 x = {a, b};
@@ -55,111 +64,80 @@ __device__ __forceinline__ void swap32(float x, float* a, float* b)
     *b = __uint_as_float(r[1]);
 }
 
-template <int kControl>
-__device__ __forceinline__ int add_moved(int x)
+// A workgroup's share of the work: tile `tile` of the sequence of rows first .. first +
+// len - 1; none with len 0.
+struct Tile {
+    int first, len, tile, pad;
+};
+
+// The tiles of all sequences, (len * per + rows - 1) / rows of each, those of the largest
+// number first (the heaviest: theirs is the longest pass), ties by sequence.  Thread t
+// writes all tiles numbered t, from N(t + 1) = sum of max(0, tiles - t - 1) on.
+// One workgroup: 48 sequences of up to 47 tiles in 5 us.
+__global__ __launch_bounds__(1024) void prompt_schedule_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
+                                                               int32_t per, int32_t rows, Tile* __restrict__ list,
+                                                               int32_t places)
 {
-    return x + __builtin_amdgcn_update_dpp(0, x, kControl, 0xF, 0xF, true);
+    __shared__ int count[kMaxSeqs], from[kMaxSeqs], size[kMaxSeqs], most;
+    if (threadIdx.x == 0)
+        most = 0;
+    __syncthreads();
+    for (int s = threadIdx.x; s < B; s += blockDim.x) {
+        from[s] = seq_first(starts, T, s);
+        size[s] = seq_end(starts, T, s) - from[s];
+        count[s] = (int)(((int64_t)size[s] * per + rows - 1) / rows);
+        atomicMax(&most, count[s]);
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t <= most; t += blockDim.x) {
+        int place = 0;
+        for (int s = 0; s < B; s++)
+            place += count[s] > t + 1 ? count[s] - t - 1 : 0;
+        for (int s = 0; s < B && place < places; s++)
+            if (count[s] > t)
+                list[place++] = Tile{from[s], size[s], t, 0};
+    }
+    int all = 0;
+    for (int s = 0; s < B; s++)
+        all += count[s];
+    for (int i = all + threadIdx.x; i < places; i += blockDim.x)
+        list[i] = Tile{0, 0, 0, 0};
 }
 
-// The sum over a wave, in every lane.
-__device__ __forceinline__ int wave_sum(int x)
+// Workgroup `rank`'s tile; of one sequence it is known without a list.
+__device__ __forceinline__ Tile tile_of(const Tile* list, const int32_t* starts, int32_t T, int rank, int per, int rows)
 {
-    x = add_moved<0xB1>(x);   // lane ^ 1
-    x = add_moved<0x4E>(x);   // lane ^ 2
-    x = add_moved<0x141>(x);  // mirrored in 8
-    x = add_moved<0x140>(x);  // mirrored in 16
-    auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = r[0] + r[1];
-    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return __builtin_amdgcn_readfirstlane(r[0] + r[1]);
+    if (list)
+        return list[rank];
+    Tile r;
+    r.first = seq_first(starts, T, 0);
+    r.len = seq_end(starts, T, 0) - r.first;
+    r.tile = (int)(((int64_t)r.len * per + rows - 1) / rows) - 1 - rank;
+    if (r.tile < 0)
+        r.len = 0;
+    return r;
 }
 
-// Workgroup `rank` of those that the sequences need, `per(length)` tiles each, the
-// tiles of the largest number first (the heaviest: theirs is the longest pass).  A
-// wave as a whole finds it: N(t) = sum of max(0, tiles - t) counts the tiles numbered
-// t and up.  False past the last one.
-template <typename F>
-__device__ __forceinline__ bool find_tile(const int32_t* starts, int32_t B, int32_t T, int rank, F per, int* seq,
-                                          int* tile)
-{
-    if (B == 1) {
-        const int n = per(seq_end(starts, T, 0) - seq_first(starts, T, 0));
-        *seq = 0;
-        *tile = n - 1 - rank;
-        return rank < n;
-    }
-    const int lane = threadIdx.x & 63;
-    int n[kMaxSeqs / 64], all = 0, most = 0;
-#pragma unroll
-    for (int i = 0; i < kMaxSeqs / 64; i++) {
-        const int s = i * 64 + lane;
-        n[i] = 0;
-        if (i * 64 < B && s < B)
-            n[i] = per(seq_end(starts, T, s) - seq_first(starts, T, s));
-        all += n[i];
-        most = n[i] > most ? n[i] : most;
-    }
-    if (rank >= wave_sum(all))
-        return false;
-    // N(low) > rank >= N(high), N(high) = 0 where every lane's most is at or below it
-    int low = 0, high = 1, above = 0;
-    auto count = [&](int t) {
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < kMaxSeqs / 64; i++)
-            if (i * 64 < B)
-                c += n[i] > t ? n[i] - t : 0;
-        return wave_sum(c);
-    };
-    while (true) {  // doubles until it passes: at most 31 turns, as tiles are below 2^30
-        const int c = count(high);
-        if (c <= rank) {
-            above = c;
-            break;
-        }
-        low = high;
-        high *= 2;
-    }
-    while (high - low > 1) {
-        const int mid = low + (high - low) / 2, c = count(mid);
-        if (c > rank) {
-            low = mid;
-        } else {
-            high = mid;
-            above = c;
-        }
-    }
-    int at = rank - above;  // among the sequences of more than `low` tiles
-    *tile = low;
-#pragma unroll
-    for (int i = 0; i < kMaxSeqs / 64; i++) {
-        if (i * 64 >= B)
-            break;
-        const uint64_t has = __ballot(n[i] > low);
-        const int c = __popcll(has);
-        if (at >= 0 && at < c) {
-            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-            const uint64_t mine = __ballot(n[i] > low && before == at);
-            *seq = i * 64 + __builtin_ctzll(mine);
-        }
-        at -= c;
-    }
-    return true;
-}
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const uint16_t* p, int64_t bytes)
+// A buffer's descriptor: address, bytes (reads past them give zeros), raw 32-bit data.
+__device__ __forceinline__ u32x4 rows_at(const uint16_t* p, int64_t bytes)
 {
     const uint64_t a = (uint64_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-    const int n = __builtin_amdgcn_readfirstlane((int)(uint32_t)bytes);
-    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), (short)0, n, 0x00020000);
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xFFFFu,
+                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
 }
 
 // 16 bytes a lane, at byte `from` of the buffer (zeros past its end), straight to LDS:
-// one KiB from `to` on, lane by lane.
-__device__ __forceinline__ void load_kib(__amdgpu_buffer_rsrc_t r, uint8_t* to, uint32_t from)
+// one KiB from `to` on, lane by lane.  In asm because the compiler would wait for all of
+// them before any later read of LDS, the other half of a double buffer's among them; it
+// has no output registers, and loads_done() comes before what it loads is read.
+__device__ __forceinline__ void load_kib(u32x4 r, uint8_t* to, uint32_t from)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDS_PTR(void, to), 16, from, 0, 0, 0);
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)LDS_PTR(uint8_t, to));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(at), "v"(from), "s"(r)
+                 : "m0", "memory");
 }
 
 // Of 64 values that 16 lanes hold the addresses of, four each (a matrix of four rows of
@@ -193,31 +171,23 @@ __device__ __forceinline__ int value_place(int row, int chunk)
 
 template <int W, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
-    const int32_t* __restrict__ starts, int32_t B, int32_t T, const uint16_t* __restrict__ q, int64_t q_ld, int32_t G,
-    const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t ld, int32_t H, int32_t D, float scale,
-    uint16_t* __restrict__ out, float* __restrict__ lse)
+    const Tile* __restrict__ list, const int32_t* __restrict__ starts, int32_t T, const uint16_t* __restrict__ q,
+    int64_t q_ld, int32_t G, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t ld, int32_t H,
+    int32_t D, float scale, uint16_t* __restrict__ out, float* __restrict__ lse)
 {
     constexpr int kTile = kKeys * W * 2;          // bytes
     constexpr int kLoads = kTile / 1024 / NW;     // 1 KiB loads of a wave, a side
     constexpr int kRows = 32 * NW;
     __shared__ __align__(1024) uint8_t key_lds[2][kTile];
     __shared__ __align__(1024) uint8_t value_lds[2][kTile];
+    __shared__ int odd_lds[2][NW];                // whether a wave's part of the values is not finite
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % H;
-    int seq, tile;
-    if (!find_tile(starts, B, T, blockIdx.x / H, [&](int n) { return (int)(((int64_t)n * G + kRows - 1) / kRows); }, &seq,
-                   &tile))
+    const Tile mine = tile_of(list, starts, T, blockIdx.x / H, G, kRows);
+    const int first = mine.first, len = mine.len;
+    if (len == 0)
         return;
-    const int first = seq_first(starts, T, seq), len = seq_end(starts, T, seq) - first;
-    const int64_t rows = (int64_t)len * G, row0 = (int64_t)tile * kRows + wave * 32;
-    const int64_t row = row0 + col < rows ? row0 + col : rows - 1;
-    const int token = (int)(row / G), head = h * G + (int)(row % G);
-    // tokens of the workgroup's last row, of the wave's first and last
-    const int64_t end_row = (int64_t)(tile + 1) * kRows - 1;
-    const int last_token = __builtin_amdgcn_readfirstlane((int)((end_row < rows ? end_row : rows - 1) / G));
-    const int wave_first = __builtin_amdgcn_readfirstlane(token), wave_last = __builtin_amdgcn_readlane(token, 31);
-    const int tiles = last_token / kKeys + 1, wave_tiles = row0 < rows ? wave_last / kKeys + 1 : 0;
 
     // loads: chunk `lane` of each KiB from where its place in LDS says
     uint32_t key_from[kLoads], value_from[kLoads];
@@ -229,18 +199,35 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
         value_from[i] = vc * 8 < D ? (uint32_t)(r * ld * 2) + vc * 16 : kOutside;
     }
     const int64_t base = (int64_t)first * ld + (int64_t)h * D;
-    auto load = [&](int t) {
+    // rows t kKeys .. of p; none past the sequence
+    auto tile_rows = [&](const uint16_t* p, int t) {
         const int left = len - t * kKeys < kKeys ? len - t * kKeys : kKeys;
-        const int64_t bytes = (left - 1) * ld * 2 + D * 2, at = base + (int64_t)t * kKeys * ld;
-        const __amdgpu_buffer_rsrc_t kr = rows_at(k + at, bytes), vr = rows_at(v + at, bytes);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            load_kib(kr, &key_lds[t & 1][(wave * kLoads + i) * 1024], key_from[i]);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            load_kib(vr, &value_lds[t & 1][(wave * kLoads + i) * 1024], value_from[i]);
+        return rows_at(p + base + (int64_t)t * kKeys * ld, left > 0 ? (left - 1) * ld * 2 + D * 2 : 0);
     };
-    load(0);
+    auto load_keys = [&](int t) {
+        const u32x4 r = tile_rows(k, t);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            load_kib(r, &key_lds[t & 1][(wave * kLoads + i) * 1024], key_from[i]);
+    };
+    auto load_values = [&](int t) {
+        const u32x4 r = tile_rows(v, t);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            load_kib(r, &value_lds[t & 1][(wave * kLoads + i) * 1024], value_from[i]);
+    };
+    load_keys(0);
+    load_values(0);
+    load_keys(1);
+
+    const int rows = len * G, row0 = mine.tile * kRows + wave * 32;  // len * G <= T * Hq <= 2^30
+    const int row = row0 + col < rows ? row0 + col : rows - 1;
+    const int token = row / G, head = h * G + row - token * G;
+    // tokens of the workgroup's first and last row, and of the wave's
+    const int end_row = (mine.tile + 1) * kRows - 1;
+    const int first_token = mine.tile * kRows / G, last_token = (end_row < rows ? end_row : rows - 1) / G;
+    const int wave_first = __builtin_amdgcn_readfirstlane(token), wave_last = __builtin_amdgcn_readlane(token, 31);
+    const int tiles = last_token / kKeys + 1, wave_tiles = row0 < rows ? wave_last / kKeys + 1 : 0;
 
     // queries: an operand of 16 columns each.  A negative scale turns their signs; one of
     // zero is zeros in their place, as 0 * -inf would not keep a key unseen.
@@ -280,29 +267,27 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
             o[i][r] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    for (int t = 0; t < tiles; t++) {
-        loads_done();
-        __syncthreads();
-        if (t + 1 < tiles)
-            load(t + 1);
-        if (t >= wave_tiles)
-            continue;
+    floatx16 s[2];
+    Operand p[4];
+    // S^T of tile t
+    auto scores = [&](int t) {
         const uint8_t* keys = key_lds[t & 1];
-        const uint8_t* values = value_lds[t & 1];
-        floatx16 s[2];
 #pragma unroll
-        for (int b = 0; b < 2; b++) {
+        for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int r = 0; r < 16; r++)
                 s[b][r] = 0.f;
 #pragma unroll
-            for (int i = 0; i < W / 16; i++) {
+        for (int i = 0; i < W / 16; i++)
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
                 const bf16x8 a = *(const bf16x8*)(keys + key_at[i] + b * 32 * W * 2);
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qs[i].b, s[b], 0, 0, 0);
             }
-        }
-        const bool edge = t * kKeys + kKeys - 1 > wave_first;  // some row does not see some key
-        if (edge) {
+    };
+    // P of tile t; edge: some row does not see some key of it
+    auto weights = [&](int t, auto edge) {
+        if (decltype(edge)::value) {
             const int seen = token - t * kKeys - 4 * half;
 #pragma unroll
             for (int b = 0; b < 2; b++)
@@ -330,7 +315,6 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
             m = now;
         }
         const float less = m == -INFINITY ? 0.f : -m;
-        Operand p[4];
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < 2; b++) {
@@ -344,64 +328,36 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
                 p[2 * b + r / 8].w[(r % 8) / 2] = pack2(s[b][r], s[b][r + 1]);
         }
         l += sum[0] + sum[1];
-        if (edge) {
+    };
+    // O^T += V^T P of tile t
+    auto products = [&](int t, auto edge) {
+        const uint8_t* values = value_lds[t & 1];
+        bool odd = false;
+        if (decltype(edge)::value) {
             // a value that is not finite must not reach rows that do not see it through a
-            // product with zero: such values leave the products, and how many of each sign
-            // a row sees is counted by products of ones
-            uint32_t odd = 0;
+            // product with zero: where the tile has one, it leaves the products and is
+            // added to the rows that see it
+            int any = 0;
 #pragma unroll
-            for (int j = 0; j < 4; j++)
+            for (int i = 0; i < NW; i++)
+                any |= odd_lds[t & 1][i];
+            odd = __builtin_amdgcn_readfirstlane(any) != 0;
+        }
+        if (decltype(edge)::value && __builtin_expect(odd, 0)) {
+#pragma unroll 1
+            for (int key = 0; key < kKeys; key++)
 #pragma unroll
-                for (int i = 0; i < W / 32; i++) {
-                    const u32x4 w = *(const u32x4*)(values + ((j * W / 32 + i) * 64 + lane) * 16);
+                for (int i = 0; i < W / 32; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        odd |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
-                }
-            if (__builtin_expect(__ballot(odd) != 0, 0)) {
-                const int seen = token - t * kKeys - 4 * half;
-#pragma unroll
-                for (int i = 0; i < W / 32; i++) {
-                    floatx16 up, down;
-#pragma unroll
-                    for (int r = 0; r < 16; r++)
-                        up[r] = down[r] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        Operand a, plus, minus, sees;
-#pragma unroll
-                        for (int e = 0; e < 2; e++)
-                            a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
+                    for (int r = 0; r < 16; r += 4) {
+                        const uint32_t* at = (const uint32_t*)(values + value_place<W>(key, 4 * i + r / 4) * 16 + 8 * half);
 #pragma unroll
                         for (int e = 0; e < 4; e++) {
-                            uint32_t pl = 0, mi = 0, se = 0;
-#pragma unroll
-                            for (int g = 0; g < 2; g++) {
-                                const uint32_t u = (a.w[e] >> (16 * g)) & 0xFFFFu;
-                                const bool wild = (u & 0x7F80u) == 0x7F80u, nan = wild && (u & 0x7Fu);
-                                pl |= (wild && (nan || !(u >> 15)) ? 0x3F80u : 0u) << (16 * g);
-                                mi |= (wild && (nan || (u >> 15)) ? 0x3F80u : 0u) << (16 * g);
-                                if (wild)
-                                    a.w[e] &= ~(0xFFFFu << (16 * g));
-                                const int key = 16 * j + 8 * (e / 2) + 2 * (e % 2) + g;
-                                se |= (key <= seen ? 0x3F80u : 0u) << (16 * g);
-                            }
-                            plus.w[e] = pl;
-                            minus.w[e] = mi;
-                            sees.w[e] = se;
+                            const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
+                            if ((u & 0x7F800000u) == 0x7F800000u && t * kKeys + key <= token)
+                                o[i][r + e] += __uint_as_float(u);
                         }
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
-                        up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(plus.b, sees.b, up, 0, 0, 0);
-                        down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(minus.b, sees.b, down, 0, 0, 0);
                     }
-#pragma unroll
-                    for (int r = 0; r < 16; r++) {
-                        o[i][r] += up[r] > 0.f ? INFINITY : 0.f;
-                        o[i][r] -= down[r] > 0.f ? INFINITY : 0.f;
-                    }
-                }
-                continue;
-            }
         }
 #pragma unroll
         for (int j = 0; j < 4; j++)
@@ -411,9 +367,99 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
 #pragma unroll
                 for (int e = 0; e < 2; e++)
                     a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
+                if (decltype(edge)::value && __builtin_expect(odd, 0))
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
+                        a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
+                    }
                 o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
             }
+    };
+
+    // Products and scores beside each other: reads of LDS four matrix instructions ahead.
+    auto pipeline = [&]() {
+        constexpr int kEach = W / 8, kMatrix = 0x8, kRead = 0x100;  // matrix instructions of each; 2 reads and 1
+        __builtin_amdgcn_sched_group_barrier(kRead, 8, 0);
+#pragma unroll
+        for (int i = 0; i < kEach; i++) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kEach - 8; i++) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 8, 0);
+    };
+
+    // Whether the wave's part of the values of tile t, which it loaded itself, is finite.
+    auto look = [&](int t) {
+        u32x4 most = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const u32x4 w = *(const u32x4*)&value_lds[t & 1][((wave * kLoads + i) * 64 + lane) * 16];
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                most[e] = max_u16(most[e], w[e] & 0x7FFF7FFFu);
+        }
+        const uint32_t m2 = max_u16(max_u16(most[0], most[1]), max_u16(most[2], most[3]));
+        const bool odd = (m2 & 0xFFFFu) >= 0x7F80u || m2 >= 0x7F800000u;
+        const int any = __ballot(odd) != 0;
+        if (lane == 0)
+            odd_lds[t & 1][wave] = any;
+    };
+
+    // Between two barriers a wave makes the products of tile t, then the scores and the
+    // weights of tile t + 1.
+    auto next = [&](int t) {
+        __syncthreads();
+        load_values(t + 1);
+        load_keys(t + 2);
+    };
+    const std::false_type inner;
+    const std::true_type edge;
+    auto is_edge = [&](int t) { return t * kKeys + kKeys - 1 > wave_first; };
+    const int whole = (first_token + 1) / kKeys;  // tiles that every row of the workgroup sees whole
+    loads_done();
+    if (whole == 0)
+        look(0);
+    __syncthreads();
+    if (wave_tiles > 0) {
+        scores(0);
+        if (is_edge(0))
+            weights(0, edge);
+        else
+            weights(0, inner);
     }
+    int t = 0;
+    for (; t + 1 < whole; t++) {
+        loads_done();
+        next(t);
+        products(t, inner);
+        scores(t + 1);
+        pipeline();
+        weights(t + 1, inner);
+    }
+    for (; t < tiles; t++) {
+        loads_done();
+        if (t > 0)
+            look(t);
+        next(t);
+        if (t < wave_tiles && is_edge(t))
+            products(t, edge);
+        else if (t < wave_tiles)
+            products(t, inner);
+        if (t + 1 < wave_tiles) {
+            scores(t + 1);
+            if (is_edge(t + 1))
+                weights(t + 1, edge);
+            else
+                weights(t + 1, inner);
+        }
+    }
+    loads_done();  // none is in flight when the workgroup's LDS goes to another
 
     if (row0 + col >= rows)
         return;
@@ -424,23 +470,29 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
     const int64_t at = ((int64_t)first + token) * (H * G) + head;
     if (lse && half == 0)
         lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
+    // eight in a row: the even j's or the odd ones
 #pragma unroll
     for (int i = 0; i < W / 32; i++)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int d = i * 32 + 2 * r + 4 * half;
-            if (d < D) {
-                typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-                *(u32x2*)(out + at * D + d) = u32x2{pack2(o[i][r] * inv, o[i][r + 1] * inv),
-                                                   pack2(o[i][r + 2] * inv, o[i][r + 3] * inv)};
-            }
+        for (int r = 0; r < 16; r += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
+            const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+            const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const int d = i * 32 + 2 * r + 8 * half;
+            if (d < D)
+                *(u32x4*)(out + at * D + d) = u32x4{a[0], b[0], a[1], b[1]};
         }
 }
 
 // kWeighKeys keys a wave, NW waves; rows 64 at a time from LDS.
 template <int W, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
-    const int32_t* __restrict__ starts, int32_t B, int32_t T, const uint16_t* __restrict__ q, int64_t q_ld, int32_t G,
+    const Tile* __restrict__ list, const int32_t* __restrict__ starts, int32_t T, const uint16_t* __restrict__ q,
+    int64_t q_ld, int32_t G,
     const float* __restrict__ lse, const uint16_t* __restrict__ k, int64_t ld, int32_t H, int32_t D, int32_t last,
     float scale, float* __restrict__ weight)
 {
@@ -452,15 +504,14 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % H;
-    auto per = [&](int n) { return (n + kBlock - 1) / kBlock; };
-    int seq, tile;
-    if (!find_tile(starts, B, T, blockIdx.x / H, per, &seq, &tile))
+    const Tile mine = tile_of(list, starts, T, blockIdx.x / H, 1, kBlock);
+    const int first = mine.first, len = mine.len;
+    if (len == 0)
         return;
-    const int first = seq_first(starts, T, seq), len = seq_end(starts, T, seq) - first;
-    const int key0 = (per(len) - 1 - tile) * kBlock;  // the lowest keys, which most rows see, first
+    const int key0 = ((len + kBlock - 1) / kBlock - 1 - mine.tile) * kBlock;  // the lowest keys, which most rows see, first
     const int seen_from = len - last > key0 ? len - last : key0;  // the first token whose rows count here
-    const int64_t row_begin = (int64_t)seen_from * G, rows = (int64_t)len * G - row_begin;
-    const int turns = (int)((rows + kRowTile - 1) / kRowTile);
+    const int row_begin = seen_from * G, rows = len * G - row_begin;  // len * G <= T * Hq <= 2^30
+    const int turns = (rows + kRowTile - 1) / kRowTile;
     const float c = fabsf(scale) * kLog2e;
     const uint32_t magic = 65536 / G + 1;  // x / G = x magic >> 16 for x < 128, G <= 64
 
@@ -477,11 +528,11 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     float next_less = 0.f;
     int next_token = 0;
     auto load = [&](int t) {
-        const int64_t row0 = row_begin + (int64_t)t * kRowTile;
-        const int token0 = (int)(row0 / G), rem = (int)(row0 % G);
-        const int here = rows - (int64_t)t * kRowTile < kRowTile ? (int)(rows - (int64_t)t * kRowTile) : kRowTile;
+        const int row0 = row_begin + t * kRowTile;
+        const int token0 = row0 / G, rem = row0 - token0 * G;
+        const int here = rows - t * kRowTile < kRowTile ? rows - t * kRowTile : kRowTile;
         const int tokens = ((rem + here - 1) / G);
-        const __amdgpu_buffer_rsrc_t r = rows_at(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D,
+        const u32x4 r = rows_at(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D,
                                                  tokens * q_ld * 2 + (int64_t)G * D * 2);
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
@@ -537,7 +588,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
         __syncthreads();
         if (t + 1 < turns)
             load(t + 1);
-        const int token0 = (int)((row_begin + (int64_t)t * kRowTile) / G);
+        const int token0 = (row_begin + t * kRowTile) / G;
         const bool edge = token0 < wave_key || none_lds[t & 1];
 #pragma unroll
         for (int a = 0; a < 2; a++) {
@@ -598,28 +649,46 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     }
 }
 
-// Workgroups that sequences of T rows in all, times G, need at most, at `per` rows each.
-int64_t most_tiles(int64_t rows, int64_t per, int32_t B) { return rows / per + B; }
+// Tiles of `rows` rows that sequences of T rows in all, times `per`, have at most.
+int64_t most_tiles(int64_t T, int32_t per, int32_t rows, int32_t B) { return T * per / rows + B; }
+
+// The list of a call's tiles, or none where there is one sequence.
+const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, int32_t rows, void* workspace,
+                      hipStream_t stream)
+{
+    if (B == 1)
+        return nullptr;
+    hipLaunchKernelGGL(prompt_schedule_kernel, dim3(1), dim3(1024), 0, stream, starts, B, T, per, rows,
+                       (Tile*)workspace, (int32_t)most_tiles(T, per, rows, B));
+    return (const Tile*)workspace;
+}
+
+constexpr int kLeastRows = 64;  // of a tile
 
 }  // namespace
 
+size_t prompt_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H)
+{
+    return B == 1 ? 256 : (size_t)most_tiles(T, Hq / H, kLeastRows, B) * sizeof(Tile);
+}
+
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
-                                const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale, void* out,
-                                float* lse, hipStream_t stream)
+                                const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale,
+                                void* workspace, void* out, float* lse, hipStream_t stream)
 {
     const int32_t G = Hq / H;
 #define OIL_PROMPT_ATTEND(W, NW)                                                                                   \
-    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>),                                                              \
-                       dim3((uint32_t)(most_tiles((int64_t)T * G, 32 * NW, B) * H)), dim3(NW * 64), 0, stream, starts, \
-                       B, T, (const uint16_t*)q, q_ld, G, (const uint16_t*)k, (const uint16_t*)v, ld, H, D, scale, \
+    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>), dim3((uint32_t)(most_tiles(T, G, 32 * NW, B) * H)),          \
+                       dim3(NW * 64), 0, stream, make_list(starts, B, T, G, 32 * NW, workspace, stream), starts, T, \
+                       (const uint16_t*)q, q_ld, G, (const uint16_t*)k, (const uint16_t*)v, ld, H, D, scale,       \
                        (uint16_t*)out, lse)
-    const bool wide = (int64_t)T * Hq >= 256 * 512;
+    const bool wide = (int64_t)T * Hq >= 128 * 256;
     if (D <= 64 && wide)
-        OIL_PROMPT_ATTEND(64, 8);
+        OIL_PROMPT_ATTEND(64, 4);
     else if (D <= 64)
         OIL_PROMPT_ATTEND(64, 2);
     else if (wide)
-        OIL_PROMPT_ATTEND(128, 8);
+        OIL_PROMPT_ATTEND(128, 4);
     else
         OIL_PROMPT_ATTEND(128, 2);
 #undef OIL_PROMPT_ATTEND
@@ -628,13 +697,13 @@ hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, con
 
 hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
                                const float* lse, const void* k, int64_t ld, int32_t H, int32_t D, int32_t last,
-                               float scale, float* weight, hipStream_t stream)
+                               float scale, void* workspace, float* weight, hipStream_t stream)
 {
     const int32_t G = Hq / H;
 #define OIL_PROMPT_WEIGH(W, NW)                                                                                   \
-    hipLaunchKernelGGL((prompt_weigh_kernel<W, NW>), dim3((uint32_t)(most_tiles(T, kWeighKeys * NW, B) * H)),     \
-                       dim3(NW * 64), 0, stream, starts, B, T, (const uint16_t*)q, q_ld, G, lse, (const uint16_t*)k, \
-                       ld, H, D, last, scale, weight)
+    hipLaunchKernelGGL((prompt_weigh_kernel<W, NW>), dim3((uint32_t)(most_tiles(T, 1, kWeighKeys * NW, B) * H)),  \
+                       dim3(NW * 64), 0, stream, make_list(starts, B, T, 1, kWeighKeys * NW, workspace, stream),  \
+                       starts, T, (const uint16_t*)q, q_ld, G, lse, (const uint16_t*)k, ld, H, D, last, scale, weight)
     if (D <= 64)
         OIL_PROMPT_WEIGH(64, 4);
     else

@@ -19,11 +19,12 @@ def test_prompt_statuses(L):
     f = _FakeBufs()
     P, bad = f.aligned, f.misaligned
 
-    def attend(starts=P, B=2, total=10, q=P, q_ld=256, Hq=4, k=P, v=P, ld=128, H=2, D=64, scale=1.0, out=P):
-        return L.oil_prompt_attend(starts, B, total, q, q_ld, Hq, k, v, ld, H, D, scale, out, None, None)
+    def attend(starts=P, B=2, total=10, q=P, q_ld=256, Hq=4, k=P, v=P, ld=128, H=2, D=64, scale=1.0, out=P, ws=P, nb=1 << 20):
+        return L.oil_prompt_attend(starts, B, total, q, q_ld, Hq, k, v, ld, H, D, scale, ws, nb, out, None, None)
 
-    def weigh(starts=P, B=2, total=10, q=P, q_ld=256, Hq=4, lse=P, k=P, ld=128, H=2, D=64, last=3, scale=1.0, weight=P):
-        return L.oil_prompt_weigh(starts, B, total, q, q_ld, Hq, lse, k, ld, H, D, last, scale, weight, None)
+    def weigh(starts=P, B=2, total=10, q=P, q_ld=256, Hq=4, lse=P, k=P, ld=128, H=2, D=64, last=3, scale=1.0, weight=P,
+              ws=P, nb=1 << 20):
+        return L.oil_prompt_weigh(starts, B, total, q, q_ld, Hq, lse, k, ld, H, D, last, scale, ws, nb, weight, None)
 
     common = [dict(starts=None), dict(B=0), dict(total=0), dict(total=-5), dict(q=None), dict(q=bad), dict(k=None),
               dict(k=bad), dict(Hq=3), dict(Hq=0), dict(H=0), dict(D=0), dict(D=60), dict(q_ld=248), dict(q_ld=260),
@@ -39,6 +40,13 @@ def test_prompt_statuses(L):
                dict(D=136, q_ld=1024, ld=512), dict(Hq=130, q_ld=130 * 64), dict(q_ld=(1 << 24) + 8),
                dict(ld=(1 << 24) + 8)):
         assert attend(**kw) == -3 and weigh(**kw) == -3, kw
+    need = L.oil_prompt_workspace_bytes(2, 10, 4, 2)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=bad), dict(nb=need - 1)):
+        assert attend(**kw) == -5 and weigh(**kw) == -5, kw
+    for args in ((0, 10, 4, 2), (513, 10, 4, 2), (2, 0, 4, 2), (2, (1 << 28) + 1, 4, 2), (2, 1 << 28, 8, 2), (2, 10, 3, 2),
+                 (2, 10, 0, 2), (2, 10, 4, 0), (2, 10, 130, 2), (2, 10, 257, 257)):
+        assert L.oil_prompt_workspace_bytes(*args) == 0, args
 
 
 def test_append_packed_refuses_no_handle(L):
