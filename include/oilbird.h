@@ -590,14 +590,16 @@ int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, 
  *   n_heads    1 .. OIL_KV_MAX_HEADS.   n_q_heads  a multiple of it, at most
  *              OIL_KV_MAX_GROUP times.   head_dim  a multiple of 8, 8 .. OIL_KV_MAX_DIM.
  *   scale      finite.
- *   workspace  >= oil_prompt_workspace_bytes(...), 256-byte aligned; calls on one stream may
+ *   workspace  as many bytes as the call asks for, 256-byte aligned; calls on one stream may
  *              share it.
  * Rows outside every sequence are neither read nor written. */
 #define OIL_PROMPT_MAX_ROWS (1 << 28)
 #define OIL_PROMPT_MAX_LD (1 << 24)
 
-/* Workspace bytes of the two calls; 0 for arguments they refuse. */
-size_t oil_prompt_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads);
+/* Workspace bytes of the two calls; 0 for arguments they refuse, 256 where they use none
+ * (workspace may then be NULL). */
+size_t oil_prompt_attend_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads);
+size_t oil_prompt_weigh_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads, int64_t last);
 
 /* Causal attention of packed sequences.  Query head a reads key/value head
  * a / (n_q_heads / n_heads); row i sees the rows of its sequence up to its own:
@@ -633,7 +635,8 @@ int32_t oil_prompt_weigh(const int32_t *starts, int32_t B, int64_t total, const 
 /* Largest B * max_rows of oil_token_logprobs. */
 #define OIL_LOGITS_MAX_ROWS (1 << 23)
 
-/* Workspace bytes of oil_token_logprobs; 0 for arguments it refuses. */
+/* Workspace bytes of oil_token_logprobs; 0 for arguments it refuses, 256 where it uses none
+ * (workspace may then be NULL). */
 size_t oil_token_logprobs_workspace_bytes(int32_t B, int64_t max_rows, int32_t vocab, int32_t dtype, int32_t top);
 
 /* Log probabilities.  Of every row x of logits, with log p = x - log sum exp x:

@@ -118,7 +118,8 @@ def lib():
             "oil_kv_reset": (i32, [P, P, i32, P]),
             "oil_kv_append": (i32, [P, P, i32, P, P, i32, i64, i32, P, P, P, P]),
             "oil_kv_append_packed": (i32, [P, P, i32, P, i64, P, P, i32, i64, P, P]),
-            "oil_prompt_workspace_bytes": (sz, [i32, i64, i32, i32]),
+            "oil_prompt_attend_workspace_bytes": (sz, [i32, i64, i32, i32]),
+            "oil_prompt_weigh_workspace_bytes": (sz, [i32, i64, i32, i32, i64]),
             "oil_prompt_attend": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, ctypes.c_float, P, sz, P, P, P]),
             "oil_prompt_weigh": (i32, [P, i32, i64, P, i64, i32, P, P, i64, i32, i32, i64, ctypes.c_float, P, sz, P,
                                        P]),
@@ -186,6 +187,14 @@ def _empty(shape, dtype, device, stream=None):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _new(shape, dtype, like, stream):
+    """Memory on the device of ``like`` for work on ``stream``."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def _elsewhere(t, name, index):
     raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
 
@@ -222,14 +231,16 @@ def _row_stride(t, name, index):
 def _packed_stride(t, name, index):
     """Elements between consecutive rows of a (rows, heads, dim) tensor on device ``index``
     whose rows are dense."""
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be (rows, heads, dim), got {tuple(t.shape)}")
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{name} must be (rows, heads, dim), got {tuple(shape)}")
     if t.get_device() != index:
         _elsewhere(t, name, index)
-    T, H, D = t.shape
-    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+    T, H, D = shape
+    row, head, value = t.stride()
+    if (D > 1 and value != 1) or (H > 1 and head != D):
         raise ValueError(f"{name}: the heads of a row must be dense")
-    return t.stride(0) if T > 1 else H * D
+    return row if T > 1 else H * D
 
 
 def _stream_on(stream, index):
@@ -422,15 +433,19 @@ def _prompt(q, k, v, starts):
     return index, T, Hq, D, q_ld, k.shape[1], ld, starts.numel() - 1
 
 
-def _given_or_new(workspace, nbytes, index, device, stream):
-    """A call's workspace: the one given, or torch's memory on the call's stream."""
+def _room(workspace, nbytes, index, like, stream):
+    """(address, bytes, tensor) of a call's workspace: the one given, torch's memory on the
+    call's stream, or none where the call uses none."""
     if workspace is None:
-        return _empty((nbytes,), torch.uint8, device, stream)
+        if nbytes <= 256:
+            return None, 0, None
+        workspace = _new((nbytes,), torch.uint8, like, stream)
+        return workspace.data_ptr(), nbytes, workspace
     if workspace.get_device() != index:
         _elsewhere(workspace, "workspace", index)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be dense")
-    return workspace
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None, workspace=None):
@@ -442,14 +457,16 @@ def prompt_attend(q, k, v, starts, scale=None, stream=None, out=None, workspace=
     index, T, Hq, D, q_ld, H, ld, B = _prompt(q, k, v, starts)
     on = _stream_on(stream, index)
     if out is None:
-        out = (_empty((T, Hq, D), torch.bfloat16, q.device, stream), _empty((T, Hq), torch.float32, q.device, stream))
-    o, lse = out
-    ws = _given_or_new(workspace, lib().oil_prompt_workspace_bytes(B, T, Hq, H), index, q.device, stream)
+        o, lse = _new((T, Hq, D), torch.bfloat16, q, stream), _new((T, Hq), torch.float32, q, stream)
+        o_at, lse_at = o.data_ptr(), lse.data_ptr()
+    else:
+        o, lse = out
+        o_at = _shaped(o, "out", (T, Hq, D), torch.bfloat16, index)
+        lse_at = _shaped(lse, "lse", (T, Hq), torch.float32, index)
+    at, nbytes, ws = _room(workspace, lib().oil_prompt_attend_workspace_bytes(B, T, Hq, H), index, q, stream)
     _call_on(index, "oil_prompt_attend", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
              q_ld, Hq, k.data_ptr(), v.data_ptr(), ld, H, D, 1.0 / math.sqrt(D) if scale is None else scale,
-             ws.data_ptr(), ws.numel() * ws.element_size(),
-             _shaped(o, "out", (T, Hq, D), torch.bfloat16, index),
-             _shaped(lse, "lse", (T, Hq), torch.float32, index), on)
+             at, nbytes, o_at, lse_at, on)
     return o, lse
 
 
@@ -460,12 +477,15 @@ def prompt_weigh(q, k, lse, starts, last=None, scale=None, stream=None, out=None
     index, T, Hq, D, q_ld, H, ld, B = _prompt(q, k, None, starts)
     on = _stream_on(stream, index)
     if out is None:
-        out = _empty((H, T), torch.float32, q.device, stream)
-    ws = _given_or_new(workspace, lib().oil_prompt_workspace_bytes(B, T, Hq, H), index, q.device, stream)
+        out = _new((H, T), torch.float32, q, stream)
+        out_at = out.data_ptr()
+    else:
+        out_at = _shaped(out, "out", (H, T), torch.float32, index)
+    last = T if last is None else last
+    at, nbytes, ws = _room(workspace, lib().oil_prompt_weigh_workspace_bytes(B, T, Hq, H, last), index, q, stream)
     _call_on(index, "oil_prompt_weigh", _shaped(starts, "starts", (B + 1,), torch.int32, index), B, T, q.data_ptr(),
-             q_ld, Hq, _shaped(lse, "lse", (T, Hq), torch.float32, index), k.data_ptr(), ld, H, D,
-             T if last is None else last, 1.0 / math.sqrt(D) if scale is None else scale, ws.data_ptr(),
-             ws.numel() * ws.element_size(), _shaped(out, "out", (H, T), torch.float32, index), on)
+             q_ld, Hq, _shaped(lse, "lse", (T, Hq), torch.float32, index), k.data_ptr(), ld, H, D, last,
+             1.0 / math.sqrt(D) if scale is None else scale, at, nbytes, out_at, on)
     return out
 
 
@@ -475,14 +495,15 @@ def token_logprobs(logits, tokens=None, top=0, n_rows=None, stream=None, out=Non
     the ``top`` most likely tokens (B, N, top) int32, ties to the lower one; their log
     probabilities).  ``n_rows`` (B,) int32: the rows that count; the others give -inf,
     0, -1 and -inf.  A token outside the vocabulary has -inf."""
-    index = _device_of(logits, "logits")
-    if logits.dim() != 3:
-        raise ValueError(f"logits must be (requests, rows, vocabulary), got {tuple(logits.shape)}")
-    B, N, V = logits.shape
-    if V > 1 and logits.stride(2) != 1:
+    index, shape = _device_of(logits, "logits"), logits.shape
+    if len(shape) != 3:
+        raise ValueError(f"logits must be (requests, rows, vocabulary), got {tuple(shape)}")
+    B, N, V = shape
+    request, row, value = logits.stride()
+    if V > 1 and value != 1:
         raise ValueError("logits: a row must be dense")
-    ld = logits.stride(1) if N > 1 else logits.stride(0) if B > 1 else V
-    if B > 1 and logits.stride(0) != N * ld:
+    ld = row if N > 1 else request if B > 1 else V
+    if B > 1 and request != N * ld:
         raise ValueError("logits: requests must be as far apart as their rows")
     on, f32, i32 = _stream_on(stream, index), torch.float32, torch.int32
     M = 0
@@ -490,22 +511,25 @@ def token_logprobs(logits, tokens=None, top=0, n_rows=None, stream=None, out=Non
         if tokens.dim() != 3:
             raise ValueError(f"tokens must be (requests, rows, tokens), got {tuple(tokens.shape)}")
         M = tokens.shape[2]
-    if out is None:
-        dev = logits.device
-        out = (None if tokens is None else _empty((B, N, M), f32, dev, stream), _empty((B, N), f32, dev, stream),
-               _empty((B, N, top), i32, dev, stream), _empty((B, N, top), f32, dev, stream))
-    logprob, entropy, top_tokens, top_logprobs = out
     code = _dtype_code(logits)
     nbytes = lib().oil_token_logprobs_workspace_bytes(B, N, V, code, top)
     if nbytes == 0:
-        raise ValueError(f"unsupported logits: {tuple(logits.shape)} top={top}")
-    workspace = _given_or_new(workspace, nbytes, index, logits.device, stream)
+        raise ValueError(f"unsupported logits: {tuple(shape)} top={top}")
+    if out is None:
+        logprob = None if tokens is None else _new((B, N, M), f32, logits, stream)
+        entropy = _new((B, N), f32, logits, stream)
+        top_tokens = _new((B, N, top), i32, logits, stream)
+        top_logprobs = _new((B, N, top), f32, logits, stream)
+        out = logprob, entropy, top_tokens, top_logprobs
+        to = [None if t is None else t.data_ptr() for t in out]
+    else:
+        logprob, entropy, top_tokens, top_logprobs = out
+        to = (_shaped(logprob, "logprob", (B, N, M), f32, index), _shaped(entropy, "entropy", (B, N), f32, index),
+              _shaped(top_tokens, "top_tokens", (B, N, top), i32, index),
+              _shaped(top_logprobs, "top_logprobs", (B, N, top), f32, index))
+    at, nbytes, ws = _room(workspace, nbytes, index, logits, stream)
     _call_on(index, "oil_token_logprobs", B, N, _shaped(n_rows, "n_rows", (B,), i32, index), logits.data_ptr(), code, V,
-             ld, _shaped(tokens, "tokens", (B, N, M), i32, index), M, top, workspace.data_ptr(),
-             workspace.numel() * workspace.element_size(), _shaped(logprob, "logprob", (B, N, M), f32, index),
-             _shaped(entropy, "entropy", (B, N), f32, index),
-             _shaped(top_tokens, "top_tokens", (B, N, top), i32, index),
-             _shaped(top_logprobs, "top_logprobs", (B, N, top), f32, index), on)
+             ld, _shaped(tokens, "tokens", (B, N, M), i32, index), M, top, at, nbytes, *to, on)
     return out
 
 

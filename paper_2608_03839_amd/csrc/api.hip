@@ -872,20 +872,33 @@ static int32_t prompt_status(const int32_t* starts, int32_t B, int64_t total, co
     return q_ld > OIL_PROMPT_MAX_LD || ld > OIL_PROMPT_MAX_LD ? OIL_E_UNSUPPORTED : OIL_OK;
 }
 
-size_t oil_prompt_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads)
+static bool prompt_sizes_fit(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads)
 {
-    if (B < 1 || B > OIL_MAX_B || total < 1 || total > OIL_PROMPT_MAX_ROWS || n_heads < 1 ||
-        n_heads > OIL_KV_MAX_HEADS || n_q_heads < 1 || n_q_heads % n_heads != 0 ||
-        n_q_heads / n_heads > OIL_KV_MAX_GROUP || total > ((int64_t)1 << 30) / n_q_heads)
-        return 0;
-    return oil::prompt_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads);
+    return B >= 1 && B <= OIL_MAX_B && total >= 1 && total <= OIL_PROMPT_MAX_ROWS && n_heads >= 1 &&
+           n_heads <= OIL_KV_MAX_HEADS && n_q_heads >= 1 && n_q_heads % n_heads == 0 &&
+           n_q_heads / n_heads <= OIL_KV_MAX_GROUP && total <= ((int64_t)1 << 30) / n_q_heads;
 }
 
-static bool prompt_workspace_fits(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads, const void* workspace,
-                                  size_t bytes)
+static int32_t prompt_last(int64_t last, int64_t total) { return (int32_t)(last < total ? last : total); }
+
+size_t oil_prompt_attend_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads)
 {
-    return workspace && aligned(workspace, kAlign) &&
-           bytes >= oil::prompt_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads);
+    return prompt_sizes_fit(B, total, n_q_heads, n_heads)
+               ? oil::prompt_attend_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads)
+               : 0;
+}
+
+size_t oil_prompt_weigh_workspace_bytes(int32_t B, int64_t total, int32_t n_q_heads, int32_t n_heads, int64_t last)
+{
+    return prompt_sizes_fit(B, total, n_q_heads, n_heads) && last >= 1
+               ? oil::prompt_weigh_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads, prompt_last(last, total))
+               : 0;
+}
+
+// Whether a workspace serves a call that asks for `need` bytes; kAlign are none in use.
+static bool workspace_fits(const void* workspace, size_t bytes, size_t need)
+{
+    return (need <= kAlign && !workspace) || (workspace && aligned(workspace, kAlign) && bytes >= need);
 }
 
 int32_t oil_prompt_attend(const int32_t* starts, int32_t B, int64_t total, const void* q, int64_t q_ld,
@@ -898,7 +911,8 @@ int32_t oil_prompt_attend(const int32_t* starts, int32_t B, int64_t total, const
         return st;
     if (!v || !out || !aligned(v, 16) || !aligned(out, 16))
         return OIL_E_INVALID;
-    if (!prompt_workspace_fits(B, total, n_q_heads, n_heads, workspace, workspace_bytes))
+    if (!workspace_fits(workspace, workspace_bytes,
+                        oil::prompt_attend_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads)))
         return OIL_E_WORKSPACE;
     return hip_status(oil::launch_prompt_attend(starts, B, (int32_t)total, q, q_ld, n_q_heads, k, v, ld, n_heads,
                                                 head_dim, scale, workspace, out, lse, (hipStream_t)stream));
@@ -914,10 +928,12 @@ int32_t oil_prompt_weigh(const int32_t* starts, int32_t B, int64_t total, const 
         return st;
     if (!lse || !weight || last < 1)
         return OIL_E_INVALID;
-    if (!prompt_workspace_fits(B, total, n_q_heads, n_heads, workspace, workspace_bytes))
+    if (!workspace_fits(workspace, workspace_bytes,
+                        oil::prompt_weigh_workspace_bytes(B, (int32_t)total, n_q_heads, n_heads,
+                                                          prompt_last(last, total))))
         return OIL_E_WORKSPACE;
     return hip_status(oil::launch_prompt_weigh(starts, B, (int32_t)total, q, q_ld, n_q_heads, lse, k, ld, n_heads,
-                                               head_dim, (int32_t)(last < total ? last : total), scale, workspace,
+                                               head_dim, prompt_last(last, total), scale, workspace,
                                                weight, (hipStream_t)stream));
 }
 
@@ -952,8 +968,7 @@ int32_t oil_token_logprobs(int32_t B, int64_t max_rows, const int32_t* n_rows, c
         ld > ((int64_t)1 << 60) / (B * max_rows) || n_tokens < 0 || (n_tokens > 0 && (!tokens || !logprob)) ||
         (top > 0 && (!top_tokens || !top_logprobs)))
         return OIL_E_INVALID;
-    if (!workspace || !aligned(workspace, kAlign) ||
-        workspace_bytes < oil::logprobs_workspace_bytes(B * max_rows, vocab, dtype, top))
+    if (!workspace_fits(workspace, workspace_bytes, oil::logprobs_workspace_bytes(B * max_rows, vocab, dtype, top)))
         return OIL_E_WORKSPACE;
     return hip_status(oil::launch_logprobs(B * max_rows, (int32_t)max_rows, n_rows, logits, dtype, vocab, ld, tokens,
                                            n_tokens, top, workspace, logprob, entropy, top_tokens, top_logprobs,

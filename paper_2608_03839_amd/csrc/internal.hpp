@@ -173,7 +173,8 @@ hipError_t launch_kv_evict(const KvView& c, const int32_t* slots, int32_t B, int
                            void* workspace, hipStream_t stream);
 
 // Packed prompts (prompt.hip).
-size_t prompt_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H);
+size_t prompt_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H);
+size_t prompt_weigh_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t last);
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
                                 const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale,
                                 void* workspace, void* out, float* lse, hipStream_t stream);

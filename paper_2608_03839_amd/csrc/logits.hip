@@ -1,14 +1,18 @@
 // Log probabilities of tokens from rows of logits, with the entropy and the most
 // likely tokens.  Contract: include/oilbird.h.
 //
-// One pass over a row: with m the running maximum, y = (x - m) log2 e, a lane keeps
-// s = sum 2^y and t = sum y 2^y, both rescaled when m rises.  Then
+// One pass over a row: with m the running maximum, z = (x - m) log2 e, a lane keeps
+//     s = sum 2^z,  t = sum z 2^z,
+// both rescaled when m rises.  Then
 //     log p = (x - m) - ln s,      H = ln s - ln 2 t / s,
-// where both terms of H are at least 0, so that nothing cancels.  The k best (logit
-// descending, token ascending: one 64-bit key a token) are a list over the lanes of a
-// wave, which a step of values enters only where some lane's largest reaches the
-// list's last; waves of a workgroup share the highest such bound.  The first step's
-// bound is the k-th largest of the lanes' own maxima.
+// where both terms of H are at least 0, so that nothing cancels.  9 instructions a value,
+// one of them an exponential; the pass over many rows is bound by memory.
+//
+// The k best tokens (logit descending, token ascending: one 64-bit key a token) are a
+// list over the lanes of a wave, which a step of values enters only where some lane's
+// largest reaches a bound: at first the k-th largest of the lanes' own maxima, then the
+// list's last or that of another wave of the workgroup.  The waves' lists are joined by
+// counting, for each key, those above it.
 //
 // Where rows are few, a row is cut among workgroups, and a second launch joins.
 #include "common.hpp"
@@ -18,20 +22,14 @@ namespace oil {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kDeep = 4;  // loads of a lane in flight
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kLeast = -2000.f;  // below any y whose power of two is not 0
+constexpr float kLeast = -2000.f;  // below any z whose power of two is not 0
 constexpr float kLowest = -3.4028234663852886e38f;
 
+// m, and the sums relative to it; m is -FLT_MAX at first.
 struct Sums {
     float m, s, t;
-};
-
-// What a workgroup found of its part of a row.
-struct Part {
-    Sums sums;
-    float pad;
 };
 
 __device__ __forceinline__ Sums join(Sums a, Sums b)
@@ -45,12 +43,21 @@ __device__ __forceinline__ Sums join(Sums a, Sums b)
     return r;
 }
 
+template <int kControl>
+__device__ __forceinline__ float moved(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kControl, 0xF, 0xF, true));
+}
+
+// Over a wave, in every lane: neighbours by lane moves, then halves of 16 and 32.
 __device__ __forceinline__ Sums join_wave(Sums a)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1)
-        a = join(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
-    return a;
+    a = join(a, Sums{moved<0xB1>(a.m), moved<0xB1>(a.s), moved<0xB1>(a.t)});
+    a = join(a, Sums{moved<0x4E>(a.m), moved<0x4E>(a.s), moved<0x4E>(a.t)});
+    a = join(a, Sums{moved<0x141>(a.m), moved<0x141>(a.s), moved<0x141>(a.t)});
+    a = join(a, Sums{moved<0x140>(a.m), moved<0x140>(a.s), moved<0x140>(a.t)});
+    a = join(a, Sums{__shfl_xor(a.m, 16), __shfl_xor(a.s, 16), __shfl_xor(a.t, 16)});
+    return join(a, Sums{__shfl_xor(a.m, 32), __shfl_xor(a.s, 32), __shfl_xor(a.t, 32)});
 }
 
 // A token's key: larger is better; 0: not a candidate (-inf, NaN).
@@ -65,6 +72,14 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane)
            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
 }
 
+// The key of the lane before.
+__device__ __forceinline__ uint64_t key_before(uint64_t k)
+{
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(k >> 32), 0x138, 0xF, 0xF, true);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)k, 0x138, 0xF, 0xF, true);
+    return (uint64_t)hi << 32 | lo;
+}
+
 // The best k keys a wave has seen, best first by lane (0 past them).
 struct Best {
     uint64_t mine = 0, last = 0;  // last: the k-th
@@ -77,7 +92,7 @@ struct Best {
             const int from = __builtin_ctzll(who);
             const uint64_t x = lane_key(key, from);
             const int place = __popcll(__ballot(mine > x));
-            const uint64_t up = __shfl_up((unsigned long long)mine, 1);
+            const uint64_t up = key_before(mine);
             mine = lane < place ? mine : lane == place ? x : up;
             last = lane_key(mine, k - 1);
             who &= ~(1ull << from) & __ballot(key > last);
@@ -85,28 +100,49 @@ struct Best {
     }
 };
 
-// The k-th largest of the lanes' codes (0 where fewer lanes have one).
+template <int kControl>
+__device__ __forceinline__ uint32_t max_moved(uint32_t x)
+{
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, (int)x, kControl, 0xF, 0xF, true);
+    return x > y ? x : y;
+}
+
+// At most the k-th largest of the lanes' codes (0 where fewer lanes have one): with k = 1
+// the largest, else its first 16 bits.
 __device__ __forceinline__ uint32_t kth_code(uint32_t code, int k)
 {
+    if (k == 1) {
+        code = max_moved<0x140>(max_moved<0x141>(max_moved<0x4E>(max_moved<0xB1>(code))));
+        auto r = __builtin_amdgcn_permlane16_swap(code, code, false, false);
+        code = r[0] > r[1] ? r[0] : r[1];
+        r = __builtin_amdgcn_permlane32_swap(code, code, false, false);
+        return r[0] > r[1] ? r[0] : r[1];
+    }
     uint32_t at = 0;
-    for (int bit = 31; bit >= 0; bit--) {
+#pragma unroll
+    for (int bit = 31; bit >= 16; bit--) {
         const uint32_t up = at | 1u << bit;
-        if (__popcll(__ballot(code >= up)) >= k)
-            at = up;
+        at = __popcll(__ballot(code >= up)) >= k ? up : at;
     }
     return at;
 }
 
+// A row as loads of 16 bytes, aligned; `off` values of the first lie before it.
 template <typename X>
 struct Row {
-    static constexpr int E = 16 / sizeof(X);  // values of a 16-byte load
+    static constexpr int E = 16 / sizeof(X);
     const X* x;
-    int V, off;  // off: values before the row in its first 16 bytes
+    int V, off;
 
-    __device__ __forceinline__ Row(const X* row, int v) : x(row), V(v), off((int)((uintptr_t)row % 16) / (int)sizeof(X)) {}
+    __device__ __forceinline__ Row(const X* row, int v)
+        : x(row), V(v), off((int)((uintptr_t)row % 16) / (int)sizeof(X))
+    {
+    }
     __device__ __forceinline__ int64_t loads() const { return ((int64_t)V + off + E - 1) / E; }
     // The first token of load g.
     __device__ __forceinline__ int64_t token(int64_t g) const { return g * E - off; }
+    // Whether all values of load g are the row's.
+    __device__ __forceinline__ bool whole(int64_t g) const { return token(g) >= 0 && token(g) + E <= V; }
     static __device__ __forceinline__ float value(float v) { return v; }
     static __device__ __forceinline__ float value(uint16_t v) { return bf16_bits_to_float(v); }
     __device__ __forceinline__ float one(int64_t token) const { return value(x[token]); }
@@ -117,53 +153,78 @@ struct Row {
             return __uint_as_float(w[e & 3]);
         return __uint_as_float(e & 1 ? w[e >> 1 & 3] & 0xFFFF0000u : w[e >> 1 & 3] << 16);
     }
+    // -inf in every place.
+    static __device__ __forceinline__ u32x4 none()
+    {
+        const uint32_t w = E == 4 ? 0xFF800000u : 0xFF80FF80u;
+        return u32x4{w, w, w, w};
+    }
+    // Load g with -inf where it leaves the row.
+    __device__ __forceinline__ u32x4 part(int64_t g) const
+    {
+        u32x4 w = none();
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            if (token(g) + e >= 0 && token(g) + e < V) {
+                if (E == 4)
+                    w[e & 3] = __float_as_uint(one(token(g) + e));
+                else
+                    w[e >> 1 & 3] = e & 1 ? (w[e >> 1 & 3] & 0xFFFFu) | __float_as_uint(one(token(g) + e))
+                                          : (w[e >> 1 & 3] & 0xFFFF0000u) | __float_as_uint(one(token(g) + e)) >> 16;
+            }
+        return w;
+    }
 };
 
-// The part [g0, g1) of a row's loads: the workgroup's sums (in thread 0) and, with k,
-// its best k keys in lds_keys[0 .. k) (0 past them).
-template <typename X>
-__device__ __forceinline__ Sums scan_part(const Row<X>& row, int64_t g0, int64_t g1, int k, uint64_t* lds_keys,
-                                          Sums* lds_sums, uint32_t* lds_bound)
+// LDS of a workgroup of NT threads.
+template <int NT>
+struct Shared {
+    uint64_t keys[NT / 64 * OIL_TOPK_MAX];
+    Sums sums[NT / 64];
+    uint32_t bound;
+};
+
+// The part [g0, g1) of a row's loads by NT threads: in the first wave, the part's sums in
+// every lane, and the i-th best key in lane i (0 past the k).
+template <typename X, int NT>
+__device__ __forceinline__ void scan_part(const Row<X>& row, int64_t g0, int64_t g1, int k, Shared<NT>& lds, Sums* sums,
+                                          uint64_t* key)
 {
     constexpr int E = Row<X>::E;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Sums a = {kLowest, 0.f, 0.f};
     Best best;
     uint32_t bound = 0;  // code below which nothing enters
     if (threadIdx.x == 0)
-        *lds_bound = 0;
+        lds.bound = 0;
     __syncthreads();
     bool begun = false;
-    for (int64_t g = g0 + wave * (64 * kDeep); g < g1; g += kThreads * kDeep) {
-        float x[kDeep][E];
-        const bool whole = g + 64 * kDeep <= g1 && row.token(g) >= 0 && row.token(g + 64 * kDeep) <= row.V;
-        if (whole) {
-            u32x4 w[kDeep];
+    for (int64_t g = g0 + wave * 64; g < g1; g += NT * kDeep) {
+        u32x4 w[kDeep];
+        const bool inner = row.whole(g) && g + NT * (kDeep - 1) + 64 <= g1 && row.whole(g + NT * (kDeep - 1) + 63);
+        int n = kDeep;  // loads of this step
+        if (inner) {
 #pragma unroll
             for (int i = 0; i < kDeep; i++)
-                w[i] = row.load(g + i * 64 + lane);
-#pragma unroll
-            for (int i = 0; i < kDeep; i++)
-#pragma unroll
-                for (int e = 0; e < E; e++)
-                    x[i][e] = Row<X>::of(w[i], e);
+                w[i] = row.load(g + i * NT + lane);
         } else {
+            n = 0;
 #pragma unroll
-            for (int i = 0; i < kDeep; i++)
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    const int64_t at = g + i * 64 + lane, token = row.token(at) + e;
-                    x[i][e] = at < g1 && token >= 0 && token < row.V ? row.one(token) : -INFINITY;
-                }
+            for (int i = 0; i < kDeep; i++) {
+                const int64_t at = g + i * NT + lane;
+                w[i] = Row<X>::none();
+                if (at < g1)
+                    w[i] = row.whole(at) ? row.load(at) : row.part(at);
+                n += g + i * NT < g1;
+            }
         }
-        float top[kDeep];
-        float most = kLowest;
+        float top[kDeep], most = kLowest;
 #pragma unroll
         for (int i = 0; i < kDeep; i++) {
-            top[i] = x[i][0];
+            top[i] = Row<X>::of(w[i], 0);
 #pragma unroll
             for (int e = 1; e < E; e++)
-                top[i] = fmaxf(top[i], x[i][e]);
+                top[i] = fmaxf(top[i], Row<X>::of(w[i], e));
             most = fmaxf(most, top[i]);
         }
         const float m = fmaxf(a.m, most);
@@ -171,26 +232,29 @@ __device__ __forceinline__ Sums scan_part(const Row<X>& row, int64_t g0, int64_t
         a.t = fmaf(y, a.s, a.t) * f;
         a.s *= f;
         a.m = m;
-        float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kDeep; i++)
+        for (int i = 0; i < kDeep; i++) {
+            if (i >= n)
+                break;
+            float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const float z = (x[i][e] - m) * kLog2e, p = __builtin_amdgcn_exp2f(z);
+                const float z = (Row<X>::of(w[i], e) - m) * kLog2e, p = __builtin_amdgcn_exp2f(z);
                 s[e & 1] += p;
                 t[e & 1] = fmaf(fmaxf(z, kLeast), p, t[e & 1]);
             }
-        a.s += s[0] + s[1];
-        a.t += t[0] + t[1];
+            a.s += s[0] + s[1];
+            a.t += t[0] + t[1];
+        }
         if (k == 0)
             continue;
-        uint32_t code = score_code(most);
+        const uint32_t code = score_code(most);
         if (!begun) {
             begun = true;
             const uint32_t c = kth_code(code, k);
             bound = c > bound ? c : bound;
         }
-        const uint32_t others = *(volatile uint32_t*)lds_bound;
+        const uint32_t others = *(volatile uint32_t*)&lds.bound;
         bound = others > bound ? others : bound;
         if (!__ballot(code >= bound))
             continue;
@@ -200,33 +264,46 @@ __device__ __forceinline__ Sums scan_part(const Row<X>& row, int64_t g0, int64_t
                 continue;
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const uint64_t key = token_key(x[i][e], (uint32_t)(row.token(g + i * 64 + lane) + e));
-                best.add((uint32_t)(key >> 32) >= bound ? key : 0ull, lane, k);
+                const float x = Row<X>::of(w[i], e);
+                const bool enters = score_code(x) >= bound;
+                if (__ballot(enters))
+                    best.add(enters ? token_key(x, (uint32_t)(row.token(g + i * NT + lane) + e)) : 0ull, lane, k);
             }
         }
         const uint32_t mine = (uint32_t)(best.last >> 32);
         if (mine > bound) {
             bound = mine;
             if (lane == 0)
-                atomicMax(lds_bound, mine);
+                atomicMax(&lds.bound, mine);
         }
     }
     a = join_wave(a);
     if (lane == 0)
-        lds_sums[wave] = a;
+        lds.sums[wave] = a;
     if (lane < k)
-        lds_keys[wave * k + lane] = best.mine;
+        lds.keys[wave * k + lane] = best.mine;
+    __syncthreads();
+    // keys' places: how many are above; the best k to the front, in order
+    const int all = NT / 64 * k;
+    uint64_t mine = 0;
+    int above = 0;
+    if ((int)threadIdx.x < all) {
+        mine = lds.keys[threadIdx.x];
+        for (int i = 0; i < all; i++)
+            above += lds.keys[i] > mine;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < k)
+        lds.keys[threadIdx.x] = 0;
+    __syncthreads();
+    if (mine && above < k)
+        lds.keys[above] = mine;
     __syncthreads();
     if (wave == 0) {
-        for (int i = 1; i < kWaves; i++) {
-            a = join(a, lds_sums[i]);
-            if (k)
-                best.add(lane < k ? lds_keys[i * k + lane] : 0ull, lane, k);
-        }
-        if (lane < k)
-            lds_keys[lane] = best.mine;
+        a = lane < NT / 64 ? lds.sums[lane] : Sums{kLowest, 0.f, 0.f};
+        *sums = join_wave(a);
+        *key = lane < k ? lds.keys[lane] : 0ull;
     }
-    return a;
 }
 
 // What a row of which a is known gives; by one wave, whose lane i has the i-th best key.
@@ -247,8 +324,9 @@ __device__ __forceinline__ void write_row(const Row<X>& row, int64_t r, Sums a, 
     if (entropy && lane == 0)
         entropy[r] = none ? 0.f : fmaf(-kLn2, a.t / a.s, log_s);
     if (lane < k) {
+        const float x = code_score((uint32_t)(key >> 32));
         top_tokens[r * k + lane] = key ? (int32_t)key_pos(key) : -1;
-        top_logprobs[r * k + lane] = key ? code_score((uint32_t)(key >> 32)) - a.m - log_s : -INFINITY;
+        top_logprobs[r * k + lane] = key ? x - a.m - log_s : -INFINITY;
     }
 }
 
@@ -265,90 +343,95 @@ __device__ __forceinline__ void write_none(int64_t r, int M, int k, float* logpr
     }
 }
 
-// One workgroup a (row, part); with one part the row's outputs, else a Part and keys.
-template <typename X>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(const X* __restrict__ logits, int64_t ld, int32_t V,
-                                                            int32_t max_rows, const int32_t* __restrict__ n_rows,
-                                                            const int32_t* __restrict__ tokens, int32_t M, int32_t k,
-                                                            int32_t parts, Part* __restrict__ part,
-                                                            uint64_t* __restrict__ part_keys,
-                                                            float* __restrict__ logprob, float* __restrict__ entropy,
-                                                            int32_t* __restrict__ top_tokens,
-                                                            float* __restrict__ top_logprobs)
+struct Call {
+    int64_t ld;
+    int32_t V, max_rows, M, k, parts;
+    const int32_t* n_rows;
+    const int32_t* tokens;
+    Sums* part;       // parts a row
+    uint64_t* keys;   // k a part
+    float *logprob, *entropy, *top_logprobs;
+    int32_t* top_tokens;
+
+    __device__ __forceinline__ bool none(int64_t r) const
+    {
+        return n_rows && (int)(r % max_rows) >= n_rows[r / max_rows];
+    }
+};
+
+// One workgroup a (row, part); with one part the row's outputs, else its sums and keys.
+template <typename X, int NT>
+__global__ __launch_bounds__(NT) void logprobs_kernel(const X* __restrict__ logits, Call c)
 {
-    __shared__ uint64_t lds_keys[kWaves * OIL_TOPK_MAX];
-    __shared__ Sums lds_sums[kWaves];
-    __shared__ uint32_t lds_bound;
-    const int64_t r = blockIdx.x / parts;
-    const int p = blockIdx.x % parts, lane = threadIdx.x & 63;
-    if (n_rows && (int)(r % max_rows) >= n_rows[r / max_rows]) {
-        if (parts == 1)
-            write_none(r, M, k, logprob, entropy, top_tokens, top_logprobs);
+    __shared__ Shared<NT> lds;
+    const int64_t r = blockIdx.x / c.parts;
+    const int p = blockIdx.x % c.parts, lane = threadIdx.x & 63;
+    if (c.none(r)) {
+        if (c.parts == 1)
+            write_none(r, c.M, c.k, c.logprob, c.entropy, c.top_tokens, c.top_logprobs);
         return;
     }
-    const Row<X> row(logits + r * ld, V);
-    const int64_t all = row.loads(), per = (all + parts - 1) / parts;
+    const Row<X> row(logits + r * c.ld, c.V);
+    const int64_t all = row.loads(), per = (all + c.parts - 1) / c.parts;
     const int64_t g0 = p * per, g1 = g0 + per < all ? g0 + per : all;
-    const Sums a = scan_part(row, g0, g1, k, lds_keys, lds_sums, &lds_bound);
+    Sums a;
+    uint64_t key;
+    scan_part<X, NT>(row, g0, g1, c.k, lds, &a, &key);
     if (threadIdx.x >= 64)
         return;
-    const uint64_t key = lane < k ? lds_keys[lane] : 0ull;
-    if (parts == 1) {
-        write_row(row, r, a, key, tokens, M, k, logprob, entropy, top_tokens, top_logprobs);
-    } else {
-        if (lane == 0)
-            part[r * parts + p] = Part{a, 0.f};
-        if (lane < k)
-            part_keys[(r * parts + p) * k + lane] = key;
+    if (c.parts == 1) {
+        write_row(row, r, a, key, c.tokens, c.M, c.k, c.logprob, c.entropy, c.top_tokens, c.top_logprobs);
+        return;
     }
+    if (lane == 0)
+        c.part[r * c.parts + p] = a;
+    if (lane < c.k)
+        c.keys[(r * c.parts + p) * c.k + lane] = key;
 }
 
-// One wave a row.
+// One wave a row; parts' lists by depth, so that what comes later seldom enters.
 template <typename X>
-__global__ __launch_bounds__(64) void logprobs_join_kernel(const X* __restrict__ logits, int64_t ld, int32_t V,
-                                                           int32_t max_rows, const int32_t* __restrict__ n_rows,
-                                                           const int32_t* __restrict__ tokens, int32_t M, int32_t k,
-                                                           int32_t parts, const Part* __restrict__ part,
-                                                           const uint64_t* __restrict__ part_keys,
-                                                           float* __restrict__ logprob, float* __restrict__ entropy,
-                                                           int32_t* __restrict__ top_tokens,
-                                                           float* __restrict__ top_logprobs)
+__global__ __launch_bounds__(64) void logprobs_join_kernel(const X* __restrict__ logits, Call c)
 {
     const int64_t r = blockIdx.x;
     const int lane = threadIdx.x;
-    if (n_rows && (int)(r % max_rows) >= n_rows[r / max_rows]) {
-        write_none(r, M, k, logprob, entropy, top_tokens, top_logprobs);
+    if (c.none(r)) {
+        write_none(r, c.M, c.k, c.logprob, c.entropy, c.top_tokens, c.top_logprobs);
         return;
     }
-    const Row<X> row(logits + r * ld, V);
-    Sums a = {kLowest, 0.f, 0.f};
-    for (int p = lane; p < parts; p += 64)
-        a = join(a, part[r * parts + p].sums);
-    a = join_wave(a);
+    const Row<X> row(logits + r * c.ld, c.V);
     Best best;
-    for (int i = 0; i < parts * k; i += 64)
-        best.add(i + lane < parts * k ? part_keys[r * parts * k + i + lane] : 0ull, lane, k);
-    write_row(row, r, a, best.mine, tokens, M, k, logprob, entropy, top_tokens, top_logprobs);
+    for (int i = 0; i < c.parts * c.k; i += 64) {
+        const int at = i + lane, depth = at / c.parts, p = at - depth * c.parts;
+        best.add(at < c.parts * c.k ? c.keys[(r * c.parts + p) * c.k + depth] : 0ull, lane, c.k);
+    }
+    const Sums a = join_wave(lane < c.parts ? c.part[r * c.parts + lane] : Sums{kLowest, 0.f, 0.f});
+    write_row(row, r, a, best.mine, c.tokens, c.M, c.k, c.logprob, c.entropy, c.top_tokens, c.top_logprobs);
 }
 
-constexpr int64_t kWorkgroups = 2048;  // 8 a CU
+constexpr int kThreads = 256, kWideThreads = 1024;  // of a workgroup
+constexpr int64_t kFewBytes = 160 << 10;            // of a row that one wide workgroup reads
 
-// Workgroups a row of V logits is cut among where there are `rows` of them: as many as
-// fill the chip, each with one step of its loads at least.
+// Workgroups a row is cut among, 16 KiB each at least (a step of their loads): one where
+// rows fill the chip with four a CU.
 int32_t row_parts(int64_t rows, int32_t V, int size)
 {
-    const int64_t steps = ((int64_t)V * size / 16 + kThreads * kDeep) / (kThreads * kDeep);
-    const int64_t want = (kWorkgroups + rows - 1) / rows;
-    const int64_t n = want < steps ? want : steps;
+    const int64_t bytes = (int64_t)V * size, most = (bytes + (16 << 10) - 1) / (16 << 10), want = 1024 / rows;
+    if (bytes <= kFewBytes && rows <= 512)
+        return 1;
+    const int64_t n = want < most ? want : most;
     return (int32_t)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
+
+// Whether a row's one workgroup is wide: where rows leave CUs without one otherwise.
+bool wide(int64_t rows, int32_t parts) { return parts == 1 && rows <= 512; }
 
 }  // namespace
 
 size_t logprobs_workspace_bytes(int64_t rows, int32_t V, int dtype, int32_t k)
 {
     const int64_t parts = row_parts(rows, V, dtype == 0 ? 4 : 2);
-    return parts == 1 ? 256 : (size_t)(rows * parts) * (sizeof(Part) + 8 * (size_t)k) + 256;
+    return parts == 1 ? 256 : (size_t)(rows * parts) * (8 * (size_t)k + sizeof(Sums)) + 256;
 }
 
 hipError_t launch_logprobs(int64_t rows, int32_t max_rows, const int32_t* n_rows, const void* logits, int dtype,
@@ -357,15 +440,18 @@ hipError_t launch_logprobs(int64_t rows, int32_t max_rows, const int32_t* n_rows
                            hipStream_t stream)
 {
     const int32_t parts = row_parts(rows, V, dtype == 0 ? 4 : 2);
-    Part* part = (Part*)workspace;
-    uint64_t* keys = (uint64_t*)(part + rows * parts);
-#define OIL_LOGPROBS(X)                                                                                             \
-    hipLaunchKernelGGL(logprobs_kernel<X>, dim3((uint32_t)(rows * parts)), dim3(kThreads), 0, stream,              \
-                       (const X*)logits, ld, V, max_rows, n_rows, tokens, M, k, parts, part, keys, logprob, entropy, \
-                       top_tokens, top_logprobs);                                                                  \
-    if (parts > 1)                                                                                                 \
-    hipLaunchKernelGGL(logprobs_join_kernel<X>, dim3((uint32_t)rows), dim3(64), 0, stream, (const X*)logits, ld, V, \
-                       max_rows, n_rows, tokens, M, k, parts, part, keys, logprob, entropy, top_tokens, top_logprobs)
+    uint64_t* keys = (uint64_t*)workspace;
+    const Call c = {ld,     V,    max_rows, M,       k,       parts,        n_rows,
+                    tokens, (Sums*)(keys + rows * parts * k), keys, logprob, entropy, top_logprobs, top_tokens};
+#define OIL_LOGPROBS(X)                                                                                              \
+    if (wide(rows, parts))                                                                                          \
+        hipLaunchKernelGGL((logprobs_kernel<X, kWideThreads>), dim3((uint32_t)rows), dim3(kWideThreads), 0, stream, \
+                           (const X*)logits, c);                                                                    \
+    else                                                                                                            \
+        hipLaunchKernelGGL((logprobs_kernel<X, kThreads>), dim3((uint32_t)(rows * parts)), dim3(kThreads), 0,       \
+                           stream, (const X*)logits, c);                                                            \
+    if (parts > 1)                                                                                                  \
+    hipLaunchKernelGGL(logprobs_join_kernel<X>, dim3((uint32_t)rows), dim3(64), 0, stream, (const X*)logits, c)
     if (dtype == 0) {
         OIL_LOGPROBS(float);
     } else {

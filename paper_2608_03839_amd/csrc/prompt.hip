@@ -32,7 +32,8 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 #define LDS_PTR(T, p) ((T __attribute__((address_space(3)))*)(p))
 
 constexpr int kKeys = 64;       // keys of a tile
-constexpr int kWeighKeys = 64;  // keys of a wave
+constexpr int kWeighKeys = 64;   // keys of a wave
+constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kOutside = 0xF0000000u;  // a byte offset past every buffer's end: reads as zero
@@ -70,37 +71,68 @@ struct Tile {
     int first, len, tile, pad;
 };
 
-// The tiles of all sequences, (len * per + rows - 1) / rows of each, those of the largest
-// number first (the heaviest: theirs is the longest pass), ties by sequence.  Thread t
-// writes all tiles numbered t, from N(t + 1) = sum of max(0, tiles - t - 1) on.
-// One workgroup: 48 sequences of up to 47 tiles in 5 us.
-__global__ __launch_bounds__(1024) void prompt_schedule_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
-                                                               int32_t per, int32_t rows, Tile* __restrict__ list,
-                                                               int32_t places)
+template <int kControl>
+__device__ __forceinline__ int add_moved(int x)
 {
-    __shared__ int count[kMaxSeqs], from[kMaxSeqs], size[kMaxSeqs], most;
-    if (threadIdx.x == 0)
-        most = 0;
-    __syncthreads();
-    for (int s = threadIdx.x; s < B; s += blockDim.x) {
-        from[s] = seq_first(starts, T, s);
-        size[s] = seq_end(starts, T, s) - from[s];
-        count[s] = (int)(((int64_t)size[s] * per + rows - 1) / rows);
-        atomicMax(&most, count[s]);
+    return x + __builtin_amdgcn_update_dpp(0, x, kControl, 0xF, 0xF, true);
+}
+
+// The sum over a wave, in every lane.
+__device__ __forceinline__ int wave_sum(int x)
+{
+    x = add_moved<0xB1>(x);   // lane ^ 1
+    x = add_moved<0x4E>(x);   // lane ^ 2
+    x = add_moved<0x141>(x);  // mirrored in 8
+    x = add_moved<0x140>(x);  // mirrored in 16
+    auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = r[0] + r[1];
+    r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return __builtin_amdgcn_readfirstlane(r[0] + r[1]);
+}
+
+// The tiles of all sequences, (len * per + rows - 1) / rows of each, those of the largest
+// number first (the heaviest: theirs is the longest pass), ties by sequence.  A wave takes
+// every so many numbers t and writes the tiles numbered t from N(t + 1) = sum of max(0,
+// tiles - t - 1) on, a lane eight sequences at most.  (A search in every workgroup of
+// attention took 3.3 us of 28; the list, for 48 sequences of up to 47 tiles, 4 us in all.)
+constexpr int kListWaves = 128;
+
+__global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
+                                                          int32_t per, int32_t rows, Tile* __restrict__ list,
+                                                          int32_t places)
+{
+    const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
+    int from[kMaxSeqs / 64], size[kMaxSeqs / 64], n[kMaxSeqs / 64], all = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxSeqs / 64; i++) {
+        const int s = i * 64 + lane;
+        from[i] = size[i] = n[i] = 0;
+        if (s < B) {
+            from[i] = seq_first(starts, T, s);
+            size[i] = seq_end(starts, T, s) - from[i];
+            n[i] = (int)(((int64_t)size[i] * per + rows - 1) / rows);
+        }
+        all += n[i];
+        most = n[i] > most ? n[i] : most;
     }
-    __syncthreads();
-    for (int t = threadIdx.x; t <= most; t += blockDim.x) {
+    all = wave_sum(all);
+    for (int t = wave; __ballot(most > t); t += kListWaves) {
         int place = 0;
-        for (int s = 0; s < B; s++)
-            place += count[s] > t + 1 ? count[s] - t - 1 : 0;
-        for (int s = 0; s < B && place < places; s++)
-            if (count[s] > t)
-                list[place++] = Tile{from[s], size[s], t, 0};
+#pragma unroll
+        for (int i = 0; i < kMaxSeqs / 64; i++)
+            place += n[i] > t + 1 ? n[i] - t - 1 : 0;
+        place = wave_sum(place);
+#pragma unroll
+        for (int i = 0; i < kMaxSeqs / 64; i++) {
+            const uint64_t has = __ballot(n[i] > t);
+            const int at = place + __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32),
+                                                             __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
+            if (n[i] > t && at < places)
+                list[at] = Tile{from[i], size[i], t, 0};
+            place += __popcll(has);
+        }
     }
-    int all = 0;
-    for (int s = 0; s < B; s++)
-        all += count[s];
-    for (int i = all + threadIdx.x; i < places; i += blockDim.x)
+    for (int64_t i = (int64_t)all + wave * 64 + lane; i < places; i += kListWaves * 64)
         list[i] = Tile{0, 0, 0, 0};
 }
 
@@ -488,19 +520,24 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
         }
 }
 
-// kWeighKeys keys a wave, NW waves; rows 64 at a time from LDS.
+// kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS, 32 of them
+// multiplied while the exponentials of the 32 before are made.  Of the rows that count for
+// a tile of keys the workgroup takes blockIdx.y's `chunk` tokens' and writes part
+// blockIdx.y of the sum (a plane of n_heads x T), so that the first keys, which most rows
+// see, do not take longest.
 template <int W, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const Tile* __restrict__ list, const int32_t* __restrict__ starts, int32_t T, const uint16_t* __restrict__ q,
-    int64_t q_ld, int32_t G,
-    const float* __restrict__ lse, const uint16_t* __restrict__ k, int64_t ld, int32_t H, int32_t D, int32_t last,
-    float scale, float* __restrict__ weight)
+    int64_t q_ld, int32_t G, const float* __restrict__ lse, const uint16_t* __restrict__ k, int64_t ld, int32_t H,
+    int32_t D, int32_t last, int32_t chunk, float scale, float* __restrict__ weight)
 {
-    constexpr int kRowTile = 64, kTile = kRowTile * W * 2, kLoads = kTile / 1024 / NW, kBlock = kWeighKeys * NW;
+    constexpr int kTile = kWeighRows * W * 2, kLoads = kTile / 1024 / NW, kBlock = kWeighKeys * NW;
+    constexpr int kParts = kWeighRows / 32;
+    static_assert(NW * 64 >= kWeighRows, "a thread brings a row's lse");
     __shared__ __align__(1024) uint8_t row_lds[2][kTile];
-    __shared__ __align__(16) float less_lds[2][kRowTile];
-    __shared__ __align__(16) int token_lds[2][kRowTile];  // -1: the row counts nowhere
-    __shared__ int none_lds[2];                           // whether the tile has such a row
+    __shared__ __align__(16) float less_lds[2][kWeighRows];
+    __shared__ __align__(16) int token_lds[2][kWeighRows];  // -1: the row counts nowhere
+    __shared__ int none_lds[2][NW];                         // whether the wave brought such a row
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % H;
@@ -509,45 +546,48 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     if (len == 0)
         return;
     const int key0 = ((len + kBlock - 1) / kBlock - 1 - mine.tile) * kBlock;  // the lowest keys, which most rows see, first
-    const int seen_from = len - last > key0 ? len - last : key0;  // the first token whose rows count here
-    const int row_begin = seen_from * G, rows = len * G - row_begin;  // len * G <= T * Hq <= 2^30
-    const int turns = (rows + kRowTile - 1) / kRowTile;
+    const int all_from = len - last > key0 ? len - last : key0;  // the first token whose rows count here
+    if ((int64_t)blockIdx.y * chunk >= len - all_from)
+        return;
+    const int seen_from = all_from + blockIdx.y * chunk;
+    const int seen_to = len - seen_from < chunk ? len : seen_from + chunk;
+    const int row_begin = seen_from * G, rows = (seen_to - seen_from) * G;  // len * G <= T * Hq <= 2^30
+    const int turns = (rows + kWeighRows - 1) / kWeighRows;
     const float c = fabsf(scale) * kLog2e;
-    const uint32_t magic = 65536 / G + 1;  // x / G = x magic >> 16 for x < 128, G <= 64
+    const uint32_t magic = 65536 / G + 1;  // x / G = x magic >> 16 for x < 64 + kWeighRows, G <= 64
 
-    // rows: token seen_from + x / G, head x % G; a tile's are at its first token's base
-    uint32_t chunk_from[kLoads];
-    int row_of[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; i++) {
-        const int at = (wave * kLoads + i) * 64 + lane, r = at / (W / 8);
-        const int qc = key_place<W>(r, at % (W / 8)) - r * (W / 8);
-        row_of[i] = r;
-        chunk_from[i] = qc * 8 < D ? qc * 16 : kOutside;
-    }
+    // A tile's rows are read from its first token's base: row x = rem + i is token x / G,
+    // head x % G.  Rows past the last token's lie past the buffer's end.
+    uint32_t from[kLoads];
+    int from_rem = -1;
     float next_less = 0.f;
     int next_token = 0;
     auto load = [&](int t) {
-        const int row0 = row_begin + t * kRowTile;
+        const int row0 = row_begin + t * kWeighRows;
         const int token0 = row0 / G, rem = row0 - token0 * G;
-        const int here = rows - t * kRowTile < kRowTile ? rows - t * kRowTile : kRowTile;
-        const int tokens = ((rem + here - 1) / G);
-        const u32x4 r = rows_at(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D,
-                                                 tokens * q_ld * 2 + (int64_t)G * D * 2);
+        const int here = rows - t * kWeighRows < kWeighRows ? rows - t * kWeighRows : kWeighRows;
+        const int tokens = (rem + here - 1) / G;
+        if (rem != from_rem) {
+            from_rem = rem;
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            const uint32_t x = rem + row_of[i], d = x * magic >> 16;
-            const uint32_t from = row_of[i] < here && chunk_from[i] != kOutside
-                                      ? (uint32_t)(d * q_ld * 2) + (x - d * G) * D * 2 + chunk_from[i]
-                                      : kOutside;
-            load_kib(r, &row_lds[t & 1][(wave * kLoads + i) * 1024], from);
+            for (int i = 0; i < kLoads; i++) {
+                const int at = (wave * kLoads + i) * 64 + lane, r = at / (W / 8);
+                const int qc = key_place<W>(r, at % (W / 8)) - r * (W / 8);
+                const uint32_t x = rem + r, d = x * magic >> 16;
+                from[i] = qc * 8 < D ? (uint32_t)(d * q_ld * 2) + (x - d * G) * D * 2 + qc * 16 : kOutside;
+            }
         }
-        if (wave == 0) {
-            const uint32_t x = rem + lane, d = x * magic >> 16;
+        const u32x4 r = rows_at(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D,
+                                tokens * q_ld * 2 + (int64_t)G * D * 2);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            load_kib(r, &row_lds[t & 1][(wave * kLoads + i) * 1024], from[i]);
+        if ((int)threadIdx.x < kWeighRows) {
+            const uint32_t x = rem + threadIdx.x, d = x * magic >> 16;
             float y = -INFINITY;
-            if (lane < here)
+            if ((int)threadIdx.x < here)
                 y = lse[((int64_t)first + token0 + d) * (H * G) + h * G + (x - d * G)];
-            next_less = y * kLog2e;
+            next_less = y * -kLog2e;
             next_token = y == -INFINITY ? -1 : (int)(token0 + d);
         }
     };
@@ -561,11 +601,11 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     for (int b = 0; b < 2; b++) {
         key[b] = key0 + wave * kWeighKeys + b * 32 + col;
         const int at = key[b] < len ? key[b] : len - 1;
-        const uint16_t* from = k + ((int64_t)first + at) * ld + (int64_t)h * D;
+        const uint16_t* row = k + ((int64_t)first + at) * ld + (int64_t)h * D;
 #pragma unroll
         for (int i = 0; i < W / 16; i++) {
             const int d = i * 16 + half * 8;
-            ks[b][i].w = d < D ? *(const u32x4*)(from + d) : u32x4{0, 0, 0, 0};
+            ks[b][i].w = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
             ks[b][i].w ^= turn;
         }
     }
@@ -574,78 +614,105 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     for (int i = 0; i < W / 16; i++)
         row_at[i] = key_place<W>(col, 2 * i + half) * 16;
 
+    // S of the tile's rows 32 a .. 32 a + 31
+    typedef floatx16 Scores[2];
+    auto scores = [&](int t, int a, Scores& s) {
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                s[b][r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W / 16; i++) {
+            const bf16x8 x = *(const bf16x8*)(row_lds[t & 1] + row_at[i] + a * 32 * W * 2);
+#pragma unroll
+            for (int b = 0; b < 2; b++)
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, ks[b][i].b, s[b], 0, 0, 0);
+        }
+    };
+    float total[2] = {0.f, 0.f}, part[2][2] = {};  // parts of 16 tiles, so that long sums lose little
+    auto add = [&](int t, int a, Scores& s, auto edge) {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const floatx4 less = *(const floatx4*)&less_lds[t & 1][a * 32 + 2 * r + 4 * half];
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+#pragma unroll
+                for (int b = 0; b < 2; b++) {
+                    float x = __builtin_amdgcn_exp2f(fmaf(s[b][r + e], c, less[e]));
+                    if (decltype(edge)::value)
+                        x = key[b] <= token_lds[t & 1][a * 32 + 2 * r + 4 * half + e] ? x : 0.f;
+                    part[b][e & 1] += x;
+                }
+        }
+    };
+
     const int wave_key = key0 + wave * kWeighKeys + kWeighKeys - 1;  // the wave's last
-    float total[2] = {0.f, 0.f}, part[2] = {0.f, 0.f};  // parts of 32 tiles, so that long sums lose little
     for (int t = 0; t < turns; t++) {
         loads_done();
-        if (wave == 0) {
-            less_lds[t & 1][lane] = next_less;
-            token_lds[t & 1][lane] = next_token;
-            const bool none = __ballot(next_token < 0) != 0;
-            if (lane == 0)
-                none_lds[t & 1] = none;
+        if ((int)threadIdx.x < kWeighRows) {
+            less_lds[t & 1][threadIdx.x] = next_less;
+            token_lds[t & 1][threadIdx.x] = next_token;
         }
+        const int any = __ballot((int)threadIdx.x < kWeighRows && next_token < 0) != 0;
+        if (lane == 0)
+            none_lds[t & 1][wave] = any;
         __syncthreads();
         if (t + 1 < turns)
             load(t + 1);
-        const int token0 = (row_begin + t * kRowTile) / G;
-        const bool edge = token0 < wave_key || none_lds[t & 1];
+        int none = 0;
 #pragma unroll
-        for (int a = 0; a < 2; a++) {
-            floatx16 s[2];
-#pragma unroll
-            for (int b = 0; b < 2; b++)
-#pragma unroll
-                for (int r = 0; r < 16; r++)
-                    s[b][r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < W / 16; i++) {
-                const bf16x8 x = *(const bf16x8*)(row_lds[t & 1] + row_at[i] + a * 32 * W * 2);
-#pragma unroll
-                for (int b = 0; b < 2; b++)
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, ks[b][i].b, s[b], 0, 0, 0);
+        for (int i = 0; i < NW; i++)
+            none |= none_lds[t & 1][i];
+        Scores s[2];
+        if ((row_begin + t * kWeighRows) / G < wave_key || __builtin_amdgcn_readfirstlane(none)) {
+#pragma unroll 1
+            for (int a = 0; a < kParts; a++) {
+                scores(t, a, s[0]);
+                add(t, a, s[0], std::true_type());
             }
+        } else {
+            scores(t, 0, s[0]);
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const floatx4 less = *(const floatx4*)&less_lds[t & 1][a * 32 + 2 * r + 4 * half];
-#pragma unroll
-                for (int b = 0; b < 2; b++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        s[b][r + e] = __builtin_amdgcn_exp2f(fmaf(s[b][r + e], c, -less[e]));
-            }
-            if (edge) {
-#pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const int token = token_lds[t & 1][a * 32 + 8 * (r / 4) + 4 * half + r % 4];
-#pragma unroll
-                    for (int b = 0; b < 2; b++)
-                        s[b][r] = key[b] <= token ? s[b][r] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < 2; b++) {
-                float two[2] = {0.f, 0.f};
-#pragma unroll
-                for (int r = 0; r < 16; r++)
-                    two[r & 1] += s[b][r];
-                part[b] += two[0] + two[1];
+            for (int a = 0; a < kParts; a++) {
+                if (a + 1 < kParts)
+                    scores(t, a + 1, s[(a + 1) & 1]);
+                add(t, a, s[a & 1], std::false_type());
             }
         }
-        if ((t & 31) == 31) {
+        if ((t & 15) == 15) {
 #pragma unroll
             for (int b = 0; b < 2; b++) {
-                total[b] += part[b];
-                part[b] = 0.f;
+                total[b] += part[b][0] + part[b][1];
+                part[b][0] = part[b][1] = 0.f;
             }
         }
     }
 #pragma unroll
     for (int b = 0; b < 2; b++) {
         float x, y;
-        swap32(total[b] + part[b], &x, &y);
+        swap32(total[b] + (part[b][0] + part[b][1]), &x, &y);
         if (half == 0 && key[b] < len)
-            weight[(int64_t)h * T + first + key[b]] = x + y;
+            weight[((int64_t)blockIdx.y * H + h) * T + first + key[b]] = x + y;
+    }
+}
+
+// The parts of every position's weight, added in order.
+__global__ __launch_bounds__(256) void prompt_weigh_join_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
+                                                                int32_t H, int32_t last, int32_t chunk,
+                                                                const float* __restrict__ parts,
+                                                                float* __restrict__ weight, int32_t block)
+{
+    const int s = blockIdx.y, first = seq_first(starts, T, s), len = seq_end(starts, T, s) - first;
+    const int64_t plane = (int64_t)H * T;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < (int64_t)len * H; i += gridDim.x * 256ll) {
+        const int h = (int)(i / len), j = (int)(i - (int64_t)h * len), key0 = j / block * block;
+        const int from = len - last > key0 ? len - last : key0, n = (len - from + chunk - 1) / chunk;
+        const int64_t at = (int64_t)h * T + first + j;
+        float x = parts[at];
+        for (int p = 1; p < n; p++)
+            x += parts[p * plane + at];
+        weight[at] = x;
     }
 }
 
@@ -658,18 +725,43 @@ const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, 
 {
     if (B == 1)
         return nullptr;
-    hipLaunchKernelGGL(prompt_schedule_kernel, dim3(1), dim3(1024), 0, stream, starts, B, T, per, rows,
+    hipLaunchKernelGGL(prompt_list_kernel, dim3(kListWaves / 4), dim3(256), 0, stream, starts, B, T, per, rows,
                        (Tile*)workspace, (int32_t)most_tiles(T, per, rows, B));
     return (const Tile*)workspace;
 }
 
-constexpr int kLeastRows = 64;  // of a tile
+constexpr int kLeastRows = 64;  // of a tile of attention
+constexpr int kWeighBlock = kWeighKeys * 4;
+constexpr int64_t kWeighWork = 2048;  // workgroups that leave no CU idle long, whatever their shares
+
+// Chunks that the rows of a call are cut into, and their tokens.
+int32_t weigh_chunks(int32_t B, int32_t T, int32_t G, int32_t H, int32_t last, int32_t* chunk)
+{
+    const int64_t n = kWeighWork / (most_tiles(T, 1, kWeighBlock, B) * H);
+    const int32_t most = last < T ? last : T, least = (kWeighRows + G - 1) / G;
+    const int64_t want = n < 1 ? most : (most + n - 1) / n;
+    *chunk = (int32_t)(want < least ? least : want);
+    return (most + *chunk - 1) / *chunk;
+}
+
+// 256 where there is none.
+size_t list_bytes(int32_t B, int64_t tiles)
+{
+    return B == 1 ? 256 : 256 + (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256;
+}
 
 }  // namespace
 
-size_t prompt_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H)
+size_t prompt_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H)
 {
-    return B == 1 ? 256 : (size_t)most_tiles(T, Hq / H, kLeastRows, B) * sizeof(Tile);
+    return list_bytes(B, most_tiles(T, Hq / H, kLeastRows, B));
+}
+
+size_t prompt_weigh_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t last)
+{
+    int32_t chunk;
+    const int32_t chunks = weigh_chunks(B, T, Hq / H, H, last, &chunk);
+    return list_bytes(B, most_tiles(T, 1, kWeighBlock, B)) + (chunks > 1 ? (size_t)chunks * H * T * 4 : 0);
 }
 
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
@@ -700,15 +792,25 @@ hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, cons
                                float scale, void* workspace, float* weight, hipStream_t stream)
 {
     const int32_t G = Hq / H;
-#define OIL_PROMPT_WEIGH(W, NW)                                                                                   \
-    hipLaunchKernelGGL((prompt_weigh_kernel<W, NW>), dim3((uint32_t)(most_tiles(T, 1, kWeighKeys * NW, B) * H)),  \
-                       dim3(NW * 64), 0, stream, make_list(starts, B, T, 1, kWeighKeys * NW, workspace, stream),  \
-                       starts, T, (const uint16_t*)q, q_ld, G, lse, (const uint16_t*)k, ld, H, D, last, scale, weight)
+    int32_t chunk;
+    const int32_t chunks = weigh_chunks(B, T, G, H, last, &chunk);
+    const int64_t tiles = most_tiles(T, 1, kWeighBlock, B);
+    const Tile* list = make_list(starts, B, T, 1, kWeighBlock, workspace, stream);
+    float* parts = chunks > 1 ? (float*)((uint8_t*)workspace + list_bytes(B, tiles)) : weight;
+#define OIL_PROMPT_WEIGH(W)                                                                                         \
+    hipLaunchKernelGGL((prompt_weigh_kernel<W, kWeighBlock / kWeighKeys>), dim3((uint32_t)(tiles * H), chunks),    \
+                       dim3(kWeighBlock), 0, stream, list, starts, T, (const uint16_t*)q, q_ld, G, lse,            \
+                       (const uint16_t*)k, ld, H, D, last, chunk, scale, parts)
     if (D <= 64)
-        OIL_PROMPT_WEIGH(64, 4);
+        OIL_PROMPT_WEIGH(64);
     else
-        OIL_PROMPT_WEIGH(128, 4);
+        OIL_PROMPT_WEIGH(128);
 #undef OIL_PROMPT_WEIGH
+    if (chunks > 1) {
+        const int64_t blocks = ((int64_t)T * H / B + 255) / 256;
+        hipLaunchKernelGGL(prompt_weigh_join_kernel, dim3((uint32_t)(blocks < 1 ? 1 : blocks > 1024 ? 1024 : blocks), B),
+                           dim3(256), 0, stream, starts, B, T, H, last, chunk, parts, weight, kWeighBlock);
+    }
     return hipGetLastError();
 }
 

@@ -40,13 +40,20 @@ def test_prompt_statuses(L):
                dict(D=136, q_ld=1024, ld=512), dict(Hq=130, q_ld=130 * 64), dict(q_ld=(1 << 24) + 8),
                dict(ld=(1 << 24) + 8)):
         assert attend(**kw) == -3 and weigh(**kw) == -3, kw
-    need = L.oil_prompt_workspace_bytes(2, 10, 4, 2)
+    need = L.oil_prompt_attend_workspace_bytes(2, 10, 4, 2)
     assert need > 0
     for kw in (dict(ws=None), dict(ws=bad), dict(nb=need - 1)):
-        assert attend(**kw) == -5 and weigh(**kw) == -5, kw
+        assert attend(**kw) == -5, kw
+    need = L.oil_prompt_weigh_workspace_bytes(2, 10, 4, 2, 3)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=bad), dict(nb=need - 1)):
+        assert weigh(**kw) == -5, kw
+    assert L.oil_prompt_attend_workspace_bytes(1, 10, 4, 2) == L.oil_prompt_weigh_workspace_bytes(1, 10, 4, 2, 3) == 256
+    assert attend(B=1, ws=bad) == weigh(B=1, ws=bad) == -5
     for args in ((0, 10, 4, 2), (513, 10, 4, 2), (2, 0, 4, 2), (2, (1 << 28) + 1, 4, 2), (2, 1 << 28, 8, 2), (2, 10, 3, 2),
                  (2, 10, 0, 2), (2, 10, 4, 0), (2, 10, 130, 2), (2, 10, 257, 257)):
-        assert L.oil_prompt_workspace_bytes(*args) == 0, args
+        assert L.oil_prompt_attend_workspace_bytes(*args) == L.oil_prompt_weigh_workspace_bytes(*args, 3) == 0, args
+    assert L.oil_prompt_weigh_workspace_bytes(2, 10, 4, 2, 0) == 0
 
 
 def test_append_packed_refuses_no_handle(L):
@@ -72,7 +79,8 @@ def test_logprobs_statuses(L):
         assert call(**kw) == -3, kw
     need = L.oil_token_logprobs_workspace_bytes(2, 3, 100, 1, 2)
     assert need > 0
-    assert call(ws=None) == call(ws=bad) == call(nb=need - 1) == -5
+    assert call(ws=bad) == call(nb=need - 1) == -5
+    assert call(V=200000, ld=200000, ws=None) == -5
     for args in ((0, 3, 100, 1, 2), (2, 0, 100, 1, 2), (2, 3, 0, 1, 2), (2, 3, 100, 7, 2), (2, 3, 100, 1, 65),
                  (1 << 12, 1 << 12, 100, 1, 2)):
         assert L.oil_token_logprobs_workspace_bytes(*args) == 0, args
