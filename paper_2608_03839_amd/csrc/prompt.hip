@@ -90,11 +90,12 @@ __device__ __forceinline__ int wave_sum(int x)
     return __builtin_amdgcn_readfirstlane(r[0] + r[1]);
 }
 
-// The tiles of all sequences, (len * per + rows - 1) / rows of each, those of the largest
-// number first (the heaviest: theirs is the longest pass), ties by sequence.  A wave takes
-// every so many numbers t and writes the tiles numbered t from N(t + 1) = sum of max(0,
-// tiles - t - 1) on, a lane eight sequences at most.  (A search in every workgroup of
-// attention took 3.3 us of 28; the list, for 48 sequences of up to 47 tiles, 4 us in all.)
+// The tiles of all sequences, (len * per + rows - 1) / rows of each: the longest sequence
+// first (ties by number), of each the tiles of the largest number first.  So the
+// workgroups that run at one time read the keys of few sequences, from L2, and the last
+// ones are short.  (The largest numbers of all sequences first: 48 sequences of up to
+// 1,500 tokens 727 us; their keys came from memory again and again.  A search in every
+// workgroup instead of the list: 3.3 us of 28.)  A wave takes every so many sequences.
 constexpr int kListWaves = 128;
 
 __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
@@ -102,35 +103,28 @@ __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restr
                                                           int32_t places)
 {
     const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
-    int from[kMaxSeqs / 64], size[kMaxSeqs / 64], n[kMaxSeqs / 64], all = 0, most = 0;
+    auto tiles = [&](int s, int* from, int* size) {
+        *from = seq_first(starts, T, s);
+        *size = seq_end(starts, T, s) - *from;
+        return (int)(((int64_t)*size * per + rows - 1) / rows);
+    };
+    int n[kMaxSeqs / 64], all = 0, from, size;
 #pragma unroll
     for (int i = 0; i < kMaxSeqs / 64; i++) {
-        const int s = i * 64 + lane;
-        from[i] = size[i] = n[i] = 0;
-        if (s < B) {
-            from[i] = seq_first(starts, T, s);
-            size[i] = seq_end(starts, T, s) - from[i];
-            n[i] = (int)(((int64_t)size[i] * per + rows - 1) / rows);
-        }
+        n[i] = i * 64 + lane < B ? tiles(i * 64 + lane, &from, &size) : 0;
         all += n[i];
-        most = n[i] > most ? n[i] : most;
     }
     all = wave_sum(all);
-    for (int t = wave; __ballot(most > t); t += kListWaves) {
-        int place = 0;
+    for (int s = wave; s < B; s += kListWaves) {
+        const int mine = tiles(s, &from, &size);
+        int before = 0;
 #pragma unroll
         for (int i = 0; i < kMaxSeqs / 64; i++)
-            place += n[i] > t + 1 ? n[i] - t - 1 : 0;
-        place = wave_sum(place);
-#pragma unroll
-        for (int i = 0; i < kMaxSeqs / 64; i++) {
-            const uint64_t has = __ballot(n[i] > t);
-            const int at = place + __builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32),
-                                                             __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0));
-            if (n[i] > t && at < places)
-                list[at] = Tile{from[i], size[i], t, 0};
-            place += __popcll(has);
-        }
+            before += n[i] > mine || (n[i] == mine && i * 64 + lane < s) ? n[i] : 0;
+        before = wave_sum(before);
+        for (int t = lane; t < mine; t += 64)
+            if (before + mine - 1 - t < places)
+                list[before + mine - 1 - t] = Tile{from, size, t, 0};
     }
     for (int64_t i = (int64_t)all + wave * 64 + lane; i < places; i += kListWaves * 64)
         list[i] = Tile{0, 0, 0, 0};
@@ -738,7 +732,8 @@ constexpr int64_t kWeighWork = 2048;  // workgroups that leave no CU idle long, 
 int32_t weigh_chunks(int32_t B, int32_t T, int32_t G, int32_t H, int32_t last, int32_t* chunk)
 {
     const int64_t n = kWeighWork / (most_tiles(T, 1, kWeighBlock, B) * H);
-    const int32_t most = last < T ? last : T, least = (kWeighRows + G - 1) / G;
+    // eight tiles of rows to a chunk, but one where there is little to do
+    const int32_t most = last < T ? last : T, least = ((n > 4 ? 1 : 8) * kWeighRows + G - 1) / G;
     const int64_t want = n < 1 ? most : (most + n - 1) / n;
     *chunk = (int32_t)(want < least ? least : want);
     return (most + *chunk - 1) / *chunk;
