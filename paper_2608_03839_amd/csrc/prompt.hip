@@ -35,6 +35,7 @@ constexpr int kKeys = 64;       // keys of a tile
 constexpr int kWeighKeys = 64;   // keys of a wave
 constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
+constexpr int kXcds = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kOutside = 0xF0000000u;  // a byte offset past every buffer's end: reads as zero
 
@@ -100,9 +101,13 @@ constexpr int kListWaves = 128;
 
 __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
                                                           int32_t per, int32_t rows, Tile* __restrict__ list,
-                                                          int32_t places)
+                                                          int32_t places, int32_t* __restrict__ taken)
 {
     const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (taken && wave == 0 && lane < kXcds)
+        taken[lane] = 0;
+    if (!list)
+        return;
     auto tiles = [&](int s, int* from, int* size) {
         *from = seq_first(starts, T, s);
         *size = seq_end(starts, T, s) - *from;
@@ -145,12 +150,11 @@ __device__ __forceinline__ Tile tile_of(const Tile* list, const int32_t* starts,
 }
 
 // A buffer's descriptor: address, bytes (reads past them give zeros), raw 32-bit data.
-__device__ __forceinline__ u32x4 rows_at(const uint16_t* p, int64_t bytes)
+__device__ __forceinline__ u32x4 rows_at(uint64_t a, uint32_t bytes)
 {
-    const uint64_t a = (uint64_t)p;
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
                  (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) & 0xFFFFu,
-                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
+                 (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
 
 // 16 bytes a lane, at byte `from` of the buffer (zeros past its end), straight to LDS:
@@ -195,11 +199,28 @@ __device__ __forceinline__ int value_place(int row, int chunk)
     return row * (W / 8) + (W == 128 ? chunk ^ ((row & 3) << 2) : chunk ^ ((row & 2) << 1));
 }
 
+// A unit of work is a tile of rows for a key/value head, unit u that of head u % H.  The
+// workgroups that fit the chip take unit blockIdx.x first; with `taken` (a count for each
+// XCD, 0 at first) they go on with those that are left, of their XCD's heads, so that one
+// unit's first loads are on their way while the one before is divided and stored.
+// (One unit a workgroup: 48 sequences of up to 1,500 tokens 643 us, of which 6 of 25 us a
+// workgroup for the first loads and the end.)
+constexpr int kResident = 2 * 256;  // workgroups the chip holds at two a CU
+
+struct Attend {
+    const Tile* list;
+    const int32_t* starts;
+    const uint16_t *q, *k, *v;
+    int64_t q_ld, ld;
+    uint16_t* out;
+    float* lse;
+    int32_t* taken;
+    int32_t T, G, H, D, units;
+    float scale;
+};
+
 template <int W, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
-    const Tile* __restrict__ list, const int32_t* __restrict__ starts, int32_t T, const uint16_t* __restrict__ q,
-    int64_t q_ld, int32_t G, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, int64_t ld, int32_t H,
-    int32_t D, float scale, uint16_t* __restrict__ out, float* __restrict__ lse)
+__global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
 {
     constexpr int kTile = kKeys * W * 2;          // bytes
     constexpr int kLoads = kTile / 1024 / NW;     // 1 KiB loads of a wave, a side
@@ -207,74 +228,27 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
     __shared__ __align__(1024) uint8_t key_lds[2][kTile];
     __shared__ __align__(1024) uint8_t value_lds[2][kTile];
     __shared__ int odd_lds[2][NW];                // whether a wave's part of the values is not finite
+    __shared__ int next_lds;
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = blockIdx.x % H;
-    const Tile mine = tile_of(list, starts, T, blockIdx.x / H, G, kRows);
-    const int first = mine.first, len = mine.len;
-    if (len == 0)
-        return;
+    // The arguments, read where they are used: held throughout they would take the scalar
+    // registers that the loop over the keys needs.
+    auto args = [&]() {
+        const Attend __attribute__((address_space(4)))* p =
+            (const Attend __attribute__((address_space(4)))*)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(p));
+        return p;
+    };
 
     // loads: chunk `lane` of each KiB from where its place in LDS says
     uint32_t key_from[kLoads], value_from[kLoads];
+    const uint32_t row_bytes = (uint32_t)args()->ld * 2, value_bytes = args()->D * 2;
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
         const int at = (wave * kLoads + i) * 64 + lane, r = at / (W / 8);
         const int kc = key_place<W>(r, at % (W / 8)) - r * (W / 8), vc = value_place<W>(r, at % (W / 8)) - r * (W / 8);
-        key_from[i] = kc * 8 < D ? (uint32_t)(r * ld * 2) + kc * 16 : kOutside;
-        value_from[i] = vc * 8 < D ? (uint32_t)(r * ld * 2) + vc * 16 : kOutside;
-    }
-    const int64_t base = (int64_t)first * ld + (int64_t)h * D;
-    // rows t kKeys .. of p; none past the sequence
-    auto tile_rows = [&](const uint16_t* p, int t) {
-        const int left = len - t * kKeys < kKeys ? len - t * kKeys : kKeys;
-        return rows_at(p + base + (int64_t)t * kKeys * ld, left > 0 ? (left - 1) * ld * 2 + D * 2 : 0);
-    };
-    auto load_keys = [&](int t) {
-        const u32x4 r = tile_rows(k, t);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            load_kib(r, &key_lds[t & 1][(wave * kLoads + i) * 1024], key_from[i]);
-    };
-    auto load_values = [&](int t) {
-        const u32x4 r = tile_rows(v, t);
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-            load_kib(r, &value_lds[t & 1][(wave * kLoads + i) * 1024], value_from[i]);
-    };
-    load_keys(0);
-    load_values(0);
-    load_keys(1);
-
-    const int rows = len * G, row0 = mine.tile * kRows + wave * 32;  // len * G <= T * Hq <= 2^30
-    const int row = row0 + col < rows ? row0 + col : rows - 1;
-    const int token = row / G, head = h * G + row - token * G;
-    // tokens of the workgroup's first and last row, and of the wave's
-    const int end_row = (mine.tile + 1) * kRows - 1;
-    const int first_token = mine.tile * kRows / G, last_token = (end_row < rows ? end_row : rows - 1) / G;
-    const int wave_first = __builtin_amdgcn_readfirstlane(token), wave_last = __builtin_amdgcn_readlane(token, 31);
-    const int tiles = last_token / kKeys + 1, wave_tiles = row0 < rows ? wave_last / kKeys + 1 : 0;
-
-    // queries: an operand of 16 columns each.  A negative scale turns their signs; one of
-    // zero is zeros in their place, as 0 * -inf would not keep a key unseen.
-    const float c = scale == 0.f ? 1.f : fabsf(scale) * kLog2e;
-    Operand qs[W / 16];
-    {
-        const uint16_t* from = q + ((int64_t)first + token) * q_ld + (int64_t)head * D;
-        const uint32_t turn = scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-        for (int i = 0; i < W / 16; i++) {
-            const int d = i * 16 + half * 8;
-            qs[i].w = d < D ? *(const u32x4*)(from + d) : u32x4{0, 0, 0, 0};
-            qs[i].w ^= turn;
-            if (scale == 0.f)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const uint32_t w = qs[i].w[e];
-                    qs[i].w[e] = ((w & 0x7F80u) == 0x7F80u ? 0x7FC0u : 0u) |
-                                 ((w & 0x7F800000u) == 0x7F800000u ? 0x7FC00000u : 0u);
-                }
-        }
+        key_from[i] = kc * 16 < (int)value_bytes ? r * row_bytes + kc * 16 : kOutside;
+        value_from[i] = vc * 16 < (int)value_bytes ? r * row_bytes + vc * 16 : kOutside;
     }
     int key_at[W / 16], value_at[W / 32];
 #pragma unroll
@@ -284,15 +258,84 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
     for (int i = 0; i < W / 32; i++)
         value_at[i] = value_place<W>(4 * half + (lane & 15) / 4, i * 4 + 2 * (col >> 4) + ((lane & 3) >> 1)) * 16 +
                       (lane & 1) * 8;
+    const float scale = args()->scale, c = scale == 0.f ? 1.f : fabsf(scale) * kLog2e;
+
+    // the unit: its sequence's rows and where its keys and values begin, the lane's token,
+    // tiles of keys that the workgroup sees, and how many of them every row of it sees whole
+    int len, token, tiles, whole;
+    uint64_t key_base, value_base;
+    int to;  // the row and head of the outputs, -1 past the sequence
+    // rows t kKeys .. of a side; none past the sequence
+    auto tile_rows = [&](uint64_t side, int t) {
+        const int left = len - t * kKeys < kKeys ? len - t * kKeys : kKeys;
+        return rows_at(side + (uint64_t)(t * kKeys) * row_bytes, left > 0 ? (left - 1) * row_bytes + value_bytes : 0u);
+    };
+    auto load_keys = [&](int t) {
+        const u32x4 r = tile_rows(key_base, t);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            load_kib(r, &key_lds[t & 1][(wave * kLoads + i) * 1024], key_from[i]);
+    };
+    auto load_values = [&](int t) {
+        const u32x4 r = tile_rows(value_base, t);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+            load_kib(r, &value_lds[t & 1][(wave * kLoads + i) * 1024], value_from[i]);
+    };
+    Operand qs[W / 16];  // queries: an operand of 16 columns each
+    auto begin = [&](int unit) {
+        const auto* a = args();
+        if (unit >= a->units)
+            return false;
+        const int H = a->H, G = a->G, D = a->D, h = unit % H;
+        const Tile mine = tile_of(a->list, a->starts, a->T, unit / H, G, kRows);
+        const int first = __builtin_amdgcn_readfirstlane(mine.first), tile = __builtin_amdgcn_readfirstlane(mine.tile);
+        len = __builtin_amdgcn_readfirstlane(mine.len);
+        if (len == 0)
+            return false;
+        const int64_t base = ((int64_t)first * a->ld + (int64_t)h * D) * 2;
+        key_base = (uint64_t)a->k + base;
+        value_base = (uint64_t)a->v + base;
+        load_keys(0);
+        load_values(0);
+        load_keys(1);
+        const int rows = len * G, row0 = tile * kRows + wave * 32;  // len * G <= T * Hq <= 2^30
+        const int row = row0 + col < rows ? row0 + col : rows - 1;
+        token = row / G;
+        const int head = h * G + row - token * G;
+        const uint16_t* from = a->q + ((int64_t)first + token) * a->q_ld + (int64_t)head * D;
+#pragma unroll
+        for (int i = 0; i < W / 16; i++) {
+            const int d = i * 16 + half * 8;
+            qs[i].w = d < D ? *(const u32x4*)(from + d) : u32x4{0, 0, 0, 0};
+        }
+        to = row0 + col < rows ? (first + token) * (H * G) + head : -1;
+        const int end_row = (tile + 1) * kRows - 1;
+        const int first_token = tile * kRows / G, last_token = (end_row < rows ? end_row : rows - 1) / G;
+        tiles = last_token / kKeys + 1;
+        whole = (first_token + 1) / kKeys;
+        // a negative scale turns the signs; one of zero is zeros in the queries' place, as
+        // 0 * -inf would not keep a key unseen
+        if (scale < 0.f) {
+#pragma unroll
+            for (int i = 0; i < W / 16; i++)
+                qs[i].w ^= 0x80008000u;
+        } else if (scale == 0.f) {
+#pragma unroll
+            for (int i = 0; i < W / 16; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    // what is not finite becomes NaN: its exponent has all bits set
+                    const uint32_t w = qs[i].w[e] & 0x7F807F80u;
+                    const uint32_t odd = ((w + 0x00800080u) >> 15) & 0x00010001u;
+                    qs[i].w[e] = odd * 0x7FC0u;
+                }
+        }
+        return true;
+    };
 
     floatx16 o[W / 32];
-#pragma unroll
-    for (int i = 0; i < W / 32; i++)
-#pragma unroll
-        for (int r = 0; r < 16; r++)
-            o[i][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
-
+    float m, l;
     floatx16 s[2];
     Operand p[4];
     // S^T of tile t
@@ -311,7 +354,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qs[i].b, s[b], 0, 0, 0);
             }
     };
-    // P of tile t; edge: some row does not see some key of it
+    // P of tile t; edge: some row of the workgroup does not see some key of it
     auto weights = [&](int t, auto edge) {
         if (decltype(edge)::value) {
             const int seen = token - t * kKeys - 4 * half;
@@ -355,6 +398,14 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
         }
         l += sum[0] + sum[1];
     };
+    // 16 keys j, columns 32 i .. 32 i + 31 of V^T
+    auto value_part = [&](const uint8_t* values, int j, int i) {
+        Operand a;
+#pragma unroll
+        for (int e = 0; e < 2; e++)
+            a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
+        return a;
+    };
     // O^T += V^T P of tile t
     auto products = [&](int t, auto edge) {
         const uint8_t* values = value_lds[t & 1];
@@ -384,23 +435,25 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
                                 o[i][r + e] += __uint_as_float(u);
                         }
                     }
-        }
 #pragma unroll
-        for (int j = 0; j < 4; j++)
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int i = 0; i < W / 32; i++) {
-                Operand a;
-#pragma unroll
-                for (int e = 0; e < 2; e++)
-                    a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
-                if (decltype(edge)::value && __builtin_expect(odd, 0))
+                for (int i = 0; i < W / 32; i++) {
+                    Operand a = value_part(values, j, i);
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
                         a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
                     }
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
-            }
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < W / 32; i++)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_part(values, j, i).b, p[j].b, o[i], 0, 0, 0);
+        }
     };
 
     // Products and scores beside each other: reads of LDS four matrix instructions ahead.
@@ -446,72 +499,80 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(
     };
     const std::false_type inner;
     const std::true_type edge;
-    auto is_edge = [&](int t) { return t * kKeys + kKeys - 1 > wave_first; };
-    const int whole = (first_token + 1) / kKeys;  // tiles that every row of the workgroup sees whole
-    loads_done();
-    if (whole == 0)
-        look(0);
-    __syncthreads();
-    if (wave_tiles > 0) {
+    bool more = begin(blockIdx.x);
+    while (more) {
+        int got = 0;  // units of the XCD that were taken before
+        int32_t* const taken = args()->taken;
+        if (taken && threadIdx.x == 0)
+            got = atomicAdd(&taken[blockIdx.x % kXcds], 1);
+#pragma unroll
+        for (int i = 0; i < W / 32; i++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                o[i][r] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
+        loads_done();
+        if (whole <= 1)
+            look(0);
+        __syncthreads();
         scores(0);
-        if (is_edge(0))
-            weights(0, edge);
-        else
-            weights(0, inner);
-    }
-    int t = 0;
-    for (; t + 1 < whole; t++) {
-        loads_done();
-        next(t);
-        products(t, inner);
-        scores(t + 1);
-        pipeline();
-        weights(t + 1, inner);
-    }
-    for (; t < tiles; t++) {
-        loads_done();
-        if (t > 0)
-            look(t);
-        next(t);
-        if (t < wave_tiles && is_edge(t))
-            products(t, edge);
-        else if (t < wave_tiles)
+        weights(0, edge);
+        int t = 0;
+        for (; t + 1 < whole; t++) {
+            loads_done();
+            next(t);
             products(t, inner);
-        if (t + 1 < wave_tiles) {
             scores(t + 1);
-            if (is_edge(t + 1))
+            pipeline();
+            weights(t + 1, inner);
+        }
+        for (; t < tiles; t++) {
+            loads_done();
+            if (t > 0)
+                look(t);
+            next(t);
+            products(t, edge);
+            if (t + 1 < tiles) {
+                scores(t + 1);
                 weights(t + 1, edge);
-            else
-                weights(t + 1, inner);
+            }
         }
-    }
-    loads_done();  // none is in flight when the workgroup's LDS goes to another
+        loads_done();  // none is in flight when the buffers are filled anew, or go to another workgroup
 
-    if (row0 + col >= rows)
-        return;
-    float x, y;
-    swap32(l, &x, &y);
-    l = x + y;
-    const float inv = l == 0.f ? 0.f : 1.f / l;  // scores of -inf alone give zeros
-    const int64_t at = ((int64_t)first + token) * (H * G) + head;
-    if (lse && half == 0)
-        lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-    // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
-    // eight in a row: the even j's or the odd ones
-#pragma unroll
-    for (int i = 0; i < W / 32; i++)
-#pragma unroll
-        for (int r = 0; r < 16; r += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
-            const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-            const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-            const int d = i * 32 + 2 * r + 8 * half;
-            if (d < D)
-                *(u32x4*)(out + at * D + d) = u32x4{a[0], b[0], a[1], b[1]};
+        const int row = to;
+        more = false;
+        if (args()->taken) {
+            if (threadIdx.x == 0)
+                next_lds = got;
+            __syncthreads();
+            more = begin((int)gridDim.x + __builtin_amdgcn_readfirstlane(next_lds) * kXcds + (int)blockIdx.x % kXcds);
         }
+        float x, y;
+        swap32(l, &x, &y);
+        const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
+        const auto* a = args();
+        if (row >= 0 && a->lse && half == 0)
+            a->lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        const int D = a->D;
+        uint16_t* const out = a->out + (int64_t)row * D;
+        // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
+        // eight in a row: the even j's or the odd ones
+#pragma unroll
+        for (int i = 0; i < W / 32; i++)
+#pragma unroll
+            for (int r = 0; r < 16; r += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
+                const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                const int d = i * 32 + 2 * r + 8 * half;
+                if (row >= 0 && d < D)
+                    *(u32x4*)(out + d) = u32x4{even[0], odd[0], even[1], odd[1]};
+            }
+    }
 }
 
 // kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS, 32 of them
@@ -571,8 +632,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
                 from[i] = qc * 8 < D ? (uint32_t)(d * q_ld * 2) + (x - d * G) * D * 2 + qc * 16 : kOutside;
             }
         }
-        const u32x4 r = rows_at(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D,
-                                tokens * q_ld * 2 + (int64_t)G * D * 2);
+        const u32x4 r = rows_at((uint64_t)(q + ((int64_t)first + token0) * q_ld + (int64_t)h * G * D),
+                                (uint32_t)(tokens * q_ld * 2 + G * D * 2));
 #pragma unroll
         for (int i = 0; i < kLoads; i++)
             load_kib(r, &row_lds[t & 1][(wave * kLoads + i) * 1024], from[i]);
@@ -713,18 +774,15 @@ __global__ __launch_bounds__(256) void prompt_weigh_join_kernel(const int32_t* _
 // Tiles of `rows` rows that sequences of T rows in all, times `per`, have at most.
 int64_t most_tiles(int64_t T, int32_t per, int32_t rows, int32_t B) { return T * per / rows + B; }
 
-// The list of a call's tiles, or none where there is one sequence.
-const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, int32_t rows, void* workspace,
-                      hipStream_t stream)
+// Fills the list of a call's tiles (of more than one sequence) and clears the counts.
+void make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, int32_t rows, Tile* list, int32_t* taken,
+               hipStream_t stream)
 {
-    if (B == 1)
-        return nullptr;
-    hipLaunchKernelGGL(prompt_list_kernel, dim3(kListWaves / 4), dim3(256), 0, stream, starts, B, T, per, rows,
-                       (Tile*)workspace, (int32_t)most_tiles(T, per, rows, B));
-    return (const Tile*)workspace;
+    if (list || taken)
+        hipLaunchKernelGGL(prompt_list_kernel, dim3(list ? kListWaves / 4 : 1), dim3(256), 0, stream, starts, B, T, per,
+                           rows, list, (int32_t)most_tiles(T, per, rows, B), taken);
 }
 
-constexpr int kLeastRows = 64;  // of a tile of attention
 constexpr int kWeighBlock = kWeighKeys * 4;
 constexpr int64_t kWeighWork = 2048;  // workgroups that leave no CU idle long, whatever their shares
 
@@ -739,42 +797,59 @@ int32_t weigh_chunks(int32_t B, int32_t T, int32_t G, int32_t H, int32_t last, i
     return (most + *chunk - 1) / *chunk;
 }
 
-// 256 where there is none.
-size_t list_bytes(int32_t B, int64_t tiles)
+// A list's bytes, a multiple of 256.
+size_t list_bytes(int32_t B, int64_t tiles) { return B == 1 ? 0 : (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256; }
+
+// Workspaces begin with 256 bytes: the counts, where there are any.
+constexpr size_t kCountBytes = 256;
+
+// Waves of a workgroup of attention: two where four would leave CUs without one.
+int attend_waves(int64_t T, int32_t Hq) { return T * Hq >= 128 * 256 ? 4 : 2; }
+
+int64_t attend_units(int32_t B, int32_t T, int32_t Hq, int32_t H)
 {
-    return B == 1 ? 256 : 256 + (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256;
+    return most_tiles(T, Hq / H, 32 * attend_waves(T, Hq), B) * H;
+}
+
+bool attend_resident(int32_t B, int32_t T, int32_t Hq, int32_t H)
+{
+    return attend_waves(T, Hq) == 4 && attend_units(B, T, Hq, H) > kResident;
 }
 
 }  // namespace
 
 size_t prompt_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H)
 {
-    return list_bytes(B, most_tiles(T, Hq / H, kLeastRows, B));
+    // more than 256 where any of it is used
+    const size_t list = list_bytes(B, most_tiles(T, Hq / H, 32 * attend_waves(T, Hq), B));
+    return kCountBytes + list + (list == 0 && attend_resident(B, T, Hq, H) ? 256 : 0);
 }
 
 size_t prompt_weigh_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t last)
 {
     int32_t chunk;
     const int32_t chunks = weigh_chunks(B, T, Hq / H, H, last, &chunk);
-    return list_bytes(B, most_tiles(T, 1, kWeighBlock, B)) + (chunks > 1 ? (size_t)chunks * H * T * 4 : 0);
+    return kCountBytes + list_bytes(B, most_tiles(T, 1, kWeighBlock, B)) +
+           (chunks > 1 ? (size_t)chunks * H * T * 4 : 0);
 }
 
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
                                 const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale,
                                 void* workspace, void* out, float* lse, hipStream_t stream)
 {
-    const int32_t G = Hq / H;
-#define OIL_PROMPT_ATTEND(W, NW)                                                                                   \
-    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>), dim3((uint32_t)(most_tiles(T, G, 32 * NW, B) * H)),          \
-                       dim3(NW * 64), 0, stream, make_list(starts, B, T, G, 32 * NW, workspace, stream), starts, T, \
-                       (const uint16_t*)q, q_ld, G, (const uint16_t*)k, (const uint16_t*)v, ld, H, D, scale,       \
-                       (uint16_t*)out, lse)
-    const bool wide = (int64_t)T * Hq >= 128 * 256;
-    if (D <= 64 && wide)
+    const int32_t G = Hq / H, waves = attend_waves(T, Hq), units = (int32_t)attend_units(B, T, Hq, H);
+    int32_t* taken = attend_resident(B, T, Hq, H) ? (int32_t*)workspace : nullptr;
+    Tile* list = B > 1 ? (Tile*)((uint8_t*)workspace + kCountBytes) : nullptr;
+    make_list(starts, B, T, G, 32 * waves, list, taken, stream);
+    const Attend a = {list, starts, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_ld, ld,
+                      (uint16_t*)out, lse, taken, T, G, H, D, units, scale};
+#define OIL_PROMPT_ATTEND(W, NW) \
+    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>), dim3(taken ? kResident : units), dim3(NW * 64), 0, stream, a)
+    if (D <= 64 && waves == 4)
         OIL_PROMPT_ATTEND(64, 4);
     else if (D <= 64)
         OIL_PROMPT_ATTEND(64, 2);
-    else if (wide)
+    else if (waves == 4)
         OIL_PROMPT_ATTEND(128, 4);
     else
         OIL_PROMPT_ATTEND(128, 2);
@@ -790,8 +865,9 @@ hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, cons
     int32_t chunk;
     const int32_t chunks = weigh_chunks(B, T, G, H, last, &chunk);
     const int64_t tiles = most_tiles(T, 1, kWeighBlock, B);
-    const Tile* list = make_list(starts, B, T, 1, kWeighBlock, workspace, stream);
-    float* parts = chunks > 1 ? (float*)((uint8_t*)workspace + list_bytes(B, tiles)) : weight;
+    Tile* list = B > 1 ? (Tile*)((uint8_t*)workspace + kCountBytes) : nullptr;
+    make_list(starts, B, T, 1, kWeighBlock, list, nullptr, stream);
+    float* parts = chunks > 1 ? (float*)((uint8_t*)workspace + kCountBytes + list_bytes(B, tiles)) : weight;
 #define OIL_PROMPT_WEIGH(W)                                                                                         \
     hipLaunchKernelGGL((prompt_weigh_kernel<W, kWeighBlock / kWeighKeys>), dim3((uint32_t)(tiles * H), chunks),    \
                        dim3(kWeighBlock), 0, stream, list, starts, T, (const uint16_t*)q, q_ld, G, lse,            \
