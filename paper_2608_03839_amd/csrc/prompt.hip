@@ -35,7 +35,6 @@ constexpr int kKeys = 64;       // keys of a tile
 constexpr int kWeighKeys = 64;   // keys of a wave
 constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
-constexpr int kXcds = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kOutside = 0xF0000000u;  // a byte offset past every buffer's end: reads as zero
 
@@ -101,13 +100,9 @@ constexpr int kListWaves = 128;
 
 __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
                                                           int32_t per, int32_t rows, Tile* __restrict__ list,
-                                                          int32_t places, int32_t* __restrict__ taken)
+                                                          int32_t places)
 {
     const int lane = threadIdx.x & 63, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (taken && wave == 0 && lane < kXcds)
-        taken[lane] = 0;
-    if (!list)
-        return;
     auto tiles = [&](int s, int* from, int* size) {
         *from = seq_first(starts, T, s);
         *size = seq_end(starts, T, s) - *from;
@@ -199,14 +194,6 @@ __device__ __forceinline__ int value_place(int row, int chunk)
     return row * (W / 8) + (W == 128 ? chunk ^ ((row & 3) << 2) : chunk ^ ((row & 2) << 1));
 }
 
-// A unit of work is a tile of rows for a key/value head, unit u that of head u % H.  The
-// workgroups that fit the chip take unit blockIdx.x first; with `taken` (a count for each
-// XCD, 0 at first) they go on with those that are left, of their XCD's heads, so that one
-// unit's first loads are on their way while the one before is divided and stored.
-// (One unit a workgroup: 48 sequences of up to 1,500 tokens 643 us, of which 6 of 25 us a
-// workgroup for the first loads and the end.)
-constexpr int kResident = 2 * 256;  // workgroups the chip holds at two a CU
-
 struct Attend {
     const Tile* list;
     const int32_t* starts;
@@ -214,8 +201,7 @@ struct Attend {
     int64_t q_ld, ld;
     uint16_t* out;
     float* lse;
-    int32_t* taken;
-    int32_t T, G, H, D, units;
+    int32_t T, G, H, D;
     float scale;
 };
 
@@ -228,7 +214,6 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     __shared__ __align__(1024) uint8_t key_lds[2][kTile];
     __shared__ __align__(1024) uint8_t value_lds[2][kTile];
     __shared__ int odd_lds[2][NW];                // whether a wave's part of the values is not finite
-    __shared__ int next_lds;
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // The arguments, read where they are used: held throughout they would take the scalar
@@ -260,7 +245,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                       (lane & 1) * 8;
     const float scale = args()->scale, c = scale == 0.f ? 1.f : fabsf(scale) * kLog2e;
 
-    // the unit: its sequence's rows and where its keys and values begin, the lane's token,
+    // its sequence's rows and where its keys and values begin, the lane's token,
     // tiles of keys that the workgroup sees, and how many of them every row of it sees whole
     int len, token, tiles, whole;
     uint64_t key_base, value_base;
@@ -283,16 +268,14 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             load_kib(r, &value_lds[t & 1][(wave * kLoads + i) * 1024], value_from[i]);
     };
     Operand qs[W / 16];  // queries: an operand of 16 columns each
-    auto begin = [&](int unit) {
+    {
         const auto* a = args();
-        if (unit >= a->units)
-            return false;
-        const int H = a->H, G = a->G, D = a->D, h = unit % H;
-        const Tile mine = tile_of(a->list, a->starts, a->T, unit / H, G, kRows);
+        const int H = a->H, G = a->G, D = a->D, h = blockIdx.x % H;
+        const Tile mine = tile_of(a->list, a->starts, a->T, blockIdx.x / H, G, kRows);
         const int first = __builtin_amdgcn_readfirstlane(mine.first), tile = __builtin_amdgcn_readfirstlane(mine.tile);
         len = __builtin_amdgcn_readfirstlane(mine.len);
         if (len == 0)
-            return false;
+            return;
         const int64_t base = ((int64_t)first * a->ld + (int64_t)h * D) * 2;
         key_base = (uint64_t)a->k + base;
         value_base = (uint64_t)a->v + base;
@@ -331,8 +314,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                     qs[i].w[e] = odd * 0x7FC0u;
                 }
         }
-        return true;
-    };
+    }
 
     floatx16 o[W / 32];
     float m, l;
@@ -461,16 +443,16 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         constexpr int kEach = W / 8, kMatrix = 0x8, kRead = 0x100;  // matrix instructions of each; 2 reads and 1
         __builtin_amdgcn_sched_group_barrier(kRead, 8, 0);
 #pragma unroll
-        for (int i = 0; i < kEach; i++) {
+        for (int i = 0; i < kEach - 4; i++) {
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
         }
 #pragma unroll
-        for (int i = 0; i < kEach - 8; i++) {
+        for (int i = 0; i < kEach; i++) {
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
     };
 
     // Whether the wave's part of the values of tile t, which it loaded itself, is finite.
@@ -499,80 +481,65 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     };
     const std::false_type inner;
     const std::true_type edge;
-    bool more = begin(blockIdx.x);
-    while (more) {
-        int got = 0;  // units of the XCD that were taken before
-        int32_t* const taken = args()->taken;
-        if (taken && threadIdx.x == 0)
-            got = atomicAdd(&taken[blockIdx.x % kXcds], 1);
 #pragma unroll
-        for (int i = 0; i < W / 32; i++)
+    for (int i = 0; i < W / 32; i++)
 #pragma unroll
-            for (int r = 0; r < 16; r++)
-                o[i][r] = 0.f;
-        m = -INFINITY;
-        l = 0.f;
+        for (int r = 0; r < 16; r++)
+            o[i][r] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    loads_done();
+    if (whole <= 1)
+        look(0);
+    __syncthreads();
+    scores(0);
+    weights(0, edge);
+    int t = 0;
+    for (; t + 1 < whole; t++) {
         loads_done();
-        if (whole <= 1)
-            look(0);
-        __syncthreads();
-        scores(0);
-        weights(0, edge);
-        int t = 0;
-        for (; t + 1 < whole; t++) {
-            loads_done();
-            next(t);
-            products(t, inner);
-            scores(t + 1);
-            pipeline();
-            weights(t + 1, inner);
-        }
-        for (; t < tiles; t++) {
-            loads_done();
-            if (t > 0)
-                look(t);
-            next(t);
-            products(t, edge);
-            if (t + 1 < tiles) {
-                scores(t + 1);
-                weights(t + 1, edge);
-            }
-        }
-        loads_done();  // none is in flight when the buffers are filled anew, or go to another workgroup
-
-        const int row = to;
-        more = false;
-        if (args()->taken) {
-            if (threadIdx.x == 0)
-                next_lds = got;
-            __syncthreads();
-            more = begin((int)gridDim.x + __builtin_amdgcn_readfirstlane(next_lds) * kXcds + (int)blockIdx.x % kXcds);
-        }
-        float x, y;
-        swap32(l, &x, &y);
-        const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
-        const auto* a = args();
-        if (row >= 0 && a->lse && half == 0)
-            a->lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
-        const int D = a->D;
-        uint16_t* const out = a->out + (int64_t)row * D;
-        // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
-        // eight in a row: the even j's or the odd ones
-#pragma unroll
-        for (int i = 0; i < W / 32; i++)
-#pragma unroll
-            for (int r = 0; r < 16; r += 8) {
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
-                const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-                const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-                const int d = i * 32 + 2 * r + 8 * half;
-                if (row >= 0 && d < D)
-                    *(u32x4*)(out + d) = u32x4{even[0], odd[0], even[1], odd[1]};
-            }
+        next(t);
+        products(t, inner);
+        scores(t + 1);
+        pipeline();
+        weights(t + 1, inner);
     }
+    for (; t < tiles; t++) {
+        loads_done();
+        if (t > 0)
+            look(t);
+        next(t);
+        products(t, edge);
+        if (t + 1 < tiles) {
+            scores(t + 1);
+            weights(t + 1, edge);
+        }
+    }
+    loads_done();  // none is in flight when the buffers go to another workgroup
+
+    float x, y;
+    swap32(l, &x, &y);
+    const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
+    const auto* a = args();
+    if (to >= 0 && a->lse && half == 0)
+        a->lse[to] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    const int D = a->D;
+    uint16_t* const out = a->out + (int64_t)to * D;
+    // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
+    // eight in a row: the even j's or the odd ones
+#pragma unroll
+    for (int i = 0; i < W / 32; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
+            const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+            const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const int d = i * 32 + 2 * r + 8 * half;
+            if (to >= 0 && d < D)
+                *(u32x4*)(out + d) = u32x4{even[0], odd[0], even[1], odd[1]};
+        }
 }
 
 // kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS, 32 of them
@@ -774,13 +741,15 @@ __global__ __launch_bounds__(256) void prompt_weigh_join_kernel(const int32_t* _
 // Tiles of `rows` rows that sequences of T rows in all, times `per`, have at most.
 int64_t most_tiles(int64_t T, int32_t per, int32_t rows, int32_t B) { return T * per / rows + B; }
 
-// Fills the list of a call's tiles (of more than one sequence) and clears the counts.
-void make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, int32_t rows, Tile* list, int32_t* taken,
-               hipStream_t stream)
+// Fills the list of a call's tiles, where it takes one.
+const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, int32_t rows, void* workspace,
+                      hipStream_t stream)
 {
-    if (list || taken)
-        hipLaunchKernelGGL(prompt_list_kernel, dim3(list ? kListWaves / 4 : 1), dim3(256), 0, stream, starts, B, T, per,
-                           rows, list, (int32_t)most_tiles(T, per, rows, B), taken);
+    if (B == 1)
+        return nullptr;
+    hipLaunchKernelGGL(prompt_list_kernel, dim3(kListWaves / 4), dim3(256), 0, stream, starts, B, T, per, rows,
+                       (Tile*)workspace, (int32_t)most_tiles(T, per, rows, B));
+    return (const Tile*)workspace;
 }
 
 constexpr int kWeighBlock = kWeighKeys * 4;
@@ -797,54 +766,40 @@ int32_t weigh_chunks(int32_t B, int32_t T, int32_t G, int32_t H, int32_t last, i
     return (most + *chunk - 1) / *chunk;
 }
 
-// A list's bytes, a multiple of 256.
-size_t list_bytes(int32_t B, int64_t tiles) { return B == 1 ? 0 : (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256; }
-
-// Workspaces begin with 256 bytes: the counts, where there are any.
-constexpr size_t kCountBytes = 256;
+// A list's bytes: 256 without one, more with one.
+size_t list_bytes(int32_t B, int64_t tiles)
+{
+    return B == 1 ? 256 : 256 + (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256;
+}
 
 // Waves of a workgroup of attention: two where four would leave CUs without one.
 int attend_waves(int64_t T, int32_t Hq) { return T * Hq >= 128 * 256 ? 4 : 2; }
-
-int64_t attend_units(int32_t B, int32_t T, int32_t Hq, int32_t H)
-{
-    return most_tiles(T, Hq / H, 32 * attend_waves(T, Hq), B) * H;
-}
-
-bool attend_resident(int32_t B, int32_t T, int32_t Hq, int32_t H)
-{
-    return attend_waves(T, Hq) == 4 && attend_units(B, T, Hq, H) > kResident;
-}
 
 }  // namespace
 
 size_t prompt_attend_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H)
 {
-    // more than 256 where any of it is used
-    const size_t list = list_bytes(B, most_tiles(T, Hq / H, 32 * attend_waves(T, Hq), B));
-    return kCountBytes + list + (list == 0 && attend_resident(B, T, Hq, H) ? 256 : 0);
+    return list_bytes(B, most_tiles(T, Hq / H, 32 * attend_waves(T, Hq), B));
 }
 
 size_t prompt_weigh_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t H, int32_t last)
 {
     int32_t chunk;
     const int32_t chunks = weigh_chunks(B, T, Hq / H, H, last, &chunk);
-    return kCountBytes + list_bytes(B, most_tiles(T, 1, kWeighBlock, B)) +
-           (chunks > 1 ? (size_t)chunks * H * T * 4 : 0);
+    return list_bytes(B, most_tiles(T, 1, kWeighBlock, B)) + (chunks > 1 ? (size_t)chunks * H * T * 4 : 0);
 }
 
 hipError_t launch_prompt_attend(const int32_t* starts, int32_t B, int32_t T, const void* q, int64_t q_ld, int32_t Hq,
                                 const void* k, const void* v, int64_t ld, int32_t H, int32_t D, float scale,
                                 void* workspace, void* out, float* lse, hipStream_t stream)
 {
-    const int32_t G = Hq / H, waves = attend_waves(T, Hq), units = (int32_t)attend_units(B, T, Hq, H);
-    int32_t* taken = attend_resident(B, T, Hq, H) ? (int32_t*)workspace : nullptr;
-    Tile* list = B > 1 ? (Tile*)((uint8_t*)workspace + kCountBytes) : nullptr;
-    make_list(starts, B, T, G, 32 * waves, list, taken, stream);
+    const int32_t G = Hq / H, waves = attend_waves(T, Hq);
+    const Tile* list = make_list(starts, B, T, G, 32 * waves, workspace, stream);
     const Attend a = {list, starts, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, q_ld, ld,
-                      (uint16_t*)out, lse, taken, T, G, H, D, units, scale};
+                      (uint16_t*)out, lse, T, G, H, D, scale};
+    const dim3 grid((uint32_t)(most_tiles(T, G, 32 * waves, B) * H));
 #define OIL_PROMPT_ATTEND(W, NW) \
-    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>), dim3(taken ? kResident : units), dim3(NW * 64), 0, stream, a)
+    hipLaunchKernelGGL((prompt_attend_kernel<W, NW>), grid, dim3(NW * 64), 0, stream, a)
     if (D <= 64 && waves == 4)
         OIL_PROMPT_ATTEND(64, 4);
     else if (D <= 64)
@@ -865,9 +820,8 @@ hipError_t launch_prompt_weigh(const int32_t* starts, int32_t B, int32_t T, cons
     int32_t chunk;
     const int32_t chunks = weigh_chunks(B, T, G, H, last, &chunk);
     const int64_t tiles = most_tiles(T, 1, kWeighBlock, B);
-    Tile* list = B > 1 ? (Tile*)((uint8_t*)workspace + kCountBytes) : nullptr;
-    make_list(starts, B, T, 1, kWeighBlock, list, nullptr, stream);
-    float* parts = chunks > 1 ? (float*)((uint8_t*)workspace + kCountBytes + list_bytes(B, tiles)) : weight;
+    const Tile* list = make_list(starts, B, T, 1, kWeighBlock, workspace, stream);
+    float* parts = chunks > 1 ? (float*)((uint8_t*)workspace + list_bytes(B, tiles)) : weight;
 #define OIL_PROMPT_WEIGH(W)                                                                                         \
     hipLaunchKernelGGL((prompt_weigh_kernel<W, kWeighBlock / kWeighKeys>), dim3((uint32_t)(tiles * H), chunks),    \
                        dim3(kWeighBlock), 0, stream, list, starts, T, (const uint16_t*)q, q_ld, G, lse,            \
