@@ -582,7 +582,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     // head x % G.  Rows past the last token's lie past the buffer's end.
     uint32_t from[kLoads];
     int from_rem = -1;
-    float next_less = 0.f;
+    float next_lse = 0.f;  // of row threadIdx.x, looked at once the tile is there: not to wait for it here
     int next_token = 0;
     auto load = [&](int t) {
         const int row0 = row_begin + t * kWeighRows;
@@ -606,11 +606,10 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             load_kib(r, &row_lds[t & 1][(wave * kLoads + i) * 1024], from[i]);
         if ((int)threadIdx.x < kWeighRows) {
             const uint32_t x = rem + threadIdx.x, d = x * magic >> 16;
-            float y = -INFINITY;
+            next_lse = -INFINITY;
             if ((int)threadIdx.x < here)
-                y = lse[((int64_t)first + token0 + d) * (H * G) + h * G + (x - d * G)];
-            next_less = y * -kLog2e;
-            next_token = y == -INFINITY ? -1 : (int)(token0 + d);
+                next_lse = lse[((int64_t)first + token0 + d) * (H * G) + h * G + (x - d * G)];
+            next_token = (int)(token0 + d);
         }
     };
     load(0);
@@ -672,11 +671,12 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const int wave_key = key0 + wave * kWeighKeys + kWeighKeys - 1;  // the wave's last
     for (int t = 0; t < turns; t++) {
         loads_done();
+        const bool unused = next_lse == -INFINITY;
         if ((int)threadIdx.x < kWeighRows) {
-            less_lds[t & 1][threadIdx.x] = next_less;
-            token_lds[t & 1][threadIdx.x] = next_token;
+            less_lds[t & 1][threadIdx.x] = next_lse * -kLog2e;
+            token_lds[t & 1][threadIdx.x] = unused ? -1 : next_token;
         }
-        const int any = __ballot((int)threadIdx.x < kWeighRows && next_token < 0) != 0;
+        const int any = __ballot((int)threadIdx.x < kWeighRows && unused) != 0;
         if (lane == 0)
             none_lds[t & 1][wave] = any;
         __syncthreads();
