@@ -623,7 +623,7 @@ int32_t oil_prompt_attend(const int32_t *starts, int32_t B, int64_t total, const
  *   lse        as oil_prompt_attend wrote it; a row at -inf adds nothing.
  *   last       >= 1.
  *   weight     n_heads x total float32.
- * Sums are binary32, each added up by one workgroup in one order. */
+ * Sums are binary32, added in an order that the sizes alone decide. */
 int32_t oil_prompt_weigh(const int32_t *starts, int32_t B, int64_t total, const void *q, int64_t q_ld,
                          int32_t n_q_heads, const float *lse, const void *k, int64_t ld, int32_t n_heads,
                          int32_t head_dim, int64_t last, float scale, void *workspace, size_t workspace_bytes,

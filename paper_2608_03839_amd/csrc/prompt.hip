@@ -36,7 +36,8 @@ constexpr int kWeighKeys = 64;   // keys of a wave
 constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr uint32_t kOutside = 0xF0000000u;  // a byte offset past every buffer's end: reads as zero
+// A byte offset past every buffer's end (128 rows of 2^25 bytes at most): reads as zero.
+constexpr uint32_t kOutside = 0xFFFFFF00u;
 
 union Operand {
     u32x4 w;
@@ -115,6 +116,8 @@ __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restr
         all += n[i];
     }
     all = wave_sum(all);
+    // starts that do not ascend can name more tiles than there are places, or than 31 bits hold
+    all = (uint32_t)all > (uint32_t)places ? places : all;
     for (int s = wave; s < B; s += kListWaves) {
         const int mine = tiles(s, &from, &size);
         int before = 0;
@@ -123,10 +126,10 @@ __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restr
             before += n[i] > mine || (n[i] == mine && i * 64 + lane < s) ? n[i] : 0;
         before = wave_sum(before);
         for (int t = lane; t < mine; t += 64)
-            if (before + mine - 1 - t < places)
+            if ((uint32_t)(before + mine - 1 - t) < (uint32_t)places)
                 list[before + mine - 1 - t] = Tile{from, size, t, 0};
     }
-    for (int64_t i = (int64_t)all + wave * 64 + lane; i < places; i += kListWaves * 64)
+    for (int i = all + wave * 64 + lane; i < places; i += kListWaves * 64)
         list[i] = Tile{0, 0, 0, 0};
 }
 
