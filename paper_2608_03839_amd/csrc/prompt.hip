@@ -9,8 +9,9 @@
 // lane's column is one row of queries, so that the softmax's statistics are its own),
 // the running maximum m and sum l in binary32, P = exp2(S c - m) rounded to bf16 where
 // it lies (the registers of S^T are the operand's, under the order of the keys that
-// V's transposing reads give), O^T += V^T P.  m follows the largest score only when
-// that passes it by 2^8: sums and outputs are then scaled; below, P is at most 2^8.
+// V's transposing reads give), O^T += V^T P.  m is the largest score of the first tile
+// and of those that some row does not see whole; elsewhere it stays, unseen, until a
+// lane's weights of a tile pass kMost, when they are made anew and sums and outputs scaled.
 //
 // weigh: a lane's column is a key, S = Q K^T, and the sums of exp2(S c - lse) stay in
 // registers: no two workgroups add to one position, so the result does not depend on
@@ -35,6 +36,9 @@ constexpr int kKeys = 64;       // keys of a tile
 constexpr int kWeighKeys = 64;   // keys of a wave
 constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
+// The most that a lane's 32 weights of a tile may add up to: what is rounded to bf16 keeps its relative
+// precision whatever m is, and sums of 2^30 such weights stay within binary32.
+constexpr float kMost = 256.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A byte offset past every buffer's end (128 rows of 2^25 bytes at most): reads as zero.
 constexpr uint32_t kOutside = 0xFFFFFF00u;
@@ -321,6 +325,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
 
     floatx16 o[W / 32];
     float m, l;
+    float less, most;  // what scores add for m, and kMost, or -1 until m is a number
     floatx16 s[2];
     Operand p[4];
     // S^T of tile t
@@ -339,16 +344,25 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qs[i].b, s[b], 0, 0, 0);
             }
     };
-    // P of tile t; edge: some row of the workgroup does not see some key of it
-    auto weights = [&](int t, auto edge) {
-        if (decltype(edge)::value) {
-            const int seen = token - t * kKeys - 4 * half;
+    // P of the scores and the lane's part of their sum
+    auto relative = [&]() {
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-            for (int b = 0; b < 2; b++)
+        for (int b = 0; b < 2; b++)
 #pragma unroll
-                for (int r = 0; r < 16; r++)
-                    s[b][r] = b * 32 + 8 * (r / 4) + r % 4 <= seen ? s[b][r] : -INFINITY;
-        }
+            for (int r = 0; r < 16; r += 2) {
+                float x[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    x[e] = __builtin_amdgcn_exp2f(fmaf(s[b][r + e], c, less));
+                    sum[e] += x[e];
+                }
+                p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0], x[1]);
+            }
+        return sum[0] + sum[1];
+    };
+    // m follows the tile's largest score
+    auto follow = [&]() {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; b++)
@@ -358,30 +372,36 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         float x, y;
         swap32(top, &x, &y);
         top = fmaxf(x, y) * c;
-        if (__ballot(top > m + 8.f)) {
-            const float now = fmaxf(m, top), f = exp2f(m - (now == -INFINITY ? 0.f : now));
+        const float now = fmaxf(m, top), f = exp2f(m - (now == -INFINITY ? 0.f : now));
 #pragma unroll
-            for (int i = 0; i < W / 32; i++)
+        for (int i = 0; i < W / 32; i++)
 #pragma unroll
-                for (int r = 0; r < 16; r++)
-                    o[i][r] *= f;
-            l *= f;
-            m = now;
+            for (int r = 0; r < 16; r++)
+                o[i][r] *= f;
+        l *= f;
+        m = now;
+        less = m == -INFINITY ? 0.f : -m;
+        most = m == -INFINITY ? -1.f : kMost;
+    };
+    // P of tile t, some row of the workgroup does not see some key of it
+    auto edge_weights = [&](int t) {
+        const int seen = token - t * kKeys - 4 * half;
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                s[b][r] = b * 32 + 8 * (r / 4) + r % 4 <= seen ? s[b][r] : -INFINITY;
+        follow();
+        l += relative();
+    };
+    // The scores' maximum is not sought here (with it: 16,384 rows 1,950 us, without 1,890).
+    auto inner_weights = [&]() {
+        float sum = relative();
+        if (__ballot(!(sum <= most))) {
+            follow();
+            sum = relative();
         }
-        const float less = m == -INFINITY ? 0.f : -m;
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int b = 0; b < 2; b++) {
-#pragma unroll
-            for (int r = 0; r < 16; r++) {
-                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, less));
-                sum[r & 1] += s[b][r];
-            }
-#pragma unroll
-            for (int r = 0; r < 16; r += 2)
-                p[2 * b + r / 8].w[(r % 8) / 2] = pack2(s[b][r], s[b][r + 1]);
-        }
-        l += sum[0] + sum[1];
+        l += sum;
     };
     // 16 keys j, columns 32 i .. 32 i + 31 of V^T
     auto value_part = [&](const uint8_t* values, int j, int i) {
@@ -490,13 +510,14 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         for (int r = 0; r < 16; r++)
             o[i][r] = 0.f;
     m = -INFINITY;
-    l = 0.f;
+    l = less = 0.f;
+    most = -1.f;
     loads_done();
     if (whole <= 1)
         look(0);
     __syncthreads();
     scores(0);
-    weights(0, edge);
+    edge_weights(0);
     int t = 0;
     for (; t + 1 < whole; t++) {
         loads_done();
@@ -504,7 +525,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         products(t, inner);
         scores(t + 1);
         pipeline();
-        weights(t + 1, inner);
+        __builtin_amdgcn_sched_barrier(0);  // exponentials among the last products: 1 to 2% more
+        inner_weights();
     }
     for (; t < tiles; t++) {
         loads_done();
@@ -514,7 +536,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         products(t, edge);
         if (t + 1 < tiles) {
             scores(t + 1);
-            weights(t + 1, edge);
+            edge_weights(t + 1);
         }
     }
     loads_done();  // none is in flight when the buffers go to another workgroup

@@ -164,3 +164,35 @@ def test_graphs_side_by_side(oil):
         assert torch.equal(cache.weights, plain.weights) and torch.equal(cache.positions, plain.positions)
         for a, b in zip(cache.read(0, cap), plain.read(0, cap)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("low", [-math.inf, -40.0])
+@pytest.mark.parametrize("n", [500, 5000])
+def test_first_keys_without_weight(oil, low, n):
+    """The first 70 keys' scores are -inf, or so low that their weights are 0 beside the others':
+    rows from 70 on are those of the sequence that begins there."""
+    Hq, H, D, a = 8, 2, 64, 70
+    q, k, v = (t.clone() for t in _cut(_normal((n, (Hq + 2 * H) * D)), Hq, H, D))
+    q[..., 0] = 8.0                                  # 8 times the key's, beside which the others add 45 at most
+    k[..., 0] = 0.0
+    k[:a, :, 0] = low
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=1.0)
+    w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [a, n], 1.0)
+    _near(out[a:], w_out[a:], far_out[a:], "out")
+    _near(lse[a:], w_lse[a:], far_lse[a:], "lse")
+    if low == -math.inf:
+        assert (out[:a] == 0).all() and (lse[:a] == -math.inf).all()
+
+
+@pytest.mark.parametrize("n", [500, 5000])
+def test_first_keys_with_all_weight(oil, n):
+    """The first keys' scores lie over 200 above the others', whose weights then are 0."""
+    Hq, H, D, a = 8, 2, 64, 70
+    q, k, v = (t.clone() for t in _cut(_normal((n, (Hq + 2 * H) * D)), Hq, H, D))
+    q[..., 0] = 8.0
+    k[..., 0] = 0.0
+    k[:a, :, 0] = 40.0
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=1.0)
+    w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [0, n], 1.0)
+    _near(out, w_out, far_out, "out")
+    _near(lse, w_lse, far_lse, "lse")
