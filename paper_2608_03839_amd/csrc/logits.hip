@@ -6,7 +6,9 @@
 // both rescaled when m rises.  Then
 //     log p = (x - m) - ln s,      H = ln s - ln 2 t / s,
 // where both terms of H are at least 0, so that nothing cancels.  9 instructions a value,
-// one of them an exponential; the pass over many rows is bound by memory.
+// one of them an exponential; the pass over many rows is bound by memory: 4,084 rows of
+// 50,021 binary32 values 143 us (5.7 TB/s), 1,635 of 131,072 bf16 values with
+// eight alternatives 98 us (4.4 TB/s, and some 0.65 of the VALU).
 //
 // The k best tokens (logit descending, token ascending: one 64-bit key a token) are a
 // list over the lanes of a wave, which a step of values enters only where some lane's
@@ -14,7 +16,9 @@
 // list's last or that of another wave of the workgroup.  The waves' lists are joined by
 // counting, for each key, those above it.
 //
-// Where rows are few, a row is cut among workgroups, and a second launch joins.
+// Where rows are few, a row is cut among workgroups, and a second launch joins: 61 rows of
+// 131,072 bf16 values 8.6 and 3.6 us.  A row of up to 160 KiB stays one wide workgroup's, as
+// a second launch costs more: one of 32,003 binary32 values 12.4 us, two rounds of loads.
 #include "common.hpp"
 #include "internal.hpp"
 

@@ -10,12 +10,22 @@
 // the running maximum m and sum l in binary32, P = exp2(S c - m) rounded to bf16 where
 // it lies (the registers of S^T are the operand's, under the order of the keys that
 // V's transposing reads give), O^T += V^T P.  m is the largest score of the first tile
-// and of those that some row does not see whole; elsewhere it stays, unseen, until a
-// lane's weights of a tile pass kMost, when they are made anew and sums and outputs scaled.
+// and stays, unseen, until a lane's weights of a tile pass kMost, when m rises, they are
+// made anew, and sums and outputs are scaled.
+// Bound by matrix cores, exponentials and LDS together, at a clock that power sets: at 128
+// columns a wave's tile of 64 keys is 32 matrix instructions of 32 cycles, some 560 cycles of
+// exponentials, scaling and sums, and 256 cycles of LDS, which the CU's eight waves share.
+// 16,384 rows, 32 heads over 8 of 128 columns: 1,845 to 1,920 us on different cards, 1,145 to
+// 1,190 TFLOP/s (a library product of 16,384^3: 1,586); 8,191 rows 495 us; 65,533 rows, 2
+// heads over 1: 1,990 us; 48 sequences of 375 to 1,500 rows 580 us, 785 TFLOP/s: a workgroup
+// passes over some ten tiles there, and 6 of its 20 us are its first loads and its end.
 //
 // weigh: a lane's column is a key, S = Q K^T, and the sums of exp2(S c - lse) stay in
-// registers: no two workgroups add to one position, so the result does not depend on
-// any order.
+// registers: no two workgroups add to one sum, so the result does not depend on the order
+// in which they run.  Bound by exponentials beside the products, of which there is one a
+// score here: without either the other alone takes three quarters of the time.  8,192 rows
+// over themselves, 32 heads over 8 of 128 columns: 315 us, 874 TFLOP/s; four sequences of
+// 2,048 to 8,191 rows, their last 64 rows: 25 us, of which the list 4; the keys are 45 MB.
 #include "common.hpp"
 #include "internal.hpp"
 
@@ -361,8 +371,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             }
         return sum[0] + sum[1];
     };
-    // m follows the tile's largest score
-    auto follow = [&]() {
+    // the row's largest score, scaled
+    auto largest = [&]() {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; b++)
@@ -371,34 +381,38 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 top = fmaxf(top, s[b][r]);
         float x, y;
         swap32(top, &x, &y);
-        top = fmaxf(x, y) * c;
-        const float now = fmaxf(m, top), f = exp2f(m - (now == -INFINITY ? 0.f : now));
-#pragma unroll
-        for (int i = 0; i < W / 32; i++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-                o[i][r] *= f;
-        l *= f;
-        m = now;
-        less = m == -INFINITY ? 0.f : -m;
-        most = m == -INFINITY ? -1.f : kMost;
+        return fmaxf(x, y) * c;
     };
-    // P of tile t, some row of the workgroup does not see some key of it
-    auto edge_weights = [&](int t) {
+    auto set_m = [&](float now) {
+        m = now;
+        less = now == -INFINITY ? 0.f : -now;
+        most = now == -INFINITY ? -1.f : kMost;
+    };
+    // Keys of tile t that a row does not see have no part in its scores.
+    auto mask = [&](int t) {
         const int seen = token - t * kKeys - 4 * half;
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int r = 0; r < 16; r++)
                 s[b][r] = b * 32 + 8 * (r / 4) + r % 4 <= seen ? s[b][r] : -INFINITY;
-        follow();
-        l += relative();
     };
-    // The scores' maximum is not sought here (with it: 16,384 rows 1,950 us, without 1,890).
-    auto inner_weights = [&]() {
+    // P of a tile's scores: m stays where it is, and the scores' maximum is not sought, unless
+    // they turn out too large (with it: 16,384 rows 1,950 us, without 1,890).
+    auto weights = [&]() {
         float sum = relative();
-        if (__ballot(!(sum <= most))) {
-            follow();
+        const uint64_t over = __ballot(!(sum <= most));
+        if (over) {
+            // only of such rows: what other rows of the wave hold changes no bit of a row
+            const float top = largest(), now = (over >> col | over >> (col + 32)) & 1 ? fmaxf(m, top) : m;
+            const float f = exp2f(m - (now == -INFINITY ? 0.f : now));
+#pragma unroll
+            for (int i = 0; i < W / 32; i++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    o[i][r] *= f;
+            l *= f;
+            set_m(now);
             sum = relative();
         }
         l += sum;
@@ -478,7 +492,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
     };
 
-    // Whether the wave's part of the values of tile t, which it loaded itself, is finite.
+    // Whether the wave's part of the values of tile t, which it loaded itself, is finite; asked
+    // of tiles whose products are made at the edge.
     auto look = [&](int t) {
         u32x4 most = {0, 0, 0, 0};
 #pragma unroll
@@ -509,24 +524,27 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
 #pragma unroll
         for (int r = 0; r < 16; r++)
             o[i][r] = 0.f;
-    m = -INFINITY;
-    l = less = 0.f;
-    most = -1.f;
     loads_done();
-    if (whole <= 1)
+    if (whole == 0 || tiles == 1)
         look(0);
     __syncthreads();
     scores(0);
-    edge_weights(0);
+    if (whole == 0)
+        mask(0);
+    set_m(largest());
+    l = relative();
+    // products of tiles that every row sees, the scores of the next beside them
     int t = 0;
-    for (; t + 1 < whole; t++) {
+    for (; t < whole && t + 1 < tiles; t++) {
         loads_done();
         next(t);
         products(t, inner);
         scores(t + 1);
         pipeline();
         __builtin_amdgcn_sched_barrier(0);  // exponentials among the last products: 1 to 2% more
-        inner_weights();
+        if (t + 1 == whole)
+            mask(whole);
+        weights();
     }
     for (; t < tiles; t++) {
         loads_done();
@@ -536,7 +554,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         products(t, edge);
         if (t + 1 < tiles) {
             scores(t + 1);
-            edge_weights(t + 1);
+            mask(t + 1);
+            weights();
         }
     }
     loads_done();  // none is in flight when the buffers go to another workgroup
@@ -567,7 +586,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         }
 }
 
-// kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS, 32 of them
+// kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS (64 at a time, which
+// lets three workgroups into a CU: 400 for 345 us, registers spill), 32 of them
 // multiplied while the exponentials of the 32 before are made.  Of the rows that count for
 // a tile of keys the workgroup takes blockIdx.y's `chunk` tokens' and writes part
 // blockIdx.y of the sum (a plane of n_heads x T), so that the first keys, which most rows
@@ -778,7 +798,9 @@ const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, 
 }
 
 constexpr int kWeighBlock = kWeighKeys * 4;
-constexpr int64_t kWeighWork = 2048;  // workgroups that leave no CU idle long, whatever their shares
+// Workgroups that leave no CU idle long, whatever their shares (4,096: 8,192 rows 343 for 328 us,
+// 65,536 rows of one head 1,186 for 1,220).
+constexpr int64_t kWeighWork = 2048;
 
 // Chunks that the rows of a call are cut into, and their tokens.
 int32_t weigh_chunks(int32_t B, int32_t T, int32_t G, int32_t H, int32_t last, int32_t* chunk)
@@ -797,7 +819,7 @@ size_t list_bytes(int32_t B, int64_t tiles)
     return B == 1 ? 256 : 256 + (size_t)(tiles * sizeof(Tile) + 255) / 256 * 256;
 }
 
-// Waves of a workgroup of attention: two where four would leave CUs without one.
+// Waves of a workgroup of attention: two where four would leave CUs without one, 256 of 128 rows.
 int attend_waves(int64_t T, int32_t Hq) { return T * Hq >= 128 * 256 ? 4 : 2; }
 
 }  // namespace

@@ -196,3 +196,22 @@ def test_first_keys_with_all_weight(oil, n):
     w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [0, n], 1.0)
     _near(out, w_out, far_out, "out")
     _near(lse, w_lse, far_lse, "lse")
+
+
+@pytest.mark.parametrize("Hq,H,D", [(8, 2, 128), (12, 12, 64), (5, 1, 40)])
+def test_rows_depend_on_what_they_see(oil, Hq, H, D):
+    """A row's bits are the same whatever other rows ask for, and whatever its sequence is packed with."""
+    lens = [300, 1, 1900, 64]
+    at = _starts(lens)
+    q, k, v = _cut(_normal((at[-1], (Hq + 2 * H) * D)), Hq, H, D)
+    out, lse = oil.prompt_attend(q, k, v, _int(at))
+    for a, z in zip(at, at[1:]):
+        alone = oil.prompt_attend(q[a:z], k[a:z], v[a:z], _int([0, z - a]))
+        assert torch.equal(alone[0], out[a:z]) and torch.equal(alone[1], lse[a:z])
+    wild = q.clone()
+    wild[::3] *= 40.0                                  # scores that leave their first tile's far behind
+    wild[1::3, :, 0] = math.nan
+    kept = torch.arange(at[-1], device="cuda") % 3 == 2
+    got = oil.prompt_attend(wild, k.clone(), v.clone(), _int(at))
+    assert torch.equal(got[0][kept], out[kept]) and torch.equal(got[1][kept], lse[kept])
+    assert torch.isnan(got[0][1::3]).all() and torch.isfinite(got[0][::3]).all()
