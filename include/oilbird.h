@@ -606,8 +606,10 @@ size_t oil_prompt_weigh_workspace_bytes(int32_t B, int64_t total, int32_t n_q_he
  *     S = scale * q . k;  lse = log sum exp S;  out = sum exp(S - lse) v.
  *   out        total x n_q_heads x head_dim bf16, dense, 16-byte aligned.
  *   lse        total x n_q_heads float32 (natural logarithm) or NULL.
- * What a row does not see does not reach it, whatever it holds.  A row whose scores are
- * all -inf gives zeros and -inf; a score that is NaN or passes binary32 makes its row NaN.
+ * What a row does not see does not reach it, whatever it holds: no bit of it depends on other
+ * rows of q, on later rows of k and v, or on other sequences.  A row whose scores are all
+ * -inf gives zeros and -inf; a score (or its q . k) that is NaN or above binary32's range makes
+ * its row NaN, one below counts as -inf.
  * Sums, the softmax's statistics and lse are binary32.  Rounded to fewer bits are the
  * weights exp(S - m), m a number for each row, to bf16 for their product with v (half a
  * step is 2^-8 of each; the sum that divides is of unrounded ones), and out. */

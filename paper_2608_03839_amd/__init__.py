@@ -821,7 +821,13 @@ class KvCache:
 
     def _call(self, name, *args):
         """The C call with the cache's device current, which launches go to."""
-        _call_on(self._index, name, *args)
+        call = getattr(lib(), name)
+        if torch._C._cuda_getDevice() == self._index:
+            status = call(*args)
+        else:
+            with torch.cuda.device(self._index):
+                status = call(*args)
+        _check(name, status)
 
     def _workspace(self, stream, on, given, call, *sizes):
         """Address and bytes of the workspace of a call of these sizes on the stream ``on``:
@@ -844,7 +850,11 @@ class KvCache:
 
     def _on(self, stream):
         """The stream's handle: torch's current one of the cache's device by default."""
-        return _stream_on(stream, self._index)
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        if stream.device.index != self._index:
+            raise ValueError(f"the stream must be on cuda:{self._index}, got {stream.device}")
+        return stream.cuda_stream
 
     def _heads(self, t, name):
         if t.dim() != 4 or t.shape[3] != self.head_dim:
