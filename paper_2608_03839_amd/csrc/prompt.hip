@@ -24,7 +24,7 @@
 // registers: no two workgroups add to one sum, so the result does not depend on the order
 // in which they run.  Bound by exponentials beside the products, of which there is one a
 // score here: without either the other alone takes three quarters of the time.  8,192 rows
-// over themselves, 32 heads over 8 of 128 columns: 315 us, 874 TFLOP/s; four sequences of
+// over themselves, 32 heads over 8 of 128 columns: 308 us, 892 TFLOP/s; four sequences of
 // 2,048 to 8,191 rows, their last 64 rows: 25 us, of which the list 4; the keys are 45 MB.
 #include "common.hpp"
 #include "internal.hpp"
@@ -618,7 +618,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
         return;
     const int seen_from = all_from + blockIdx.y * chunk;
     const int seen_to = len - seen_from < chunk ? len : seen_from + chunk;
-    const int row_begin = seen_from * G, rows = (seen_to - seen_from) * G;  // len * G <= T * Hq <= 2^30
+    const int rows = (seen_to - seen_from) * G;  // len * G <= T * Hq <= 2^30
     const int turns = (rows + kWeighRows - 1) / kWeighRows;
     const float c = fabsf(scale) * kLog2e;
     const uint32_t magic = 65536 / G + 1;  // x / G = x magic >> 16 for x < 64 + kWeighRows, G <= 64
@@ -629,11 +629,12 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     int from_rem = -1;
     float next_lse = 0.f;  // of row threadIdx.x, looked at once the tile is there: not to wait for it here
     int next_token = 0;
+    // the tile's first token and its first row's place in it, from tile to tile
+    int token0 = seen_from, rem = 0;
+    const int more_tokens = kWeighRows / G, more_rem = kWeighRows - more_tokens * G;
     auto load = [&](int t) {
-        const int row0 = row_begin + t * kWeighRows;
-        const int token0 = row0 / G, rem = row0 - token0 * G;
         const int here = rows - t * kWeighRows < kWeighRows ? rows - t * kWeighRows : kWeighRows;
-        const int tokens = (rem + here - 1) / G;
+        const int tokens = (int)((rem + here - 1) * magic >> 16);
         if (rem != from_rem) {
             from_rem = rem;
 #pragma unroll
@@ -658,6 +659,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
         }
     };
     load(0);
+    int first_token = seen_from;  // of the tile at work
 
     // the wave's keys: operands of 16 columns
     Operand ks[2][W / 16];
@@ -725,14 +727,23 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
         if (lane == 0)
             none_lds[t & 1][wave] = any;
         __syncthreads();
-        if (t + 1 < turns)
+        const int least = first_token;
+        if (t + 1 < turns) {
+            token0 += more_tokens;
+            rem += more_rem;
+            if (rem >= G) {
+                rem -= G;
+                token0++;
+            }
+            first_token = token0;
             load(t + 1);
+        }
         int none = 0;
 #pragma unroll
         for (int i = 0; i < NW; i++)
             none |= none_lds[t & 1][i];
         Scores s[2];
-        if ((row_begin + t * kWeighRows) / G < wave_key || __builtin_amdgcn_readfirstlane(none)) {
+        if (least < wave_key || __builtin_amdgcn_readfirstlane(none)) {
 #pragma unroll 1
             for (int a = 0; a < kParts; a++) {
                 scores(t, a, s[0]);
@@ -745,6 +756,24 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
                 if (a + 1 < kParts)
                     scores(t, a + 1, s[(a + 1) & 1]);
                 add(t, a, s[a & 1], std::false_type());
+            }
+            // At 128 columns reads of LDS eight ahead, which leaves the exponentials where they
+            // are beside products: 16 + 32 + 16 matrix instructions, 48 reads.  (Without: 8,192
+            // rows 340 for 330 us; at 64 columns the compiler's own order is as fast.)
+            constexpr int kMatrix = 0x8, kRead = 0x100;
+            if (W == 128) {
+                __builtin_amdgcn_sched_group_barrier(kRead, 8, 0);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 16, 0);
             }
         }
         if ((t & 15) == 15) {
