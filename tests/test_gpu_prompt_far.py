@@ -198,7 +198,7 @@ def test_first_keys_with_all_weight(oil, n):
     _near(lse, w_lse, far_lse, "lse")
 
 
-@pytest.mark.parametrize("Hq,H,D", [(8, 2, 128), (12, 12, 64), (5, 1, 40)])
+@pytest.mark.parametrize("Hq,H,D", [(8, 2, 128), (12, 12, 64), (5, 1, 40), (16, 4, 128)])
 def test_rows_depend_on_what_they_see(oil, Hq, H, D):
     """A row's bits are the same whatever other rows ask for, and whatever its sequence is packed with."""
     lens = [300, 1, 1900, 64]
