@@ -13,8 +13,8 @@
 // The k best tokens (logit descending, token ascending: one 64-bit key a token) are a
 // list over the lanes of a wave, which a step of values enters only where some lane's
 // largest reaches a bound: at first the k-th largest of the lanes' own maxima, then the
-// list's last or that of another wave of the workgroup.  The waves' lists are joined by
-// counting, for each key, those above it.
+// list's last or that of another wave of the workgroup.  A few keys enter one after the other, more
+// are sorted and joined with the list; so are the waves' lists, in pairs.
 //
 // Where rows are few, a row is cut among workgroups, and a second launch joins: 61 rows of
 // 131,072 bf16 values 8.6 and 3.6 us.  A row of up to 160 KiB stays one wide workgroup's, as
@@ -84,14 +84,94 @@ __device__ __forceinline__ uint64_t key_before(uint64_t k)
     return (uint64_t)hi << 32 | lo;
 }
 
-// The best k keys a wave has seen, best first by lane (0 past them).
+template <int kControl>
+__device__ __forceinline__ uint64_t moved_key(uint64_t k)
+{
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(k >> 32), kControl, 0xF, 0xF, true);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)k, kControl, 0xF, 0xF, true);
+    return (uint64_t)hi << 32 | lo;
+}
+
+// The larger (or smaller) of a lane's key and that of lane ^ kFar.
+template <int kFar>
+__device__ __forceinline__ uint64_t exchanged(uint64_t k, bool larger)
+{
+    uint64_t a = k, b;
+    if (kFar == 1)
+        b = moved_key<0xB1>(k);
+    else if (kFar == 2)
+        b = moved_key<0x4E>(k);
+    else if (kFar == 4)
+        b = moved_key<0x1B>(moved_key<0x141>(k));  // mirrored in 8, then in 4
+    else if (kFar == 8)
+        b = moved_key<0x128>(k);  // turned by 8 in 16
+    else {
+        // the two lanes' keys in both
+        const auto lo = kFar == 16 ? __builtin_amdgcn_permlane16_swap((uint32_t)k, (uint32_t)k, false, false)
+                                   : __builtin_amdgcn_permlane32_swap((uint32_t)k, (uint32_t)k, false, false);
+        const auto hi = kFar == 16
+                            ? __builtin_amdgcn_permlane16_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false)
+                            : __builtin_amdgcn_permlane32_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
+        a = (uint64_t)hi[0] << 32 | lo[0];
+        b = (uint64_t)hi[1] << 32 | lo[1];
+    }
+    return (a > b) == larger ? a : b;
+}
+
+// Sorts keys that rise and then fall, or the other way round, by lane (or kSize lanes each):
+// the largest first where `falling`.
+template <int kSize>
+__device__ __forceinline__ uint64_t merged(uint64_t k, int lane, bool falling)
+{
+    if (kSize >= 64)
+        k = exchanged<32>(k, ((lane & 32) == 0) == falling);
+    if (kSize >= 32)
+        k = exchanged<16>(k, ((lane & 16) == 0) == falling);
+    if (kSize >= 16)
+        k = exchanged<8>(k, ((lane & 8) == 0) == falling);
+    if (kSize >= 8)
+        k = exchanged<4>(k, ((lane & 4) == 0) == falling);
+    if (kSize >= 4)
+        k = exchanged<2>(k, ((lane & 2) == 0) == falling);
+    return exchanged<1>(k, ((lane & 1) == 0) == falling);
+}
+
+// A wave's keys, the smallest first.
+__device__ __forceinline__ uint64_t rising(uint64_t k, int lane)
+{
+    k = merged<2>(k, lane, (lane & 2) != 0);
+    k = merged<4>(k, lane, (lane & 4) != 0);
+    k = merged<8>(k, lane, (lane & 8) != 0);
+    k = merged<16>(k, lane, (lane & 16) != 0);
+    k = merged<32>(k, lane, (lane & 32) != 0);
+    return merged<64>(k, lane, false);
+}
+
+// The best keys a wave has seen, best first by lane; k of them count.  kMany: more than kSerial keys
+// that are to enter are sorted first (2 x 82 rows of 1,279 values, k = 64: 56 us without, 15 with; k = 8
+// has few such steps, and 32 trees of 131,072 values 101 us with, 98 without, in registers that leave
+// room for fewer waves).
+constexpr int kSerial = 6, kFewKeys = 16;
+
+template <bool kMany>
 struct Best {
     uint64_t mine = 0, last = 0;  // last: the k-th
+
+    // The best of two lists, the other's lanes turned round.
+    __device__ __forceinline__ void join(uint64_t other, int lane, int k)
+    {
+        mine = merged<64>(mine > other ? mine : other, lane, true);
+        last = lane_key(mine, k - 1);
+    }
 
     // Enters one key a lane; 0 enters nothing.
     __device__ __forceinline__ void add(uint64_t key, int lane, int k)
     {
         uint64_t who = __ballot(key > last);
+        if (kMany && __popcll(who) > kSerial) {
+            join(rising(key > last ? key : 0ull, lane), lane, k);
+            return;
+        }
         while (who) {
             const int from = __builtin_ctzll(who);
             const uint64_t x = lane_key(key, from);
@@ -190,14 +270,14 @@ struct Shared {
 
 // The part [g0, g1) of a row's loads by NT threads: in the first wave, the part's sums in
 // every lane, and the i-th best key in lane i (0 past the k).
-template <typename X, int NT>
+template <typename X, int NT, bool kMany>
 __device__ __forceinline__ void scan_part(const Row<X>& row, int64_t g0, int64_t g1, int k, Shared<NT>& lds, Sums* sums,
                                           uint64_t* key)
 {
     constexpr int E = Row<X>::E;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Sums a = {kLowest, 0.f, 0.f};
-    Best best;
+    Best<kMany> best;
     uint32_t bound = 0;  // code below which nothing enters
     if (threadIdx.x == 0)
         lds.bound = 0;
@@ -284,29 +364,22 @@ __device__ __forceinline__ void scan_part(const Row<X>& row, int64_t g0, int64_t
     a = join_wave(a);
     if (lane == 0)
         lds.sums[wave] = a;
+    // waves' lists in pairs
     if (lane < k)
         lds.keys[wave * k + lane] = best.mine;
-    __syncthreads();
-    // keys' places: how many are above; the best k to the front, in order
-    const int all = NT / 64 * k;
-    uint64_t mine = 0;
-    int above = 0;
-    if ((int)threadIdx.x < all) {
-        mine = lds.keys[threadIdx.x];
-        for (int i = 0; i < all; i++)
-            above += lds.keys[i] > mine;
+    for (int n = NT / 128; n >= 1; n /= 2) {
+        __syncthreads();
+        if (k > 0 && wave < n) {
+            best.mine = lane < k ? best.mine : 0ull;
+            best.join(63 - lane < k ? lds.keys[(wave + n) * k + 63 - lane] : 0ull, lane, k);
+            if (lane < k)
+                lds.keys[wave * k + lane] = best.mine;
+        }
     }
-    __syncthreads();
-    if ((int)threadIdx.x < k)
-        lds.keys[threadIdx.x] = 0;
-    __syncthreads();
-    if (mine && above < k)
-        lds.keys[above] = mine;
-    __syncthreads();
     if (wave == 0) {
         a = lane < NT / 64 ? lds.sums[lane] : Sums{kLowest, 0.f, 0.f};
         *sums = join_wave(a);
-        *key = lane < k ? lds.keys[lane] : 0ull;
+        *key = lane < k ? best.mine : 0ull;
     }
 }
 
@@ -364,7 +437,7 @@ struct Call {
 };
 
 // One workgroup a (row, part); with one part the row's outputs, else its sums and keys.
-template <typename X, int NT>
+template <typename X, int NT, bool kMany>
 __global__ __launch_bounds__(NT) void logprobs_kernel(const X* __restrict__ logits, Call c)
 {
     __shared__ Shared<NT> lds;
@@ -380,7 +453,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(const X* __restrict__ logi
     const int64_t g0 = p * per, g1 = g0 + per < all ? g0 + per : all;
     Sums a;
     uint64_t key;
-    scan_part<X, NT>(row, g0, g1, c.k, lds, &a, &key);
+    scan_part<X, NT, kMany>(row, g0, g1, c.k, lds, &a, &key);
     if (threadIdx.x >= 64)
         return;
     if (c.parts == 1) {
@@ -404,7 +477,7 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(const X* __restrict__
         return;
     }
     const Row<X> row(logits + r * c.ld, c.V);
-    Best best;
+    Best<true> best;
     for (int i = 0; i < c.parts * c.k; i += 64) {
         const int at = i + lane, depth = at / c.parts, p = at - depth * c.parts;
         best.add(at < c.parts * c.k ? c.keys[(r * c.parts + p) * c.k + depth] : 0ull, lane, c.k);
@@ -447,14 +520,19 @@ hipError_t launch_logprobs(int64_t rows, int32_t max_rows, const int32_t* n_rows
     uint64_t* keys = (uint64_t*)workspace;
     const Call c = {ld,     V,    max_rows, M,       k,       parts,        n_rows,
                     tokens, (Sums*)(keys + rows * parts * k), keys, logprob, entropy, top_logprobs, top_tokens};
-#define OIL_LOGPROBS(X)                                                                                              \
-    if (wide(rows, parts))                                                                                          \
-        hipLaunchKernelGGL((logprobs_kernel<X, kWideThreads>), dim3((uint32_t)rows), dim3(kWideThreads), 0, stream, \
-                           (const X*)logits, c);                                                                    \
-    else                                                                                                            \
-        hipLaunchKernelGGL((logprobs_kernel<X, kThreads>), dim3((uint32_t)(rows * parts)), dim3(kThreads), 0,       \
-                           stream, (const X*)logits, c);                                                            \
-    if (parts > 1)                                                                                                  \
+#define OIL_LOGPROBS_OF(X, NT, MANY)                                                                      \
+    hipLaunchKernelGGL((logprobs_kernel<X, NT, MANY>), dim3((uint32_t)(rows * parts)), dim3(NT), 0, stream, \
+                       (const X*)logits, c)
+#define OIL_LOGPROBS(X)                             \
+    if (wide(rows, parts) && k > kFewKeys)          \
+        OIL_LOGPROBS_OF(X, kWideThreads, true);     \
+    else if (wide(rows, parts))                     \
+        OIL_LOGPROBS_OF(X, kWideThreads, false);    \
+    else if (k > kFewKeys)                          \
+        OIL_LOGPROBS_OF(X, kThreads, true);         \
+    else                                            \
+        OIL_LOGPROBS_OF(X, kThreads, false);        \
+    if (parts > 1)                                  \
     hipLaunchKernelGGL(logprobs_join_kernel<X>, dim3((uint32_t)rows), dim3(64), 0, stream, (const X*)logits, c)
     if (dtype == 0) {
         OIL_LOGPROBS(float);
@@ -462,6 +540,7 @@ hipError_t launch_logprobs(int64_t rows, int32_t max_rows, const int32_t* n_rows
         OIL_LOGPROBS(uint16_t);
     }
 #undef OIL_LOGPROBS
+#undef OIL_LOGPROBS_OF
     return hipGetLastError();
 }
 

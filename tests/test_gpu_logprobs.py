@@ -54,7 +54,8 @@ def _check(oil, x, tokens, top, n_rows=None):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("B,N,V,top,pad", [
     (1, 1, 1, 1, 0), (1, 1, 5, 8, 0), (2, 3, 63, 64, 1), (1, 2, 1000, 5, 3), (1, 1, 32003, 8, 0), (3, 7, 4099, 20, 5),
-    (1, 61, 131072, 1, 0), (2, 5, 131073, 64, 7), (2, 1500, 1029, 2, 0), (1, 1, 262147, 64, 1), (4, 700, 333, 0, 0)])
+    (1, 61, 131072, 1, 0), (2, 5, 131073, 64, 7), (2, 1500, 1029, 2, 0), (1, 1, 262147, 64, 1), (4, 700, 333, 0, 0),
+    (3, 40, 2050, 16, 0), (3, 300, 700, 17, 0), (2, 9, 5000, 33, 1), (2, 300, 900, 64, 0), (1, 5, 90000, 63, 3)])
 def test_rows(oil, dtype, B, N, V, top, pad):
     x, tokens = _logits(B, N, V, dtype, pad=pad)
     tokens[0, 0, 0], tokens[-1, -1, 1] = -1, V
