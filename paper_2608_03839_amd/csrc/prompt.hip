@@ -12,10 +12,11 @@
 // V's transposing reads give), O^T += V^T P.  m is the largest score of the first tile
 // and stays, unseen, until a lane's weights of a tile pass kMost, when m rises, they are
 // made anew, and sums and outputs are scaled.
-// Bound by matrix cores, exponentials and LDS together, at a clock that power sets: at 128
+// Bound by power, which leaves a clock of 1.4 to 1.7 GHz with matrix cores busy two thirds of
+// the time, and by matrix cores, exponentials and LDS, which overlap in part: at 128
 // columns a wave's tile of 64 keys is 32 matrix instructions of 32 cycles, some 560 cycles of
 // exponentials, scaling and sums, and 256 cycles of LDS, which the CU's eight waves share.
-// 16,384 rows, 32 heads over 8 of 128 columns: 1,845 to 1,920 us on different cards, 1,145 to
+// 16,384 rows, 32 heads over 8 of 128 columns: 1,845 to 2,015 us on different cards, 1,090 to
 // 1,190 TFLOP/s (a library product of 16,384^3: 1,586); 8,191 rows 495 us; 65,533 rows, 2
 // heads over 1: 1,990 us; 48 sequences of 375 to 1,500 rows 580 us, 785 TFLOP/s: a workgroup
 // passes over some ten tiles there, and 6 of its 20 us are its first loads and its end.
