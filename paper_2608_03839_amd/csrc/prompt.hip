@@ -12,6 +12,9 @@
 // V's transposing reads give), O^T += V^T P.  m is the largest score of the first tile
 // and stays, unseen, until a lane's weights of a tile pass kMost, when m rises, they are
 // made anew, and sums and outputs are scaled.
+// c is log2 e times the scale, rounded, and so is m, while S c is exact: where scores are
+// so large that this tells (kFar), and wherever else a result is not finite, a second pass
+// makes the row from (S - max S) scale.
 // Bound by power, which leaves a clock of 1.4 to 1.7 GHz with matrix cores busy two thirds of
 // the time, and by matrix cores, exponentials and LDS, which overlap in part: at 128
 // columns a wave's tile of 64 keys is 32 matrix instructions of 32 cycles, some 560 cycles of
@@ -50,6 +53,8 @@ constexpr int kMaxSeqs = 512;
 // The most that a lane's 32 weights of a tile may add up to: what is rounded to bf16 keeps its relative
 // precision whatever m is, and sums of 2^30 such weights stay within binary32.
 constexpr float kMost = 256.f;
+// Scores in base 2 from which on, in size, binary32 holds m with an error that matters beside them.
+constexpr float kFar = 0x1p24f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A byte offset past every buffer's end (128 rows of 2^25 bytes at most): reads as zero.
 constexpr uint32_t kOutside = 0xFFFFFF00u;
@@ -232,6 +237,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     __shared__ __align__(1024) uint8_t key_lds[2][kTile];
     __shared__ __align__(1024) uint8_t value_lds[2][kTile];
     __shared__ int odd_lds[2][NW];                // whether a wave's part of the values is not finite
+    __shared__ int again_lds[NW];                 // whether a wave has results that are made again
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // The arguments, read where they are used: held throughout they would take the scalar
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     }
 
     floatx16 o[W / 32];
-    float m, l;
+    float top, l;      // the score, unscaled, that m is made of
     float less, most;  // what scores add for m, and kMost, or -1 until m is a number
     floatx16 s[2];
     Operand p[4];
@@ -372,21 +378,23 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             }
         return sum[0] + sum[1];
     };
-    // the row's largest score, scaled
+    // the row's largest score, unscaled
     auto largest = [&]() {
-        float top = s[0][0];
+        float most = s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
             for (int r = 0; r < 16; r++)
-                top = fmaxf(top, s[b][r]);
+                most = fmaxf(most, s[b][r]);
         float x, y;
-        swap32(top, &x, &y);
-        return fmaxf(x, y) * c;
+        swap32(most, &x, &y);
+        return fmaxf(x, y);
     };
+    // m = top c, rounded.  The product of scores and c is not: past kFar what m lacks is no small part of a
+    // weight, and the row becomes NaN here, to be made again.
     auto set_m = [&](float now) {
-        m = now;
-        less = now == -INFINITY ? 0.f : -now;
+        top = now;
+        less = now == -INFINITY ? 0.f : fabsf(now * c) < kFar ? -(now * c) : __builtin_nanf("");
         most = now == -INFINITY ? -1.f : kMost;
     };
     // Keys of tile t that a row does not see have no part in its scores.
@@ -402,18 +410,19 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     // they turn out too large (with it: 16,384 rows 1,950 us, without 1,890).
     auto weights = [&]() {
         float sum = relative();
-        const uint64_t over = __ballot(!(sum <= most));
+        const uint64_t over = __ballot(sum > most);
         if (over) {
             // only of such rows: what other rows of the wave hold changes no bit of a row
-            const float top = largest(), now = (over >> col | over >> (col + 32)) & 1 ? fmaxf(m, top) : m;
-            const float f = exp2f(m - (now == -INFINITY ? 0.f : now));
+            const float high = largest(), now = (over >> col | over >> (col + 32)) & 1 ? fmaxf(top, high) : top;
+            const float was = less, none = most;
+            set_m(now);
+            const float f = none < 0.f ? 0.f : exp2f(less - was);
 #pragma unroll
             for (int i = 0; i < W / 32; i++)
 #pragma unroll
                 for (int r = 0; r < 16; r++)
                     o[i][r] *= f;
             l *= f;
-            set_m(now);
             sum = relative();
         }
         l += sum;
@@ -426,47 +435,56 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
         return a;
     };
+    // whether a wave found tile t's values not finite
+    auto is_odd = [&](int t) __attribute__((always_inline)) {
+        int any = 0;
+#pragma unroll
+        for (int i = 0; i < NW; i++)
+            any |= odd_lds[t & 1][i];
+        return __builtin_amdgcn_readfirstlane(any) != 0;
+    };
+    // What of tile t's values is not finite, added to the rows that see it.
+    auto add_odd = [&](int t) __attribute__((always_inline)) {
+        const uint8_t* values = value_lds[t & 1];
+#pragma unroll 1
+        for (int key = 0; key < kKeys; key++)
+#pragma unroll
+            for (int i = 0; i < W / 32; i++)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const uint32_t* at = (const uint32_t*)(values + value_place<W>(key, 4 * i + r / 4) * 16 + 8 * half);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
+                        if ((u & 0x7F800000u) == 0x7F800000u && t * kKeys + key <= token)
+                            o[i][r + e] += __uint_as_float(u);
+                    }
+                }
+    };
+    // O^T += V^T P of tile t without it.
+    auto even_products = [&](int t) __attribute__((always_inline)) {
+        const uint8_t* values = value_lds[t & 1];
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int i = 0; i < W / 32; i++) {
+                Operand a = value_part(values, j, i);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
+                    a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
+                }
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
+            }
+    };
     // O^T += V^T P of tile t
     auto products = [&](int t, auto edge) {
         const uint8_t* values = value_lds[t & 1];
-        bool odd = false;
-        if (decltype(edge)::value) {
-            // a value that is not finite must not reach rows that do not see it through a
-            // product with zero: where the tile has one, it leaves the products and is
-            // added to the rows that see it
-            int any = 0;
-#pragma unroll
-            for (int i = 0; i < NW; i++)
-                any |= odd_lds[t & 1][i];
-            odd = __builtin_amdgcn_readfirstlane(any) != 0;
-        }
-        if (decltype(edge)::value && __builtin_expect(odd, 0)) {
-#pragma unroll 1
-            for (int key = 0; key < kKeys; key++)
-#pragma unroll
-                for (int i = 0; i < W / 32; i++)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const uint32_t* at = (const uint32_t*)(values + value_place<W>(key, 4 * i + r / 4) * 16 + 8 * half);
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
-                            if ((u & 0x7F800000u) == 0x7F800000u && t * kKeys + key <= token)
-                                o[i][r + e] += __uint_as_float(u);
-                        }
-                    }
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-#pragma unroll
-                for (int i = 0; i < W / 32; i++) {
-                    Operand a = value_part(values, j, i);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
-                        a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
-                    }
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
-                }
+        // a value that is not finite must not reach rows that do not see it through a product with zero:
+        // where the tile has one, it leaves the products and is added to the rows that see it
+        if (decltype(edge)::value && __builtin_expect(is_odd(t), 0)) {
+            add_odd(t);
+            even_products(t);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -561,30 +579,124 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     }
     loads_done();  // none is in flight when the buffers go to another workgroup
 
-    float x, y;
-    swap32(l, &x, &y);
-    const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
-    const auto* a = args();
-    if (to >= 0 && a->lse && half == 0)
-        a->lse[to] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
-    const int D = a->D;
-    uint16_t* const out = a->out + (int64_t)to * D;
-    // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
-    // eight in a row: the even j's or the odd ones
+    // Writes the row; `again`: where what is there is not finite.  Whether anything written is not finite.
+    auto store = [&](auto again) {
+        float x, y;
+        swap32(l, &x, &y);
+        const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
+        const auto* a = args();
+        if (to >= 0 && a->lse && half == 0) {
+            // with the score itself, not with m: to the last place of what the score alone has
+            const float lacks = decltype(again)::value ? 0.f : fmaf(top, c, less);
+            const float lse = sum == 0.f ? -INFINITY
+                                         : fmaf(top, fabsf(a->scale), (__builtin_amdgcn_logf(sum) - lacks) * kLn2);
+            if (!decltype(again)::value || isnan(a->lse[to]))
+                a->lse[to] = lse;
+        }
+        const int D = a->D;
+        uint16_t* const out = a->out + (int64_t)to * D;
+        uint32_t size = 0;
+        // a lane has columns 8 j + 4 half .. + 3 of its row; halves trade so that it writes
+        // eight in a row: the even j's or the odd ones
+#pragma unroll
+        for (int i = 0; i < W / 32; i++)
+#pragma unroll
+            for (int r = 0; r < 16; r += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
+                const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                const int d = i * 32 + 2 * r + 8 * half;
+                if (to < 0 || d >= D)
+                    continue;
+                u32x4 now = {even[0], odd[0], even[1], odd[1]};
+                if (decltype(again)::value) {
+                    const u32x4 was = *(const u32x4*)(out + d);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t low = (was[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u;
+                        const uint32_t high = (was[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
+                        now[e] = (now[e] & (low | high)) | (was[e] & ~(low | high));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        size = max_u16(size, now[e] & 0x7FFF7FFFu);
+                }
+                *(u32x4*)(out + d) = now;
+            }
+        return (size & 0xFFFFu) >= 0x7F80u || size >= 0x7F800000u;
+    };
+    const bool odd = store(std::false_type());
+
+    // Results that are not finite are made again, with the largest score sought in every tile, unscaled, and
+    // taken from the others before they are scaled: exact where it matters, whatever the scores.  Rare, so made
+    // simply; what is finite stays as it was, so that a row's bits do not depend on those beside it.
+    const int any = __ballot(odd) != 0;
+    if (lane == 0)
+        again_lds[wave] = any;
+    __syncthreads();
+    int again = 0;
+#pragma unroll
+    for (int i = 0; i < NW; i++)
+        again |= again_lds[i];
+    if (!__builtin_amdgcn_readfirstlane(again))
+        return;
+    const float by = scale == 0.f ? 1.f : fabsf(scale);
 #pragma unroll
     for (int i = 0; i < W / 32; i++)
 #pragma unroll
-        for (int r = 0; r < 16; r += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
-            const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-            const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-            const int d = i * 32 + 2 * r + 8 * half;
-            if (to >= 0 && d < D)
-                *(u32x4*)(out + d) = u32x4{even[0], odd[0], even[1], odd[1]};
+        for (int r = 0; r < 16; r++)
+            o[i][r] = 0.f;
+    l = 0.f;
+    top = -INFINITY;
+    load_keys(0);
+    load_values(0);
+#pragma unroll 1
+    for (int t = 0; t < tiles; t++) {
+        loads_done();
+        look(t);
+        __syncthreads();
+        if (t + 1 < tiles) {
+            load_keys(t + 1);
+            load_values(t + 1);
         }
+        scores(t);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t >= whole)
+            mask(t);
+        const float now = fmaxf(top, largest()), most = now * by;
+        // a score past binary32's range makes the row NaN, below it all weigh nothing
+        const float base = most == INFINITY ? __builtin_nanf("") : most == -INFINITY ? INFINITY : now;
+        const float f = top == now ? 1.f : __builtin_amdgcn_exp2f((top - now) * by * kLog2e);
+#pragma unroll
+        for (int i = 0; i < W / 32; i++)
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                o[i][r] *= f;
+        l *= f;
+        top = now;
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                float x[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    x[e] = __builtin_amdgcn_exp2f((s[b][r + e] - base) * by * kLog2e);
+                    l += x[e];
+                }
+                p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0], x[1]);
+            }
+        if (is_odd(t))
+            add_odd(t);
+        __builtin_amdgcn_sched_barrier(0);
+        even_products(t);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    store(std::true_type());
 }
 
 // kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS (64 at a time, which

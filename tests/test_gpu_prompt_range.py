@@ -1,0 +1,145 @@
+"""Packed prompts at the ends of binary32: scores up to its range and past it."""
+import math
+
+import pytest
+import torch
+
+from tests import _prompt_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+INF = math.inf
+
+
+@pytest.fixture(scope="module")
+def oil():
+    assert torch.cuda.is_available(), "GPU tests need a visible MI355X"
+    import paper_2608_03839_amd as m
+    m.lib()
+    return m
+
+
+def _int(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _normal(shape, seed=5):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+
+
+def _f32(x):
+    return torch.tensor(x, dtype=torch.float32).item()
+
+
+def _one_column(n, Hq, H, D, product, keys):
+    """q, k whose products are product * keys[j], exactly: one column of each is not zero.  q is a power
+    of two, about the square root of the product."""
+    q = torch.zeros((n, Hq, D), dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros((n, H, D), dtype=torch.bfloat16, device="cuda")
+    a = 2.0 ** (math.frexp(abs(product))[1] // 2)
+    q[..., 1] = a
+    k[..., 1] = (product / a * keys).to(torch.bfloat16)[:, None]
+    assert (k[:, 0, 1].double() == product / a * keys.double()).all()
+    return q, k
+
+
+def _exact(q, k, v, scale):
+    """out, lse, sum of weights times |v|, in 64 bits, of one causal sequence."""
+    T, Hq, D = q.shape
+    G = Hq // k.shape[1]
+    out, size = (torch.zeros((T, Hq, D), dtype=torch.float64, device="cuda") for _ in range(2))
+    lse = torch.zeros((T, Hq), dtype=torch.float64, device="cuda")
+    unseen = torch.ones((T, T), dtype=torch.bool, device="cuda").triu(1)
+    for head in range(Hq):
+        s = (scale * (q[:, head].double() @ k[:, head // G].double().T)).masked_fill(unseen, -INF)
+        m = s.amax(1, keepdim=True)
+        p = torch.exp(s - m)
+        total = p.sum(1, keepdim=True)
+        lse[:, head] = (m + total.log())[:, 0]
+        out[:, head] = p / total @ v[:, head // G].double()
+        size[:, head] = p / total @ v[:, head // G].double().abs()
+    return out, lse, size
+
+
+# (rows, query heads, heads, columns): one tile and several, two waves and four, both widths
+SIZES = [(1, 1, 1, 8), (150, 4, 2, 8), (150, 2, 1, 72), (2100, 16, 16, 8), (1100, 32, 4, 128)]
+# q . k of the keys that count most
+PRODUCTS = [2.0 ** 13, -2.0 ** 20, 2.0 ** 24, 7516192768.0, 3221225472.0, -2.0 ** 31, 2.0 ** 40, -2.0 ** 60, 2.0 ** 60,
+            2.0 ** 126, -1.75 * 2.0 ** 127, 1.75 * 2.0 ** 127]
+
+
+@pytest.mark.parametrize("n,Hq,H,D", SIZES)
+@pytest.mark.parametrize("scale", [1.0, _f32(128 ** -0.5), -0.75])
+def test_large_scores(oil, n, Hq, H, D, scale):
+    """Every key at one score, or one in ten a quarter nearer to zero: differences of 2^11 times the scale at
+    least, so that keys weigh the same or nothing."""
+    v = _normal((n, H, D))
+    for product in PRODUCTS:
+        for keys in (torch.ones(n), torch.where(torch.arange(n) % 10 == 3, 0.75, 1.0)):
+            q, k = _one_column(n, Hq, H, D, product, keys.cuda())
+            out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=scale)
+            w_out, w_lse, size = _exact(q, k, v, scale)
+            # weights alike, rounded to bf16 alike; sums of n values and of n weights, the quotient, bf16
+            far = 2 * 2.0 ** -8 * w_out.abs() + (n + 8) * 2.0 ** -23 * size
+            assert ((out.double() - w_out).abs() <= far).all(), (product, keys[3:4])
+            # the score, the logarithm and their sum
+            far = 2.0 ** -23 * (w_lse.abs() + 1) + 2.0 ** -22 * math.log(n + 1)
+            assert ((lse.double() - w_lse).abs() <= far).all(), (product, keys[3:4])
+
+
+@pytest.mark.parametrize("at", [0, 5, 100, 2000])
+@pytest.mark.parametrize("D", [16, 104])
+def test_one_large_score(oil, at, D):
+    """A key whose score leaves the others' far behind, in the first tile or a later one, before it and
+    after it ordinary rows; the other head's rows are ordinary throughout."""
+    n = 2100
+    q, k, v = _normal((n, 2, D), 1), _normal((n, 2, D), 2), _normal((n, 2, D), 3)
+    clean_out, clean_lse = oil.prompt_attend(q, k, v, _int([0, n]))
+    scale = 1 / math.sqrt(D)
+    for size in (2.0 ** 10, 2.0 ** 32, 2.0 ** 60):
+        qq, kk = q.clone(), k.clone()
+        qq[:, 1, 0] = size
+        kk[:, 1, 0] = 0.0
+        kk[at, 1, 0] = size
+        out, lse = oil.prompt_attend(qq, kk, v, _int([0, n]))
+        assert torch.equal(out[:, 0], clean_out[:, 0]) and torch.equal(lse[:, 0], clean_lse[:, 0])
+        w_out, w_lse, far_out, far_lse = ref.attend(qq[:at, 1:], kk[:at, 1:], v[:at, 1:], [0, at], scale)
+        assert ((out[:at, 1:].double() - w_out).abs() <= far_out).all()
+        # one weight and out, to bf16; where the row is made of it alone, nothing is rounded
+        assert ((out[at:, 1].double() - v[at, 1].double()).abs() <= 2.01 * 2.0 ** -8 * v[at, 1].double().abs()).all()
+        if size > 2.0 ** 30:
+            assert (out[at:, 1] == v[at, 1]).all()
+        score = scale * size * size + scale * (qq[at:, 1, 1:].double() @ kk[at, 1, 1:].double())
+        # D products and sums, scaled
+        assert ((lse[at:, 1].double() - score).abs() <= (D + 4) * 2.0 ** -23 * score).all()
+
+
+@pytest.mark.parametrize("n,Hq,H,D", SIZES)
+def test_scores_past_the_range(oil, n, Hq, H, D):
+    """Above it the row is NaN, below it the score is -inf."""
+    v = _normal((n, H, D))
+    for at in sorted({0, n // 2, n - 1}):
+        keys = torch.zeros(n, device="cuda")
+        keys[at] = 1.0
+        q, k = _one_column(n, Hq, H, D, 2.0 ** 127, keys)
+        out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=4.0)
+        assert torch.isnan(out[at:]).all() and torch.isnan(lse[at:]).all()
+        assert torch.isfinite(out[:at]).all() and torch.isfinite(lse[:at]).all()
+        weight = oil.prompt_weigh(q, k, lse, _int([0, n]), scale=4.0)
+        assert torch.isnan(weight).all()
+        # that key alone weighs nothing
+        out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=-4.0)
+        seen = torch.ones((n, n), dtype=torch.float64, device="cuda").tril()
+        seen[:, at] = 0.0
+        count = seen.sum(1)
+        values = v.double().repeat_interleave(Hq // H, 1).flatten(1)
+        want = (seen @ values / count.clamp(min=1.0)[:, None]).view(n, Hq, D)
+        size = (seen @ values.abs() / count.clamp(min=1.0)[:, None]).view(n, Hq, D)
+        far = 2 * 2.0 ** -8 * want.abs() + (n + 8) * 2.0 ** -23 * size
+        assert ((out.double() - want).abs() <= far).all()
+        w_lse = count.log()[:, None].expand(n, Hq)
+        assert torch.equal(lse == -INF, w_lse == -INF)
+        some = w_lse > -INF
+        assert ((lse.double() - w_lse)[some].abs() <= 2.0 ** -22 * (1 + w_lse[some])).all()
