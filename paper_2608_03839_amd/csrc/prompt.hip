@@ -55,6 +55,9 @@ constexpr int kMaxSeqs = 512;
 constexpr float kMost = 256.f;
 // Scores in base 2 from which on, in size, binary32 holds m with an error that matters beside them.
 constexpr float kFar = 0x1p24f;
+// An lse from which on, in size, weights are not taken from S c - lse log2 e: its roundings are some 2.5 x 2^-24
+// of lse, 2^-10.7 of a weight here.
+constexpr float kFarLse = 0x1p12f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A byte offset past every buffer's end (128 rows of 2^25 bytes at most): reads as zero.
 constexpr uint32_t kOutside = 0xFFFFFF00u;
@@ -717,7 +720,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     __shared__ __align__(1024) uint8_t row_lds[2][kTile];
     __shared__ __align__(16) float less_lds[2][kWeighRows];
     __shared__ __align__(16) int token_lds[2][kWeighRows];  // -1: the row counts nowhere
-    __shared__ int none_lds[2][NW];                         // whether the wave brought such a row
+    __shared__ int odd_lds[2][NW];  // whether the wave brought such a row or one past kFarLse (then + 2)
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = blockIdx.x % H;
@@ -733,7 +736,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const int seen_to = len - seen_from < chunk ? len : seen_from + chunk;
     const int rows = (seen_to - seen_from) * G;  // len * G <= T * Hq <= 2^30
     const int turns = (rows + kWeighRows - 1) / kWeighRows;
-    const float c = fabsf(scale) * kLog2e;
+    const float by = fabsf(scale), c = by * kLog2e;
     const uint32_t magic = 65536 / G + 1;  // x / G = x magic >> 16 for x < 64 + kWeighRows, G <= 64
 
     // A tile's rows are read from its first token's base: row x = rem + i is token x / G,
@@ -812,7 +815,9 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
         }
     };
     float total[2] = {0.f, 0.f}, part[2][2] = {};  // parts of 16 tiles, so that long sums lose little
-    auto add = [&](int t, int a, Scores& s, auto edge) {
+    // edge: rows count for the keys that they see; far: by (S scale - lse) log2 e, whose product is exact
+    // beside lse, so that weights are right wherever lse is
+    auto add = [&](int t, int a, Scores& s, auto edge, auto far) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const floatx4 less = *(const floatx4*)&less_lds[t & 1][a * 32 + 2 * r + 4 * half];
@@ -820,7 +825,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             for (int e = 0; e < 4; e++)
 #pragma unroll
                 for (int b = 0; b < 2; b++) {
-                    float x = __builtin_amdgcn_exp2f(fmaf(s[b][r + e], c, less[e]));
+                    float x = fmaf(s[b][r + e], decltype(far)::value ? by : c, less[e]);
+                    x = __builtin_amdgcn_exp2f(decltype(far)::value ? x * kLog2e : x);
                     if (decltype(edge)::value)
                         x = key[b] <= token_lds[t & 1][a * 32 + 2 * r + 4 * half + e] ? x : 0.f;
                     part[b][e & 1] += x;
@@ -831,14 +837,19 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const int wave_key = key0 + wave * kWeighKeys + kWeighKeys - 1;  // the wave's last
     for (int t = 0; t < turns; t++) {
         loads_done();
-        const bool unused = next_lse == -INFINITY;
-        if ((int)threadIdx.x < kWeighRows) {
-            less_lds[t & 1][threadIdx.x] = next_lse * -kLog2e;
-            token_lds[t & 1][threadIdx.x] = unused ? -1 : next_token;
+        const bool mine_too = (int)threadIdx.x < kWeighRows;
+        float less = next_lse * -kLog2e;
+        int odd = __ballot(mine_too && !(fabsf(next_lse) < kFarLse)) != 0;
+        if (odd && __ballot(mine_too && !(fabsf(next_lse) < kFarLse) && next_lse != -INFINITY)) {
+            odd = 3;
+            less = -next_lse;  // of all the wave's rows
         }
-        const int any = __ballot((int)threadIdx.x < kWeighRows && unused) != 0;
+        if (mine_too) {
+            less_lds[t & 1][threadIdx.x] = less;
+            token_lds[t & 1][threadIdx.x] = next_lse == -INFINITY ? -1 : next_token;
+        }
         if (lane == 0)
-            none_lds[t & 1][wave] = any;
+            odd_lds[t & 1][wave] = odd;
         __syncthreads();
         const int least = first_token;
         if (t + 1 < turns) {
@@ -851,16 +862,22 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             first_token = token0;
             load(t + 1);
         }
-        int none = 0;
+        int any = 0;
 #pragma unroll
-        for (int i = 0; i < NW; i++)
-            none |= none_lds[t & 1][i];
+        for (int i = 0; i < kWeighRows / 64; i++)
+            any |= odd_lds[t & 1][i] << (2 * i);
+        any = __builtin_amdgcn_readfirstlane(any);
         Scores s[2];
-        if (least < wave_key || __builtin_amdgcn_readfirstlane(none)) {
+        const std::true_type yes;
+        const std::false_type no;
+        if (least < wave_key || any) {
 #pragma unroll 1
             for (int a = 0; a < kParts; a++) {
                 scores(t, a, s[0]);
-                add(t, a, s[0], std::true_type());
+                if (any >> (2 * (a / 2)) & 2)
+                    add(t, a, s[0], yes, yes);
+                else
+                    add(t, a, s[0], yes, no);
             }
         } else {
             scores(t, 0, s[0]);
@@ -868,7 +885,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             for (int a = 0; a < kParts; a++) {
                 if (a + 1 < kParts)
                     scores(t, a + 1, s[(a + 1) & 1]);
-                add(t, a, s[a & 1], std::false_type());
+                add(t, a, s[a & 1], no, no);
             }
             // At 128 columns reads of LDS eight ahead, which leaves the exponentials where they
             // are beside products: 16 + 32 + 16 matrix instructions, 48 reads.  (Without: 8,192

@@ -143,3 +143,54 @@ def test_scores_past_the_range(oil, n, Hq, H, D):
         assert torch.equal(lse == -INF, w_lse == -INF)
         some = w_lse > -INF
         assert ((lse.double() - w_lse)[some].abs() <= 2.0 ** -22 * (1 + w_lse[some])).all()
+
+
+def _weigh(q, k, lse, last, scale):
+    """weight (H, T) of one sequence and its bound, in 64 bits from the lse given."""
+    T, Hq, D = q.shape
+    H = k.shape[1]
+    weight, far = (torch.zeros((H, T), dtype=torch.float64, device="cuda") for _ in range(2))
+    seen = torch.ones((T, T), dtype=torch.bool, device="cuda").tril()
+    seen[:max(0, T - last)] = False
+    for head in range(Hq):
+        h, size = head // (Hq // H), lse[:, head, None].double()
+        s = scale * (q[:, head].double() @ k[:, h].double().T)
+        x = s - size
+        p = torch.where(seen, torch.exp(x), 0.0)
+        # the difference, its product with log2 e, the exponential; below 2^12 both sides' products as well
+        e = (x.abs() + 1) * 2.0 ** -22 + torch.where(size.abs() < 4096, (s.abs() + size.abs()) * 2.0 ** -22, 0.0)
+        weight[h] += p.sum(0)
+        far[h] += torch.where(seen, p * e, 0.0).sum(0)
+    return weight, far + weight * (T * (Hq // H) + 8) * 2.0 ** -24 + 2.0 ** -126
+
+
+@pytest.mark.parametrize("n,Hq,H,D", SIZES)
+@pytest.mark.parametrize("scale", [1.0, _f32(128 ** -0.5), -0.75])
+def test_weights_of_large_scores(oil, n, Hq, H, D, scale):
+    """lse as it rounds to binary32, and as attention gives it."""
+    v = _normal((n, H, D))
+    for product in PRODUCTS:
+        for keys in (torch.ones(n), torch.where(torch.arange(n) % 10 == 3, 0.75, 1.0)):
+            q, k = _one_column(n, Hq, H, D, product, keys.cuda())
+            for lse in (_exact(q, k, v, scale)[1].float(), oil.prompt_attend(q, k, v, _int([0, n]), scale=scale)[1]):
+                for last in (n, 70):
+                    got = oil.prompt_weigh(q, k, lse, _int([0, n]), last=last, scale=scale)
+                    want, far = _weigh(q, k, lse, last, scale)
+                    # beside lse's last place a score may be past all exponentials: infinities have no difference
+                    near = ((got.double() - want).abs() <= far) | (got == want.float())
+                    assert near.all(), (product, last, keys[3:4])
+
+
+@pytest.mark.parametrize("D", [16, 104])
+def test_weights_beside_large_scores(oil, D):
+    """One head of a group asks with scores past 2^12, the other with ordinary ones.  Whole numbers, so
+    that every score is exact."""
+    n = 700
+    q, k, v = (_normal((n, h, D), i).float().mul(1.5).round().to(torch.bfloat16) for i, h in ((1, 4), (2, 2), (3, 2)))
+    q[:, 1] *= 2048.0
+    lse = _exact(q, k, v, 0.25)[1].float()
+    assert (lse[200:, 1] > 4096).all() and (lse[:, 0] < 4096).all()
+    for last in (n, 130):
+        got = oil.prompt_weigh(q, k, lse, _int([0, n]), last=last, scale=0.25)
+        want, far = _weigh(q, k, lse, last, 0.25)
+        assert ((got.double() - want).abs() <= far).all()
