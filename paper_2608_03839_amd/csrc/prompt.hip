@@ -81,6 +81,15 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
 }
 
+// bf16 values times zero, without the sign: NaN where they are not finite (all bits of the exponent set).
+__device__ __forceinline__ u32x4 times_zero(u32x4 w)
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        w[e] = (((w[e] & 0x7F807F80u) + 0x00800080u) >> 15 & 0x00010001u) * 0x7FC0u;
+    return w;
+}
+
 // A value beside its counterpart 32 lanes away.
 __device__ __forceinline__ void swap32(float x, float* a, float* b)
 {
@@ -333,13 +342,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         } else if (scale == 0.f) {
 #pragma unroll
             for (int i = 0; i < W / 16; i++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    // what is not finite becomes NaN: its exponent has all bits set
-                    const uint32_t w = qs[i].w[e] & 0x7F807F80u;
-                    const uint32_t odd = ((w + 0x00800080u) >> 15) & 0x00010001u;
-                    qs[i].w[e] = odd * 0x7FC0u;
-                }
+                qs[i].w = times_zero(qs[i].w);
         }
     }
 
@@ -792,6 +795,14 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             ks[b][i].w = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
             ks[b][i].w ^= turn;
         }
+    }
+    if (scale == 0.f) {
+        // as in attention, so that a product past binary32's range does not become NaN
+#pragma unroll
+        for (int b = 0; b < 2; b++)
+#pragma unroll
+            for (int i = 0; i < W / 16; i++)
+                ks[b][i].w = times_zero(ks[b][i].w);
     }
     int row_at[W / 16];
 #pragma unroll

@@ -194,3 +194,28 @@ def test_weights_beside_large_scores(oil, D):
         got = oil.prompt_weigh(q, k, lse, _int([0, n]), last=last, scale=0.25)
         want, far = _weigh(q, k, lse, last, 0.25)
         assert ((got.double() - want).abs() <= far).all()
+
+
+@pytest.mark.parametrize("n,Hq,H,D", SIZES)
+def test_scale_zero(oil, n, Hq, H, D):
+    """Finite rows' scores are 0, their products in binary32's range or not; others' are NaN."""
+    q, k, v = (_normal((n, h, D), i) for i, h in ((1, Hq), (2, H), (3, H)))
+    q[..., 3], k[..., 3] = 2.0 ** 70, 2.0 ** 70
+    k[n // 2, :, 3] = -2.0 ** 70
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=0.0)
+    count = torch.arange(1, n + 1, dtype=torch.float64, device="cuda")[:, None]
+    # the logarithm is right to a unit, 2^-23 of it; ln 2, the product and its sum with the score to half of one each
+    assert ((lse.double() - count.log()).abs() <= (2.0 ** -23 + 3 * 2.0 ** -24) * count.log()).all()
+    for last in (n, 17):
+        weight = oil.prompt_weigh(q, k, lse, _int([0, n]), last=last, scale=0.0)
+        rows = torch.where(torch.arange(n, device="cuda") >= n - last, 1 / count[:, 0], 0.0) * (Hq // H)
+        want = rows.flip(0).cumsum(0).flip(0)
+        # lse, its product with log2 e, the exponential, sums
+        far = want * ((math.log(n) + 2) * 2.0 ** -22 + (n * (Hq // H) + 8) * 2.0 ** -24)
+        assert ((weight.double() - want).abs() <= far).all()
+    if n > 1:
+        k[1, 0, 2] = INF
+        got, size = oil.prompt_attend(q, k, v, _int([0, n]), scale=0.0)
+        assert torch.isnan(size[1:, :Hq // H]).all() and torch.equal(size[:, Hq // H:], lse[:, Hq // H:])
+        weight = oil.prompt_weigh(q, k, lse, _int([0, n]), scale=0.0)
+        assert torch.isnan(weight[0, 1]) and torch.isfinite(weight[0, 2:]).all() and torch.isfinite(weight[1:]).all()
