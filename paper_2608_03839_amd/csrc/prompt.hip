@@ -449,8 +449,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             any |= odd_lds[t & 1][i];
         return __builtin_amdgcn_readfirstlane(any) != 0;
     };
-    // What of tile t's values is not finite, added to the rows that see it.
-    auto add_odd = [&](int t) __attribute__((always_inline)) {
+    // What of tile t's values is not finite, added to the rows that see it: those of keys of which sees is true.
+    auto add_odd = [&](int t, auto sees) __attribute__((always_inline)) {
         const uint8_t* values = value_lds[t & 1];
 #pragma unroll 1
         for (int key = 0; key < kKeys; key++)
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
 #pragma unroll
                     for (int e = 0; e < 4; e++) {
                         const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
-                        if ((u & 0x7F800000u) == 0x7F800000u && t * kKeys + key <= token)
+                        if ((u & 0x7F800000u) == 0x7F800000u && sees(key))
                             o[i][r + e] += __uint_as_float(u);
                     }
                 }
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         // a value that is not finite must not reach rows that do not see it through a product with zero:
         // where the tile has one, it leaves the products and is added to the rows that see it
         if (decltype(edge)::value && __builtin_expect(is_odd(t), 0)) {
-            add_odd(t);
+            add_odd(t, [&](int key) { return t * kKeys + key <= token; });
             even_products(t);
         } else {
 #pragma unroll
@@ -681,7 +681,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
         for (int i = 0; i < W / 32; i++)
 #pragma unroll
             for (int r = 0; r < 16; r++)
-                o[i][r] *= f;
+                o[i][r] *= __builtin_isfinite(o[i][r]) ? f : 1.f;
         l *= f;
         top = now;
 #pragma unroll
@@ -696,8 +696,18 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 }
                 p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0], x[1]);
             }
-        if (is_odd(t))
-            add_odd(t);
+        if (is_odd(t)) {
+            // a value that is not finite counts wherever the score is above -inf, even if the weight is 0 in
+            // binary32: so tiles and the order of keys decide nothing
+            uint32_t mine = 0;
+#pragma unroll
+            for (int b = 0; b < 2; b++)
+#pragma unroll
+                for (int r = 0; r < 16; r++)
+                    mine |= (uint32_t)!(s[b][r] * by == -INFINITY) << (16 * b + r);
+            const auto seen = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+            add_odd(t, [&](int key) { return seen[key >> 2 & 1] >> (key / 32 * 16 + key % 32 / 8 * 4 + key % 4) & 1; });
+        }
         __builtin_amdgcn_sched_barrier(0);
         even_products(t);
         __builtin_amdgcn_sched_barrier(0);

@@ -219,3 +219,48 @@ def test_scale_zero(oil, n, Hq, H, D):
         assert torch.isnan(size[1:, :Hq // H]).all() and torch.equal(size[:, Hq // H:], lse[:, Hq // H:])
         weight = oil.prompt_weigh(q, k, lse, _int([0, n]), scale=0.0)
         assert torch.isnan(weight[0, 1]) and torch.isfinite(weight[0, 2:]).all() and torch.isfinite(weight[1:]).all()
+
+
+@pytest.mark.parametrize("Hq,H,D", [(4, 2, 64), (2, 2, 128), (3, 1, 24)])
+@pytest.mark.parametrize("at", [0, 3, 70, 200])
+def test_values_that_are_not_finite_without_weight(oil, Hq, H, D, at):
+    """Under a weight that is 0 in binary32 they count, under a score of -inf they do not; alike for a
+    sequence alone, in tiles of 64 rows, and packed, in tiles of 128."""
+    n, G = 300, Hq // H
+    more = 128 * 256 // Hq + 1
+    q, k, v = (_normal((n + more, h, D), i) for i, h in ((1, Hq), (2, H), (3, H)))
+    q[..., 0], k[..., 0] = 32.0, 0.0
+    v[at, 0, 5], v[at, 0, 6], v[at, 0, 7] = INF, -INF, math.nan
+    for low in (-300.0, -INF):
+        k[at, 0, 0] = low                              # below the others by some 9,600, or without a score
+        alone = oil.prompt_attend(q[:n], k[:n], v[:n], _int([0, n]), scale=1.0)
+        packed = oil.prompt_attend(q, k, v, _int([0, n, n + more]), scale=1.0)
+        for a, b in zip(alone, packed):
+            assert ((a == b[:n]) | (a.isnan() & b[:n].isnan())).all()
+        out, lse = alone
+        clean = oil.prompt_attend(q[:n], k[:n], torch.where(v[:n].isfinite(), v[:n], 0.0), _int([0, n]), scale=1.0)
+        assert torch.equal(lse, clean[1])
+        same = torch.ones_like(out, dtype=torch.bool)
+        same[at:, :G, 5:8] = False
+        assert torch.equal(out[same], clean[0][same])
+        if low != -INF:
+            assert (out[at:, :G, 5] == INF).all() and (out[at:, :G, 6] == -INF).all()
+            assert torch.isnan(out[at:, :G, 7]).all()
+        else:
+            # made in another way, with weights rounded to bf16 and out rounded in both
+            size = oil.prompt_attend(q[:n], k[:n], torch.where(v[:n].isfinite(), v[:n].abs(), 0.0), _int([0, n]),
+                                     scale=1.0)[0].double() * (1 + 2.0 ** -6)
+            off = (out.double() - clean[0].double()).abs()
+            assert (off <= 2 * 2.0 ** -8 * (size + clean[0].double().abs()) * (1 + 2.0 ** -7)).all()
+            if at == 0:                                # a row of this key alone
+                assert (out[0, :G] == 0).all() and (lse[0, :G] == -INF).all()
+
+
+@pytest.mark.parametrize("n,Hq,H,D", [(90, 2, 1, 64), (2100, 16, 16, 128)])
+def test_rows_without_scores(oil, n, Hq, H, D):
+    """Scores of -inf alone give zeros, whatever the values are."""
+    q, k, v = (_normal((n, h, D), i) for i, h in ((1, Hq), (2, H), (3, H)))
+    q[..., 1], k[..., 1] = 2.0, -INF
+    v[::5], v[1::5], v[2::5] = INF, -INF, math.nan
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]))
+    assert (out == 0).all() and (lse == -INF).all()
