@@ -249,7 +249,6 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     __shared__ __align__(1024) uint8_t key_lds[2][kTile];
     __shared__ __align__(1024) uint8_t value_lds[2][kTile];
     __shared__ int odd_lds[2][NW];                // whether a wave's part of the values is not finite
-    __shared__ int again_lds[NW];                 // whether a wave has results that are made again
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // The arguments, read where they are used: held throughout they would take the scalar
@@ -441,56 +440,47 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             a.h[e] = column_of(values + value_at[i] + (16 * j + 8 * e) * W * 2);
         return a;
     };
-    // whether a wave found tile t's values not finite
-    auto is_odd = [&](int t) __attribute__((always_inline)) {
-        int any = 0;
-#pragma unroll
-        for (int i = 0; i < NW; i++)
-            any |= odd_lds[t & 1][i];
-        return __builtin_amdgcn_readfirstlane(any) != 0;
-    };
-    // What of tile t's values is not finite, added to the rows that see it: those of keys of which sees is true.
-    auto add_odd = [&](int t, auto sees) __attribute__((always_inline)) {
-        const uint8_t* values = value_lds[t & 1];
-#pragma unroll 1
-        for (int key = 0; key < kKeys; key++)
-#pragma unroll
-            for (int i = 0; i < W / 32; i++)
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const uint32_t* at = (const uint32_t*)(values + value_place<W>(key, 4 * i + r / 4) * 16 + 8 * half);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
-                        if ((u & 0x7F800000u) == 0x7F800000u && sees(key))
-                            o[i][r + e] += __uint_as_float(u);
-                    }
-                }
-    };
-    // O^T += V^T P of tile t without it.
-    auto even_products = [&](int t) __attribute__((always_inline)) {
-        const uint8_t* values = value_lds[t & 1];
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int i = 0; i < W / 32; i++) {
-                Operand a = value_part(values, j, i);
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
-                    a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
-                }
-                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
-            }
-    };
     // O^T += V^T P of tile t
     auto products = [&](int t, auto edge) {
         const uint8_t* values = value_lds[t & 1];
-        // a value that is not finite must not reach rows that do not see it through a product with zero:
-        // where the tile has one, it leaves the products and is added to the rows that see it
-        if (decltype(edge)::value && __builtin_expect(is_odd(t), 0)) {
-            add_odd(t, [&](int key) { return t * kKeys + key <= token; });
-            even_products(t);
+        bool odd = false;
+        if (decltype(edge)::value) {
+            // a value that is not finite must not reach rows that do not see it through a
+            // product with zero: where the tile has one, it leaves the products and is
+            // added to the rows that see it
+            int any = 0;
+#pragma unroll
+            for (int i = 0; i < NW; i++)
+                any |= odd_lds[t & 1][i];
+            odd = __builtin_amdgcn_readfirstlane(any) != 0;
+        }
+        if (decltype(edge)::value && __builtin_expect(odd, 0)) {
+#pragma unroll 1
+            for (int key = 0; key < kKeys; key++)
+#pragma unroll
+                for (int i = 0; i < W / 32; i++)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4) {
+                        const uint32_t* at = (const uint32_t*)(values + value_place<W>(key, 4 * i + r / 4) * 16 + 8 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const uint32_t u = e & 1 ? at[e / 2] & 0xFFFF0000u : at[e / 2] << 16;
+                            if ((u & 0x7F800000u) == 0x7F800000u && t * kKeys + key <= token)
+                                o[i][r + e] += __uint_as_float(u);
+                        }
+                    }
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < W / 32; i++) {
+                    Operand a = value_part(values, j, i);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        a.w[e] = (a.w[e] & 0x7F80u) == 0x7F80u ? a.w[e] & 0xFFFF0000u : a.w[e];
+                        a.w[e] = (a.w[e] & 0x7F800000u) == 0x7F800000u ? a.w[e] & 0xFFFFu : a.w[e];
+                    }
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
+                }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -585,7 +575,8 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     }
     loads_done();  // none is in flight when the buffers go to another workgroup
 
-    // Writes the row; `again`: where what is there is not finite.  Whether anything written is not finite.
+    // Writes the row; `again`: where what is there is not finite.  Whether anything written is not finite, but
+    // for rows that a score of NaN makes NaN.
     auto store = [&](auto again) {
         float x, y;
         swap32(l, &x, &y);
@@ -633,24 +624,18 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 }
                 *(u32x4*)(out + d) = now;
             }
-        return (size & 0xFFFFu) >= 0x7F80u || size >= 0x7F800000u;
+        return ((size & 0xFFFFu) >= 0x7F80u || size >= 0x7F800000u) &&
+               !(isnan(sum) && (isnan(top) || !isnan(less)));
     };
-    const bool odd = store(std::false_type());
+    if (!__ballot(store(std::false_type())))
+        return;
 
     // Results that are not finite are made again, with the largest score sought in every tile, unscaled, and
     // taken from the others before they are scaled: exact where it matters, whatever the scores.  Rare, so made
-    // simply; what is finite stays as it was, so that a row's bits do not depend on those beside it.
-    const int any = __ballot(odd) != 0;
-    if (lane == 0)
-        again_lds[wave] = any;
-    __syncthreads();
-    int again = 0;
-#pragma unroll
-    for (int i = 0; i < NW; i++)
-        again |= again_lds[i];
-    if (!__builtin_amdgcn_readfirstlane(again))
-        return;
+    // simply, by each wave that has some, from memory; what is finite stays as it was, so that a row's bits do
+    // not depend on those beside it.
     const float by = scale == 0.f ? 1.f : fabsf(scale);
+    const int D = args()->D;
 #pragma unroll
     for (int i = 0; i < W / 32; i++)
 #pragma unroll
@@ -658,21 +643,25 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             o[i][r] = 0.f;
     l = 0.f;
     top = -INFINITY;
-    load_keys(0);
-    load_values(0);
 #pragma unroll 1
     for (int t = 0; t < tiles; t++) {
-        loads_done();
-        look(t);
-        __syncthreads();
-        if (t + 1 < tiles) {
-            load_keys(t + 1);
-            load_values(t + 1);
+#pragma unroll
+        for (int b = 0; b < 2; b++) {
+            const int key = t * kKeys + b * 32 + col;
+            const uint16_t* from = (const uint16_t*)(key_base + (uint64_t)(key < len ? key : len - 1) * row_bytes);
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+                s[b][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < W / 16; i++) {
+                Operand a;
+                a.w = 16 * i + 8 * half < D ? *(const u32x4*)(from + 16 * i + 8 * half) : u32x4{0, 0, 0, 0};
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, qs[i].b, s[b], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        scores(t);
+        mask(t);
         __builtin_amdgcn_sched_barrier(0);
-        if (t >= whole)
-            mask(t);
         const float now = fmaxf(top, largest()), most = now * by;
         // a score past binary32's range makes the row NaN, below it all weigh nothing
         const float base = most == INFINITY ? __builtin_nanf("") : most == -INFINITY ? INFINITY : now;
@@ -684,6 +673,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 o[i][r] *= __builtin_isfinite(o[i][r]) ? f : 1.f;
         l *= f;
         top = now;
+        uint32_t counts = 0;  // keys, in the order of s, of scores above -inf
 #pragma unroll
         for (int b = 0; b < 2; b++)
 #pragma unroll
@@ -693,24 +683,76 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 for (int e = 0; e < 2; e++) {
                     x[e] = __builtin_amdgcn_exp2f((s[b][r + e] - base) * by * kLog2e);
                     l += x[e];
+                    counts |= (uint32_t)!(s[b][r + e] * by == -INFINITY) << (16 * b + r + e);
                 }
                 p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0], x[1]);
             }
-        if (is_odd(t)) {
-            // a value that is not finite counts wherever the score is above -inf, even if the weight is 0 in
-            // binary32: so tiles and the order of keys decide nothing
-            uint32_t mine = 0;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int b = 0; b < 2; b++)
+        for (int i = 0; i < W / 32; i++) {
+            // the lane's column of V^T; columns past D are not written, keys past the sequence do not count
+            const uint64_t from = value_base + (32 * i + col < D ? 32 * i + col : 0) * 2;
+            Operand values[2];  // of two j: more loads in flight at once take a wave from a SIMD at 64 columns
 #pragma unroll
-                for (int r = 0; r < 16; r++)
-                    mine |= (uint32_t)!(s[b][r] * by == -INFINITY) << (16 * b + r);
-            const auto seen = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
-            add_odd(t, [&](int key) { return seen[key >> 2 & 1] >> (key / 32 * 16 + key % 32 / 8 * 4 + key % 4) & 1; });
+            for (int j = 0; j < 4; j++) {
+                if (j % 2 == 0) {
+                    int first_key = t * kKeys + 16 * j + 4 * half;
+                    asm volatile("" : "+v"(first_key));  // addresses are made here, not held for every i
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        uint32_t u[2];
+#pragma unroll
+                        for (int z = 0; z < 2; z++) {
+                            const int key = first_key + 8 * (e / 2) + 2 * (e % 2) + z;
+                            u[z] = *(const uint16_t*)(from + (uint64_t)(key < len ? key : len - 1) * row_bytes);
+                        }
+                        values[e / 4].w[e % 4] = u[0] | u[1] << 16;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                Operand a = values[j % 2];
+                uint32_t size = 0;
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    size = max_u16(size, a.w[e] & 0x7FFF7FFFu);
+                asm volatile("" : "+v"(counts));  // nor what is made of this
+                if (__ballot((size & 0xFFFFu) >= 0x7F80u || size >= 0x7F800000u)) {
+                    // a value that is not finite counts wherever the score is above -inf, even if the weight is 0
+                    // in binary32, so that tiles and the order of keys decide nothing: how many infinities of
+                    // either sign do, NaN as both
+                    Operand up, down, count;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        up.w[e] = down.w[e] = count.w[e] = 0;
+#pragma unroll
+                        for (int z = 0; z < 2; z++) {
+                            const uint32_t u = a.w[e] >> (16 * z) & 0xFFFFu, one = 0x3F80u << (16 * z);
+                            const bool odd = (u & 0x7F80u) == 0x7F80u;
+                            up.w[e] |= odd && u != 0xFF80u ? one : 0u;
+                            down.w[e] |= odd && u != 0x7F80u ? one : 0u;
+                            count.w[e] |= counts >> (8 * j + 2 * e + z) & 1 ? one : 0u;
+                            a.w[e] &= odd ? ~(0xFFFFu << (16 * z)) : ~0u;
+                        }
+                    }
+                    floatx16 n;
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        n[r] = 0.f;
+                    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up.b, count.b, n, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        o[i][r] += n[r] > 0.f ? INFINITY : 0.f;
+                        n[r] = 0.f;
+                    }
+                    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down.b, count.b, n, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        o[i][r] -= n[r] > 0.f ? INFINITY : 0.f;
+                }
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.b, p[j].b, o[i], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        even_products(t);
-        __builtin_amdgcn_sched_barrier(0);
     }
     store(std::true_type());
 }
