@@ -612,6 +612,7 @@ size_t oil_prompt_weigh_workspace_bytes(int32_t B, int64_t total, int32_t n_q_he
  * its row NaN, one below counts as -inf.  With scale 0 the scores of finite rows are 0.
  * A value that is not finite makes its column of a row what a weight above zero would,
  * however small it is, and nothing where the score is -inf.
+ * out stays within bf16 wherever the values do.
  * Sums, the softmax's statistics and lse are binary32.  Rounded to fewer bits are the
  * weights exp(S - m), m a number for each row, to bf16 for their product with v (half a
  * step is 2^-8 of each; the sum that divides is of unrounded ones), and out. */

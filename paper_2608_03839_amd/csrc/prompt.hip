@@ -51,13 +51,15 @@ constexpr int kWeighKeys = 64;   // keys of a wave
 constexpr int kWeighRows = 128;  // rows of a tile
 constexpr int kMaxSeqs = 512;
 // The most that a lane's 32 weights of a tile may add up to: what is rounded to bf16 keeps its relative
-// precision whatever m is, and sums of 2^30 such weights stay within binary32.
+// precision whatever m is, and sums of 2^30 such weights stay within binary32.  Their products with values need
+// not, though what they are divided to does: such results are made again with weights that add up to less than 1.
 constexpr float kMost = 256.f;
 // Scores in base 2 from which on, in size, binary32 holds m with an error that matters beside them.
 constexpr float kFar = 0x1p24f;
 // An lse from which on, in size, weights are not taken from S c - lse log2 e: its roundings are some 2.5 x 2^-24
 // of lse, 2^-10.7 of a weight here.
 constexpr float kFarLse = 0x1p12f;
+constexpr float kLargest = 0x1.FEp127f;  // of bf16
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A byte offset past every buffer's end (128 rows of 2^25 bytes at most): reads as zero.
 constexpr uint32_t kOutside = 0xFFFFFF00u;
@@ -575,12 +577,15 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     }
     loads_done();  // none is in flight when the buffers go to another workgroup
 
+    // what a second pass's weights are multiplied by: a power of two below 1 / (2 len)
+    const float small = __uint_as_float((uint32_t)(127 - 33 + __builtin_clz(len)) << 23);
     // Writes the row; `again`: where what is there is not finite.  Whether anything written is not finite, but
     // for rows that a score of NaN makes NaN.
     auto store = [&](auto again) {
         float x, y;
         swap32(l, &x, &y);
-        const float sum = x + y, inv = sum == 0.f ? 0.f : 1.f / sum;  // scores of -inf alone give zeros
+        const float sum = x + y;
+        const float inv = sum == 0.f ? 0.f : (decltype(again)::value ? 1.f / small : 1.f) / sum;  // scores of -inf alone give zeros
         const auto* a = args();
         if (to >= 0 && a->lse && half == 0) {
             // with the score itself, not with m: to the last place of what the score alone has
@@ -601,8 +606,18 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
             for (int r = 0; r < 16; r += 8) {
                 uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    w[e] = pack2(o[i][r + 2 * e] * inv, o[i][r + 2 * e + 1] * inv);
+                for (int e = 0; e < 4; e++) {
+                    float z[2];
+#pragma unroll
+                    for (int n = 0; n < 2; n++) {
+                        const float u = o[i][r + 2 * e + n];
+                        z[n] = u * inv;
+                        // no mean is past all values, which a weight's rounding can bring it
+                        if (decltype(again)::value && __builtin_isfinite(u))
+                            z[n] = fminf(fmaxf(z[n], -kLargest), kLargest);
+                    }
+                    w[e] = pack2(z[0], z[1]);
+                }
                 const auto even = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
                 const auto odd = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
                 const int d = i * 32 + 2 * r + 8 * half;
@@ -685,7 +700,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                     l += x[e];
                     counts |= (uint32_t)!(s[b][r + e] * by == -INFINITY) << (16 * b + r + e);
                 }
-                p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0], x[1]);
+                p[2 * b + r / 8].w[(r % 8) / 2] = pack2(x[0] * small, x[1] * small);
             }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

@@ -264,3 +264,49 @@ def test_rows_without_scores(oil, n, Hq, H, D):
     v[::5], v[1::5], v[2::5] = INF, -INF, math.nan
     out, lse = oil.prompt_attend(q, k, v, _int([0, n]))
     assert (out == 0).all() and (lse == -INF).all()
+
+
+def _finite_and_near(out, want, far):
+    assert torch.isfinite(out).all()
+    off = (out.double() - want).abs()
+    assert (off <= far).all(), (off / far).max().item()
+
+
+@pytest.mark.parametrize("n,Hq,H,D", [(1, 1, 1, 8), (300, 4, 2, 24), (300, 2, 2, 128), (2100, 16, 16, 64), (1500, 32, 8, 128)])
+def test_large_values(oil, n, Hq, H, D):
+    """Values up to the largest of bf16: a mean of them is no larger, whatever their weighted sum is."""
+    q, k = _normal((n, Hq, D), 1), _normal((n, H, D), 2)
+    scale = 1 / math.sqrt(D)
+    largest = torch.finfo(torch.bfloat16).max
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    signs = torch.randint(2, (n, H, D), generator=g, device="cuda") * 2.0 - 1
+    # a few scores: the largest far from the first tile's, where weights are above 1
+    wide = q * 3
+    for v in (torch.full((n, H, D), largest), torch.full((n, H, D), -2.0 ** 127), signs * largest,
+              _normal((n, H, D), 3).float() * 2.0 ** 122):
+        v = v.to(device="cuda", dtype=torch.bfloat16)
+        for asks in (q, wide, q * 0):
+            out, lse = oil.prompt_attend(asks, k, v, _int([0, n]), scale=scale)
+            w_out, w_lse, far_out, far_lse = ref.attend(asks, k, v, [0, n], scale)
+            _finite_and_near(out, w_out, far_out)
+            assert ((lse.double() - w_lse).abs() <= far_lse).all()
+        if (v == v[:1]).all():  # equal weights of equal values
+            assert (out == v[0].repeat_interleave(Hq // H, 0)).all()
+
+
+@pytest.mark.parametrize("at", [70, 1000, 2000])
+@pytest.mark.parametrize("D", [8, 128])
+def test_large_values_of_a_later_key(oil, at, D):
+    """A key nearly 8 powers of two above the first tile's weighs 200 times the others' ones."""
+    n = 2100
+    q = torch.zeros((n, 2, D), dtype=torch.bfloat16, device="cuda")
+    k, v = torch.zeros_like(q), _normal((n, 2, D), 3)
+    q[..., 0] = 1.0
+    k[at, :, 0] = 5.25
+    v[at] = 2.0 ** 121
+    v[at, 1] = -2.0 ** 127
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=1.0)
+    w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [0, n], 1.0)
+    _finite_and_near(out, w_out, far_out)
+    assert ((lse.double() - w_lse).abs() <= far_lse).all()
