@@ -492,6 +492,8 @@ int32_t oil_kv_append(oil_kv *kv, const int32_t *slots, int32_t B, const void *k
  * `total` rows of k and v, whose other arguments are oil_kv_append's.
  *   starts     B + 1 int32 (device), ascending within 0 .. total; values past those
  *              bounds count as the bound, a sequence that ends before it begins as empty.
+ *              Of starts that do not ascend either every sequence is appended or, where
+ *              the call's workgroups are too few, none, and no slot changes.
  *   total      1 .. OIL_PROMPT_MAX_ROWS.
  *   weight     n_heads x total float32 by row, as oil_prompt_weigh wrote it, or NULL for 0. */
 int32_t oil_kv_append_packed(oil_kv *kv, const int32_t *slots, int32_t B, const int32_t *starts, int64_t total,
@@ -581,7 +583,9 @@ int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, 
  * (oil_kv_append_packed).
  *
  * Common arguments:
- *   starts     B + 1 int32 (device) as in oil_kv_append_packed.  B 1 .. OIL_MAX_B.
+ *   starts     B + 1 int32 (device), ascending within 0 .. total; bounds and empty sequences
+ *              as in oil_kv_append_packed.  What is written for rows of sequences that overlap,
+ *              and of those after them, is undefined.  B 1 .. OIL_MAX_B.
  *   total      rows of every buffer, 1 .. OIL_PROMPT_MAX_ROWS; times n_q_heads at most 2^30.
  *   q          total rows of n_q_heads x head_dim bf16, 16-byte aligned, rows q_ld
  *              elements apart (>= n_q_heads * head_dim, a multiple of 8, at most

@@ -83,20 +83,17 @@ __device__ __forceinline__ void kv_advance(const KvView& c, int slot, int32_t le
     st[kKvNext] = next < INT32_MAX ? (int32_t)next : INT32_MAX;
 }
 
-// The state after an append (rows of max_rows, nodes, count; or of packed sequences,
-// with starts) or, with max_rows 0, a reset; one workgroup per request.
+// The state after an append (rows of max_rows, nodes, count) or, with max_rows
+// 0, a reset; one workgroup per request.
 __global__ __launch_bounds__(64) void kv_state_kernel(KvView c, const int32_t* __restrict__ slots, int32_t max_rows,
                                                       const int32_t* __restrict__ nodes,
-                                                      const int32_t* __restrict__ count,
-                                                      const int32_t* __restrict__ starts)
+                                                      const int32_t* __restrict__ count)
 {
     __shared__ int bound;
     const int b = blockIdx.x, slot = kv_slot(c, slots, b);
     if (slot < 0)
         return;
-    const int cnt = starts     ? seq_end(starts, max_rows, b) - seq_first(starts, max_rows, b)
-                    : max_rows ? kv_count(nodes, count, b, max_rows, &bound)
-                               : 0;
+    const int cnt = max_rows ? kv_count(nodes, count, b, max_rows, &bound) : 0;
     if (threadIdx.x != 0)
         return;
     if (max_rows)
@@ -213,6 +210,47 @@ struct KvRowRegs {
 __device__ __forceinline__ int64_t kv_packed_place(const int32_t* starts, int32_t total, int b)
 {
     return seq_first(starts, total, b) / kKvTile + 2ll * b;
+}
+
+// The tiles that its n rows can touch.
+__device__ __forceinline__ int64_t kv_packed_tiles(int n) { return n > 0 ? n / kKvTile + 2ll : 0; }
+
+// The state after an append of packed sequences, a thread a request.  Starts that do not ascend can leave a
+// request without its workgroups: then no request has got rows, and what the append wrote past the slots'
+// lengths is cleared.
+__global__ __launch_bounds__(256) void kv_packed_state_kernel(KvView c, const int32_t* __restrict__ slots, int32_t B,
+                                                              const int32_t* __restrict__ starts, int32_t total)
+{
+    __shared__ int short_of;
+    if (threadIdx.x == 0)
+        short_of = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < B; b += 256) {
+        const int64_t next = b + 1 < B ? kv_packed_place(starts, total, b + 1) : total / kKvTile + 2ll * B;
+        if (next - kv_packed_place(starts, total, b) <
+            kv_packed_tiles(seq_end(starts, total, b) - seq_first(starts, total, b)))
+            short_of = 1;
+    }
+    __syncthreads();
+    if (short_of) {
+        for (int b = blockIdx.x * 256; b < B && b < (int)blockIdx.x * 256 + 256; b++) {
+            const int slot = kv_slot(c, slots, b);
+            if (slot < 0)
+                continue;
+            const int64_t len = kv_len(c, slot), past = len + seq_end(starts, total, b) - seq_first(starts, total, b);
+            const int64_t end = past < c.cap ? past : c.cap;
+            for (int h = 0; h < c.H; h++)
+                for (int64_t i = kv_row(c, slot, h) + len + threadIdx.x; i < kv_row(c, slot, h) + end; i += 256) {
+                    c.pos[i] = -1;
+                    c.weight[i] = 0.f;
+                }
+        }
+        return;
+    }
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    const int slot = b < B ? kv_slot(c, slots, b) : -1;
+    if (slot >= 0)
+        kv_advance(c, slot, kv_len(c, slot), seq_end(starts, total, b) - seq_first(starts, total, b));
 }
 
 // kPacked: `starts` tells the rows of each of the B requests (oil_kv_append_packed), of
@@ -792,7 +830,7 @@ hipError_t launch_kv_reset(const KvView& c, const int32_t* slots, int32_t B, hip
     const int64_t blocks = (c.cap + 4095) / 4096 < 64 ? (c.cap + 4095) / 4096 : 64;
     hipLaunchKernelGGL(kv_reset_kernel, dim3((unsigned)blocks, c.H, B), dim3(256), 0, stream, c, slots);
     if (blocks * c.H > kTickets)
-        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, 0, nullptr, nullptr, nullptr);
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, 0, nullptr, nullptr);
     return hipGetLastError();
 }
 
@@ -817,7 +855,7 @@ hipError_t launch_kv_append(const KvView& c, const int32_t* slots, int32_t B, co
         OIL_KV_APPEND(128, uint16_t);
 #undef OIL_KV_APPEND
     if ((int64_t)grid.x * c.H > kTickets)
-        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, max_rows, nodes, count, nullptr);
+        hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, max_rows, nodes, count);
     return hipGetLastError();
 }
 
@@ -838,7 +876,7 @@ hipError_t launch_kv_append_packed(const KvView& c, const int32_t* slots, int32_
     else
         OIL_KV_APPEND(128, uint16_t);
 #undef OIL_KV_APPEND
-    hipLaunchKernelGGL(kv_state_kernel, dim3(B), dim3(64), 0, stream, c, slots, total, nullptr, nullptr, starts);
+    hipLaunchKernelGGL(kv_packed_state_kernel, dim3((B + 255) / 256), dim3(256), 0, stream, c, slots, B, starts, total);
     return hipGetLastError();
 }
 
