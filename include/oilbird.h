@@ -584,8 +584,8 @@ int32_t oil_kv_evict(oil_kv *kv, const int32_t *slots, int32_t B, int64_t keep, 
  *
  * Common arguments:
  *   starts     B + 1 int32 (device), ascending within 0 .. total; bounds and empty sequences
- *              as in oil_kv_append_packed.  What is written for rows of sequences that overlap,
- *              and of those after them, is undefined.  B 1 .. OIL_MAX_B.
+ *              as in oil_kv_append_packed.  Where sequences overlap, what is written is
+ *              undefined, and rows of any sequence may stay as they were.  B 1 .. OIL_MAX_B.
  *   total      rows of every buffer, 1 .. OIL_PROMPT_MAX_ROWS; times n_q_heads at most 2^30.
  *   q          total rows of n_q_heads x head_dim bf16, 16-byte aligned, rows q_ld
  *              elements apart (>= n_q_heads * head_dim, a multiple of 8, at most

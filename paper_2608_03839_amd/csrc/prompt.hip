@@ -577,8 +577,9 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
     }
     loads_done();  // none is in flight when the buffers go to another workgroup
 
-    // what a second pass's weights are multiplied by: a power of two below 1 / (2 len)
-    const float small = __uint_as_float((uint32_t)(127 - 33 + __builtin_clz(len)) << 23);
+    // what a second pass's weights are multiplied by: a power of two below half of one over the keys that the row
+    // sees (not over all of its sequence: later keys change no bit of a row)
+    const float small = __uint_as_float((uint32_t)(127 - 33 + __builtin_clz(token + 1)) << 23);
     // Writes the row; `again`: where what is there is not finite.  Whether anything written is not finite, but
     // for rows that a score of NaN makes NaN.
     auto store = [&](auto again) {

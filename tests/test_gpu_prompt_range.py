@@ -310,3 +310,33 @@ def test_large_values_of_a_later_key(oil, at, D):
     w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [0, n], 1.0)
     _finite_and_near(out, w_out, far_out)
     assert ((lse.double() - w_lse).abs() <= far_lse).all()
+
+
+@pytest.mark.parametrize("Hq,H,D", [(8, 2, 128), (12, 12, 64), (5, 1, 40)])
+def test_results_made_again_depend_on_what_they_see(oil, Hq, H, D):
+    """Rows whose scores or values leave the ordinary pass: alone and packed, as part of a longer sequence and
+    beside rows that hold anything, bit by bit."""
+    lens = [300, 1, 1900, 64]
+    at = [0, 300, 301, 2201, 2265]
+    q, k, v = (_normal((at[-1], h, D), i) for i, h in ((1, Hq), (2, H), (3, H)))
+    q[::3, :, 0] = 2.0 ** 40
+    k[::7, :, 0] = 2.0 ** 30
+    v[..., 1] = 2.0 ** 127
+    v[::5, :, 1] *= -1.0
+    v[3::50, 0, 2] = INF
+    q[1::3, 0] *= 2.0 ** -100
+    same = lambda a, b: ((a == b) | (a.isnan() & b.isnan())).all()  # noqa: E731
+    out, lse = oil.prompt_attend(q, k, v, _int(at))
+    assert torch.isfinite(out[..., 1]).all() and torch.isfinite(out[..., 3:]).all()
+    for a, z in zip(at, at[1:]):
+        alone = oil.prompt_attend(q[a:z], k[a:z], v[a:z], _int([0, z - a]))
+        assert same(alone[0], out[a:z]) and torch.equal(alone[1], lse[a:z])
+        half = a + (z - a + 1) // 2
+        begun = oil.prompt_attend(q[a:half], k[a:half], v[a:half], _int([0, half - a]))
+        assert same(begun[0], out[a:half]) and torch.equal(begun[1], lse[a:half])
+    wild = q.clone()
+    wild[2::3] = math.nan
+    got = oil.prompt_attend(wild, k, v, _int(at))
+    kept = torch.arange(at[-1], device="cuda") % 3 != 2
+    assert same(got[0][kept], out[kept]) and torch.equal(got[1][kept], lse[kept])
+    assert torch.isnan(got[0][~kept]).all()
