@@ -6,7 +6,7 @@
 // both rescaled when m rises.  Then
 //     log p = (x - m) - ln s,      H = ln s - ln 2 t / s,
 // where both terms of H are at least 0, so that nothing cancels.  9 instructions a value,
-// one of them an exponential; the pass over many rows is bound by memory: 4,084 rows of
+// one of them an exponential; the pass over many rows is bound by memory: 4,054 rows of
 // 50,021 binary32 values 143 us (5.7 TB/s), 1,635 of 131,072 bf16 values with
 // eight alternatives 98 us (4.4 TB/s, and the VALU 0.77 of the cycles).
 //

@@ -15,21 +15,23 @@
 // c is log2 e times the scale, rounded, and so is m, while S c is exact: where scores are
 // so large that this tells (kFar), and wherever else a result is not finite, a second pass
 // makes the row from (S - max S) scale.
-// Bound by power, which leaves a clock of 1.4 to 1.7 GHz with matrix cores busy two thirds of
-// the time, and by matrix cores, exponentials and LDS, which overlap in part: at 128
-// columns a wave's tile of 64 keys is 32 matrix instructions of 32 cycles, some 560 cycles of
-// exponentials, scaling and sums, and 256 cycles of LDS, which the CU's eight waves share.
-// 16,384 rows, 32 heads over 8 of 128 columns: 1,845 to 2,015 us on different cards, 1,090 to
-// 1,190 TFLOP/s (a library product of 16,384^3: 1,586); 8,191 rows 495 us; 65,533 rows, 2
-// heads over 1: 1,990 us; 48 sequences of 375 to 1,500 rows 580 us, 785 TFLOP/s: a workgroup
-// passes over some ten tiles there, and 6 of its 20 us are its first loads and its end.
+// Bound by matrix cores, exponentials and LDS, which overlap in part: at 128 columns a wave's
+// tile of 64 keys is 32 matrix instructions of 32 cycles, some 560 cycles of exponentials,
+// scaling and sums, and 256 cycles of LDS, which the CU's eight waves share.  So the matrix
+// cores are busy 0.65 of the cycles of 16,384 rows (0.41 of 48 short sequences'); a library
+// product of 16,384^3 on the same card keeps them busy 0.90 of the cycles at the same clock, 1.7 GHz.
+// 16,384 rows, 32 heads over 8 of 128 columns: 1,895 to 2,060 us on different cards, 1,070 to
+// 1,160 TFLOP/s (the library product: 1,586); 8,191 rows 497 to 537 us; 65,533 rows, 2
+// heads over 1: 1,950 to 2,110 us; 48 sequences of 390 to 1,500 rows 585 to 630 us, 720 to 780: a
+// workgroup passes over some ten tiles there, and 6 of its 20 us are its first loads and its end.
+// 8,191 rows of 64 columns 292 us; 72 to 120 columns are made as 128 are (72: 440 us, 96: 460).
 //
 // weigh: a lane's column is a key, S = Q K^T, and the sums of exp2(S c - lse) stay in
 // registers: no two workgroups add to one sum, so the result does not depend on the order
 // in which they run.  Bound by exponentials beside the products, of which there is one a
 // score here: without either the other alone takes three quarters of the time.  8,192 rows
-// over themselves, 32 heads over 8 of 128 columns: 308 us, 892 TFLOP/s; four sequences of
-// 2,048 to 8,191 rows, their last 64 rows: 25 us, of which the list 4; the keys are 45 MB.
+// over themselves, 32 heads over 8 of 128 columns: 302 to 312 us, 880 to 910 TFLOP/s; four sequences
+// of 2,866 to 8,191 rows, their last 64 rows: 26 us, of which the list 4; the keys are 45 MB.
 #include "common.hpp"
 #include "internal.hpp"
 
@@ -129,8 +131,8 @@ __device__ __forceinline__ int wave_sum(int x)
 // first (ties by number), of each the tiles of the largest number first.  So the
 // workgroups that run at one time read the keys of few sequences, from L2, and the last
 // ones are short.  (The largest numbers of all sequences first: 48 sequences of up to
-// 1,500 tokens 727 us; their keys came from memory again and again.  A search in every
-// workgroup instead of the list: 3.3 us of 28.)  A wave takes every so many sequences.
+// 1,500 tokens took 1.13 times as long; their keys came from memory again and again.  A search in
+// every workgroup instead of the list: 3.3 us of 28.)  A wave takes every so many sequences.
 constexpr int kListWaves = 128;
 
 __global__ __launch_bounds__(256) void prompt_list_kernel(const int32_t* __restrict__ starts, int32_t B, int32_t T,
@@ -414,7 +416,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
                 s[b][r] = b * 32 + 8 * (r / 4) + r % 4 <= seen ? s[b][r] : -INFINITY;
     };
     // P of a tile's scores: m stays where it is, and the scores' maximum is not sought, unless
-    // they turn out too large (with it: 16,384 rows 1,950 us, without 1,890).
+    // they turn out too large (sought in every tile: 16,384 rows 1.03 times as long).
     auto weights = [&]() {
         float sum = relative();
         const uint64_t over = __ballot(sum > most);
@@ -774,11 +776,11 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_attend_kernel(Attend)
 }
 
 // kWeighKeys keys a wave, NW waves; rows kWeighRows at a time from LDS (64 at a time, which
-// lets three workgroups into a CU: 400 for 345 us, registers spill), 32 of them
-// multiplied while the exponentials of the 32 before are made.  Of the rows that count for
-// a tile of keys the workgroup takes blockIdx.y's `chunk` tokens' and writes part
-// blockIdx.y of the sum (a plane of n_heads x T), so that the first keys, which most rows
-// see, do not take longest.
+// lets three workgroups into a CU: 1.16 times as long, registers spill; with 128 all 256 are used at
+// 128 columns and two spilled), 32 of them multiplied while the exponentials of the 32
+// before are made.  Of the rows that count for a tile of keys the workgroup takes
+// blockIdx.y's `chunk` tokens' and writes part blockIdx.y of the sum (a plane of n_heads x
+// T), so that the first keys, which most rows see, do not take longest.
 template <int W, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const Tile* __restrict__ list, const int32_t* __restrict__ starts, int32_t T, const uint16_t* __restrict__ q,
@@ -968,7 +970,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
             }
             // At 128 columns reads of LDS eight ahead, which leaves the exponentials where they
             // are beside products: 16 + 32 + 16 matrix instructions, 48 reads.  (Without: 8,192
-            // rows 340 for 330 us; at 64 columns the compiler's own order is as fast.)
+            // rows 1.03 times as long; at 64 columns the compiler's own order is as fast.)
             constexpr int kMatrix = 0x8, kRead = 0x100;
             if (W == 128) {
                 __builtin_amdgcn_sched_group_barrier(kRead, 8, 0);
@@ -1036,8 +1038,8 @@ const Tile* make_list(const int32_t* starts, int32_t B, int32_t T, int32_t per, 
 }
 
 constexpr int kWeighBlock = kWeighKeys * 4;
-// Workgroups that leave no CU idle long, whatever their shares (4,096: 8,192 rows 343 for 328 us,
-// 65,536 rows of one head 1,186 for 1,220).
+// Workgroups that leave no CU idle long, whatever their shares (4,096: 8,192 rows 1.05 times as
+// long, 65,536 rows of one head 0.97 times).
 constexpr int64_t kWeighWork = 2048;
 
 // Chunks that the rows of a call are cut into, and their tokens.
