@@ -918,10 +918,11 @@ __global__ __launch_bounds__(NW * 64, 2) void prompt_weigh_kernel(
     const int wave_key = key0 + wave * kWeighKeys + kWeighKeys - 1;  // the wave's last
     for (int t = 0; t < turns; t++) {
         loads_done();
+        // rows past kFarLse, and all where c is past binary32's range, which the scale need not be
         const bool mine_too = (int)threadIdx.x < kWeighRows;
         float less = next_lse * -kLog2e;
-        int odd = __ballot(mine_too && !(fabsf(next_lse) < kFarLse)) != 0;
-        if (odd && __ballot(mine_too && !(fabsf(next_lse) < kFarLse) && next_lse != -INFINITY)) {
+        int odd = __ballot(mine_too && !(fabsf(next_lse) < kFarLse && c < INFINITY)) != 0;
+        if (odd && __ballot(mine_too && !(fabsf(next_lse) < kFarLse && c < INFINITY) && next_lse != -INFINITY)) {
             odd = 3;
             less = -next_lse;  // of all the wave's rows
         }

@@ -340,3 +340,24 @@ def test_results_made_again_depend_on_what_they_see(oil, Hq, H, D):
     kept = torch.arange(at[-1], device="cuda") % 3 != 2
     assert same(got[0][kept], out[kept]) and torch.equal(got[1][kept], lse[kept])
     assert torch.isnan(got[0][~kept]).all()
+
+
+@pytest.mark.parametrize("n,Hq,H,D", SIZES)
+@pytest.mark.parametrize("scale", [1.5 * 2.0 ** 127, -2.0 ** 127, 2.0 ** -126, 2.0 ** -140])
+def test_scales_at_the_ends(oil, n, Hq, H, D, scale):
+    """Scales up to binary32's largest and down to subnormal ones, with products that bring the scores back as
+    far as binary32 holds them."""
+    q, k, v = (_normal((n, h, D), i) for i, h in ((1, Hq), (2, H), (3, H)))
+    # products by 2^(e - 1), half of it in each; 128 of up to 2^4.5 each add up to less than 2^(e + 11)
+    e = min(-math.frexp(scale)[1], 117)
+    q, k = q * 2.0 ** (e // 2), k * 2.0 ** (e - e // 2 - 1)
+    out, lse = oil.prompt_attend(q, k, v, _int([0, n]), scale=scale)
+    w_out, w_lse, far_out, far_lse = ref.attend(q, k, v, [0, n], scale)
+    # a subnormal scale times log2 e is rounded by 2^-150 at most
+    lost = 2.0 ** (e + 11 - 150) if abs(scale) < 2.0 ** -125 else 0.0
+    assert ((out.double() - w_out).abs() <= far_out + 2 * lost * v.double().abs().max()).all()
+    assert ((lse.double() - w_lse).abs() <= far_lse + lost).all()
+    for last in (n, 17):
+        weight = oil.prompt_weigh(q, k, lse, _int([0, n]), last=last, scale=scale)
+        want, far = ref.weigh(q, k, lse, [0, n], last, scale)
+        assert ((weight.double() - want).abs() <= far + 2 * lost * want).all()
